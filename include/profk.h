@@ -389,6 +389,71 @@ int profk_topk_noalloc_f32(const float* in, int64_t rows, int64_t N, int64_t k, 
                            uint64_t seed, void* stream, float* out_vals, int64_t* out_idx);
 
 /*
+ * OPERATORS AROUND A SELECTION IN A DECODING LOOP.  A language model answers with a selection from its logits; the calls
+ * below are what stands on either side of it: the log probabilities that the selection is made from (with their
+ * gradient), the forking of the cache pages of the sequences that it continues, and the attention of the next token
+ * over those pages.  They follow the conventions at the top of this header, with three differences: fp16 is a type of
+ * theirs too, tensors have strides, and scratch memory is an argument (the registered workspace is not touched, so
+ * profk_read_stats still reports the last selection).
+ */
+
+/*
+ * Log probabilities of given tokens, entropy and the k most probable tokens of every row, in one read of the logits.
+ * With z = x / temperature:  lse = ln sum_v e^(z_v),  ln p_v = z_v - lse,  entropy = -sum_v p_v ln p_v.
+ *   logits        [device] rows x V elements, row r at logits + r * row_stride (row_stride >= V), any element alignment
+ *   tokens        [device] rows int64, or NULL (then logprob is NULL too); a negative token means that none is given
+ *                 (log probability 0), a token >= V gives NaN
+ *   k             0 <= k <= min(V, 128): alternatives per row, ordered by logit descending, equal logits by index
+ *                 ascending (profk_topk_* selects more of them)
+ *   temperature   > 0, finite
+ *   logprob, lse  [device] rows floats (logprob NULL iff tokens is)
+ *   lse_rest      [device] rows floats, or NULL: what the rounding of lse to fp32 left off.  The backward call takes the
+ *                 probabilities from lse + lse_rest: beside a large maximum one float alone loses ln s
+ *   entropy       [device] rows floats, or NULL: not computed
+ *   top_logprobs, top_tokens   [device] rows x k floats / int64; NULL iff k = 0
+ * All statistics are kept in fp32, sums relative to the row's largest logit.  -inf masks a token: probability 0, no part
+ * in the entropy.  A row of nothing but -inf has lse = -inf, log probabilities -inf, entropy 0.  A NaN or +inf anywhere in
+ * a row makes its lse, log probabilities and entropy NaN; a NaN is never among the alternatives (places that nothing else
+ * fills get token -1, log probability NaN).
+ * The result does not depend on how a row is cut into parts except in the last bits of the sums; it is the same in every
+ * call with the same arguments.  Errors: PROFK_EINVAL, PROFK_ECUDA.
+ */
+int profk_logprobs_f32(const float* logits, int64_t rows, int64_t V, int64_t row_stride, const int64_t* tokens, int64_t k,
+                       double temperature, void* stream, float* logprob, float* lse, float* lse_rest, float* entropy, float* top_logprobs,
+                       int64_t* top_tokens);
+int profk_logprobs_bf16(const void* logits, int64_t rows, int64_t V, int64_t row_stride, const int64_t* tokens, int64_t k,
+                        double temperature, void* stream, float* logprob, float* lse, float* lse_rest, float* entropy, float* top_logprobs,
+                        int64_t* top_tokens);
+int profk_logprobs_f16(const void* logits, int64_t rows, int64_t V, int64_t row_stride, const int64_t* tokens, int64_t k,
+                       double temperature, void* stream, float* logprob, float* lse, float* lse_rest, float* entropy, float* top_logprobs,
+                       int64_t* top_tokens);
+
+/*
+ * The gradient of the above with respect to the logits.  With upstream gradients g_lp, g_H, g_lse (rows floats) and g_j
+ * (rows x k floats, of the alternatives' log probabilities),
+ *   grad_v = (1 / temperature) [ -p_v (G + g_H (ln p_v + H)) + g_lp 1[v = token] + sum_j g_j 1[v = top_token_j] ],
+ *   G = g_lp + sum_j g_j - g_lse.
+ *   lse, lse_rest, entropy, tokens, top_tokens   what the forward call took and gave (lse_rest may be NULL: 0)
+ *   grad_logprob (needs tokens), grad_entropy (needs entropy), grad_lse, grad_top (needs top_tokens)   each may be NULL: 0
+ *   grad_logits   [device] rows x V elements of the logits' type, row stride grad_row_stride; may be `logits` itself only
+ *                 if grad_row_stride == row_stride and neither grad_logprob nor grad_top is given
+ * The sum is taken in fp32 and rounded once.  Rows with lse = -inf get zeros; tokens outside [0, V) get nothing.
+ * Errors: PROFK_EINVAL, PROFK_ECUDA.
+ */
+int profk_logprobs_backward_f32(const float* logits, int64_t rows, int64_t V, int64_t row_stride, double temperature,
+                                const float* lse, const float* lse_rest, const int64_t* tokens, const float* grad_logprob, const float* entropy,
+                                const float* grad_entropy, const float* grad_lse, int64_t k, const int64_t* top_tokens,
+                                const float* grad_top, void* stream, float* grad_logits, int64_t grad_row_stride);
+int profk_logprobs_backward_bf16(const void* logits, int64_t rows, int64_t V, int64_t row_stride, double temperature,
+                                 const float* lse, const float* lse_rest, const int64_t* tokens, const float* grad_logprob, const float* entropy,
+                                 const float* grad_entropy, const float* grad_lse, int64_t k, const int64_t* top_tokens,
+                                 const float* grad_top, void* stream, void* grad_logits, int64_t grad_row_stride);
+int profk_logprobs_backward_f16(const void* logits, int64_t rows, int64_t V, int64_t row_stride, double temperature,
+                                const float* lse, const float* lse_rest, const int64_t* tokens, const float* grad_logprob, const float* entropy,
+                                const float* grad_entropy, const float* grad_lse, int64_t k, const int64_t* top_tokens,
+                                const float* grad_top, void* stream, void* grad_logits, int64_t grad_row_stride);
+
+/*
  * Copies the statistics of the last call that used the registered workspace to
  * the host and waits for `stream`.  out: [host] rows entries.  Every wait inside
  * the kernels is bounded (the grid barriers of the exact-selection and large-k

@@ -26,6 +26,8 @@ EXPORTS = [
     "profk_shard_bounds", "profk_shard_sample_keys_f32", "profk_shard_sample_keys_bf16", "profk_threshold_from_keys_f32",
     "profk_threshold_from_keys_bf16", "profk_filter_shard_f32", "profk_filter_shard_bf16", "profk_refine_gathered_f32",
     "profk_refine_gathered_bf16",
+    "profk_logprobs_f32", "profk_logprobs_bf16", "profk_logprobs_f16", "profk_logprobs_backward_f32",
+    "profk_logprobs_backward_bf16", "profk_logprobs_backward_f16",
 ]
 
 FILTER_COUNT_STRIDE = 8      # PROFK_FILTER_COUNT_STRIDE: uint32 words per row in the counts array of profk_filter_*
@@ -444,3 +446,6 @@ def read_stats(rows: int):
 
 def last_launch_count() -> int:
     return int(lib().profk_last_launch_count())
+
+
+from .decode import LogProbs, logprobs, logprobs_backward  # noqa: E402  (the module uses the names above)

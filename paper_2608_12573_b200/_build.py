@@ -9,7 +9,7 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libprofk.so")
-SOURCES = ["profk_api.cu", "plan.cpp"]
+SOURCES = ["profk_api.cu", "decode_api.cu", "plan.cpp"]
 
 
 def _newest_source_mtime() -> float:
@@ -20,7 +20,7 @@ def _newest_source_mtime() -> float:
 def nvcc_command(extra: list[str] | None = None) -> list[str]:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+           "-Xcompiler", "-fPIC", "-shared", "--threads", "0", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
            "-o", LIB_PATH] + [os.path.join(CSRC, s) for s in SOURCES]
     return cmd + (extra or []) + os.environ.get("PROFK_NVCC_FLAGS", "").split()
 
