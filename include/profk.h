@@ -454,6 +454,97 @@ int profk_logprobs_backward_f16(const void* logits, int64_t rows, int64_t V, int
                                 const float* grad_top, void* stream, void* grad_logits, int64_t grad_row_stride);
 
 /*
+ * PAGED CACHE.  Keys and values of a sequence lie in pages of page_size tokens; a row of the page table names them in
+ * order, and sequences may share pages.  One page number holds for all layers.  State, all int32 [device]:
+ *   tables   n rows of `width` entries, row i at tables + i * table_stride; entry c is the page of the tokens
+ *            [c * page_size, (c + 1) * page_size).  Entries at or behind a sequence's length are not read; a number outside
+ *            [0, pages) stands for a page that is not there (its tokens take no part, nothing is copied)
+ *   lengths  n tokens held, taken into [0, width * page_size]
+ *   refs     one per page: how many table entries (or other owners) hold it; <= 0 is free
+ */
+
+/* A cache of `layers` layers, keys and values: the row of (layer l, 0 = key / 1 = value x, page, kv head, token) begins at
+ * base + l * pool.layer + x * pool.kv + page * pool.page + head * pool.head + token * pool.token (strides in bytes; base, strides and row_bytes
+ * multiples of 16).  Any element type; page_size tokens per page. */
+typedef struct profk_pool {
+    void* base;                           /* [device] */
+    int64_t layers, kv_heads, page_size, row_bytes;
+    int64_t layer, kv, page, head, token;
+} profk_pool_t;
+
+/* Strides of one layer's keys or values, between pages, kv heads and tokens. */
+typedef struct profk_page_strides { int64_t page, head, token; } profk_page_strides_t;
+
+/*
+ * Forks, grows and releases sequences.  New sequence i continues old sequence parents[i] ([device] n int32; a number outside
+ * [0, n_old) begins an empty one) and gets room for `grow` more tokens.  Full pages are shared.  A partly filled last page
+ * stays with the parent's first child (lowest i); the others get a fresh page and a copy of its tokens.  Fresh pages are
+ * the lowest-numbered ones that are free before the call, handed out in the order of need (by i, then by position).  Old
+ * sequences without a child are released:  out_refs = refs - (old entries) + (new entries).
+ *   pool         what the copies move, or NULL: tables and counts only
+ *   out_tables   n x width (entries without a page are -1), out_lengths n (at most width * page_size), out_refs pages,
+ *                out_missing 1: pages that were needed but not to be had (no free page, or no room in the table); a -1
+ *                stands in the table in place of each that has room there.  Must not overlap the inputs
+ *   workspace    [device] profk_pages_fork_workspace_bytes, 256-byte aligned
+ * n = 0 releases all.  Errors: PROFK_EINVAL, PROFK_EWORKSPACE, PROFK_ECUDA.
+ */
+int profk_pages_fork_workspace_bytes(int64_t n_old, int64_t n, int64_t pages, int64_t page_size, int64_t grow, size_t* bytes /* [host] */);
+int profk_pages_fork(const profk_pool_t* pool /* [host] */, const int32_t* tables, int64_t n_old, int64_t width, int64_t table_stride,
+                     const int32_t* lengths, const int32_t* refs, int64_t pages, const int32_t* parents, int64_t n, int64_t page_size,
+                     int64_t grow, void* workspace, size_t workspace_bytes, void* stream, int32_t* out_tables, int32_t* out_lengths,
+                     int32_t* out_refs, int32_t* out_missing);
+
+/*
+ * Moves the L live pages (refs > 0) to the pages [0, L): live pages at or behind L go to the free ones in front of it, both
+ * in ascending order; the others stay.
+ *   out_tables     n x width: the new numbers (-1 for numbers outside [0, pages) and for pages that are free)
+ *   out_refs       pages;  out_page_map  pages: the new number of each live page, -1 for the others;  out_live  1: L
+ *   workspace      [device] profk_pages_compact_workspace_bytes, 256-byte aligned
+ * Errors: PROFK_EINVAL, PROFK_EWORKSPACE, PROFK_ECUDA.
+ */
+int profk_pages_compact_workspace_bytes(int64_t pages, size_t* bytes /* [host] */);
+int profk_pages_compact(const profk_pool_t* pool /* [host] */, const int32_t* tables, int64_t n, int64_t width, int64_t table_stride,
+                        const int32_t* refs, int64_t pages, void* workspace, size_t workspace_bytes, void* stream, int32_t* out_tables,
+                        int32_t* out_refs, int32_t* out_page_map, int32_t* out_live);
+
+/* Copies page src[j] to page dst[j], all layers (n int32 each, [device]).  No dst may occur twice or among src; pairs with a
+ * number outside [0, pages) are passed over.  Errors: PROFK_EINVAL, PROFK_ECUDA. */
+int profk_pages_copy(const profk_pool_t* pool /* [host] */, int64_t pages, const int32_t* src, const int32_t* dst, int64_t n, void* stream);
+
+/* Writes the keys and values of the last `tokens` tokens of every sequence (positions length - tokens .. length - 1) to
+ * their places in one layer's pages.  k, v: [device] (seqs, tokens, kv_heads) rows of row_bytes; *_strides [host] three
+ * strides each; kp, vp: those of the pages; all strides in bytes, multiples of 16.  Tokens before position 0 or on a page
+ * that is not there are passed over.  No two sequences may write to one page.  Errors: PROFK_EINVAL, PROFK_ECUDA. */
+int profk_pages_append(const void* k, const void* v, const int64_t* k_strides, const int64_t* v_strides, void* k_pages, void* v_pages,
+                       const profk_page_strides_t* kp, const profk_page_strides_t* vp, const int32_t* tables, int64_t table_stride,
+                       const int32_t* lengths, int64_t seqs, int64_t tokens, int64_t kv_heads, int64_t row_bytes, int64_t page_size,
+                       int64_t pages, int64_t width, void* stream);
+
+/*
+ * Attention of one new token per sequence over one layer's pages:  out_h = sum_j p_j v_j,  p = softmax_j(scale q_h . k_j) over
+ * the tokens j < length,  lse_h = ln sum_j e^(scale q_h . k_j).  Query head h reads kv head h / (heads / kv_heads).
+ *   q            [device] seqs x heads rows of dim elements; strides in elements, even
+ *   k_pages, v_pages   [device] 16-byte aligned; strides in elements, multiples of 8
+ *   dim          a multiple of 8, up to 256
+ *   scale        > 0, finite
+ *   out          [device] seqs x heads x dim, dense, of the cache's type;  lse  [device] seqs x heads floats
+ *   workspace    [device] profk_paged_attention_workspace_bytes(dim), 256-byte aligned
+ * Statistics and sums are kept in fp32.  A sequence without tokens gets out = 0, lse = -inf.  The same call gives the same
+ * bits every time.  Errors: PROFK_EINVAL, PROFK_EWORKSPACE, PROFK_ECUDA.
+ */
+int profk_paged_attention_workspace_bytes(int64_t dim, size_t* bytes /* [host] */);
+int profk_paged_attention_bf16(const void* q, int64_t q_seq_stride, int64_t q_head_stride, const void* k_pages, const void* v_pages,
+                               const profk_page_strides_t* k_strides, const profk_page_strides_t* v_strides, const int32_t* tables,
+                               int64_t table_stride, const int32_t* lengths, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t dim,
+                               int64_t page_size, int64_t pages, int64_t width, double scale, void* workspace, size_t workspace_bytes,
+                               void* stream, void* out, float* lse);
+int profk_paged_attention_f16(const void* q, int64_t q_seq_stride, int64_t q_head_stride, const void* k_pages, const void* v_pages,
+                              const profk_page_strides_t* k_strides, const profk_page_strides_t* v_strides, const int32_t* tables,
+                              int64_t table_stride, const int32_t* lengths, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t dim,
+                              int64_t page_size, int64_t pages, int64_t width, double scale, void* workspace, size_t workspace_bytes,
+                              void* stream, void* out, float* lse);
+
+/*
  * Copies the statistics of the last call that used the registered workspace to
  * the host and waits for `stream`.  out: [host] rows entries.  Every wait inside
  * the kernels is bounded (the grid barriers of the exact-selection and large-k

@@ -28,6 +28,9 @@ EXPORTS = [
     "profk_refine_gathered_bf16",
     "profk_logprobs_f32", "profk_logprobs_bf16", "profk_logprobs_f16", "profk_logprobs_backward_f32",
     "profk_logprobs_backward_bf16", "profk_logprobs_backward_f16",
+    "profk_paged_attention_workspace_bytes", "profk_paged_attention_bf16", "profk_paged_attention_f16",
+    "profk_pages_fork_workspace_bytes", "profk_pages_fork", "profk_pages_compact_workspace_bytes", "profk_pages_compact",
+    "profk_pages_copy", "profk_pages_append",
 ]
 
 FILTER_COUNT_STRIDE = 8      # PROFK_FILTER_COUNT_STRIDE: uint32 words per row in the counts array of profk_filter_*
@@ -448,4 +451,6 @@ def last_launch_count() -> int:
     return int(lib().profk_last_launch_count())
 
 
-from .decode import LogProbs, logprobs, logprobs_backward  # noqa: E402  (the module uses the names above)
+# (behind the names above, which the module uses)
+from .decode import (LogProbs, PagesCompacted, PagesForked, logprobs, logprobs_backward, paged_attention,  # noqa: E402
+                     pages_append, pages_compact, pages_copy, pages_fork)

@@ -7,6 +7,8 @@
 #include <mutex>
 
 #include "logprobs.cuh"
+#include "paged_attention.cuh"
+#include "pages.cuh"
 #include "profk.h"
 
 using namespace profk;
@@ -141,6 +143,88 @@ int lp_backward(const T* logits, int64_t rows, int64_t V, int64_t row_stride, do
     return PROFK_OK;
 }
 
+// ---- paged attention -------------------------------------------------------------------------
+
+constexpr int PA_MAX_DIM = 256;
+
+int pa_tile_dim(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
+unsigned pa_ctas(int64_t dim, int sms) { return (unsigned)sms * (pa_tile_dim(dim) == 256 ? PaShape<256>::CTAS : PaShape<128>::CTAS); }
+size_t pa_meta_bytes(unsigned ctas) { return ((size_t)ctas * sizeof(PaMeta) + 255) / 256 * 256; }
+size_t pa_workspace(int64_t dim, int sms) {
+    const unsigned ctas = pa_ctas(dim, sms);
+    return pa_meta_bytes(ctas) + (size_t)ctas * 2 * PA_ROWS * (pa_tile_dim(dim) + 2) * sizeof(float);
+}
+
+template <typename T, int D>
+int pa_launch(const PaParams& p, unsigned ctas, void* stream) {
+    static uint64_t done = 0;
+    static std::mutex mutex;
+    DEC_TRY(prepare_kernel(paged_attention_kernel<T, D>, PaShape<D>::SMEM, false, &done, &mutex));
+    Launch l(ctas, PA_THREADS, PaShape<D>::SMEM, stream);
+    DEC_TRY(cudaLaunchKernelEx(&l.cfg, paged_attention_kernel<T, D>, p));
+    Launch j(ctas, PJ_THREADS, 0, stream);
+    j.cfg.gridDim.y = (unsigned)p.rows;
+    DEC_TRY(cudaLaunchKernelEx(&j.cfg, paged_attention_join_kernel<T, D>, p));
+    return PROFK_OK;
+}
+
+bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+template <typename T>
+int pa_run(const T* q, int64_t q_seq, int64_t q_head, const T* k, const T* v, const profk_page_strides_t* ks, const profk_page_strides_t* vs,
+           const int32_t* tables, int64_t table_stride, const int32_t* lengths, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t dim,
+           int64_t page_size, int64_t pages, int64_t width, double scale, void* workspace, size_t workspace_bytes, void* stream, T* out, float* lse) {
+    if (!q || !k || !v || !ks || !vs || !tables || !lengths || !out || !lse || seqs < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0 ||
+        dim < 8 || dim > PA_MAX_DIM || dim % 8 != 0 || page_size < 1 || pages < 1 || width < 1 || seqs > (1 << 24) || heads > (1 << 16) ||
+        page_size > (1 << 24) || pages > 0x7FFFFFFFll || width * page_size > 0x7FFFFF00ll || table_stride < 0 || !(scale > 0) || !std::isfinite(scale) ||
+        !aligned_to(q, 4) || q_seq % 2 != 0 || q_head % 2 != 0 || !aligned_to(k, 16) || !aligned_to(v, 16) || !aligned_to(out, 16))
+        return PROFK_EINVAL;
+    for (const profk_page_strides_t* s : {ks, vs})
+        if (s->page % 8 != 0 || s->head % 8 != 0 || s->token % 8 != 0) return PROFK_EINVAL;
+    const int sms = sm_count();
+    if (sms < 1) return PROFK_ECUDA;
+    const size_t need = pa_workspace(dim, sms);
+    if (!workspace || workspace_bytes < need || !aligned_to(workspace, 256)) return PROFK_EWORKSPACE;
+    const int32_t group = (int32_t)(heads / kv_heads), blocks = (group + PA_ROWS - 1) / PA_ROWS;
+    // no more CTAs than there can be tiles, or sequences without any
+    const int64_t most = std::max<int64_t>(seqs, seqs * kv_heads * blocks * ((width * page_size + PA_TILE - 1) / PA_TILE));
+    const unsigned ctas = (unsigned)std::min<int64_t>(pa_ctas(dim, sms), most);
+    PaParams p{q, k, v, q_seq, q_head, ks->page, ks->head, ks->token, vs->page, vs->head, vs->token, tables, table_stride, lengths,
+               (int32_t)seqs, (int32_t)heads, (int32_t)kv_heads, group, (int32_t)dim, (int32_t)page_size, (int32_t)pages, (int32_t)width,
+               blocks, (group + blocks - 1) / blocks, (float)scale, out, lse,
+               reinterpret_cast<float*>(static_cast<char*>(workspace) + pa_meta_bytes(pa_ctas(dim, sms))), static_cast<PaMeta*>(workspace)};
+    switch (pa_tile_dim(dim)) {
+        case 64: return pa_launch<T, 64>(p, ctas, stream);
+        case 128: return pa_launch<T, 128>(p, ctas, stream);
+        default: return pa_launch<T, 256>(p, ctas, stream);
+    }
+}
+
+// ---- pages -----------------------------------------------------------------------------------
+
+bool pg_pool_ok(const profk_pool_t* pool) {
+    if (!pool) return true;
+    return pool->base && aligned_to(pool->base, 16) && pool->layers >= 1 && pool->layers <= (1 << 20) && pool->kv_heads >= 1 && pool->kv_heads <= (1 << 16) &&
+           pool->page_size >= 1 && pool->row_bytes >= 16 && pool->row_bytes <= (1 << 20) && pool->row_bytes % 16 == 0 && pool->layer % 16 == 0 &&
+           pool->kv % 16 == 0 && pool->page % 16 == 0 && pool->head % 16 == 0 && pool->token % 16 == 0 &&
+           pool->kv_heads * pool->page_size * (pool->row_bytes / 16) <= (1 << 30);
+}
+PgPool pg_pool(const profk_pool_t* pool, int64_t page_size) {
+    if (!pool) return PgPool{nullptr, 0, 0, (int32_t)page_size, 0, 0, 0, 0, 0, 0};
+    return PgPool{static_cast<char*>(pool->base), (int32_t)pool->layers, (int32_t)pool->kv_heads, (int32_t)pool->page_size, (int32_t)pool->row_bytes,
+                  pool->layer, pool->kv, pool->page, pool->head, pool->token};
+}
+size_t up(size_t n) { return (n + 255) / 256 * 256; }
+int64_t fork_fresh(int64_t n, int64_t pages, int64_t page_size, int64_t grow) { return std::min(pages, n * (1 + (grow + page_size - 1) / page_size)); }
+size_t fork_workspace(int64_t n_old, int64_t n, int64_t pages, int64_t page_size, int64_t grow) {
+    return 256 + 2 * up((size_t)n_old * 4) + up((size_t)n * 4) + up((size_t)fork_fresh(n, pages, page_size, grow) * 4) + up((size_t)n * sizeof(PgMove));
+}
+bool fork_sizes_ok(int64_t n_old, int64_t n, int64_t pages, int64_t page_size, int64_t grow) {
+    return n_old >= 0 && n >= 0 && n_old <= (1 << 24) && n <= (1 << 24) && pages >= 1 && pages <= 0x7FFF0000ll && page_size >= 1 && page_size <= (1 << 24) &&
+           grow >= 0 && grow <= (1 << 24) && n * (1 + (grow + page_size - 1) / page_size) <= 0x7FFF0000ll;
+}
+constexpr unsigned PG_CTAS_PER_SM = 6;
+
 }  // namespace
 
 extern "C" {
@@ -163,5 +247,136 @@ extern "C" {
 PROFK_DEFINE_LOGPROBS(f32, float, float)
 PROFK_DEFINE_LOGPROBS(bf16, __nv_bfloat16, void)
 PROFK_DEFINE_LOGPROBS(f16, __half, void)
+
+int profk_paged_attention_workspace_bytes(int64_t dim, size_t* bytes) {
+    if (!bytes || dim < 8 || dim > PA_MAX_DIM || dim % 8 != 0) return PROFK_EINVAL;
+    const int sms = sm_count();
+    if (sms < 1) return PROFK_ECUDA;
+    *bytes = pa_workspace(dim, sms);
+    return PROFK_OK;
+}
+
+#define PROFK_DEFINE_ATTENTION(SUFFIX, ELEM)                                                                                            \
+    int profk_paged_attention_##SUFFIX(const void* q, int64_t q_seq_stride, int64_t q_head_stride, const void* k_pages, const void* v_pages, \
+                                       const profk_page_strides_t* k_strides, const profk_page_strides_t* v_strides, const int32_t* tables, \
+                                       int64_t table_stride, const int32_t* lengths, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t dim, \
+                                       int64_t page_size, int64_t pages, int64_t width, double scale, void* workspace,                  \
+                                       size_t workspace_bytes, void* stream, void* out, float* lse) {                                   \
+        return pa_run<ELEM>((const ELEM*)q, q_seq_stride, q_head_stride, (const ELEM*)k_pages, (const ELEM*)v_pages, k_strides, v_strides, tables, \
+                            table_stride, lengths, seqs, heads, kv_heads, dim, page_size, pages, width, scale, workspace, workspace_bytes, \
+                            stream, (ELEM*)out, lse);                                                                                   \
+    }
+
+PROFK_DEFINE_ATTENTION(bf16, __nv_bfloat16)
+PROFK_DEFINE_ATTENTION(f16, __half)
+
+int profk_pages_fork_workspace_bytes(int64_t n_old, int64_t n, int64_t pages, int64_t page_size, int64_t grow, size_t* bytes) {
+    if (!bytes || !fork_sizes_ok(n_old, n, pages, page_size, grow)) return PROFK_EINVAL;
+    *bytes = fork_workspace(n_old, n, pages, page_size, grow);
+    return PROFK_OK;
+}
+
+int profk_pages_fork(const profk_pool_t* pool, const int32_t* tables, int64_t n_old, int64_t width, int64_t table_stride, const int32_t* lengths,
+                     const int32_t* refs, int64_t pages, const int32_t* parents, int64_t n, int64_t page_size, int64_t grow, void* workspace,
+                     size_t workspace_bytes, void* stream, int32_t* out_tables, int32_t* out_lengths, int32_t* out_refs, int32_t* out_missing) {
+    if (!fork_sizes_ok(n_old, n, pages, page_size, grow) || width < 1 || width * page_size > 0x7FFFFF00ll || table_stride < 0 || !refs || !out_refs ||
+        out_refs == refs || !out_missing || (n_old > 0 && (!tables || !lengths)) || (n > 0 && (!parents || !out_tables || !out_lengths)) ||
+        (n > 0 && (out_tables == tables || out_lengths == lengths)) || !pg_pool_ok(pool) || (pool && pool->page_size != page_size))
+        return PROFK_EINVAL;
+    if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < fork_workspace(n_old, n, pages, page_size, grow)) return PROFK_EWORKSPACE;
+    const int sms = sm_count();
+    if (sms < 1) return PROFK_ECUDA;
+    char* w = static_cast<char*>(workspace);
+    auto take = [&](size_t bytes) { char* at = w; w += up(bytes); return at; };
+    PgForkParams p{};
+    p.tables = tables;
+    p.table_stride = table_stride;
+    p.lengths = lengths;
+    p.refs = refs;
+    p.parents = parents;
+    p.n_old = (int32_t)n_old;
+    p.n = (int32_t)n;
+    p.width = (int32_t)width;
+    p.pages = (int32_t)pages;
+    p.page_size = (int32_t)page_size;
+    p.grow = (int32_t)grow;
+    p.out_tables = out_tables;
+    p.out_lengths = out_lengths;
+    p.out_refs = out_refs;
+    p.out_missing = out_missing;
+    p.head = reinterpret_cast<PgPlanHead*>(take(sizeof(PgPlanHead)));
+    p.first = reinterpret_cast<int32_t*>(take((size_t)n_old * 4));
+    p.kids = reinterpret_cast<int32_t*>(take((size_t)n_old * 4));
+    p.need = reinterpret_cast<int32_t*>(take((size_t)n * 4));
+    p.fresh_cap = (int32_t)fork_fresh(n, pages, page_size, grow);
+    p.fresh = reinterpret_cast<int32_t*>(take((size_t)p.fresh_cap * 4));
+    p.moves = reinterpret_cast<PgMove*>(take((size_t)n * sizeof(PgMove)));
+    p.pool = pg_pool(pool, page_size);
+    const unsigned copiers = (unsigned)std::min<int64_t>(sms, (pages + PG_PLAN_THREADS - 1) / PG_PLAN_THREADS);
+    Launch plan(1 + copiers, PG_PLAN_THREADS, 0, stream);
+    DEC_TRY(cudaLaunchKernelEx(&plan.cfg, pages_fork_plan_kernel, p));
+    Launch work((unsigned)sms * PG_CTAS_PER_SM, PG_THREADS, 0, stream);
+    DEC_TRY(cudaLaunchKernelEx(&work.cfg, pages_fork_kernel, p));
+    return PROFK_OK;
+}
+
+int profk_pages_compact_workspace_bytes(int64_t pages, size_t* bytes) {
+    if (!bytes || pages < 1 || pages > 0x7FFF0000ll) return PROFK_EINVAL;
+    *bytes = 256 + up((size_t)(pages / 2 + 1) * sizeof(PgMove));
+    return PROFK_OK;
+}
+
+int profk_pages_compact(const profk_pool_t* pool, const int32_t* tables, int64_t n, int64_t width, int64_t table_stride, const int32_t* refs,
+                        int64_t pages, void* workspace, size_t workspace_bytes, void* stream, int32_t* out_tables, int32_t* out_refs,
+                        int32_t* out_page_map, int32_t* out_live) {
+    if (n < 0 || n > (1 << 24) || width < 1 || width > 0x7FFFFF00ll || table_stride < 0 || pages < 1 || pages > 0x7FFF0000ll || !refs || !out_refs ||
+        refs == out_refs || !out_page_map || !out_live || (n > 0 && (!tables || !out_tables || tables == out_tables)) || !pg_pool_ok(pool))
+        return PROFK_EINVAL;
+    if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < 256 + up((size_t)(pages / 2 + 1) * sizeof(PgMove))) return PROFK_EWORKSPACE;
+    const int sms = sm_count();
+    if (sms < 1) return PROFK_ECUDA;
+    PgCompactParams p{tables, table_stride, refs, (int32_t)n, (int32_t)width, (int32_t)pages, out_tables, out_refs, out_page_map, out_live,
+                      static_cast<PgPlanHead*>(workspace), reinterpret_cast<PgMove*>(static_cast<char*>(workspace) + 256), pg_pool(pool, 1)};
+    Launch plan(1, PG_PLAN_THREADS, 0, stream);
+    DEC_TRY(cudaLaunchKernelEx(&plan.cfg, pages_compact_plan_kernel, p));
+    Launch work((unsigned)sms * PG_CTAS_PER_SM, PG_THREADS, 0, stream);
+    DEC_TRY(cudaLaunchKernelEx(&work.cfg, pages_compact_kernel, p));
+    return PROFK_OK;
+}
+
+int profk_pages_copy(const profk_pool_t* pool, int64_t pages, const int32_t* src, const int32_t* dst, int64_t n, void* stream) {
+    if (!pool || !pg_pool_ok(pool) || pages < 1 || pages > 0x7FFF0000ll || n < 0 || n > 0x7FFF0000ll || (n > 0 && (!src || !dst))) return PROFK_EINVAL;
+    if (n == 0) return PROFK_OK;
+    const int sms = sm_count();
+    if (sms < 1) return PROFK_ECUDA;
+    PgCopyParams p{src, dst, (int32_t)n, (int32_t)pages, pg_pool(pool, pool->page_size)};
+    Launch l((unsigned)std::min<int64_t>((int64_t)sms * PG_CTAS_PER_SM, n * 2 * pool->layers), PG_THREADS, 0, stream);
+    DEC_TRY(cudaLaunchKernelEx(&l.cfg, pages_copy_kernel, p));
+    return PROFK_OK;
+}
+
+int profk_pages_append(const void* k, const void* v, const int64_t* k_strides, const int64_t* v_strides, void* k_pages, void* v_pages,
+                       const profk_page_strides_t* kp, const profk_page_strides_t* vp, const int32_t* tables, int64_t table_stride,
+                       const int32_t* lengths, int64_t seqs, int64_t tokens, int64_t kv_heads, int64_t row_bytes, int64_t page_size,
+                       int64_t pages, int64_t width, void* stream) {
+    if (!k || !v || !k_strides || !v_strides || !k_pages || !v_pages || !kp || !vp || !tables || !lengths || seqs < 1 || seqs > (1 << 24) || tokens < 1 ||
+        kv_heads < 1 || kv_heads > (1 << 16) || row_bytes < 16 || row_bytes > (1 << 20) || row_bytes % 16 != 0 || page_size < 1 || pages < 1 ||
+        pages > 0x7FFFFFFFll || width < 1 || width * page_size > 0x7FFFFF00ll || tokens > width * page_size || table_stride < 0 || !aligned_to(k, 16) ||
+        !aligned_to(v, 16) || !aligned_to(k_pages, 16) || !aligned_to(v_pages, 16))
+        return PROFK_EINVAL;
+    for (const int64_t x : {k_strides[0], k_strides[1], k_strides[2], v_strides[0], v_strides[1], v_strides[2], kp->page, kp->head, kp->token, vp->page,
+                            vp->head, vp->token})
+        if (x % 16 != 0) return PROFK_EINVAL;
+    const int sms = sm_count();
+    if (sms < 1) return PROFK_ECUDA;
+    PgAppendParams p{static_cast<const char*>(k), static_cast<const char*>(v), k_strides[0], k_strides[1], k_strides[2], v_strides[0], v_strides[1],
+                     v_strides[2], static_cast<char*>(k_pages), static_cast<char*>(v_pages), kp->page, kp->head, kp->token, vp->page, vp->head, vp->token,
+                     tables, table_stride, lengths, (int32_t)seqs, (int32_t)tokens, (int32_t)kv_heads, (int32_t)row_bytes, (int32_t)page_size,
+                     (int32_t)pages, (int32_t)width};
+    const int64_t n = seqs * tokens * kv_heads * (row_bytes / 16);
+    Launch l((unsigned)std::min<int64_t>((int64_t)sms * 8, (n + PG_THREADS - 1) / PG_THREADS), PG_THREADS, 0, stream);
+    DEC_TRY(cudaLaunchKernelEx(&l.cfg, pages_append_kernel, p));
+    return PROFK_OK;
+}
 
 }  // extern "C"

@@ -1,0 +1,463 @@
+// Attention of one new token per sequence over a paged key-value cache:
+//   out_h = sum_j p_j v_j,   p = softmax_j(scale q_h . k_j),   lse_h = ln sum_j e^(scale q_h . k_j),   j < length.
+//
+// The cache is read once and every key meets the few query heads that share it, so the kernel is bound by HBM (4 dim
+// bytes and 4 dim G operations per token and key-value head).  The work is the list of (sequence, key-value head, tile of
+// 64 tokens), cut into one contiguous share per CTA whatever the lengths; a CTA that holds only part of a (sequence,
+// head) leaves its running maximum, sum and unnormalised output for a second, small kernel that joins the parts in order.
+//
+// Inside a CTA each of four warps takes 16 tokens of a tile through a ring of its own in shared memory (cp.async; no
+// barrier until the (sequence, head) ends), and multiplies with the warp-level matrix instruction: 16 query heads x 16
+// tokens is far below what a tcgen05 tile wants, and the tensor pipe is not what bounds it.
+#pragma once
+
+#include "logits.cuh"
+
+namespace profk {
+
+constexpr int PA_WARPS = 4;
+constexpr int PA_THREADS = PA_WARPS * 32;
+constexpr int PA_WARP_TOKENS = 16;
+constexpr int PA_TILE = PA_WARPS * PA_WARP_TOKENS;      // tokens per tile
+constexpr int PA_ROWS = 16;                             // query heads per pass over a key-value head
+constexpr int PA_MERGE_COLS = 64;
+constexpr int PA_MERGE_STRIDE = PA_MERGE_COLS + 8;      // floats; 8 rows x 4 column pairs then fall on 32 banks
+
+template <int D> struct PaShape {
+    static constexpr int STAGES = D == 64 ? 6 : 3;      // of the ring: 96 KB per CTA up to D = 128, 192 KB for 256
+    static constexpr int CTAS = D == 256 ? 1 : 2;       // per SM
+    static constexpr int STAGE_BYTES = PA_WARP_TOKENS * D * 2 * 2;                       // keys, then values, of a warp
+    static constexpr size_t SMEM = (size_t)PA_WARPS * STAGES * STAGE_BYTES;
+    static constexpr int SLOT = PA_ROWS * (D + 2);      // floats of a part: output, maxima, sums
+};
+
+struct PaMeta { int32_t seq, stream, last, unused; };   // the parts of (seq, stream): this CTA's to CTA `last`'s; seq < 0: none
+
+struct PaParams {
+    const void* q;
+    const void* k;
+    const void* v;
+    int64_t q_seq, q_head;                              // strides in elements
+    int64_t k_page, k_head, k_token, v_page, v_head, v_token;
+    const int32_t* tables;
+    int64_t table_stride;
+    const int32_t* lengths;
+    int32_t seqs, heads, kv_heads, group, dim, page_size, pages, width;
+    int32_t blocks, rows;                               // passes per key-value head, query heads per pass (<= PA_ROWS)
+    float scale;
+    void* out;                                          // seqs x heads x dim
+    float* lse;                                         // seqs x heads
+    float* parts;                                       // two slots per CTA: of the share's first and of its last stream
+    PaMeta* meta;                                       // one per CTA
+};
+
+template <typename T>
+__device__ __forceinline__ void pa_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void pa_mma<__nv_bfloat16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void pa_mma<__half>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Two floats to a pair of T (the first in the low half), and what that rounding left off as another pair.
+template <typename T>
+__device__ __forceinline__ uint32_t pa_pack(float a, float b);
+template <>
+__device__ __forceinline__ uint32_t pa_pack<__nv_bfloat16>(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <>
+__device__ __forceinline__ uint32_t pa_pack<__half>(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <typename T>
+__device__ __forceinline__ float2 pa_unpack(uint32_t w);
+template <>
+__device__ __forceinline__ float2 pa_unpack<__nv_bfloat16>(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+template <>
+__device__ __forceinline__ float2 pa_unpack<__half>(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+
+__device__ __forceinline__ void pa_ldmatrix(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void pa_ldmatrix_trans(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// 16 bytes to shared memory, or 16 zero bytes (nothing is read then).
+__device__ __forceinline__ void pa_cp_async(uint32_t smem, const void* gmem, bool read) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(gmem), "r"(read ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void pa_cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void pa_cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ int32_t pa_length(const PaParams& p, int32_t seq) {
+    const int64_t room = (int64_t)p.width * p.page_size;
+    return (int32_t)max((int64_t)0, min((int64_t)p.lengths[seq], room));
+}
+
+// A place in the list of tiles.
+struct PaCursor {
+    int32_t seq, stream, tile, tiles, len;
+    // To the first tile of the next (sequence, head), past empty sequences.
+    __device__ __forceinline__ void next(const PaParams& p, int32_t streams) {
+        if (++tile < tiles) return;
+        tile = 0;
+        if (++stream < streams) return;
+        stream = 0;
+        do {
+            if (++seq >= p.seqs) { tiles = 0; return; }
+            len = pa_length(p, seq);
+            tiles = (len + PA_TILE - 1) / PA_TILE;
+        } while (tiles == 0);
+    }
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_kernel(const PaParams p) {
+    using Shape = PaShape<D>;
+    constexpr int STAGES = Shape::STAGES, CH = D / 8, KSTEPS = D / 16, NT = D / 8;
+    constexpr int ROWS_PER_LOAD = 32 / CH > 0 ? 32 / CH : 1;                 // token rows that one warp-wide copy covers
+    constexpr int LOADS = PA_WARP_TOKENS / ROWS_PER_LOAD;
+    extern __shared__ __align__(128) unsigned char pa_dyn[];
+    __shared__ __align__(16) float s_merge[PA_WARPS][8][PA_MERGE_STRIDE];
+    __shared__ float s_max[PA_WARPS][PA_ROWS], s_sum[PA_WARPS][PA_ROWS];
+    __shared__ uint32_t s_mask[PA_WARPS][STAGES];
+    __shared__ long long s_scan[PA_WARPS];
+    __shared__ long long s_start;
+    __shared__ int32_t s_seq;
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int g = lane >> 2, quad = lane & 3;
+    const int32_t streams = p.kv_heads * p.blocks;
+    pdl_wait();
+    pdl_launch_dependents();
+
+    // where the sequences' tiles begin in the list: each thread sums a run of sequences
+    const int32_t per = (p.seqs + PA_THREADS - 1) / PA_THREADS;
+    const int32_t run0 = min(p.seqs, tid * per), run1 = min(p.seqs, run0 + per);
+    long long mine = 0;
+    for (int32_t s = run0; s < run1; ++s) mine += (long long)((pa_length(p, s) + PA_TILE - 1) / PA_TILE) * streams;
+    long long incl = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long n = __shfl_up_sync(FULL_MASK, incl, d);
+        if (lane >= d) incl += n;
+    }
+    if (lane == 31) s_scan[warp] = incl;
+    __syncthreads();
+    long long total = 0;
+#pragma unroll
+    for (int w = 0; w < PA_WARPS; ++w) {
+        if (w < warp) incl += s_scan[w];
+        total += s_scan[w];
+    }
+    // sequences without tokens
+    for (int32_t s = blockIdx.x; s < p.seqs; s += gridDim.x) {
+        if (pa_length(p, s) > 0) continue;
+        T* o = reinterpret_cast<T*>(p.out) + (int64_t)s * p.heads * p.dim;
+        for (int32_t i = tid; i < p.heads * p.dim; i += PA_THREADS) o[i] = Logit<T>::from_float(0.f);
+        for (int32_t i = tid; i < p.heads; i += PA_THREADS) p.lse[(int64_t)s * p.heads + i] = -INFINITY;
+    }
+    const long long ctas = min((long long)gridDim.x, total);                  // every share then has a tile
+    if ((long long)blockIdx.x >= ctas) {
+        if (tid == 0) p.meta[blockIdx.x] = PaMeta{-1, 0, 0, 0};
+        return;
+    }
+    const long long u0 = total * blockIdx.x / ctas, u1 = total * (blockIdx.x + 1) / ctas;
+    if (incl - mine <= u0 && u0 < incl) {
+        long long at = incl - mine;
+        int32_t s = run0;
+        for (;; ++s) {
+            const long long n = (long long)((pa_length(p, s) + PA_TILE - 1) / PA_TILE) * streams;
+            if (u0 < at + n) break;
+            at += n;
+        }
+        s_seq = s;
+        s_start = at;
+    }
+    __syncthreads();
+    PaCursor work;
+    work.seq = s_seq;
+    work.len = pa_length(p, work.seq);
+    work.tiles = (work.len + PA_TILE - 1) / PA_TILE;
+    work.stream = (int32_t)((u0 - s_start) / work.tiles);
+    work.tile = (int32_t)((u0 - s_start) % work.tiles);
+    const uint32_t count = (uint32_t)(u1 - u0);
+
+    // loading side
+    PaCursor load = work;
+    uint32_t loaded = 0;
+    int load_stage = 0;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(pa_dyn) + warp * STAGES * Shape::STAGE_BYTES;
+    const int chunk = lane % CH, row0 = lane / CH;                            // (CH = 32: one row per copy)
+    const bool chunk_in = chunk * 8 < p.dim;
+    auto page_of = [&](const PaCursor& c) -> int32_t {                        // of the lane's token; -1: no token, or no page
+        const int32_t t = c.tile * PA_TILE + warp * PA_WARP_TOKENS + (lane & 15);
+        if (t >= c.len) return -1;
+        const int32_t page = p.tables[c.seq * p.table_stride + t / p.page_size];
+        return page >= 0 && page < p.pages ? page : -1;
+    };
+    int32_t page = page_of(load);
+    auto load_tile = [&]() {
+        if (loaded < count) {
+            const int32_t t = load.tile * PA_TILE + warp * PA_WARP_TOKENS + (lane & 15);
+            const int32_t slot = t % p.page_size, head = load.stream / p.blocks;
+            const bool in = page >= 0;
+            const int64_t k_off = in ? page * p.k_page + head * p.k_head + slot * p.k_token : 0;
+            const int64_t v_off = in ? page * p.v_page + head * p.v_head + slot * p.v_token : 0;
+            const uint32_t mask = __ballot_sync(FULL_MASK, in) & 0xFFFFu;
+            if (lane == 0) s_mask[warp][load_stage] = mask;
+            ++loaded;
+            load.next(p, streams);
+            if (loaded < count) page = page_of(load);                         // ready by the next call
+            const uint32_t base = ring + load_stage * Shape::STAGE_BYTES;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int row = i * ROWS_PER_LOAD + row0;
+                const int64_t ko = __shfl_sync(FULL_MASK, k_off, row), vo = __shfl_sync(FULL_MASK, v_off, row);
+                const bool read = chunk_in && (mask >> row & 1);
+                const uint32_t to = base + row * (D * 2) + ((chunk ^ (row & 7)) << 4);
+                pa_cp_async(to, reinterpret_cast<const T*>(p.k) + ko + (read ? chunk * 8 : 0), read);
+                pa_cp_async(to + PA_WARP_TOKENS * D * 2, reinterpret_cast<const T*>(p.v) + vo + (read ? chunk * 8 : 0), read);
+            }
+        }
+        pa_cp_commit();
+        load_stage = load_stage + 1 == STAGES ? 0 : load_stage + 1;
+    };
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) load_tile();
+
+    const float c = p.scale * LOG2E;
+    uint32_t qf[KSTEPS][4];
+    float o[NT][4], m[2], l[2];
+    bool fresh = true, whole = work.tile == 0;                                // a new stream begins / it began in this share
+    int stage = 0;
+    PaMeta meta{-1, 0, 0, 0};
+    for (uint32_t done = 0; done < count; ++done) {
+        load_tile();
+        const int32_t head0 = (work.stream / p.blocks) * p.group + (work.stream % p.blocks) * p.rows;
+        const int32_t rows = min(p.rows, (work.stream / p.blocks + 1) * p.group - head0);
+        if (fresh) {
+            fresh = false;
+            m[0] = m[1] = LOWEST;
+            l[0] = l[1] = 0.f;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+            const T* q = reinterpret_cast<const T*>(p.q) + work.seq * p.q_seq + head0 * p.q_head;
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = g + (i & 1) * 8, col = ks * 16 + quad * 2 + (i >> 1) * 8;
+                    qf[ks][i] = r < rows && col < p.dim ? *reinterpret_cast<const uint32_t*>(q + r * p.q_head + col) : 0u;
+                }
+        }
+        pa_cp_wait<STAGES - 1>();
+        __syncwarp();
+        const uint32_t kb = ring + stage * Shape::STAGE_BYTES, vb = kb + PA_WARP_TOKENS * D * 2;
+        // scores: 16 heads x 16 tokens
+        float s[2][4] = {};
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) {
+            const int row = (lane & 7) + ((lane >> 4) << 3), ch = ks * 2 + ((lane >> 3) & 1);
+            uint32_t b[4];
+            pa_ldmatrix(b, kb + row * (D * 2) + ((ch ^ (row & 7)) << 4));
+            pa_mma<T>(s[0], qf[ks], b[0], b[1]);
+            pa_mma<T>(s[1], qf[ks], b[2], b[3]);
+        }
+        const uint32_t mask = s_mask[warp][stage];
+        if (mask != 0xFFFFu) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!(mask >> (n * 8 + quad * 2 + (i & 1)) & 1)) s[n][i] = -INFINITY;
+        }
+        // running maximum: of row g (i = 0, 1) and of row g + 8 (i = 2, 3)
+        float top[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            top[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
+            top[h] = fmaxf(top[h], __shfl_xor_sync(FULL_MASK, top[h], 1));
+            top[h] = fmaxf(top[h], __shfl_xor_sync(FULL_MASK, top[h], 2));
+        }
+        if (__any_sync(FULL_MASK, top[0] > m[0] || top[1] > m[1])) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float to = fmaxf(m[h], top[h]), f = exp2_approx((m[h] - to) * c);
+                m[h] = to;
+                l[h] *= f;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) { o[n][2 * h] *= f; o[n][2 * h + 1] *= f; }
+            }
+        }
+        float e[2][4];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[n][i] = exp2_approx((s[n][i] - m[i >> 1]) * c);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) l[h] += (e[0][2 * h] + e[0][2 * h + 1]) + (e[1][2 * h] + e[1][2 * h + 1]);
+        // The probabilities enter the second product as two numbers of the cache's type, the rounded one and what the
+        // rounding left off: one alone would add an error as large as the rounding of the output.
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float a = e[i >> 1][(i & 1) * 2], b = e[i >> 1][(i & 1) * 2 + 1];
+            hi[i] = pa_pack<T>(a, b);
+            const float2 r = pa_unpack<T>(hi[i]);
+            lo[i] = pa_pack<T>(a - r.x, b - r.y);
+        }
+#pragma unroll
+        for (int n = 0; n < NT; n += 2) {
+            const int row = lane & 15, ch = n + (lane >> 4);
+            uint32_t b[4];
+            pa_ldmatrix_trans(b, vb + row * (D * 2) + ((ch ^ (row & 7)) << 4));
+            pa_mma<T>(o[n], hi, b[0], b[1]);
+            pa_mma<T>(o[n + 1], hi, b[2], b[3]);
+            pa_mma<T>(o[n], lo, b[0], b[1]);
+            pa_mma<T>(o[n + 1], lo, b[2], b[3]);
+        }
+        __syncwarp();                                                         // the stage may be filled again
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+
+        const bool stream_ends = work.tile + 1 == work.tiles;
+        if (stream_ends || done + 1 == count) {
+            // join the four warps
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                l[h] += __shfl_xor_sync(FULL_MASK, l[h], 1);
+                l[h] += __shfl_xor_sync(FULL_MASK, l[h], 2);
+                if (quad == 0) { s_max[warp][g + 8 * h] = m[h]; s_sum[warp][g + 8 * h] = l[h]; }
+            }
+            const bool final = whole && stream_ends;
+            float* part = p.parts + ((int64_t)blockIdx.x * 2 + (whole ? 1 : 0)) * Shape::SLOT;
+            const int64_t out_row = (int64_t)work.seq * p.heads + head0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (h * 8 >= rows) break;
+#pragma unroll
+                for (int half = 0; half < D / PA_MERGE_COLS; ++half) {
+#pragma unroll
+                    for (int n = 0; n < PA_MERGE_COLS / 8; ++n) {
+                        const int nn = half * (PA_MERGE_COLS / 8) + n;
+                        *reinterpret_cast<float2*>(&s_merge[warp][g][n * 8 + quad * 2]) = make_float2(o[nn][2 * h], o[nn][2 * h + 1]);
+                    }
+                    __syncthreads();
+                    const int r = tid / 16, col = (tid % 16) * 4, row = h * 8 + r, at = half * PA_MERGE_COLS + col;
+                    float top_row = LOWEST, sum = 0.f;
+                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int w = 0; w < PA_WARPS; ++w) top_row = fmaxf(top_row, s_max[w][row]);
+#pragma unroll
+                    for (int w = 0; w < PA_WARPS; ++w) {
+                        const float f = exp2_approx((s_max[w][row] - top_row) * c);
+                        const float4 x = *reinterpret_cast<const float4*>(&s_merge[w][r][col]);
+                        sum = fmaf(f, s_sum[w][row], sum);
+                        acc.x = fmaf(f, x.x, acc.x);
+                        acc.y = fmaf(f, x.y, acc.y);
+                        acc.z = fmaf(f, x.z, acc.z);
+                        acc.w = fmaf(f, x.w, acc.w);
+                    }
+                    if (row < rows) {
+                        if (final) {
+                            if (at < p.dim) {
+                                const float inv = sum == 0.f ? 0.f : 1.f / sum;      // nothing held a token: zeros
+                                const uint2 w2 = make_uint2(pa_pack<T>(acc.x * inv, acc.y * inv), pa_pack<T>(acc.z * inv, acc.w * inv));
+                                *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.out) + (out_row + row) * p.dim + at) = w2;
+                            }
+                            if (at == 0) p.lse[out_row + row] = sum == 0.f ? -INFINITY : fmaf(top_row, p.scale, logf(sum));
+                        } else {
+                            *reinterpret_cast<float4*>(part + row * D + at) = acc;
+                            if (at == 0) { part[PA_ROWS * D + row] = top_row; part[PA_ROWS * (D + 1) + row] = sum; }
+                        }
+                    }
+                    __syncthreads();
+                }
+            }
+            if (whole && !stream_ends) {
+                // the stream goes on in the next CTA's share: this one names the parts
+                const long long end = u0 + done + (work.tiles - work.tile);   // the first unit behind the stream
+                meta = PaMeta{work.seq, work.stream, (int32_t)((end * ctas + total - 1) / total - 1), 0};
+            }
+            fresh = whole = true;
+        }
+        work.next(p, streams);
+    }
+    pa_cp_wait<0>();
+    if (tid == 0) p.meta[blockIdx.x] = meta;
+}
+
+// Joins the parts of one head of a stream that several CTAs share.  grid: (CTAs of the first kernel, PA_ROWS).
+constexpr int PJ_THREADS = 256;
+template <typename T, int D>
+__global__ void __launch_bounds__(PJ_THREADS) paged_attention_join_kernel(const PaParams p) {
+    using Shape = PaShape<D>;
+    constexpr int LANES = D / 4, GROUPS = PJ_THREADS / LANES;                 // threads per part, parts at a time
+    __shared__ __align__(16) float s_acc[GROUPS][D];
+    __shared__ float s_red[16];
+    pdl_wait();
+    pdl_launch_dependents();
+    const PaMeta meta = p.meta[blockIdx.x];
+    if (meta.seq < 0) return;
+    const int32_t head0 = (meta.stream / p.blocks) * p.group + (meta.stream % p.blocks) * p.rows;
+    const int row = blockIdx.y, tid = threadIdx.x;
+    if (row >= min(p.rows, (meta.stream / p.blocks + 1) * p.group - head0)) return;
+    const int32_t first = blockIdx.x, n = meta.last - first + 1;
+    auto slot = [&](int32_t i) { return p.parts + ((int64_t)(first + i) * 2 + (i == 0 ? 1 : 0)) * Shape::SLOT; };
+    const float c = p.scale * LOG2E;
+    float top = LOWEST;
+    for (int32_t i = tid; i < n; i += PJ_THREADS) top = fmaxf(top, slot(i)[PA_ROWS * D + row]);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, d));
+    if ((tid & 31) == 0) s_red[tid >> 5] = top;
+    __syncthreads();
+    for (int w = 0; w < PJ_THREADS / 32; ++w) top = fmaxf(top, s_red[w]);
+    const int group = tid / LANES, col = (tid % LANES) * 4;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+    for (int32_t i = group; i < n; i += GROUPS) {
+        const float* s = slot(i);
+        const float f = exp2_approx((s[PA_ROWS * D + row] - top) * c);
+        const float4 x = *reinterpret_cast<const float4*>(s + row * D + col);
+        sum = fmaf(f, s[PA_ROWS * (D + 1) + row], sum);
+        acc.x = fmaf(f, x.x, acc.x);
+        acc.y = fmaf(f, x.y, acc.y);
+        acc.z = fmaf(f, x.z, acc.z);
+        acc.w = fmaf(f, x.w, acc.w);
+    }
+    *reinterpret_cast<float4*>(&s_acc[group][col]) = acc;
+    __syncthreads();
+    if (col == 0) s_red[group] = sum;                                         // (GROUPS <= 16; top has been read)
+    __syncthreads();
+    if (tid < LANES) {
+        float total = 0.f;
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int q = 0; q < GROUPS; ++q) {
+            const float4 x = *reinterpret_cast<const float4*>(&s_acc[q][col]);
+            total += s_red[q];
+            acc.x += x.x;
+            acc.y += x.y;
+            acc.z += x.z;
+            acc.w += x.w;
+        }
+        const int64_t out_row = (int64_t)meta.seq * p.heads + head0 + row;
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        if (col < p.dim)
+            *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.out) + out_row * p.dim + col) =
+                make_uint2(pa_pack<T>(acc.x * inv, acc.y * inv), pa_pack<T>(acc.z * inv, acc.w * inv));
+        if (tid == 0) p.lse[out_row] = total == 0.f ? -INFINITY : fmaf(top, p.scale, logf(total));
+    }
+}
+
+}  // namespace profk

@@ -1,0 +1,384 @@
+// Pages of a key-value cache that sequences share: forking, growing, releasing, compacting, copying, appending.
+//
+// A sequence is a row of a page table and a length; refs[p] counts the table entries that hold page p, 0 means free.
+// What a call decides (who keeps a page, which free page goes where) is settled by one small kernel with prefix sums, in
+// an order that the definition gives, so that the result does not depend on timing; a second kernel over the whole
+// device then writes tables and counts and moves the pages' bytes.
+#pragma once
+
+#include "select_sort.cuh"
+
+namespace profk {
+
+constexpr int PG_PLAN_THREADS = 1024;
+constexpr int PG_THREADS = 256;
+constexpr int PG_UNROLL = 4;              // 16-byte vectors per thread in flight
+
+// Where a pool's bytes lie; strides in bytes, all multiples of 16.
+struct PgPool {
+    char* base;                           // null: no pool, tables and counts only
+    int32_t layers, kv_heads, page_size;
+    int32_t row_bytes;                    // of one token and head
+    int64_t layer, kv, page, head, token;
+};
+
+struct PgMove { int32_t src, dst, tokens, unused; };
+
+struct PgPlanHead {                       // first words of the workspace
+    int32_t moves;                        // pages to copy
+    int32_t live;                         // compaction: live pages
+    int32_t fresh;                        // fork: free pages found
+    int32_t unused;
+};
+
+struct PgForkParams {
+    const int32_t* tables;
+    int64_t table_stride;
+    const int32_t* lengths;
+    const int32_t* refs;
+    const int32_t* parents;
+    int32_t n_old, n, width, pages, page_size, grow;
+    int32_t* out_tables;                  // n x width
+    int32_t* out_lengths;
+    int32_t* out_refs;
+    int32_t* out_missing;
+    PgPlanHead* head;
+    int32_t* first;                       // n_old: lowest child, or n
+    int32_t* kids;                        // n_old
+    int32_t* need;                        // n: number of the sequence's first fresh page
+    int32_t* fresh;                       // lowest free pages, ascending
+    int32_t fresh_cap;
+    PgMove* moves;                        // n
+    PgPool pool;
+};
+
+__device__ __forceinline__ int32_t pg_length(const int32_t* lengths, int32_t s, int32_t width, int32_t page_size) {
+    const int64_t room = (int64_t)width * page_size;
+    return (int32_t)max((int64_t)0, min((int64_t)lengths[s], room));
+}
+__device__ __forceinline__ int32_t pg_ceil(int64_t tokens, int32_t page_size) { return (int32_t)((tokens + page_size - 1) / page_size); }
+
+struct PgChild {
+    int32_t parent, old, length, have, want, fill, beyond;   // parent < 0: an empty sequence; beyond: pages past the table
+    bool copy;
+    __device__ __forceinline__ PgChild(const PgForkParams& p, int32_t i) {
+        parent = p.parents[i];
+        if (parent < 0 || parent >= p.n_old) parent = -1;
+        old = parent >= 0 ? pg_length(p.lengths, parent, p.width, p.page_size) : 0;
+        const int64_t wanted = (int64_t)old + p.grow;
+        length = (int32_t)min(wanted, (int64_t)p.width * p.page_size);
+        have = pg_ceil(old, p.page_size);
+        want = pg_ceil(length, p.page_size);
+        beyond = pg_ceil(wanted, p.page_size) - want;
+        fill = old % p.page_size;
+        copy = parent >= 0 && fill > 0 && p.first[parent] != i;
+    }
+    __device__ __forceinline__ int32_t fresh_from() const { return have - (copy ? 1 : 0); }   // columns from here on are fresh
+};
+
+// Block-wide sum of the numbers before this thread's, and of all of them (1024 threads).
+__device__ __forceinline__ uint32_t pg_scan(uint32_t v, uint32_t* warp_sums, uint32_t* total) {
+    const uint32_t incl = block_scan_any(v, warp_sums);
+    __shared__ uint32_t s_total;
+    if (threadIdx.x == PG_PLAN_THREADS - 1) s_total = incl;
+    __syncthreads();
+    *total = s_total;
+    __syncthreads();
+    return incl - v;
+}
+
+// Block 0 plans; the others copy the counts, which the second kernel then changes.
+__global__ void __launch_bounds__(PG_PLAN_THREADS) pages_fork_plan_kernel(const PgForkParams p) {
+    __shared__ uint32_t warp_sums[32];
+    __shared__ int32_t s_moves;
+    const int tid = threadIdx.x;
+    pdl_wait();
+    pdl_launch_dependents();
+    if (blockIdx.x > 0) {
+        for (int64_t i = (int64_t)(blockIdx.x - 1) * PG_PLAN_THREADS + tid; i < p.pages; i += (int64_t)(gridDim.x - 1) * PG_PLAN_THREADS)
+            p.out_refs[i] = p.refs[i];
+        return;
+    }
+    if (tid == 0) s_moves = 0;
+    for (int32_t s = tid; s < p.n_old; s += PG_PLAN_THREADS) { p.first[s] = p.n; p.kids[s] = 0; }
+    __syncthreads();
+    for (int32_t i = tid; i < p.n; i += PG_PLAN_THREADS) {
+        const int32_t parent = p.parents[i];
+        if (parent >= 0 && parent < p.n_old) {
+            atomicMin(&p.first[parent], i);
+            atomicAdd(&p.kids[parent], 1);
+        }
+    }
+    __syncthreads();
+    // how many fresh pages each new sequence needs, numbered through
+    uint32_t total = 0, beyond = 0;
+    for (int32_t i0 = 0; i0 < p.n; i0 += PG_PLAN_THREADS) {
+        const int32_t i = i0 + tid;
+        uint32_t mine = 0, sum = 0;
+        if (i < p.n) {
+            const PgChild c(p, i);
+            mine = (uint32_t)(c.want - c.fresh_from());
+            beyond += (uint32_t)c.beyond;
+            p.out_lengths[i] = c.length;
+        }
+        const uint32_t before = pg_scan(mine, warp_sums, &sum);
+        if (i < p.n) p.need[i] = (int32_t)(total + before);
+        total += sum;
+    }
+    // the lowest-numbered free pages
+    uint32_t found = 0;
+    for (int32_t c0 = 0; c0 < p.pages && found < total; c0 += 4 * PG_PLAN_THREADS) {
+        const int32_t at = c0 + 4 * tid;
+        bool is_free[4];
+        uint32_t mine = 0, sum = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            is_free[j] = at + j < p.pages && p.refs[at + j] <= 0;
+            mine += is_free[j];
+        }
+        uint32_t number = found + pg_scan(mine, warp_sums, &sum);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (is_free[j]) {
+                if (number < total) p.fresh[number] = at + j;
+                ++number;
+            }
+        found += sum;
+    }
+    found = min(found, total);
+    __syncthreads();
+    // the partly filled pages that are copied
+    for (int32_t i = tid; i < p.n; i += PG_PLAN_THREADS) {
+        const PgChild c(p, i);
+        if (!c.copy) continue;
+        const int32_t src = p.tables[c.parent * p.table_stride + c.have - 1], number = p.need[i];
+        if (number < (int32_t)found && src >= 0 && src < p.pages) {
+            const int32_t slot = atomicAdd(&s_moves, 1);                       // (their order is of no consequence)
+            p.moves[slot] = PgMove{src, p.fresh[number], c.fill, 0};
+        }
+    }
+    uint32_t all_beyond;
+    pg_scan(beyond, warp_sums, &all_beyond);
+    if (tid == 0) {
+        *p.head = PgPlanHead{s_moves, 0, (int32_t)found, 0};
+        *p.out_missing = (int32_t)(total - found + all_beyond);
+    }
+}
+
+// One page of one layer's keys or values, by the whole CTA: `tokens` tokens of every head.
+__device__ __forceinline__ void pg_copy(const PgPool& pool, int32_t src, int32_t dst, int32_t tokens, int32_t plane) {
+    char* base = pool.base + (plane >> 1) * pool.layer + (plane & 1) * pool.kv;
+    const char* from = base + src * pool.page;
+    char* to = base + dst * pool.page;
+    // runs of bytes that lie together: all tokens of a head, all heads of a token, or neither
+    int64_t run_stride = pool.token, outer_stride = pool.head;
+    uint32_t run = (uint32_t)pool.row_bytes / 16, runs = (uint32_t)tokens, outer = (uint32_t)pool.kv_heads;
+    if (pool.token == pool.row_bytes) {
+        run *= (uint32_t)tokens;
+        runs = 1;
+    } else if (pool.head == pool.row_bytes) {
+        run *= (uint32_t)pool.kv_heads;
+        outer = 1;
+    }
+    const uint32_t n = run * runs * outer;
+    auto offset = [&](uint32_t i) {
+        const uint32_t r = i / run, o = r / runs;
+        return (int64_t)o * outer_stride + (int64_t)(r - o * runs) * run_stride + (int64_t)(i - r * run) * 16;
+    };
+    for (uint32_t i0 = threadIdx.x; i0 < n; i0 += PG_THREADS * PG_UNROLL) {
+        uint4 x[PG_UNROLL];
+        int64_t at[PG_UNROLL];
+#pragma unroll
+        for (int u = 0; u < PG_UNROLL; ++u) {
+            const uint32_t i = i0 + u * PG_THREADS;
+            if (i < n) {
+                at[u] = offset(i);
+                x[u] = *reinterpret_cast<const uint4*>(from + at[u]);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < PG_UNROLL; ++u)
+            if (i0 + u * PG_THREADS < n) *reinterpret_cast<uint4*>(to + at[u]) = x[u];
+    }
+}
+
+// The copies of a plan; no page is both read and written by them.
+__device__ __forceinline__ void pg_copy_all(const PgPool& pool, const PgMove* moves, int32_t n) {
+    if (!pool.base) return;
+    const int32_t planes = 2 * pool.layers;
+    for (int64_t unit = blockIdx.x; unit < (int64_t)n * planes; unit += gridDim.x) {
+        const PgMove m = moves[unit / planes];
+        pg_copy(pool, m.src, m.dst, m.tokens, (int32_t)(unit % planes));
+    }
+}
+
+__global__ void __launch_bounds__(PG_THREADS) pages_fork_kernel(const PgForkParams p) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const PgPlanHead head = *p.head;
+    const int64_t step = (int64_t)gridDim.x * PG_THREADS, me = (int64_t)blockIdx.x * PG_THREADS + threadIdx.x;
+    for (int64_t e = me; e < (int64_t)p.n * p.width; e += step) {
+        const int32_t i = (int32_t)(e / p.width), col = (int32_t)(e % p.width);
+        const PgChild c(p, i);
+        int32_t page = -1;
+        if (col < c.want) {
+            if (col < c.fresh_from()) {
+                page = p.tables[c.parent * p.table_stride + col];
+                if (page < 0 || page >= p.pages) page = -1;
+            } else {
+                const int32_t number = p.need[i] + col - c.fresh_from();
+                if (number < head.fresh) {
+                    page = p.fresh[number];
+                    atomicAdd(&p.out_refs[page], 1);
+                }
+            }
+        }
+        p.out_tables[e] = page;
+    }
+    // An old sequence held each of its pages once; its children hold the full ones once each, the first of them the
+    // partly filled one too.
+    for (int64_t e = me; e < (int64_t)p.n_old * p.width; e += step) {
+        const int32_t s = (int32_t)(e / p.width), col = (int32_t)(e % p.width);
+        const int32_t len = pg_length(p.lengths, s, p.width, p.page_size), kids = p.kids[s];
+        if (col >= pg_ceil(len, p.page_size)) continue;
+        const bool partial = col == len / p.page_size;
+        const int32_t change = (partial ? min(kids, 1) : kids) - 1;
+        if (change == 0) continue;
+        const int32_t page = p.tables[s * p.table_stride + col];
+        if (page >= 0 && page < p.pages) atomicAdd(&p.out_refs[page], change);
+    }
+    pg_copy_all(p.pool, p.moves, head.moves);
+}
+
+// ---- compaction ------------------------------------------------------------------------------
+
+struct PgCompactParams {
+    const int32_t* tables;
+    int64_t table_stride;
+    const int32_t* refs;
+    int32_t n, width, pages;
+    int32_t* out_tables;                  // n x width
+    int32_t* out_refs;
+    int32_t* page_map;
+    int32_t* out_live;
+    PgPlanHead* head;
+    PgMove* moves;                        // pages / 2
+    PgPool pool;
+};
+
+__global__ void __launch_bounds__(PG_PLAN_THREADS) pages_compact_plan_kernel(const PgCompactParams p) {
+    __shared__ uint32_t warp_sums[32];
+    const int tid = threadIdx.x;
+    pdl_wait();
+    pdl_launch_dependents();
+    uint32_t mine = 0, live = 0;
+    for (int32_t i = tid; i < p.pages; i += PG_PLAN_THREADS) mine += p.refs[i] > 0;
+    pg_scan(mine, warp_sums, &live);
+    // live pages behind the first `live` go to the free ones among them, both in ascending order
+    uint32_t holes = 0, movers = 0;
+    for (int32_t c0 = 0; c0 < p.pages; c0 += 4 * PG_PLAN_THREADS) {
+        const int32_t at = c0 + 4 * tid;
+        uint32_t n_holes = 0, n_movers = 0, sum_holes = 0, sum_movers = 0;
+        int32_t ref[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            ref[j] = at + j < p.pages ? p.refs[at + j] : 0;
+            const bool held = ref[j] > 0, low = at + j < (int32_t)live;
+            n_holes += low && !held;
+            n_movers += !low && held;
+            if (at + j < p.pages) {
+                p.out_refs[at + j] = low && held ? ref[j] : 0;
+                p.page_map[at + j] = held ? at + j : -1;
+            }
+        }
+        uint32_t hole = holes + pg_scan(n_holes, warp_sums, &sum_holes), mover = movers + pg_scan(n_movers, warp_sums, &sum_movers);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool held = ref[j] > 0, low = at + j < (int32_t)live;
+            if (low && !held) p.moves[hole++].dst = at + j;
+            if (!low && held) p.moves[mover++].src = at + j;
+        }
+        holes += sum_holes;
+        movers += sum_movers;
+    }
+    __syncthreads();
+    for (uint32_t i = tid; i < movers; i += PG_PLAN_THREADS) {
+        const int32_t src = p.moves[i].src, dst = p.moves[i].dst;
+        p.moves[i].tokens = p.pool.page_size;
+        p.page_map[src] = dst;
+        p.out_refs[dst] = p.refs[src];
+    }
+    if (tid == 0) {
+        *p.head = PgPlanHead{(int32_t)movers, (int32_t)live, 0, 0};
+        *p.out_live = (int32_t)live;
+    }
+}
+
+__global__ void __launch_bounds__(PG_THREADS) pages_compact_kernel(const PgCompactParams p) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int64_t step = (int64_t)gridDim.x * PG_THREADS, me = (int64_t)blockIdx.x * PG_THREADS + threadIdx.x;
+    for (int64_t e = me; e < (int64_t)p.n * p.width; e += step) {
+        const int32_t page = p.tables[e / p.width * p.table_stride + e % p.width];
+        p.out_tables[e] = page >= 0 && page < p.pages ? p.page_map[page] : -1;
+    }
+    pg_copy_all(p.pool, p.moves, p.head->moves);
+}
+
+// ---- copying given pages, appending tokens -----------------------------------------------------
+
+struct PgCopyParams {
+    const int32_t* src;
+    const int32_t* dst;
+    int32_t n, pages;
+    PgPool pool;
+};
+
+__global__ void __launch_bounds__(PG_THREADS) pages_copy_kernel(const PgCopyParams p) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int32_t planes = 2 * p.pool.layers;
+    for (int64_t unit = blockIdx.x; unit < (int64_t)p.n * planes; unit += gridDim.x) {
+        const int32_t src = p.src[unit / planes], dst = p.dst[unit / planes];
+        if (src < 0 || src >= p.pages || dst < 0 || dst >= p.pages || src == dst) continue;
+        pg_copy(p.pool, src, dst, p.pool.page_size, (int32_t)(unit % planes));
+    }
+}
+
+// Keys and values of the last `tokens` tokens of every sequence go to their places.
+struct PgAppendParams {
+    const char* k;                        // seqs x tokens x kv_heads rows; strides in bytes
+    const char* v;
+    int64_t k_seq, k_tok, k_head, v_seq, v_tok, v_head;
+    char* k_pages;
+    char* v_pages;
+    int64_t kp_page, kp_head, kp_token, vp_page, vp_head, vp_token;
+    const int32_t* tables;
+    int64_t table_stride;
+    const int32_t* lengths;
+    int32_t seqs, tokens, kv_heads, row_bytes, page_size, pages, width;
+};
+
+__global__ void __launch_bounds__(PG_THREADS) pages_append_kernel(const PgAppendParams p) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int32_t vecs = p.row_bytes / 16;
+    const int64_t n = (int64_t)p.seqs * p.tokens * p.kv_heads * vecs;
+    for (int64_t i = (int64_t)blockIdx.x * PG_THREADS + threadIdx.x; i < n; i += (int64_t)gridDim.x * PG_THREADS) {
+        const int32_t vec = (int32_t)(i % vecs);
+        int64_t rest = i / vecs;
+        const int32_t head = (int32_t)(rest % p.kv_heads);
+        rest /= p.kv_heads;
+        const int32_t tok = (int32_t)(rest % p.tokens), seq = (int32_t)(rest / p.tokens);
+        const int32_t at = pg_length(p.lengths, seq, p.width, p.page_size) - p.tokens + tok;
+        if (at < 0) continue;
+        const int32_t page = p.tables[seq * p.table_stride + at / p.page_size], slot = at % p.page_size;
+        if (page < 0 || page >= p.pages) continue;
+        const uint4 k = *reinterpret_cast<const uint4*>(p.k + seq * p.k_seq + tok * p.k_tok + head * p.k_head + vec * 16);
+        const uint4 v = *reinterpret_cast<const uint4*>(p.v + seq * p.v_seq + tok * p.v_tok + head * p.v_head + vec * 16);
+        *reinterpret_cast<uint4*>(p.k_pages + page * p.kp_page + head * p.kp_head + slot * p.kp_token + vec * 16) = k;
+        *reinterpret_cast<uint4*>(p.v_pages + page * p.vp_page + head * p.vp_head + slot * p.vp_token + vec * 16) = v;
+    }
+}
+
+}  // namespace profk
