@@ -45,6 +45,8 @@ cudaError_t prepare_kernel(K* kernel, size_t smem, bool wide_cluster, uint64_t* 
     std::lock_guard<std::mutex> lock(*mutex);
     if (*done_mask >> dev & 1) return cudaSuccess;
     err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    // all of the SM's memory as shared memory: two CTAs have to fit
+    if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (err == cudaSuccess && wide_cluster) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (err == cudaSuccess) *done_mask |= 1ull << dev;
     return err;
@@ -76,7 +78,7 @@ struct Launch {
 constexpr unsigned LP_MAX_PARTS = 16;
 
 size_t lp_smem(unsigned parts, uint32_t k) {
-    size_t bytes = (size_t)LP_STAGES * LP_UNROLL * LP_THREADS * 16;
+    size_t bytes = (size_t)LP_STAGES * LP_STEP * 16;
     if (parts > 1) bytes += 2 * (size_t)parts * ((k ? k + LP_SLACK : 0) * sizeof(uint64_t) + sizeof(LpStats));
     return bytes;
 }
@@ -110,7 +112,7 @@ int lp_launch(const LpParams& p, unsigned parts, int sms, void* stream) {
 template <typename T>
 int lp_forward(const T* logits, int64_t rows, int64_t V, int64_t row_stride, const int64_t* tokens, int64_t k, double temperature,
                void* stream, float* logprob, float* lse, float* lse_rest, float* entropy, float* top_logprobs, int64_t* top_tokens) {
-    if (!logits || !lse || rows < 1 || V < 1 || V > 0x7FFFFFFFll || rows > (1ll << 40) / V || (rows > 1 && row_stride < V) || k < 0 ||
+    if (!logits || !lse || rows < 1 || rows > 0x7FFFFFFFll || V < 1 || V > 0x7FFFFFFFll || rows > (1ll << 40) / V || (rows > 1 && row_stride < V) || k < 0 ||
         k > LP_MAX_K || k > V || !(temperature > 0) || !std::isfinite(temperature) || !std::isfinite(1.0 / temperature) ||
         (reinterpret_cast<uintptr_t>(logits) % sizeof(T)) != 0 || (k > 0) != (top_logprobs != nullptr) ||
         (k > 0) != (top_tokens != nullptr) || (tokens != nullptr) != (logprob != nullptr))

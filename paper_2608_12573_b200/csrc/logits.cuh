@@ -86,12 +86,35 @@ template <> struct Logit<__half> {
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float LOWEST = -3.402823466e38f;      // start of a running maximum: finite, so that -inf - LOWEST is no NaN
-constexpr float FAR_BELOW = -1e30f;             // stands in for differences of -inf where they meet a factor of zero
+constexpr float FAR_BELOW = -1e28f;             // stands in for differences of -inf where they meet a factor of zero (times 2^31 still finite)
 
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// Two fp32 lanes in one 64-bit register: the packed forms halve the issue slots of the elementwise arithmetic.
+struct F32x2 { unsigned long long v; };
+__device__ __forceinline__ F32x2 f2_make(float a, float b) {
+    F32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void f2_split(F32x2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
+__device__ __forceinline__ F32x2 f2_add(F32x2 a, F32x2 b) {
+    F32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F32x2 f2_mul(F32x2 a, F32x2 b) {
+    F32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F32x2 f2_fma(F32x2 a, F32x2 b, F32x2 c) {
+    F32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
 }
 __device__ __forceinline__ uint4 ld_stream_u4(const void* p) { return ld_stream(reinterpret_cast<const uint4*>(p)); }
 __device__ __forceinline__ void st_stream_u4(void* p, const uint4& v) {

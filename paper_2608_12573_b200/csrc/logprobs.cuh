@@ -7,8 +7,15 @@
 // moving both to the larger maximum, so every thread keeps a triple of its own and they are joined in a fixed order at
 // the end of the row.  T only enters as a factor of the exponent: e^(z - m) = 2^((x - mx) log2(e) / T).
 //
-// The k largest logits are found on the way: a float bound is compared with the largest element of each batch, elements
-// at or above it are appended to a list in shared memory, and when the list fills the k best of it raise the bound.
+// The k largest logits are found on the way.  Groups of lanes keep the largest logit that they have seen in a slot of
+// shared memory; the k-th largest slot is a bound that k elements of the row reach, so that only vectors whose maximum
+// reaches the bound can matter.  Their numbers are noted in a list, a few times k of them for a row in any ordinary order;
+// the bound is renewed whenever the number of batches has doubled, without a barrier: a stale slot only makes it lower.
+// At the end of the row the noted vectors are read once more and their elements above the last bound are ordered.  Where
+// the list overflows all the same (ascending order, a flood of equal values) the whole row is read once more instead.
+//
+// Eleven warps of a CTA stream; the twelfth finishes rows (joins the statistics, orders the list, writes the results)
+// while the others are in the next one.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -19,11 +26,14 @@ namespace profk {
 
 namespace cg = cooperative_groups;
 
-constexpr int LP_THREADS = 512;
+constexpr int LP_THREADS = 384;
+constexpr int LP_STREAM_WARPS = 11;
+constexpr int LP_STREAM = LP_STREAM_WARPS * 32;
 constexpr int LP_UNROLL = 4;              // 16-byte vectors per thread and batch
-constexpr int LP_STAGES = 3;              // batches in flight or in hand per thread
-constexpr uint32_t LP_CAP = 1024;         // records the candidate list holds
-constexpr uint32_t LP_HIGH = 512;        // beyond this many the list is cut back to its k best
+constexpr int LP_STAGES = 4;              // batches in flight or in hand per thread
+constexpr uint32_t LP_STEP = LP_STREAM * LP_UNROLL;     // vectors per batch
+constexpr uint32_t LP_NOTES = 2048;       // vectors the list holds
+constexpr uint32_t LP_FIN = 512;          // elements the finishing warp holds; more than half of them it cuts back to the k best
 constexpr uint32_t LP_MAX_K = 128;        // most alternatives
 constexpr uint32_t LP_SLACK = 32;         // a selection may stop with up to k + LP_SLACK records in hand
 
@@ -51,34 +61,31 @@ __device__ __forceinline__ LpStats lp_join(const LpStats& a, const LpStats& b, f
     return LpStats{m, fa * a.s + fb * b.s, fa * fmaf(da, a.s, a.t) + fb * fmaf(db, b.s, b.t)};
 }
 
-struct LpShared {
-    uint64_t cand[LP_CAP];
-    uint64_t best[LP_MAX_K + LP_SLACK];
-    uint32_t part[2][LP_THREADS / 32];
-    uint32_t lo[LP_THREADS / 32], hi[LP_THREADS / 32];
-    LpStats stats[LP_THREADS / 32];
-    uint32_t count, fill;
-    uint64_t limit;                       // records above it are no longer of interest
+// What the streaming warps leave of a row for the finishing one; two of them, used in turn.
+struct LpRow {
+    uint32_t note[LP_NOTES];              // numbers of vectors
+    LpStats stats[LP_STREAM_WARPS];
+    uint32_t count;
     float bound;                          // elements below it are no longer of interest
-    float row_max, row_log;               // of the finished row: largest logit, ln s
 };
 
-// Sum over the CTA of one number per thread; `turn` alternates between calls, so that one barrier is enough.
-__device__ __forceinline__ uint32_t lp_block_sum(uint32_t v, LpShared& sh, int turn) {
-    const uint32_t w = __reduce_add_sync(FULL_MASK, v);
-    if (lane_id() == 0) sh.part[turn][threadIdx.x >> 5] = w;
-    __syncthreads();
-    const unsigned lane = lane_id();
-    return __reduce_add_sync(FULL_MASK, lane < LP_THREADS / 32 ? sh.part[turn][lane] : 0u);
-}
+struct LpShared {
+    LpRow row[2];
+    uint64_t fin[LP_FIN];                 // records, of the finishing warp
+    float slot[LP_STREAM];                // largest logits seen by a group of lanes
+};
 
-// The least limit found (by halving the interval of the records' value words, then of their index words) such that at
-// least k and at most `most` of the n records in `a` are <= it; fewer than k valid records (~0 is none): all of them.
-// All threads call it and get the same answer; a barrier must lie between the last write to `a` and the call.
-__device__ __forceinline__ uint64_t lp_find_limit(const uint64_t* a, uint32_t n, uint32_t k, uint32_t most, LpShared& sh) {
-    const unsigned tid = threadIdx.x, lane = lane_id();
+// Named barriers: among the streaming warps; a row is ready for the finishing warp; its place may be used again.
+enum { LP_BAR_STREAM = 1, LP_BAR_FULL = 2, LP_BAR_EMPTY = 4 };
+__device__ __forceinline__ void lp_bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ void lp_bar_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// By one warp: a limit (found by halving the interval of the records' value words, then of their index words) such that
+// at least k and at most `most` of the n records in `a` are <= it; no more than `most` valid records (~0 is none): all of
+// them.  A warp barrier must lie between the last write to `a` and the call.
+__device__ __forceinline__ uint64_t lp_find_limit(const uint64_t* a, uint32_t n, uint32_t k, uint32_t most) {
     uint32_t lo = 0xFFFFFFFFu, hi = 0u, valid = 0;
-    for (uint32_t i = tid; i < n; i += LP_THREADS) {
+    for (uint32_t i = lane_id(); i < n; i += 32) {
         const uint64_t r = a[i];
         if (r != ~0ull) {
             const uint32_t h = (uint32_t)(r >> 32);
@@ -89,19 +96,14 @@ __device__ __forceinline__ uint64_t lp_find_limit(const uint64_t* a, uint32_t n,
     }
     lo = __reduce_min_sync(FULL_MASK, lo);
     hi = __reduce_max_sync(FULL_MASK, hi);
-    if (lane == 0) { sh.lo[tid >> 5] = lo; sh.hi[tid >> 5] = hi; }
-    const uint32_t total = lp_block_sum(valid, sh, 0);      // its barrier also covers lo and hi
-    if (total <= most) return ~0ull - 1;
-    lo = __reduce_min_sync(FULL_MASK, lane < LP_THREADS / 32 ? sh.lo[lane] : 0xFFFFFFFFu);
-    hi = __reduce_max_sync(FULL_MASK, lane < LP_THREADS / 32 ? sh.hi[lane] : 0u);
-    int turn = 1;
-    // smallest value word `lo` with at least k records at or below it
+    if (__reduce_add_sync(FULL_MASK, valid) <= most) return ~0ull - 1;
+    // smallest value word `lo` with at least k records at or below it (a ~0 record lies above every limit used)
     while (lo < hi) {
         const uint32_t mid = lo + ((hi - lo) >> 1);
         uint32_t c = 0;
-        for (uint32_t i = tid; i < n; i += LP_THREADS) c += (uint32_t)(a[i] >> 32) <= mid && a[i] != ~0ull;
-        c = lp_block_sum(c, sh, turn);
-        turn ^= 1;
+#pragma unroll 4
+        for (uint32_t i = lane_id(); i < n; i += 32) c += (uint32_t)(a[i] >> 32) <= mid;
+        c = __reduce_add_sync(FULL_MASK, c);
         if (c >= k) {
             hi = mid;
             if (c <= most) return ((uint64_t)mid << 32) | 0xFFFFFFFFull;
@@ -115,9 +117,8 @@ __device__ __forceinline__ uint64_t lp_find_limit(const uint64_t* a, uint32_t n,
         const uint32_t mid = ilo + ((ihi - ilo) >> 1);
         const uint64_t limit = ((uint64_t)word << 32) | mid;
         uint32_t c = 0;
-        for (uint32_t i = tid; i < n; i += LP_THREADS) c += a[i] <= limit;
-        c = lp_block_sum(c, sh, turn);
-        turn ^= 1;
+        for (uint32_t i = lane_id(); i < n; i += 32) c += a[i] <= limit;
+        c = __reduce_add_sync(FULL_MASK, c);
         if (c >= k) {
             ihi = mid;
             if (c <= most) break;
@@ -125,51 +126,57 @@ __device__ __forceinline__ uint64_t lp_find_limit(const uint64_t* a, uint32_t n,
             ilo = mid + 1;
         }
     }
-    __syncthreads();
     return ((uint64_t)word << 32) | ihi;
 }
 
-// Copies the records <= limit of a[0, n) into sh.best (at most `room` of them) and returns how many there are.
-__device__ __forceinline__ uint32_t lp_collect(const uint64_t* a, uint32_t n, uint64_t limit, uint32_t room, LpShared& sh) {
-    __syncthreads();
-    if (threadIdx.x == 0) sh.fill = 0;
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < n; i += LP_THREADS) {
-        const uint64_t r = a[i];
-        if (r <= limit) {
-            const uint32_t pos = atomicAdd(&sh.fill, 1u);
-            if (pos < room) sh.best[pos] = r;
+// Lanes that share a slot: the coarser the slots the cheaper the bound, the finer the tighter (the k-th largest of n slots
+// has about n ln(n / (n - k)) elements above it).
+constexpr uint32_t LP_FEW_K = 16;         // up to here 22 slots, one per lane of a warp, whose k-th largest is found by counting
+__device__ __forceinline__ uint32_t lp_slot_lanes(uint32_t k) { return k <= LP_FEW_K ? 16 : k <= 64 ? 4 : 1; }
+
+__device__ __forceinline__ void lp_write_slot(float seen, uint32_t lanes, LpShared& sh) {
+    if (lanes >= 4) {
+        seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 1));
+        seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 2));
+    }
+    if (lanes == 16) {
+        seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 4));
+        seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 8));
+    }
+    if ((threadIdx.x & (lanes - 1)) == 0) sh.slot[threadIdx.x / lanes] = seen;
+}
+
+// By one warp: (nearly) the k-th largest slot.  Slots hold LOWEST at least, and so does the bound: -inf is never appended
+// on the way.
+__device__ __forceinline__ float lp_slot_bound(uint32_t k, uint32_t lanes, const LpShared& sh) {
+    const uint32_t n = LP_STREAM / lanes, lane = lane_id();
+    const volatile float* slot = sh.slot;
+    if (lanes == 16) {
+        const float mine = lane < n ? slot[lane] : -INFINITY;
+        uint32_t above = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) above += __shfl_sync(FULL_MASK, mine, i) > mine;
+        // of the slots with fewer than k larger ones the smallest: at least k slots reach it
+        const uint32_t key = above < k && lane < n ? key_from_bits32(float_bits_exact(mine)) : 0xFFFFFFFFu;
+        return __uint_as_float(bits32_from_key(__reduce_min_sync(FULL_MASK, key)));
+    }
+    uint32_t top = 0;
+    for (uint32_t at = lane; at < n; at += 32) top = max(top, key_from_bits32(float_bits_exact(slot[at])));
+    uint32_t lo = key_from_bits32(0xFF7FFFFFu), hi = __reduce_max_sync(FULL_MASK, top) + 1u;
+    while (lo + 1 < hi) {
+        const uint32_t mid = lo + ((hi - lo) >> 1);
+        uint32_t c = 0;                                                           // (a slot that rises meanwhile does no harm)
+#pragma unroll 4
+        for (uint32_t at = lane; at < n; at += 32) c += key_from_bits32(float_bits_exact(slot[at])) >= mid;
+        c = __reduce_add_sync(FULL_MASK, c);
+        if (c >= k) {
+            lo = mid;
+            if (c <= k + k / 8) break;
+        } else {
+            hi = mid;
         }
     }
-    __syncthreads();
-    return min(sh.fill, room);
-}
-
-// Cuts the candidate list back to its k best and raises the bound above the worst of them: what follows has higher
-// indices, so that an equal element no longer counts.
-__device__ __forceinline__ void lp_cut_list(uint32_t stored, uint32_t k, LpShared& sh) {
-    // exactly k: the k-th record is then the bound for everything that follows
-    const uint64_t limit = lp_find_limit(sh.cand, stored, k, k, sh);
-    const uint32_t m = lp_collect(sh.cand, stored, limit, LP_MAX_K + LP_SLACK, sh);
-    for (uint32_t i = threadIdx.x; i < m; i += LP_THREADS) sh.cand[i] = sh.best[i];
-    if (threadIdx.x == 0) {
-        sh.count = m;
-        sh.limit = limit;
-        sh.bound = __uint_as_float(bits32_from_key(~(uint32_t)(limit >> 32) + 1u));
-    }
-    __syncthreads();
-}
-
-template <typename T>
-__device__ __forceinline__ uint64_t lp_record(float x, uint32_t idx) { return make_record(key_from_bits32(float_bits_exact(x)), idx); }
-
-template <typename T>
-__device__ __forceinline__ void lp_append(float x, uint32_t idx, LpShared& sh) {
-    const uint64_t rec = lp_record<T>(x, idx);
-    if (rec <= sh.limit) {
-        const uint32_t pos = atomicAdd(&sh.count, 1u);
-        if (pos < LP_CAP) sh.cand[pos] = rec;
-    }
+    return __uint_as_float(bits32_from_key(lo));
 }
 
 __device__ __forceinline__ void lp_cp_async16(uint32_t smem, const void* gmem) {
@@ -196,282 +203,387 @@ struct LpShare {
     __device__ __forceinline__ const T* vec(uint32_t v) const { return x + head + (size_t)v * Logit<T>::VEC; }
 };
 
+// ---- the finishing warp's part of a selection; `n` records are in sh.fin, all lanes agree on it
+
+// Drops the records above `limit`; keeps the others' order.
+__device__ __forceinline__ uint32_t lp_fin_drop(uint32_t n, uint64_t limit, LpShared& sh) {
+    uint32_t kept = 0;
+    for (uint32_t i0 = 0; i0 < n; i0 += 32) {
+        const uint64_t r = i0 + lane_id() < n ? sh.fin[i0 + lane_id()] : ~0ull;
+        __syncwarp();
+        const bool keep = r <= limit && r != ~0ull;
+        const unsigned who = __ballot_sync(FULL_MASK, keep);
+        if (keep) sh.fin[kept + __popc(who & ((1u << lane_id()) - 1u))] = r;
+        kept += __popc(who);
+        __syncwarp();
+    }
+    return kept;
+}
+// Adds each lane's element if it has one; cuts back to the k best before the room runs out.
+__device__ __forceinline__ uint32_t lp_fin_add(uint32_t n, bool has, float x, uint32_t idx, LpShared& sh) {
+    const unsigned who = __ballot_sync(FULL_MASK, has);
+    if (who == 0) return n;
+    if (has) sh.fin[n + __popc(who & ((1u << lane_id()) - 1u))] = make_record(key_from_bits32(float_bits_exact(x)), idx);
+    __syncwarp();
+    return n + __popc(who);
+}
+// The elements of one vector per lane (`has`) that reach the bound; cuts back to the k best before the room runs out, and
+// then raises the bound above the worst of them where what follows has higher indices only (`ascending`).
+template <typename T>
+__device__ __forceinline__ uint32_t lp_fin_vector(uint32_t n, bool has, const uint4& vec, uint32_t at, float& bound, bool ascending, uint32_t k, LpShared& sh) {
+    has = has && Logit<T>::vec_max(vec) >= bound;
+    if (!__any_sync(FULL_MASK, has)) return n;
+    float x[Logit<T>::VEC];
+    Logit<T>::unpack(vec, x);
+#pragma unroll
+    for (int j = 0; j < Logit<T>::VEC; ++j) n = lp_fin_add(n, has && x[j] >= bound, x[j], at + j, sh);
+    if (n > LP_FIN / 2) {
+        const uint64_t limit = lp_find_limit(sh.fin, n, k, k);
+        n = lp_fin_drop(n, limit, sh);
+        if (ascending) bound = __uint_as_float(bits32_from_key(~(uint32_t)(limit >> 32) + 1u));
+    }
+    return n;
+}
+
+// The candidates of a row's share, at most k + LP_SLACK of them, the k best of the share among them.
+template <typename T>
+__device__ __forceinline__ uint32_t lp_fin_select(const LpShare<T> mine, uint32_t k, bool first, bool last, uint32_t V, const LpRow& r, LpShared& sh) {
+    constexpr int VEC = Logit<T>::VEC;
+    const uint32_t lane = lane_id(), lim = k + LP_SLACK;
+    uint32_t n = 0;
+    float bound = r.bound;
+    const uint32_t notes = r.count, tail = mine.head + mine.nvec * VEC;
+    const bool in_head = first && lane < mine.head, in_tail = last && tail + lane < V;
+    const float hx = in_head ? Logit<T>::to_float(mine.x[lane]) : -INFINITY, tx = in_tail ? Logit<T>::to_float(mine.x[tail + lane]) : -INFINITY;
+    n = lp_fin_add(n, hx >= bound, hx, lane, sh);
+    if (notes <= LP_NOTES) {
+        for (uint32_t i0 = 0; i0 < notes; i0 += 128) {
+            uint32_t w[4];
+            uint4 vec[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t i = i0 + u * 32 + lane;
+                w[u] = i < notes ? r.note[i] : 0u;
+                if (i < notes) vec[u] = *reinterpret_cast<const uint4*>(mine.vec(w[u]));
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (i0 + u * 32 < notes) n = lp_fin_vector<T>(n, i0 + u * 32 + lane < notes, vec[u], mine.head + w[u] * VEC, bound, false, k, sh);
+        }
+    } else {
+        for (uint32_t v = mine.v0; v < mine.v1; v += 128) {
+            uint4 vec[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (v + u * 32 + lane < mine.v1) vec[u] = ld_stream_u4(mine.vec(v + u * 32 + lane));
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                n = lp_fin_vector<T>(n, v + u * 32 + lane < mine.v1, vec[u], mine.head + (v + u * 32 + lane) * VEC, bound, true, k, sh);
+        }
+    }
+    n = lp_fin_add(n, tx >= bound, tx, tail + lane, sh);
+    // Masked tokens (-inf) fill the places that nothing else takes, lowest indices first.
+    const uint32_t e1 = last ? V : mine.head + mine.v1 * VEC;
+    for (uint32_t e = (first ? 0 : mine.head + mine.v0 * VEC); n < k && e < e1; e += 32)
+        n = lp_fin_add(n, e + lane < e1 && Logit<T>::to_float(mine.x[e + lane]) == -INFINITY, -INFINITY, e + lane, sh);
+    if (n > lim) n = lp_fin_drop(n, lp_find_limit(sh.fin, n, k, lim), sh);
+    return n;
+}
+
 // One cluster of `parts` CTAs takes a row at a time (parts = 1: a plain CTA).  The vectors of the row come through a ring
 // in shared memory that each thread fills and empties for itself (cp.async, no barrier), and that runs on into the next
 // row, so that HBM stays busy while a row is finished.
 template <typename T, bool ENT, bool TOPK>
 __global__ void __launch_bounds__(LP_THREADS, 2) logprobs_kernel(const LpParams p) {
     constexpr int VEC = Logit<T>::VEC, U = LP_UNROLL;
-    constexpr uint32_t STEP = LP_THREADS * U;
     extern __shared__ __align__(16) unsigned char lp_dyn[];
     __shared__ LpShared sh;
-    uint4* ring = reinterpret_cast<uint4*>(lp_dyn);                               // [LP_STAGES][U][LP_THREADS]
+    uint4* ring = reinterpret_cast<uint4*>(lp_dyn);                               // [LP_STAGES][U][LP_STREAM]
     const uint32_t lim = TOPK ? p.k + LP_SLACK : 0;
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t parts = cluster.num_blocks(), part = cluster.block_rank();
     // what the parts of a row hand to the first of them: two sets, used in turn
-    uint64_t* in_recs = reinterpret_cast<uint64_t*>(ring + (size_t)LP_STAGES * U * LP_THREADS);   // [2][parts][lim]
+    uint64_t* in_recs = reinterpret_cast<uint64_t*>(ring + (size_t)LP_STAGES * LP_STEP);                    // [2][parts][lim]
     LpStats* in_stats = reinterpret_cast<LpStats*>(in_recs + (parts > 1 ? 2 * (size_t)parts * lim : 0));   // [2][parts]
 
     const unsigned tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
-    const int64_t first = blockIdx.x / parts, stride = gridDim.x / parts;
+    const int32_t rows = (int32_t)p.rows, first = (int32_t)(blockIdx.x / parts), stride = (int32_t)(gridDim.x / parts);
     const float c = p.scale * LOG2E;
     pdl_wait();
     pdl_launch_dependents();
     if (parts > 1) cluster.sync();                                                // every CTA of the cluster has started
 
-    // the loading side runs LP_STAGES - 1 batches ahead of the working side
-    int64_t load_row = first;
-    LpShare<T> ld;
-    uint32_t load_v = 0;
-    int load_stage = 0;
-    if (load_row < p.rows) { ld.set(p, load_row, part, parts); load_v = ld.v0; }
-    const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(ring);
-    auto load_batch = [&]() {
-        if (load_row < p.rows) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const uint32_t v = load_v + u * LP_THREADS + tid;
-                if (v < ld.v1) lp_cp_async16(ring_addr + ((load_stage * U + u) * LP_THREADS + tid) * 16u, ld.vec(v));
-            }
-            load_v += STEP;
-            if (load_v >= ld.v1) {
-                load_row += stride;
-                if (load_row < p.rows) { ld.set(p, load_row, part, parts); load_v = ld.v0; }
-            }
-        }
-        lp_cp_commit();
-        load_stage = load_stage + 1 == LP_STAGES ? 0 : load_stage + 1;
-    };
-#pragma unroll
-    for (int s = 0; s < LP_STAGES - 1; ++s) load_batch();
-
-    int stage = 0;
-    uint32_t turn = 0;                                                            // of the hand-over sets
-    for (int64_t row = first; row < p.rows; row += stride) {
-        LpShare<T> mine;
-        mine.set(p, row, part, parts);
-        LpStats st{LOWEST, 0.f, 0.f};
-        if constexpr (TOPK) {
-            if (tid == 0) { sh.count = 0; sh.limit = ~0ull - 1; sh.bound = -INFINITY; }
-            __syncthreads();
-        }
-        auto one = [&](float x) {                                                 // a single element
-            if (x > st.m) {
-                const float d = fmaxf(st.m - x, FAR_BELOW), f = exp2_approx(d * c);
-                st.t = f * fmaf(d, st.s, st.t);
-                st.s *= f;
-                st.m = x;
-            }
-            const float d = x - st.m, e = exp2_approx(d * c);
-            st.s += e;
-            if constexpr (ENT) st.t = fmaf(e, fmaxf(d, FAR_BELOW), st.t);
+    int turn = 0;
+    if (warp == LP_STREAM_WARPS) {
+        // ---- the finishing warp
+        auto make_empty = [&](int t) {
+            if (lane == 0) { sh.row[t].count = 0; sh.row[t].bound = LOWEST; }
+            __syncwarp();
+            lp_bar_arrive(LP_BAR_EMPTY + t, LP_THREADS);
         };
-        // elements before the first whole vector
-        if (part == 0 && tid < mine.head) {
-            const float x = Logit<T>::to_float(mine.x[tid]);
-            one(x);
-            if (TOPK && x >= -INFINITY) lp_append<T>(x, tid, sh);
-        }
-        bool opening = true;
-        uint32_t v = mine.v0;
-        do {                                                                      // (an empty share still takes its batch)
-            load_batch();
-            lp_cp_wait<LP_STAGES - 1>();
-            uint4 vec[U];
-            float vmax[U], bmax = -INFINITY;
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const bool in = v + u * LP_THREADS + tid < mine.v1;
-                vec[u] = ring[(stage * U + u) * LP_THREADS + tid];
-                vmax[u] = in ? Logit<T>::vec_max(vec[u]) : -INFINITY;
-                bmax = fmaxf(bmax, vmax[u]);
-            }
-            if (bmax > st.m) {
-                const float d = fmaxf(st.m - bmax, FAR_BELOW), f = exp2_approx(d * c);
-                st.t = f * fmaf(d, st.s, st.t);
-                st.s *= f;
-                st.m = bmax;
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (v + u * LP_THREADS + tid < mine.v1) {
-                    float x[VEC];
-                    Logit<T>::unpack(vec[u], x);
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        const float d = x[j] - st.m, e = exp2_approx(d * c);
-                        st.s += e;
-                        if constexpr (ENT) st.t = fmaf(e, fmaxf(d, FAR_BELOW), st.t);
-                    }
+        if (first < rows) make_empty(0);
+        if (stride < rows - first) make_empty(1);
+        for (int32_t row = first; row < rows; row += stride) {
+            const int64_t token = p.tokens ? p.tokens[row] : -1;
+            float token_x = 0.f;
+            if (token >= 0 && token < (int64_t)p.V) token_x = Logit<T>::to_float((reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.row_stride)[token]);
+            lp_bar_sync(LP_BAR_FULL + turn, LP_THREADS);
+            LpRow& r = sh.row[turn];
+            // join the warps' statistics, in a fixed order; every lane gets the result
+            auto join_lanes = [&](LpStats st, int width) {
+                for (int d = width / 2; d > 0; d >>= 1) {
+                    LpStats o;
+                    o.m = __shfl_xor_sync(FULL_MASK, st.m, d);
+                    o.s = __shfl_xor_sync(FULL_MASK, st.s, d);
+                    o.t = __shfl_xor_sync(FULL_MASK, st.t, d);
+                    st = (lane & d) ? lp_join(o, st, c) : lp_join(st, o, c);
                 }
-            }
+                return st;
+            };
+            LpStats all = join_lanes(lane % 16 < LP_STREAM_WARPS ? r.stats[lane % 16] : LpStats{LOWEST, 0.f, 0.f}, 16);
+            uint32_t found = 0;
             if constexpr (TOPK) {
-                if (opening) {
-                    // The k-th largest of the threads' maxima has k elements at or above it: a first bound, found by
-                    // halving the interval of the order keys until at most k + LP_SLACK maxima reach it.
-                    opening = false;
-                    const uint32_t key = key_from_bits32(float_bits_exact(bmax));
-                    uint32_t lo = 0x007FFFFFu, hi = 0xFF800001u;                  // keys of -inf and of +inf + 1
-                    // invariant: at least k maxima have a key >= lo (every thread has at least -inf)
-                    while (lo + 1 < hi) {
-                        const uint32_t mid = lo + ((hi - lo) >> 1);
-                        const uint32_t n = (uint32_t)__syncthreads_count(key >= mid);
-                        if (n >= p.k) {
-                            lo = mid;
-                            if (n <= p.k + LP_SLACK) break;
-                        } else {
-                            hi = mid;
-                        }
-                    }
-                    if (tid == 0) sh.bound = __uint_as_float(bits32_from_key(lo));
-                    __syncthreads();
+                LpShare<T> mine;
+                mine.set(p, row, part, parts);
+                found = lp_fin_select<T>(mine, p.k, part == 0, part == parts - 1, p.V, r, sh);
+            }
+            if (parts > 1) {
+                // hand statistics and records to the cluster's first CTA
+                if constexpr (TOPK) {
+                    uint64_t* to_recs = cluster.map_shared_rank(in_recs, 0) + ((size_t)turn * parts + part) * lim;
+                    for (uint32_t i = lane; i < lim; i += 32) to_recs[i] = i < found ? sh.fin[i] : ~0ull;
                 }
-                const uint32_t before = sh.count;                                 // read behind a barrier of this or the last batch
-                __syncthreads();
-                for (;;) {
-                    const float bound = sh.bound;
-                    if (bmax >= bound) {
-#pragma unroll
-                        for (int u = 0; u < U; ++u) {
-                            if (vmax[u] >= bound && v + u * LP_THREADS + tid < mine.v1) {
-                                float x[VEC];
-                                Logit<T>::unpack(vec[u], x);
-                                const uint32_t at = mine.head + (v + u * LP_THREADS + tid) * VEC;
-#pragma unroll
-                                for (int j = 0; j < VEC; ++j)
-                                    if (x[j] >= bound) lp_append<T>(x[j], at + j, sh);
-                            }
+                if (lane == 0) *(cluster.map_shared_rank(in_stats, 0) + turn * parts + part) = all;
+                cluster.sync();
+                if (part == 0) {
+                    all = join_lanes(lane % 16 < parts ? in_stats[turn * parts + lane % 16] : LpStats{LOWEST, 0.f, 0.f}, 16);
+                    if constexpr (TOPK) {
+                        const uint64_t* recs = in_recs + (size_t)turn * parts * lim;
+                        const uint64_t limit = lp_find_limit(recs, parts * lim, p.k, lim);
+                        found = 0;
+                        for (uint32_t i0 = 0; i0 < parts * lim; i0 += 32) {
+                            const uint64_t rec = i0 + lane < parts * lim ? recs[i0 + lane] : ~0ull;
+                            const unsigned who = __ballot_sync(FULL_MASK, rec <= limit);
+                            if (rec <= limit) sh.fin[found + __popc(who & ((1u << lane) - 1u))] = rec;
+                            found += __popc(who);
                         }
+                        __syncwarp();
                     }
-                    __syncthreads();
-                    const uint32_t now = sh.count;
-                    if (now <= LP_CAP) {
-                        if (now > LP_HIGH) {
-                            __syncthreads();
-                            lp_cut_list(now, p.k, sh);
-                        }
-                        break;
-                    }
-                    // More than the list holds: the k best of what it holds bound what this batch may still add.  The
-                    // batch's own records are dropped again and the batch is looked at once more under that bound.
-                    __syncthreads();
-                    const uint64_t limit = lp_find_limit(sh.cand, LP_CAP, p.k, p.k, sh);
-                    if (tid == 0) {
-                        sh.limit = limit;
-                        sh.bound = __uint_as_float(bits32_from_key(~(uint32_t)(limit >> 32)));
-                        sh.count = before;
-                    }
-                    __syncthreads();
                 }
             }
-            stage = stage + 1 == LP_STAGES ? 0 : stage + 1;
-            v += STEP;
-        } while (v < mine.v1);
-        // elements behind the last whole vector (the list has room: it holds LP_HIGH records at most here)
-        const uint32_t tail = mine.head + mine.nvec * VEC;
-        if (part == parts - 1 && tail + tid < p.V) {
-            const float x = Logit<T>::to_float(mine.x[tail + tid]);
-            one(x);
-            if (TOPK && x >= -INFINITY) lp_append<T>(x, tail + tid, sh);
-        }
-
-        // join the threads' parts, in a fixed order
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) {
-            LpStats o;
-            o.m = __shfl_xor_sync(FULL_MASK, st.m, d);
-            o.s = __shfl_xor_sync(FULL_MASK, st.s, d);
-            o.t = __shfl_xor_sync(FULL_MASK, st.t, d);
-            st = (lane & d) ? lp_join(o, st, c) : lp_join(st, o, c);
-        }
-        __syncthreads();
-        if (lane == 0) sh.stats[warp] = st;
-        uint32_t found = 0;
-        if constexpr (TOPK) {
-            __syncthreads();
-            const uint32_t n = sh.count;
-            const uint64_t limit = lp_find_limit(sh.cand, n, p.k, lim, sh);
-            found = lp_collect(sh.cand, n, limit, lim, sh);
-        }
-        __syncthreads();
-        if (parts > 1) {
-            // hand statistics and records to the cluster's first CTA
-            LpStats* to_stats = cluster.map_shared_rank(in_stats, 0) + turn * parts + part;
-            uint64_t* to_recs = cluster.map_shared_rank(in_recs, 0) + ((size_t)turn * parts + part) * lim;
-            if constexpr (TOPK)
-                for (uint32_t i = tid; i < lim; i += LP_THREADS) to_recs[i] = i < found ? sh.best[i] : ~0ull;
-            if (tid == 0) {
-                LpStats all = sh.stats[0];
-                for (int w = 1; w < LP_THREADS / 32; ++w) all = lp_join(all, sh.stats[w], c);
-                *to_stats = all;
-            }
-            cluster.sync();
-        }
-        if (part == 0) {
-            if (tid == 0) {
-                LpStats all;
-                if (parts > 1) {
-                    all = in_stats[turn * parts];
-                    for (uint32_t i = 1; i < parts; ++i) all = lp_join(all, in_stats[turn * parts + i], c);
-                } else {
-                    all = sh.stats[0];
-                    for (int w = 1; w < LP_THREADS / 32; ++w) all = lp_join(all, sh.stats[w], c);
-                }
+            if (part == 0) {
                 const bool empty = all.s == 0.f;                                  // nothing but -inf
                 const float log_s = logf(all.s);
-                sh.row_max = all.m;
-                sh.row_log = log_s;
-                // lse in two floats: one alone loses ln s beside a large maximum (all of it in a row masked with fp32's
-                // lowest value), and with it the probabilities that the gradient takes from it
-                const float near = empty ? -INFINITY : fmaf(all.m, p.scale, log_s);
-                p.lse[row] = near;
-                if (p.lse_rest) p.lse_rest[row] = isinf(near) ? 0.f : fmaf(all.m, p.scale, -near) + log_s;
-                if constexpr (ENT) p.entropy[row] = empty ? 0.f : log_s - p.scale * (all.t / all.s);
-                if (p.logprob) {
-                    const int64_t token = p.tokens[row];
-                    float lp = 0.f;                                               // no token given
-                    if (token >= (int64_t)p.V) lp = NAN;
-                    else if (token >= 0)
-                        lp = empty ? -INFINITY
-                                   : (Logit<T>::to_float((reinterpret_cast<const T*>(p.logits) + row * p.row_stride)[token]) - all.m) * p.scale - log_s;
-                    p.logprob[row] = lp;
-                }
-            }
-            if constexpr (TOPK) {
-                if (parts > 1) {
-                    const uint64_t* recs = in_recs + (size_t)turn * parts * lim;
-                    const uint64_t limit = lp_find_limit(recs, parts * lim, p.k, lim, sh);
-                    found = lp_collect(recs, parts * lim, limit, lim, sh);
-                }
-                __syncthreads();                                                  // row_max, row_log, best
-                if (tid < lim && (tid < found || tid < p.k)) {
-                    uint32_t rank = tid;
-                    uint64_t rec = ~0ull;
-                    if (tid < found) {
-                        rec = sh.best[tid];
-                        rank = 0;
-                        for (uint32_t i = 0; i < found; ++i) rank += sh.best[i] < rec;
+                if (lane == 0) {
+                    // lse in two floats: one alone loses ln s beside a large maximum (all of it in a row masked with fp32's
+                    // lowest value), and with it the probabilities that the gradient takes from it
+                    const float near = empty ? -INFINITY : fmaf(all.m, p.scale, log_s);
+                    p.lse[row] = near;
+                    if (p.lse_rest) p.lse_rest[row] = isinf(near) ? 0.f : fmaf(all.m, p.scale, -near) + log_s;
+                    if constexpr (ENT) p.entropy[row] = empty ? 0.f : log_s - p.scale * (all.t / all.s);
+                    if (p.logprob) {
+                        float lp = 0.f;                                           // no token given
+                        if (token >= (int64_t)p.V) lp = NAN;
+                        else if (token >= 0) lp = empty ? -INFINITY : (token_x - all.m) * p.scale - log_s;
+                        p.logprob[row] = lp;
                     }
-                    if (rank < p.k) {
-                        float lp = NAN;                                           // fewer than k elements that are no NaN
-                        int64_t token = -1;
-                        if (rec != ~0ull) {
-                            const float x = __uint_as_float(bits32_from_key(record_key(rec)));
-                            const float log_s = sh.row_log;
-                            lp = log_s == -INFINITY ? -INFINITY : (x - sh.row_max) * p.scale - log_s;
-                            token = (int64_t)record_idx(rec);
+                }
+                if constexpr (TOPK) {
+                    for (uint32_t i = lane; i < max(found, p.k); i += 32) {
+                        uint32_t rank = i;
+                        uint64_t rec = ~0ull;
+                        if (i < found) {
+                            rec = sh.fin[i];
+                            rank = 0;
+#pragma unroll 4
+                            for (uint32_t q = 0; q < found; ++q) rank += sh.fin[q] < rec;
                         }
-                        p.top_logprobs[row * p.k + rank] = lp;
-                        p.top_tokens[row * p.k + rank] = token;
+                        if (rank < p.k) {
+                            float lp = NAN;                                       // fewer than k elements that are no NaN
+                            int64_t at = -1;
+                            if (rec != ~0ull) {
+                                const float x = __uint_as_float(bits32_from_key(record_key(rec)));
+                                lp = empty ? -INFINITY : (x - all.m) * p.scale - log_s;
+                                at = (int64_t)record_idx(rec);
+                            }
+                            p.top_logprobs[(int64_t)row * p.k + rank] = lp;
+                            p.top_tokens[(int64_t)row * p.k + rank] = at;
+                        }
                     }
                 }
             }
+            __syncwarp();
+            if ((int64_t)row + 2 * (int64_t)stride < rows) make_empty(turn);
+            turn ^= 1;
         }
-        turn ^= 1;
-        __syncthreads();
+    } else {
+        // ---- the streaming warps: the loading side runs LP_STAGES - 1 batches ahead of the working side
+        const uint32_t slot_lanes = TOPK ? lp_slot_lanes(p.k) : 1;
+        const F32x2 c2 = f2_make(c, c);
+        const float far = 32.f / c;
+        int32_t load_row = first;
+        const T* load_at = nullptr;                                               // this thread's first vector of the next batch
+        int32_t load_left = 0;                                                    // ... and how many the share still has behind it
+        int load_stage = 0;
+        auto load_from = [&]() {
+            if (load_row >= rows) return;
+            LpShare<T> ld;
+            ld.set(p, load_row, part, parts);
+            load_at = ld.vec(ld.v0 + tid);
+            load_left = (int32_t)(ld.v1 - ld.v0);
+        };
+        load_from();
+        const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(ring) + tid * 16u;
+        auto load_batch = [&]() {
+            if (load_row < rows) {
+                const uint32_t to = ring_addr + load_stage * (LP_STEP * 16u);
+                if (load_left >= (int32_t)LP_STEP) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) lp_cp_async16(to + u * (LP_STREAM * 16u), load_at + u * (LP_STREAM * VEC));
+                } else {
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        if (u * LP_STREAM + (int)tid < load_left) lp_cp_async16(to + u * (LP_STREAM * 16u), load_at + u * (LP_STREAM * VEC));
+                }
+                load_at += LP_STEP * VEC;
+                load_left -= (int32_t)LP_STEP;
+                if (load_left <= 0) {
+                    load_row = load_row > rows - stride ? rows : load_row + stride;
+                    load_from();
+                }
+            }
+            lp_cp_commit();
+            load_stage = load_stage + 1 == LP_STAGES ? 0 : load_stage + 1;
+        };
+#pragma unroll
+        for (int s = 0; s < LP_STAGES - 1; ++s) load_batch();
+
+        int stage = 0;
+        for (int32_t row = first; row < rows; row += stride) {
+            LpShare<T> mine;
+            mine.set(p, row, part, parts);
+            LpRow& r = sh.row[turn];
+            // m: what the exponents of this thread are taken relative to.  It follows the running maximum only when that is
+            // 2^32 ahead: the sums are floating point numbers, so a smaller distance costs them nothing.
+            float m = LOWEST, too_far = LOWEST, seen = LOWEST;
+            F32x2 s2 = f2_make(0.f, 0.f), t2 = s2;                                // even and odd elements apart
+            auto raise = [&](float to) {                                          // the running maximum, and s and t to it
+                const float d = fmaxf(m - to, FAR_BELOW), f = exp2_approx(d * c);
+                const F32x2 f2 = f2_make(f, f);
+                if constexpr (ENT) t2 = f2_mul(f2, f2_fma(f2_make(d, d), s2, t2));
+                s2 = f2_mul(f2, s2);
+                m = to;
+                too_far = to + far;
+            };
+            auto pair = [&](float a, float b, F32x2 minus_m) {
+                const F32x2 d = f2_add(f2_make(a, b), minus_m);
+                float ya, yb;
+                f2_split(f2_mul(d, c2), ya, yb);
+                const F32x2 e = f2_make(exp2_approx(ya), exp2_approx(yb));
+                s2 = f2_add(s2, e);
+                if constexpr (ENT) {                                              // (a masked element: 0 * -inf is no 0)
+                    float da, db;
+                    f2_split(d, da, db);
+                    t2 = f2_fma(e, f2_make(fmaxf(da, FAR_BELOW), fmaxf(db, FAR_BELOW)), t2);
+                }
+            };
+            auto one = [&](float x) {                                             // a single element
+                if (x > too_far) raise(x);
+                seen = fmaxf(seen, x);
+                pair(x, -INFINITY, f2_make(-m, -m));
+            };
+            // elements before the first whole vector
+            if (part == 0 && tid < mine.head) one(Logit<T>::to_float(mine.x[tid]));
+            lp_bar_sync(LP_BAR_EMPTY + turn, LP_THREADS);                         // the finishing warp is done with this place
+            int32_t left = (int32_t)(mine.v1 - mine.v0);                          // vectors of the share from this batch on
+            uint32_t v = mine.v0 + tid, batch = 0;                                // this thread's first vector of the batch
+            float bound = NAN;                                                    // (none yet: nothing is noted)
+            auto note = [&](uint32_t w) {
+                const uint32_t pos = atomicAdd(&r.count, 1u);
+                if (pos < LP_NOTES) r.note[pos] = w;
+            };
+            do {                                                                  // (an empty share still takes its batch)
+                load_batch();
+                lp_cp_wait<LP_STAGES - 1>();
+                const uint4* in = ring + stage * LP_STEP + tid;
+                auto vector = [&](int u) {
+                    const uint4 vec = in[u * LP_STREAM];
+                    const float top = Logit<T>::vec_max(vec);
+                    if (top > too_far) raise(top);
+                    if constexpr (TOPK) {
+                        seen = fmaxf(seen, top);
+                        if (top >= bound) note(v + u * LP_STREAM);
+                    }
+                    const F32x2 minus_m = f2_make(-m, -m);
+                    float x[VEC];
+                    Logit<T>::unpack(vec, x);
+#pragma unroll
+                    for (int j = 0; j < VEC; j += 2) pair(x[j], x[j + 1], minus_m);
+                };
+                if (left >= (int32_t)LP_STEP) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) vector(u);
+                } else {
+#pragma unroll 1
+                    for (int u = 0; u < U; ++u)
+                        if (u * LP_STREAM + (int)tid < left) vector(u);
+                }
+                if constexpr (TOPK) {
+                    volatile float* bound_at = &r.bound;
+                    if (batch == 0) {
+                        lp_write_slot(seen, slot_lanes, sh);
+                        lp_bar_sync(LP_BAR_STREAM, LP_STREAM);
+                        if (warp == 0) {
+                            bound = lp_slot_bound(p.k, slot_lanes, sh);
+                            if (lane == 0) *bound_at = bound;
+                        }
+                        lp_bar_sync(LP_BAR_STREAM, LP_STREAM);
+                        bound = *bound_at;
+#pragma unroll 1
+                        for (int u = 0; u < U; ++u)
+                            if (u * LP_STREAM + (int)tid < left && Logit<T>::vec_max(in[u * LP_STREAM]) >= bound) note(v + u * LP_STREAM);
+                    }
+                    ++batch;
+                    if ((batch & (batch - 1)) == 0) {
+                        lp_write_slot(seen, slot_lanes, sh);
+                    } else if (((batch - 1) & (batch - 2)) == 0 && warp == batch % LP_STREAM_WARPS) {
+                        const float higher = lp_slot_bound(p.k, slot_lanes, sh);
+                        if (lane == 0 && higher > *bound_at) *bound_at = higher;
+                    }
+                    bound = *bound_at;
+                }
+                stage = stage + 1 == LP_STAGES ? 0 : stage + 1;
+                v += LP_STEP;
+                left -= (int32_t)LP_STEP;
+            } while (left > 0);
+            mine.set(p, row, part, parts);                                        // (computed again rather than kept)
+            // elements behind the last whole vector
+            const uint32_t tail = mine.head + mine.nvec * VEC;
+            if (part == parts - 1 && tail + tid < p.V) one(Logit<T>::to_float(mine.x[tail + tid]));
+
+            // join the lanes' parts, in a fixed order
+            LpStats st;
+            st.m = m;
+            float a, b;
+            f2_split(s2, a, b);
+            st.s = a + b;
+            f2_split(t2, a, b);
+            st.t = a + b;
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) {
+                LpStats o;
+                o.m = __shfl_xor_sync(FULL_MASK, st.m, d);
+                o.s = __shfl_xor_sync(FULL_MASK, st.s, d);
+                o.t = ENT ? __shfl_xor_sync(FULL_MASK, st.t, d) : 0.f;
+                st = (lane & d) ? lp_join(o, st, c) : lp_join(st, o, c);
+            }
+            if (lane == 0) r.stats[warp] = st;
+            lp_bar_arrive(LP_BAR_FULL + turn, LP_THREADS);
+            if (parts > 1) cluster.sync();
+            turn ^= 1;
+        }
+        lp_cp_wait<0>();
     }
-    lp_cp_wait<0>();
     if (parts > 1) cluster.sync();                                                // no CTA leaves while its memory is written
 }
 
