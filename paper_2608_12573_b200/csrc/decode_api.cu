@@ -78,15 +78,13 @@ struct Launch {
 constexpr unsigned LP_MAX_PARTS = 16;
 
 size_t lp_smem(unsigned parts, uint32_t k) {
-    size_t bytes = (size_t)LP_STAGES * LP_STEP * 16;
-    if (parts > 1) bytes += 2 * (size_t)parts * ((k ? k + LP_SLACK : 0) * sizeof(uint64_t) + sizeof(LpStats));
-    return bytes;
+    return LP_TEAMS * sizeof(LpTeamMemory) + 2 * (size_t)parts * ((k ? k + LP_SLACK : 0) * sizeof(uint64_t) + sizeof(LpStats));
 }
 
-// CTAs per row: as many as keep the device's two CTAs per SM evenly loaded, with a fixed cost per row and part that is
-// the time of about a quarter of a million bytes divided among the parts.
+// Teams per row: as many as load the device's two teams per SM evenly, with a fixed cost per row and part that is the
+// time of some 16 KB.
 unsigned lp_parts(int64_t rows, int64_t V, size_t elem, int sms) {
-    const double slots = 2.0 * sms, fixed = 16384.0, bytes = (double)V * elem;
+    const double slots = (double)LP_TEAMS * sms, fixed = 16384.0, bytes = (double)V * elem;
     unsigned best = 1;
     double best_cost = 0;
     for (unsigned parts = 1; parts <= LP_MAX_PARTS; parts *= 2) {
@@ -99,12 +97,15 @@ unsigned lp_parts(int64_t rows, int64_t V, size_t elem, int sms) {
 }
 
 template <typename T, bool ENT, bool TOPK>
-int lp_launch(const LpParams& p, unsigned parts, int sms, void* stream) {
+int lp_launch(LpParams p, unsigned parts, int sms, void* stream) {
     static uint64_t done = 0;
     static std::mutex mutex;
-    DEC_TRY(prepare_kernel(logprobs_kernel<T, ENT, TOPK>, lp_smem(LP_MAX_PARTS, LP_MAX_K), true, &done, &mutex));
-    const int64_t clusters = std::min<int64_t>(p.rows, std::max<int64_t>(1, 2 * (int64_t)sms / parts));
-    Launch l((unsigned)(clusters * parts), LP_THREADS, lp_smem(parts, p.k), stream, parts);
+    DEC_TRY(prepare_kernel(logprobs_kernel<T, ENT, TOPK>, lp_smem(LP_MAX_PARTS, LP_MAX_K), false, &done, &mutex));
+    p.parts = parts;
+    const unsigned shares = std::max(1u, parts / LP_TEAMS);
+    const int64_t most = std::max<int64_t>(1, sms / shares);
+    const int64_t groups = std::min<int64_t>(parts > 1 ? p.rows : (p.rows + LP_TEAMS - 1) / LP_TEAMS, most);
+    Launch l((unsigned)(groups * shares), LP_THREADS, lp_smem(parts, p.k), stream, shares);
     DEC_TRY(cudaLaunchKernelEx(&l.cfg, logprobs_kernel<T, ENT, TOPK>, p));
     return PROFK_OK;
 }
@@ -119,7 +120,7 @@ int lp_forward(const T* logits, int64_t rows, int64_t V, int64_t row_stride, con
         return PROFK_EINVAL;
     const int sms = sm_count();
     if (sms < 1) return PROFK_ECUDA;
-    LpParams p{logits, rows, row_stride, (uint32_t)V, (uint32_t)k, (float)(1.0 / temperature), tokens, logprob, lse, lse_rest, entropy, top_logprobs, top_tokens};
+    LpParams p{logits, rows, row_stride, (uint32_t)V, (uint32_t)k, 1u, (float)(1.0 / temperature), tokens, logprob, lse, lse_rest, entropy, top_logprobs, top_tokens};
     const unsigned parts = lp_parts(rows, V, sizeof(T), sms);
     if (entropy) return k ? lp_launch<T, true, true>(p, parts, sms, stream) : lp_launch<T, true, false>(p, parts, sms, stream);
     return k ? lp_launch<T, false, true>(p, parts, sms, stream) : lp_launch<T, false, false>(p, parts, sms, stream);

@@ -14,8 +14,10 @@
 // At the end of the row the noted vectors are read once more and their elements above the last bound are ordered.  Where
 // the list overflows all the same (ascending order, a flood of equal values) the whole row is read once more instead.
 //
-// Eleven warps of a CTA stream; the twelfth finishes rows (joins the statistics, orders the list, writes the results)
-// while the others are in the next one.
+// A CTA holds the whole SM and is two teams of twelve warps, each with rows of its own (or a part of a row each).  Eleven
+// warps of a team stream; the first, which the scheduler prefers, finishes rows (joins the statistics, orders the list,
+// writes the results) while the others are in the next one.  The teams' warps alternate in age: as two CTAs of an SM, one
+// of them finished a third earlier than the other (89 us against 124) and left the SM half idle.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -26,11 +28,13 @@ namespace profk {
 
 namespace cg = cooperative_groups;
 
-constexpr int LP_THREADS = 384;
+constexpr int LP_TEAMS = 2;
 constexpr int LP_STREAM_WARPS = 11;
+constexpr int LP_TEAM = (LP_STREAM_WARPS + 1) * 32;     // threads of a team
 constexpr int LP_STREAM = LP_STREAM_WARPS * 32;
+constexpr int LP_THREADS = LP_TEAMS * LP_TEAM;
 constexpr int LP_UNROLL = 4;              // 16-byte vectors per thread and batch
-constexpr int LP_STAGES = 4;              // batches in flight or in hand per thread
+constexpr int LP_STAGES = 3;              // batches in flight or in hand per thread
 constexpr uint32_t LP_STEP = LP_STREAM * LP_UNROLL;     // vectors per batch
 constexpr uint32_t LP_NOTES = 2048;       // vectors the list holds
 constexpr uint32_t LP_FIN = 512;          // elements the finishing warp holds; more than half of them it cuts back to the k best
@@ -41,6 +45,7 @@ struct LpParams {
     const void* logits;
     int64_t rows, row_stride;
     uint32_t V, k;
+    uint32_t parts;                       // teams that share a row: 1, or twice the CTAs of a cluster
     float scale;                          // 1 / T
     const int64_t* tokens;                // may be null
     float* logprob;
@@ -75,10 +80,22 @@ struct LpShared {
     float slot[LP_STREAM];                // largest logits seen by a group of lanes
 };
 
-// Named barriers: among the streaming warps; a row is ready for the finishing warp; its place may be used again.
-enum { LP_BAR_STREAM = 1, LP_BAR_FULL = 2, LP_BAR_EMPTY = 4 };
-__device__ __forceinline__ void lp_bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-__device__ __forceinline__ void lp_bar_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+// Named barriers of a team: among its streaming warps; a row is ready for the finishing warp; its place may be used again.
+struct LpBarriers {
+    int base;
+    __device__ __forceinline__ explicit LpBarriers(int team) : base(1 + 5 * team) {}
+    __device__ __forceinline__ void full_arrive(int turn) const { asm volatile("bar.arrive %0, %1;" ::"r"(base + 1 + turn), "n"(LP_TEAM) : "memory"); }
+    __device__ __forceinline__ void full_sync(int turn) const { asm volatile("bar.sync %0, %1;" ::"r"(base + 1 + turn), "n"(LP_TEAM) : "memory"); }
+    __device__ __forceinline__ void empty_arrive(int turn) const { asm volatile("bar.arrive %0, %1;" ::"r"(base + 3 + turn), "n"(LP_TEAM) : "memory"); }
+    __device__ __forceinline__ void empty_sync(int turn) const { asm volatile("bar.sync %0, %1;" ::"r"(base + 3 + turn), "n"(LP_TEAM) : "memory"); }
+    // How many of the streaming threads say yes.
+    __device__ __forceinline__ uint32_t count(bool yes) const {
+        uint32_t n;
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.popc.u32 %0, %2, %3, p;\n\t}"
+                     : "=r"(n) : "r"((uint32_t)yes), "r"(base), "n"(LP_STREAM) : "memory");
+        return n;
+    }
+};
 
 // By one warp: a limit (found by halving the interval of the records' value words, then of their index words) such that
 // at least k and at most `most` of the n records in `a` are <= it; no more than `most` valid records (~0 is none): all of
@@ -134,7 +151,7 @@ __device__ __forceinline__ uint64_t lp_find_limit(const uint64_t* a, uint32_t n,
 constexpr uint32_t LP_FEW_K = 16;         // up to here 22 slots, one per lane of a warp, whose k-th largest is found by counting
 __device__ __forceinline__ uint32_t lp_slot_lanes(uint32_t k) { return k <= LP_FEW_K ? 16 : k <= 64 ? 4 : 1; }
 
-__device__ __forceinline__ void lp_write_slot(float seen, uint32_t lanes, LpShared& sh) {
+__device__ __forceinline__ void lp_write_slot(float seen, uint32_t tid, uint32_t lanes, LpShared& sh) {
     if (lanes >= 4) {
         seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 1));
         seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 2));
@@ -143,26 +160,51 @@ __device__ __forceinline__ void lp_write_slot(float seen, uint32_t lanes, LpShar
         seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 4));
         seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 8));
     }
-    if ((threadIdx.x & (lanes - 1)) == 0) sh.slot[threadIdx.x / lanes] = seen;
+    if ((tid & (lanes - 1)) == 0) sh.slot[tid / lanes] = seen;
 }
 
-// By one warp: (nearly) the k-th largest slot.  Slots hold LOWEST at least, and so does the bound: -inf is never appended
-// on the way.
-__device__ __forceinline__ float lp_slot_bound(uint32_t k, uint32_t lanes, const LpShared& sh) {
+// A count that is near enough: at least k values reach the bound, and not many more.
+__device__ __forceinline__ uint32_t lp_enough(uint32_t k) { return k + k / 8 + 1; }
+
+// By the streaming warps: (nearly) the k-th largest of the logits `seen` by their threads, by halving the interval of their
+// order keys.  They are LOWEST at least, and so is the bound: -inf is never noted on the way.
+__device__ __forceinline__ float lp_first_bound(float seen, uint32_t k, const LpBarriers& bar) {
+    const uint32_t key = key_from_bits32(float_bits_exact(seen));
+    uint32_t lo = key_from_bits32(0xFF7FFFFFu), hi = key_from_bits32(0x7F800000u) + 1u;
+    while (lo + 1 < hi) {
+        const uint32_t mid = lo + ((hi - lo) >> 1), c = bar.count(key >= mid);
+        if (c >= k) {
+            lo = mid;
+            if (c <= lp_enough(k)) break;
+        } else {
+            hi = mid;
+        }
+    }
+    return __uint_as_float(bits32_from_key(lo));
+}
+
+// By one warp: a bound from the slots that is no lower than `bound`.
+__device__ __forceinline__ float lp_slot_bound(float bound, uint32_t k, uint32_t lanes, const LpShared& sh) {
     const uint32_t n = LP_STREAM / lanes, lane = lane_id();
     const volatile float* slot = sh.slot;
     if (lanes == 16) {
         const float mine = lane < n ? slot[lane] : -INFINITY;
         uint32_t above = 0;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) above += __shfl_sync(FULL_MASK, mine, i) > mine;
+        for (int i = 0; i < LP_STREAM / 16; ++i) above += __shfl_sync(FULL_MASK, mine, i) > mine;
         // of the slots with fewer than k larger ones the smallest: at least k slots reach it
         const uint32_t key = above < k && lane < n ? key_from_bits32(float_bits_exact(mine)) : 0xFFFFFFFFu;
-        return __uint_as_float(bits32_from_key(__reduce_min_sync(FULL_MASK, key)));
+        return fmaxf(bound, __uint_as_float(bits32_from_key(__reduce_min_sync(FULL_MASK, key))));
     }
-    uint32_t top = 0;
-    for (uint32_t at = lane; at < n; at += 32) top = max(top, key_from_bits32(float_bits_exact(slot[at])));
-    uint32_t lo = key_from_bits32(0xFF7FFFFFu), hi = __reduce_max_sync(FULL_MASK, top) + 1u;
+    uint32_t top = 0, reach = 0;
+    uint32_t lo = key_from_bits32(float_bits_exact(bound));
+    for (uint32_t at = lane; at < n; at += 32) {
+        const uint32_t key = key_from_bits32(float_bits_exact(slot[at]));
+        top = max(top, key);
+        reach += key >= lo;
+    }
+    if (__reduce_add_sync(FULL_MASK, reach) < k) return bound;                    // (slots of groups: coarser than the first bound)
+    uint32_t hi = __reduce_max_sync(FULL_MASK, top) + 1u;
     while (lo + 1 < hi) {
         const uint32_t mid = lo + ((hi - lo) >> 1);
         uint32_t c = 0;                                                           // (a slot that rises meanwhile does no harm)
@@ -171,7 +213,7 @@ __device__ __forceinline__ float lp_slot_bound(uint32_t k, uint32_t lanes, const
         c = __reduce_add_sync(FULL_MASK, c);
         if (c >= k) {
             lo = mid;
-            if (c <= k + k / 8) break;
+            if (c <= lp_enough(k)) break;
         } else {
             hi = mid;
         }
@@ -235,8 +277,21 @@ __device__ __forceinline__ uint32_t lp_fin_vector(uint32_t n, bool has, const ui
     if (!__any_sync(FULL_MASK, has)) return n;
     float x[Logit<T>::VEC];
     Logit<T>::unpack(vec, x);
+    uint32_t hits = 0;
 #pragma unroll
-    for (int j = 0; j < Logit<T>::VEC; ++j) n = lp_fin_add(n, has && x[j] >= bound, x[j], at + j, sh);
+    for (int j = 0; j < Logit<T>::VEC; ++j) hits |= (has && x[j] >= bound ? 1u : 0u) << j;
+    uint32_t incl = __popc(hits);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t up = __shfl_up_sync(FULL_MASK, incl, d);
+        if (lane_id() >= (uint32_t)d) incl += up;
+    }
+    uint32_t pos = n + incl - __popc(hits);
+#pragma unroll
+    for (int j = 0; j < Logit<T>::VEC; ++j)
+        if (hits >> j & 1) sh.fin[pos++] = make_record(key_from_bits32(float_bits_exact(x[j])), at + j);
+    n += __shfl_sync(FULL_MASK, incl, 31);
+    __syncwarp();
     if (n > LP_FIN / 2) {
         const uint64_t limit = lp_find_limit(sh.fin, n, k, k);
         n = lp_fin_drop(n, limit, sh);
@@ -290,36 +345,49 @@ __device__ __forceinline__ uint32_t lp_fin_select(const LpShare<T> mine, uint32_
     return n;
 }
 
-// One cluster of `parts` CTAs takes a row at a time (parts = 1: a plain CTA).  The vectors of the row come through a ring
-// in shared memory that each thread fills and empties for itself (cp.async, no barrier), and that runs on into the next
-// row, so that HBM stays busy while a row is finished.
+struct LpTeamMemory {
+    uint4 ring[LP_STAGES * LP_STEP];
+    LpShared sh;
+};
+
+// A team takes a row at a time (parts = 1), or the teams of a cluster of CTAs a part of a row each.  The vectors of
+// the row come through a ring in shared memory that each thread fills and empties for itself (cp.async, no barrier), and
+// that runs on into the next row, so that HBM stays busy while a row is finished.
 template <typename T, bool ENT, bool TOPK>
-__global__ void __launch_bounds__(LP_THREADS, 2) logprobs_kernel(const LpParams p) {
+__global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams p) {
     constexpr int VEC = Logit<T>::VEC, U = LP_UNROLL;
     extern __shared__ __align__(16) unsigned char lp_dyn[];
-    __shared__ LpShared sh;
-    uint4* ring = reinterpret_cast<uint4*>(lp_dyn);                               // [LP_STAGES][U][LP_STREAM]
+    const uint32_t lane = lane_id(), cta_warp = threadIdx.x >> 5;
+    const int team = (cta_warp >> 2) & 1;
+    const int warp = (int)((cta_warp >> 3) * 4 + (cta_warp & 3)) - 1;              // of the team: -1 finishes, 0 .. stream
+    const uint32_t tid = warp * 32 + lane;
+    LpTeamMemory& mem = reinterpret_cast<LpTeamMemory*>(lp_dyn)[team];
+    LpShared& sh = mem.sh;
+    const uint4* ring = mem.ring;                                                 // [LP_STAGES][U][LP_STREAM]
+    const LpBarriers bar(team);
     const uint32_t lim = TOPK ? p.k + LP_SLACK : 0;
     cg::cluster_group cluster = cg::this_cluster();
-    const uint32_t parts = cluster.num_blocks(), part = cluster.block_rank();
+    const uint32_t parts = p.parts, part = parts > 1 ? cluster.block_rank() * LP_TEAMS + team : 0;
     // what the parts of a row hand to the first of them: two sets, used in turn
-    uint64_t* in_recs = reinterpret_cast<uint64_t*>(ring + (size_t)LP_STAGES * LP_STEP);                    // [2][parts][lim]
-    LpStats* in_stats = reinterpret_cast<LpStats*>(in_recs + (parts > 1 ? 2 * (size_t)parts * lim : 0));   // [2][parts]
+    uint64_t* in_recs = reinterpret_cast<uint64_t*>(lp_dyn + LP_TEAMS * sizeof(LpTeamMemory));              // [2][parts][lim]
+    LpStats* in_stats = reinterpret_cast<LpStats*>(in_recs + 2 * (size_t)parts * lim);                     // [2][parts]
 
-    const unsigned tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
-    const int32_t rows = (int32_t)p.rows, first = (int32_t)(blockIdx.x / parts), stride = (int32_t)(gridDim.x / parts);
+    const uint32_t shares = parts > 1 ? parts / LP_TEAMS : 1;                     // CTAs per row
+    const int32_t rows = (int32_t)p.rows;
+    const int32_t first = parts > 1 ? (int32_t)(blockIdx.x / shares) : (int32_t)(blockIdx.x * LP_TEAMS + team);
+    const int32_t stride = parts > 1 ? (int32_t)(gridDim.x / shares) : (int32_t)(gridDim.x * LP_TEAMS);
     const float c = p.scale * LOG2E;
     pdl_wait();
     pdl_launch_dependents();
     if (parts > 1) cluster.sync();                                                // every CTA of the cluster has started
 
     int turn = 0;
-    if (warp == LP_STREAM_WARPS) {
+    if (warp < 0) {
         // ---- the finishing warp
         auto make_empty = [&](int t) {
             if (lane == 0) { sh.row[t].count = 0; sh.row[t].bound = LOWEST; }
             __syncwarp();
-            lp_bar_arrive(LP_BAR_EMPTY + t, LP_THREADS);
+            bar.empty_arrive(t);
         };
         if (first < rows) make_empty(0);
         if (stride < rows - first) make_empty(1);
@@ -327,7 +395,7 @@ __global__ void __launch_bounds__(LP_THREADS, 2) logprobs_kernel(const LpParams 
             const int64_t token = p.tokens ? p.tokens[row] : -1;
             float token_x = 0.f;
             if (token >= 0 && token < (int64_t)p.V) token_x = Logit<T>::to_float((reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.row_stride)[token]);
-            lp_bar_sync(LP_BAR_FULL + turn, LP_THREADS);
+            bar.full_sync(turn);
             LpRow& r = sh.row[turn];
             // join the warps' statistics, in a fixed order; every lane gets the result
             auto join_lanes = [&](LpStats st, int width) {
@@ -389,26 +457,34 @@ __global__ void __launch_bounds__(LP_THREADS, 2) logprobs_kernel(const LpParams 
                     }
                 }
                 if constexpr (TOPK) {
-                    for (uint32_t i = lane; i < max(found, p.k); i += 32) {
-                        uint32_t rank = i;
-                        uint64_t rec = ~0ull;
-                        if (i < found) {
-                            rec = sh.fin[i];
-                            rank = 0;
-#pragma unroll 4
-                            for (uint32_t q = 0; q < found; ++q) rank += sh.fin[q] < rec;
+                    constexpr int PER = (LP_MAX_K + LP_SLACK) / 32;
+                    uint64_t rec[PER];
+                    uint32_t rank[PER];
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) {
+                        const uint32_t at = i * 32 + lane;
+                        rec[i] = at < found ? sh.fin[at] : ~0ull;
+                        rank[i] = at < found ? 0 : at;
+                    }
+#pragma unroll 2
+                    for (uint32_t q = 0; q < found; ++q) {
+                        const uint64_t other = sh.fin[q];
+#pragma unroll
+                        for (int i = 0; i < PER; ++i)
+                            if (i * 32 < found) rank[i] += other < rec[i] && i * 32 + lane < found;
+                    }
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) {
+                        if (rank[i] >= p.k) continue;
+                        float lp = NAN;                                           // fewer than k elements that are no NaN
+                        int64_t at = -1;
+                        if (rec[i] != ~0ull) {
+                            const float x = __uint_as_float(bits32_from_key(record_key(rec[i])));
+                            lp = empty ? -INFINITY : (x - all.m) * p.scale - log_s;
+                            at = (int64_t)record_idx(rec[i]);
                         }
-                        if (rank < p.k) {
-                            float lp = NAN;                                       // fewer than k elements that are no NaN
-                            int64_t at = -1;
-                            if (rec != ~0ull) {
-                                const float x = __uint_as_float(bits32_from_key(record_key(rec)));
-                                lp = empty ? -INFINITY : (x - all.m) * p.scale - log_s;
-                                at = (int64_t)record_idx(rec);
-                            }
-                            p.top_logprobs[(int64_t)row * p.k + rank] = lp;
-                            p.top_tokens[(int64_t)row * p.k + rank] = at;
-                        }
+                        p.top_logprobs[(int64_t)row * p.k + rank[i]] = lp;
+                        p.top_tokens[(int64_t)row * p.k + rank[i]] = at;
                     }
                 }
             }
@@ -494,7 +570,7 @@ __global__ void __launch_bounds__(LP_THREADS, 2) logprobs_kernel(const LpParams 
             };
             // elements before the first whole vector
             if (part == 0 && tid < mine.head) one(Logit<T>::to_float(mine.x[tid]));
-            lp_bar_sync(LP_BAR_EMPTY + turn, LP_THREADS);                         // the finishing warp is done with this place
+            bar.empty_sync(turn);                                                 // the finishing warp is done with this place
             int32_t left = (int32_t)(mine.v1 - mine.v0);                          // vectors of the share from this batch on
             uint32_t v = mine.v0 + tid, batch = 0;                                // this thread's first vector of the batch
             float bound = NAN;                                                    // (none yet: nothing is noted)
@@ -531,26 +607,20 @@ __global__ void __launch_bounds__(LP_THREADS, 2) logprobs_kernel(const LpParams 
                 if constexpr (TOPK) {
                     volatile float* bound_at = &r.bound;
                     if (batch == 0) {
-                        lp_write_slot(seen, slot_lanes, sh);
-                        lp_bar_sync(LP_BAR_STREAM, LP_STREAM);
-                        if (warp == 0) {
-                            bound = lp_slot_bound(p.k, slot_lanes, sh);
-                            if (lane == 0) *bound_at = bound;
-                        }
-                        lp_bar_sync(LP_BAR_STREAM, LP_STREAM);
-                        bound = *bound_at;
+                        bound = lp_first_bound(seen, p.k, bar);
+                        if (tid == 0) *bound_at = bound;                          // (nobody else writes it before two more batches)
 #pragma unroll 1
                         for (int u = 0; u < U; ++u)
                             if (u * LP_STREAM + (int)tid < left && Logit<T>::vec_max(in[u * LP_STREAM]) >= bound) note(v + u * LP_STREAM);
                     }
                     ++batch;
                     if ((batch & (batch - 1)) == 0) {
-                        lp_write_slot(seen, slot_lanes, sh);
+                        lp_write_slot(seen, tid, slot_lanes, sh);
                     } else if (((batch - 1) & (batch - 2)) == 0 && warp == batch % LP_STREAM_WARPS) {
-                        const float higher = lp_slot_bound(p.k, slot_lanes, sh);
+                        const float higher = lp_slot_bound(*bound_at, p.k, slot_lanes, sh);
                         if (lane == 0 && higher > *bound_at) *bound_at = higher;
                     }
-                    bound = *bound_at;
+                    if (batch > 2) bound = *bound_at;
                 }
                 stage = stage + 1 == LP_STAGES ? 0 : stage + 1;
                 v += LP_STEP;
@@ -578,7 +648,7 @@ __global__ void __launch_bounds__(LP_THREADS, 2) logprobs_kernel(const LpParams 
                 st = (lane & d) ? lp_join(o, st, c) : lp_join(st, o, c);
             }
             if (lane == 0) r.stats[warp] = st;
-            lp_bar_arrive(LP_BAR_FULL + turn, LP_THREADS);
+            bar.full_arrive(turn);
             if (parts > 1) cluster.sync();
             turn ^= 1;
         }
