@@ -102,6 +102,7 @@ int lp_launch(LpParams p, unsigned parts, int sms, void* stream) {
     static std::mutex mutex;
     DEC_TRY(prepare_kernel(logprobs_kernel<T, ENT, TOPK>, lp_smem(LP_MAX_PARTS, LP_MAX_K), false, &done, &mutex));
     p.parts = parts;
+    for (p.parts_log2 = 0; (1u << p.parts_log2) < parts; ++p.parts_log2) {}
     const unsigned shares = std::max(1u, parts / LP_TEAMS);
     const int64_t most = std::max<int64_t>(1, sms / shares);
     const int64_t groups = std::min<int64_t>(parts > 1 ? p.rows : (p.rows + LP_TEAMS - 1) / LP_TEAMS, most);
@@ -120,7 +121,7 @@ int lp_forward(const T* logits, int64_t rows, int64_t V, int64_t row_stride, con
         return PROFK_EINVAL;
     const int sms = sm_count();
     if (sms < 1) return PROFK_ECUDA;
-    LpParams p{logits, rows, row_stride, (uint32_t)V, (uint32_t)k, 1u, (float)(1.0 / temperature), tokens, logprob, lse, lse_rest, entropy, top_logprobs, top_tokens};
+    LpParams p{logits, rows, row_stride, (uint32_t)V, (uint32_t)k, 1u, 0u, (float)(1.0 / temperature), tokens, logprob, lse, lse_rest, entropy, top_logprobs, top_tokens};
     const unsigned parts = lp_parts(rows, V, sizeof(T), sms);
     if (entropy) return k ? lp_launch<T, true, true>(p, parts, sms, stream) : lp_launch<T, true, false>(p, parts, sms, stream);
     return k ? lp_launch<T, false, true>(p, parts, sms, stream) : lp_launch<T, false, false>(p, parts, sms, stream);

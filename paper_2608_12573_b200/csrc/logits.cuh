@@ -11,6 +11,12 @@ namespace profk {
 template <typename T> struct Logit;
 
 template <> struct Logit<float> {
+    static __device__ __forceinline__ uint4 masked() { return make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u); }   // all -inf
+    // Largest element of a vector in the form in which such maxima are joined cheaply (NaN never wins).
+    using Top = float;
+    static __device__ __forceinline__ Top top_of(const uint4& v) { return vec_max(v); }
+    static __device__ __forceinline__ Top join(Top a, Top b) { return fmaxf(a, b); }
+    static __device__ __forceinline__ float value(Top t) { return t; }
     static constexpr int VEC = 4;
     static __device__ __forceinline__ float to_float(float v) { return v; }
     static __device__ __forceinline__ float from_float(float v) { return v; }
@@ -27,6 +33,14 @@ template <> struct Logit<float> {
 };
 
 template <> struct Logit<__nv_bfloat16> {
+    static __device__ __forceinline__ uint4 masked() { return make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u); }
+    using Top = __nv_bfloat162;
+    static __device__ __forceinline__ Top top_of(const uint4& v) {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+        return __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    }
+    static __device__ __forceinline__ Top join(Top a, Top b) { return __hmax2(a, b); }
+    static __device__ __forceinline__ float value(Top t) { return fmaxf(__low2float(t), __high2float(t)); }
     static constexpr int VEC = 8;
     static __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
     static __device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16(v); }
@@ -55,6 +69,14 @@ template <> struct Logit<__nv_bfloat16> {
 };
 
 template <> struct Logit<__half> {
+    static __device__ __forceinline__ uint4 masked() { return make_uint4(0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u); }
+    using Top = __half2;
+    static __device__ __forceinline__ Top top_of(const uint4& v) {
+        const __half2* h = reinterpret_cast<const __half2*>(&v);
+        return __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    }
+    static __device__ __forceinline__ Top join(Top a, Top b) { return __hmax2(a, b); }
+    static __device__ __forceinline__ float value(Top t) { return fmaxf(__low2float(t), __high2float(t)); }
     static constexpr int VEC = 8;
     static __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
     static __device__ __forceinline__ __half from_float(float v) { return __float2half(v); }

@@ -45,7 +45,7 @@ struct LpParams {
     const void* logits;
     int64_t rows, row_stride;
     uint32_t V, k;
-    uint32_t parts;                       // teams that share a row: 1, or twice the CTAs of a cluster
+    uint32_t parts, parts_log2;           // teams that share a row: 1, or twice the CTAs of a cluster (a power of two)
     float scale;                          // 1 / T
     const int64_t* tokens;                // may be null
     float* logprob;
@@ -166,23 +166,6 @@ __device__ __forceinline__ void lp_write_slot(float seen, uint32_t tid, uint32_t
 // A count that is near enough: at least k values reach the bound, and not many more.
 __device__ __forceinline__ uint32_t lp_enough(uint32_t k) { return k + k / 8 + 1; }
 
-// By the streaming warps: (nearly) the k-th largest of the logits `seen` by their threads, by halving the interval of their
-// order keys.  They are LOWEST at least, and so is the bound: -inf is never noted on the way.
-__device__ __forceinline__ float lp_first_bound(float seen, uint32_t k, const LpBarriers& bar) {
-    const uint32_t key = key_from_bits32(float_bits_exact(seen));
-    uint32_t lo = key_from_bits32(0xFF7FFFFFu), hi = key_from_bits32(0x7F800000u) + 1u;
-    while (lo + 1 < hi) {
-        const uint32_t mid = lo + ((hi - lo) >> 1), c = bar.count(key >= mid);
-        if (c >= k) {
-            lo = mid;
-            if (c <= lp_enough(k)) break;
-        } else {
-            hi = mid;
-        }
-    }
-    return __uint_as_float(bits32_from_key(lo));
-}
-
 // By one warp: a bound from the slots that is no lower than `bound`.
 __device__ __forceinline__ float lp_slot_bound(float bound, uint32_t k, uint32_t lanes, const LpShared& sh) {
     const uint32_t n = LP_STREAM / lanes, lane = lane_id();
@@ -221,6 +204,28 @@ __device__ __forceinline__ float lp_slot_bound(float bound, uint32_t k, uint32_t
     return __uint_as_float(bits32_from_key(lo));
 }
 
+// By the streaming warps: (nearly) the k-th largest of the logits `seen` by their threads, by halving the interval of their
+// order keys.  They are LOWEST at least, and so is the bound: -inf is never noted on the way.
+__device__ __forceinline__ float lp_first_bound(float seen, uint32_t k, uint32_t lanes, uint32_t tid, LpShared& sh, const LpBarriers& bar) {
+    if (lanes == 16) {
+        lp_write_slot(seen, tid, lanes, sh);
+        bar.count(true);
+        return lp_slot_bound(LOWEST, k, lanes, sh);
+    }
+    const uint32_t key = key_from_bits32(float_bits_exact(seen));
+    uint32_t lo = key_from_bits32(0xFF7FFFFFu), hi = key_from_bits32(0x7F800000u) + 1u;
+    while (lo + 1 < hi) {
+        const uint32_t mid = lo + ((hi - lo) >> 1), c = bar.count(key >= mid);
+        if (c >= k) {
+            lo = mid;
+            if (c <= lp_enough(k)) break;
+        } else {
+            hi = mid;
+        }
+    }
+    return __uint_as_float(bits32_from_key(lo));
+}
+
 __device__ __forceinline__ void lp_cp_async16(uint32_t smem, const void* gmem) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(gmem) : "memory");
 }
@@ -234,13 +239,13 @@ struct LpShare {
     uint32_t head;         // elements before the first 16-byte boundary
     uint32_t nvec;         // vectors of the row
     uint32_t v0, v1;       // this CTA's vectors
-    __device__ __forceinline__ void set(const LpParams& p, int64_t row, uint32_t part, uint32_t parts) {
+    __device__ __forceinline__ void set(const LpParams& p, int64_t row, uint32_t part) {
         x = reinterpret_cast<const T*>(p.logits) + row * p.row_stride;
         const uint32_t mis = (uint32_t)(reinterpret_cast<uintptr_t>(x) & 15u);
         head = min(p.V, mis ? (16u - mis) / (uint32_t)sizeof(T) : 0u);
         nvec = (p.V - head) / Logit<T>::VEC;
-        v0 = (uint32_t)((uint64_t)nvec * part / parts);
-        v1 = (uint32_t)((uint64_t)nvec * (part + 1) / parts);
+        v0 = (uint32_t)((uint64_t)nvec * part >> p.parts_log2);
+        v1 = (uint32_t)((uint64_t)nvec * (part + 1) >> p.parts_log2);
     }
     __device__ __forceinline__ const T* vec(uint32_t v) const { return x + head + (size_t)v * Logit<T>::VEC; }
 };
@@ -412,7 +417,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
             uint32_t found = 0;
             if constexpr (TOPK) {
                 LpShare<T> mine;
-                mine.set(p, row, part, parts);
+                mine.set(p, row, part);
                 found = lp_fin_select<T>(mine, p.k, part == 0, part == parts - 1, p.V, r, sh);
             }
             if (parts > 1) {
@@ -504,7 +509,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
         auto load_from = [&]() {
             if (load_row >= rows) return;
             LpShare<T> ld;
-            ld.set(p, load_row, part, parts);
+            ld.set(p, load_row, part);
             load_at = ld.vec(ld.v0 + tid);
             load_left = (int32_t)(ld.v1 - ld.v0);
         };
@@ -537,7 +542,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
         int stage = 0;
         for (int32_t row = first; row < rows; row += stride) {
             LpShare<T> mine;
-            mine.set(p, row, part, parts);
+            mine.set(p, row, part);
             LpRow& r = sh.row[turn];
             // m: what the exponents of this thread are taken relative to.  It follows the running maximum only when that is
             // 2^32 ahead: the sums are floating point numbers, so a smaller distance costs them nothing.
@@ -551,28 +556,35 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
                 m = to;
                 too_far = to + far;
             };
-            auto pair = [&](float a, float b, F32x2 minus_m) {
+            auto pair = [&](float a, float b, F32x2 minus_m) {                    // (a masked element makes t NaN: 0 * -inf)
                 const F32x2 d = f2_add(f2_make(a, b), minus_m);
                 float ya, yb;
                 f2_split(f2_mul(d, c2), ya, yb);
                 const F32x2 e = f2_make(exp2_approx(ya), exp2_approx(yb));
                 s2 = f2_add(s2, e);
-                if constexpr (ENT) {                                              // (a masked element: 0 * -inf is no 0)
-                    float da, db;
-                    f2_split(d, da, db);
-                    t2 = f2_fma(e, f2_make(fmaxf(da, FAR_BELOW), fmaxf(db, FAR_BELOW)), t2);
-                }
+                if constexpr (ENT) t2 = f2_fma(e, d, t2);
+            };
+            auto masked_pair = [&](float a, float b, F32x2 minus_m) {             // t alone, a masked element adds nothing to it
+                float da, db;
+                f2_split(f2_add(f2_make(a, b), minus_m), da, db);
+                t2 = f2_fma(f2_make(exp2_approx(da * c), exp2_approx(db * c)), f2_make(fmaxf(da, FAR_BELOW), fmaxf(db, FAR_BELOW)), t2);
             };
             auto one = [&](float x) {                                             // a single element
                 if (x > too_far) raise(x);
                 seen = fmaxf(seen, x);
+                const F32x2 before = t2;
                 pair(x, -INFINITY, f2_make(-m, -m));
+                if constexpr (ENT) {
+                    t2 = before;
+                    masked_pair(x, -INFINITY, f2_make(-m, -m));
+                }
             };
             // elements before the first whole vector
             if (part == 0 && tid < mine.head) one(Logit<T>::to_float(mine.x[tid]));
             bar.empty_sync(turn);                                                 // the finishing warp is done with this place
             int32_t left = (int32_t)(mine.v1 - mine.v0);                          // vectors of the share from this batch on
             uint32_t v = mine.v0 + tid, batch = 0;                                // this thread's first vector of the batch
+            const uint32_t raise_at = (2u << warp) + 1u;                          // the warp's turn to renew the bound
             float bound = NAN;                                                    // (none yet: nothing is noted)
             auto note = [&](uint32_t w) {
                 const uint32_t pos = atomicAdd(&r.count, 1u);
@@ -582,41 +594,84 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
                 load_batch();
                 lp_cp_wait<LP_STAGES - 1>();
                 const uint4* in = ring + stage * LP_STEP + tid;
-                auto vector = [&](int u) {
-                    const uint4 vec = in[u * LP_STREAM];
-                    const float top = Logit<T>::vec_max(vec);
-                    if (top > too_far) raise(top);
-                    if constexpr (TOPK) {
-                        seen = fmaxf(seen, top);
-                        if (top >= bound) note(v + u * LP_STREAM);
+                // (vectors behind the share count as masked where maxima are taken, and are left out of the sums)
+                const bool full = left >= (int32_t)LP_STEP;
+                uint4 vec[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) vec[u] = in[u * LP_STREAM];
+                if (!full) {
+                    asm volatile("" ::: "memory");                                // (a branch, not sixteen selections per batch)
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        if (u * LP_STREAM + (int)tid >= left) vec[u] = Logit<T>::masked();
+                }
+                // One look at the batch's largest element decides whether the exponents' reference moves and whether any
+                // vector has to be noted; both are rare, and decided by warp, which then stays together.
+                typename Logit<T>::Top tops[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) tops[u] = Logit<T>::top_of(vec[u]);
+                const float top = Logit<T>::value(Logit<T>::join(Logit<T>::join(tops[0], tops[1]), Logit<T>::join(tops[2], tops[3])));
+                if (__any_sync(FULL_MASK, top > too_far)) raise(fmaxf(m, top));
+                if constexpr (TOPK) {
+                    seen = fmaxf(seen, top);
+                    if (__any_sync(FULL_MASK, top >= bound)) {
+#pragma unroll
+                        for (int u = 0; u < U; ++u)
+                            if (Logit<T>::value(tops[u]) >= bound) note(v + u * LP_STREAM);
+                        __syncwarp();
                     }
-                    const F32x2 minus_m = f2_make(-m, -m);
-                    float x[VEC];
-                    Logit<T>::unpack(vec, x);
+                }
+                const F32x2 minus_m = f2_make(-m, -m), before = t2;
+                if (full) {
 #pragma unroll
-                    for (int j = 0; j < VEC; j += 2) pair(x[j], x[j + 1], minus_m);
-                };
-                if (left >= (int32_t)LP_STEP) {
+                    for (int u = 0; u < U; ++u) {
+                        float x[VEC];
+                        Logit<T>::unpack(vec[u], x);
 #pragma unroll
-                    for (int u = 0; u < U; ++u) vector(u);
+                        for (int j = 0; j < VEC; j += 2) pair(x[j], x[j + 1], minus_m);
+                    }
                 } else {
 #pragma unroll 1
-                    for (int u = 0; u < U; ++u)
-                        if (u * LP_STREAM + (int)tid < left) vector(u);
+                    for (int u = 0; u < U; ++u) {
+                        if (u * LP_STREAM + (int)tid >= left) break;
+                        float x[VEC];
+                        Logit<T>::unpack(in[u * LP_STREAM], x);
+#pragma unroll
+                        for (int j = 0; j < VEC; j += 2) pair(x[j], x[j + 1], minus_m);
+                    }
+                    __syncwarp();
+                }
+                if constexpr (ENT) {
+                    // Masked elements in the batch (or NaN): t once more, slowly.
+                    float a, b;
+                    f2_split(t2, a, b);
+                    if (__any_sync(FULL_MASK, isnan(a + b))) {
+                        t2 = before;
+#pragma unroll 1
+                        for (int u = 0; u < U; ++u) {
+                            if (u * LP_STREAM + (int)tid >= left) break;
+                            float x[VEC];
+                            Logit<T>::unpack(in[u * LP_STREAM], x);
+#pragma unroll
+                            for (int j = 0; j < VEC; j += 2) masked_pair(x[j], x[j + 1], minus_m);
+                        }
+                        __syncwarp();
+                    }
                 }
                 if constexpr (TOPK) {
                     volatile float* bound_at = &r.bound;
                     if (batch == 0) {
-                        bound = lp_first_bound(seen, p.k, bar);
+                        bound = lp_first_bound(seen, p.k, slot_lanes, tid, sh, bar);
                         if (tid == 0) *bound_at = bound;                          // (nobody else writes it before two more batches)
-#pragma unroll 1
+#pragma unroll
                         for (int u = 0; u < U; ++u)
-                            if (u * LP_STREAM + (int)tid < left && Logit<T>::vec_max(in[u * LP_STREAM]) >= bound) note(v + u * LP_STREAM);
+                            if (Logit<T>::value(tops[u]) >= bound) note(v + u * LP_STREAM);
+                        __syncwarp();
                     }
                     ++batch;
                     if ((batch & (batch - 1)) == 0) {
                         lp_write_slot(seen, tid, slot_lanes, sh);
-                    } else if (((batch - 1) & (batch - 2)) == 0 && warp == batch % LP_STREAM_WARPS) {
+                    } else if (batch == raise_at) {                               // one warp, a batch later: the slots are written
                         const float higher = lp_slot_bound(*bound_at, p.k, slot_lanes, sh);
                         if (lane == 0 && higher > *bound_at) *bound_at = higher;
                     }
@@ -626,7 +681,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
                 v += LP_STEP;
                 left -= (int32_t)LP_STEP;
             } while (left > 0);
-            mine.set(p, row, part, parts);                                        // (computed again rather than kept)
+            mine.set(p, row, part);                                        // (computed again rather than kept)
             // elements behind the last whole vector
             const uint32_t tail = mine.head + mine.nvec * VEC;
             if (part == parts - 1 && tail + tid < p.V) one(Logit<T>::to_float(mine.x[tail + tid]));
