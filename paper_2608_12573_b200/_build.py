@@ -1,4 +1,4 @@
-"""In-tree build of the CUDA library: nvcc -> paper_2608_12573_b200/libprofk.so (sm_100a only)."""
+"""In-tree build of the CUDA library (nvcc -> libprofk.so, sm_100a only) and of the binding of its decoding operators."""
 from __future__ import annotations
 
 import os
@@ -9,11 +9,13 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libprofk.so")
+BINDING_PATH = os.path.join(PKG_DIR, "_decode.so")
+BINDING_SOURCE = os.path.join(CSRC, "decode_binding.cpp")
 SOURCES = ["profk_api.cu", "decode_api.cu", "plan.cpp"]
 
 
 def _newest_source_mtime() -> float:
-    paths = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "profk.h")]
+    paths = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f != os.path.basename(BINDING_SOURCE)] + [os.path.join(ROOT, "include", "profk.h")]
     return max(os.path.getmtime(p) for p in paths)
 
 
@@ -25,9 +27,36 @@ def nvcc_command(extra: list[str] | None = None) -> list[str]:
     return cmd + (extra or []) + os.environ.get("PROFK_NVCC_FLAGS", "").split()
 
 
+def binding_command() -> list[str]:
+    """g++ -> paper_2608_12573_b200/_decode.so, the CPython binding of the decoding operators over torch's tensors."""
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths, library_paths
+
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"]]
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    cmd += [f"-I{p}" for p in include_paths() + [os.path.join(cuda, "include")]]
+    cmd += [BINDING_SOURCE, "-o", BINDING_PATH, f"-L{PKG_DIR}", "-l:" + os.path.basename(LIB_PATH), "-Wl,-rpath,$ORIGIN"]
+    cmd += [f"-L{p}" for p in library_paths()] + ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch", "-ltorch_python"]
+    return cmd
+
+
+def _build_binding(force: bool) -> None:
+    deps = [BINDING_SOURCE, os.path.join(ROOT, "include", "profk.h")]
+    if not force and os.path.exists(BINDING_PATH) and os.path.getmtime(BINDING_PATH) >= max(os.path.getmtime(d) for d in deps):
+        return
+    res = subprocess.run(binding_command(), capture_output=True, text=True)
+    if res.returncode != 0:
+        sys.stderr.write(res.stdout + res.stderr)
+        raise RuntimeError("g++ failed building _decode.so")
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile the library unless an up-to-date one is already in the tree; returns its path."""
+    """Compile the library and the binding unless up-to-date ones are already in the tree; returns the library's path."""
     if not force and os.path.exists(LIB_PATH) and os.path.getmtime(LIB_PATH) >= _newest_source_mtime():
+        _build_binding(force)
         return LIB_PATH
     cmd = nvcc_command(["-Xptxas", "-v"] if verbose else None)
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -36,6 +65,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         raise RuntimeError("nvcc failed building libprofk.so")
     if verbose:
         sys.stderr.write(res.stdout + res.stderr)
+    _build_binding(force)
     return LIB_PATH
 
 
