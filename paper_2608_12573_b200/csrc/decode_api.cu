@@ -159,19 +159,28 @@ size_t pa_workspace(int64_t dim, int sms) {
     return pa_meta_bytes(ctas) + (size_t)ctas * 2 * PA_ROWS * (pa_tile_dim(dim) + 2) * sizeof(float);
 }
 
-template <typename T, int D>
+template <typename T, int D, int N8>
 int pa_launch(const PaParams& p, unsigned ctas, void* stream) {
     static uint64_t done = 0;
     static std::mutex mutex;
-    DEC_TRY(prepare_kernel(paged_attention_kernel<T, D>, PaShape<D>::SMEM, false, &done, &mutex));
+    DEC_TRY(prepare_kernel(paged_attention_kernel<T, D, N8>, PaShape<D>::SMEM, false, &done, &mutex));
     Launch l(ctas, PA_THREADS, PaShape<D>::SMEM, stream);
-    DEC_TRY(cudaLaunchKernelEx(&l.cfg, paged_attention_kernel<T, D>, p));
+    DEC_TRY(cudaLaunchKernelEx(&l.cfg, paged_attention_kernel<T, D, N8>, p));
     Launch j(ctas, PJ_THREADS, 0, stream);
     j.cfg.gridDim.y = (unsigned)p.rows;
     DEC_TRY(cudaLaunchKernelEx(&j.cfg, paged_attention_join_kernel<T, D>, p));
     return PROFK_OK;
 }
+template <typename T, int D>
+int pa_launch(const PaParams& p, unsigned ctas, void* stream) {
+    return p.rows <= 8 ? pa_launch<T, D, 1>(p, ctas, stream) : pa_launch<T, D, 2>(p, ctas, stream);
+}
 
+int32_t log2_of(int64_t n) {      // -1: no power of two
+    int32_t s = 0;
+    while ((int64_t)1 << s < n) ++s;
+    return (int64_t)1 << s == n ? s : -1;
+}
 bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 template <typename T>
@@ -195,7 +204,7 @@ int pa_run(const T* q, int64_t q_seq, int64_t q_head, const T* k, const T* v, co
     const unsigned ctas = (unsigned)std::min<int64_t>(pa_ctas(dim, sms), most);
     PaParams p{q, k, v, q_seq, q_head, ks->page, ks->head, ks->token, vs->page, vs->head, vs->token, tables, table_stride, lengths,
                (int32_t)seqs, (int32_t)heads, (int32_t)kv_heads, group, (int32_t)dim, (int32_t)page_size, (int32_t)pages, (int32_t)width,
-               blocks, (group + blocks - 1) / blocks, (float)scale, out, lse,
+               blocks, (group + blocks - 1) / blocks, log2_of(page_size), page_size % PA_WARP_TOKENS == 0, (float)scale, out, lse,
                reinterpret_cast<float*>(static_cast<char*>(workspace) + pa_meta_bytes(pa_ctas(dim, sms))), static_cast<PaMeta*>(workspace)};
     switch (pa_tile_dim(dim)) {
         case 64: return pa_launch<T, 64>(p, ctas, stream);

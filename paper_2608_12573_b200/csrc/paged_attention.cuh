@@ -7,8 +7,10 @@
 // head) leaves its running maximum, sum and unnormalised output for a second, small kernel that joins the parts in order.
 //
 // Inside a CTA each of four warps takes 16 tokens of a tile through a ring of its own in shared memory (cp.async; no
-// barrier until the (sequence, head) ends), and multiplies with the warp-level matrix instruction: 16 query heads x 16
-// tokens is far below what a tcgen05 tile wants, and the tensor pipe is not what bounds it.
+// barrier until the (sequence, head) ends), and multiplies with the warp-level matrix instruction, tokens (and then
+// dimensions) along its 16 rows and query heads along its 8 columns: K Q^T, then V^T P^T.  The few heads that share a key
+// are the narrow side of the product, far below the 128 rows that a tcgen05 tile wants, and the tensor pipe is not what
+// bounds it.
 #pragma once
 
 #include "logits.cuh"
@@ -19,9 +21,9 @@ constexpr int PA_WARPS = 4;
 constexpr int PA_THREADS = PA_WARPS * 32;
 constexpr int PA_WARP_TOKENS = 16;
 constexpr int PA_TILE = PA_WARPS * PA_WARP_TOKENS;      // tokens per tile
-constexpr int PA_ROWS = 16;                             // query heads per pass over a key-value head
+constexpr int PA_ROWS = 16;                             // most query heads per pass over a key-value head
 constexpr int PA_MERGE_COLS = 64;
-constexpr int PA_MERGE_STRIDE = PA_MERGE_COLS + 8;      // floats; 8 rows x 4 column pairs then fall on 32 banks
+constexpr int PA_MERGE_STRIDE = PA_MERGE_COLS + 4;      // floats; 4 row pairs x 8 columns then fall on 32 banks
 
 template <int D> struct PaShape {
     static constexpr int STAGES = D == 64 ? 6 : 3;      // of the ring: 96 KB per CTA up to D = 128, 192 KB for 256
@@ -44,6 +46,8 @@ struct PaParams {
     const int32_t* lengths;
     int32_t seqs, heads, kv_heads, group, dim, page_size, pages, width;
     int32_t blocks, rows;                               // passes per key-value head, query heads per pass (<= PA_ROWS)
+    int32_t page_shift;                                 // log2 of the page size, or -1
+    int32_t one_page;                                   // the page size is a multiple of 16: a warp's tokens lie in one page
     float scale;
     void* out;                                          // seqs x heads x dim
     float* lse;                                         // seqs x heads
@@ -121,11 +125,19 @@ struct PaCursor {
     }
 };
 
-template <typename T, int D>
+// Transposes an 8 x 8 matrix of 16-bit numbers held by the warp (lane 4 r + q: row r, columns 2 q and 2 q + 1).
+__device__ __forceinline__ uint32_t pa_transpose(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// N8: groups of eight query heads per pass (rows <= 8 N8).
+template <typename T, int D, int N8>
 __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_kernel(const PaParams p) {
     using Shape = PaShape<D>;
-    constexpr int STAGES = Shape::STAGES, CH = D / 8, KSTEPS = D / 16, NT = D / 8;
-    constexpr int ROWS_PER_LOAD = 32 / CH > 0 ? 32 / CH : 1;                 // token rows that one warp-wide copy covers
+    constexpr int STAGES = Shape::STAGES, CH = D / 8, KSTEPS = D / 16, MT = D / 16;
+    constexpr int ROWS_PER_LOAD = 32 / CH;                                   // token rows that one warp-wide copy covers
     constexpr int LOADS = PA_WARP_TOKENS / ROWS_PER_LOAD;
     extern __shared__ __align__(128) unsigned char pa_dyn[];
     __shared__ __align__(16) float s_merge[PA_WARPS][8][PA_MERGE_STRIDE];
@@ -200,34 +212,73 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(pa_dyn) + warp * STAGES * Shape::STAGE_BYTES;
     const int chunk = lane % CH, row0 = lane / CH;                            // (CH = 32: one row per copy)
     const bool chunk_in = chunk * 8 < p.dim;
-    auto page_of = [&](const PaCursor& c) -> int32_t {                        // of the lane's token; -1: no token, or no page
-        const int32_t t = c.tile * PA_TILE + warp * PA_WARP_TOKENS + (lane & 15);
+    const uint32_t to0 = row0 * (D * 2) + ((chunk ^ (row0 & 7)) << 4);
+    auto page_number = [&](int32_t t) { return p.page_shift >= 0 ? t >> p.page_shift : t / p.page_size; };
+    // page of the lane's token (one_page: of the warp's first token); -1: no token, or no page
+    auto page_of = [&](const PaCursor& c) -> int32_t {
+        const int32_t t = c.tile * PA_TILE + warp * PA_WARP_TOKENS + (p.one_page ? 0 : (lane & 15));
         if (t >= c.len) return -1;
-        const int32_t page = p.tables[c.seq * p.table_stride + t / p.page_size];
+        const int32_t page = p.tables[c.seq * p.table_stride + page_number(t)];
         return page >= 0 && page < p.pages ? page : -1;
     };
     int32_t page = page_of(load);
     auto load_tile = [&]() {
         if (loaded < count) {
-            const int32_t t = load.tile * PA_TILE + warp * PA_WARP_TOKENS + (lane & 15);
-            const int32_t slot = t % p.page_size, head = load.stream / p.blocks;
-            const bool in = page >= 0;
-            const int64_t k_off = in ? page * p.k_page + head * p.k_head + slot * p.k_token : 0;
-            const int64_t v_off = in ? page * p.v_page + head * p.v_head + slot * p.v_token : 0;
-            const uint32_t mask = __ballot_sync(FULL_MASK, in) & 0xFFFFu;
-            if (lane == 0) s_mask[warp][load_stage] = mask;
+            const int32_t t0 = load.tile * PA_TILE + warp * PA_WARP_TOKENS, head = load.stream / p.blocks;
+            const uint32_t base = ring + load_stage * Shape::STAGE_BYTES;
+            if (p.one_page) {
+                const int32_t slot = t0 - page_number(t0) * p.page_size;
+                const int32_t n = page < 0 ? 0 : min(PA_WARP_TOKENS, load.len - t0);
+                const T* kp = reinterpret_cast<const T*>(p.k);
+                const T* vp = reinterpret_cast<const T*>(p.v);
+                if (n > 0 && chunk_in) {
+                    kp += page * p.k_page + head * p.k_head + (slot + row0) * p.k_token + chunk * 8;
+                    vp += page * p.v_page + head * p.v_head + (slot + row0) * p.v_token + chunk * 8;
+                }
+                if (lane == 0) s_mask[warp][load_stage] = (1u << n) - 1u;
+                if (n == PA_WARP_TOKENS && chunk_in) {
+#pragma unroll
+                    for (int i = 0; i < LOADS; ++i) {
+                        const uint32_t to = base + ((to0 ^ ((i * ROWS_PER_LOAD & 7) << 4)) + i * ROWS_PER_LOAD * (D * 2));
+                        pa_cp_async(to, kp + i * ROWS_PER_LOAD * p.k_token, true);
+                        pa_cp_async(to + PA_WARP_TOKENS * D * 2, vp + i * ROWS_PER_LOAD * p.v_token, true);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < LOADS; ++i) {
+                        const int row = i * ROWS_PER_LOAD + row0;
+                        const bool read = chunk_in && row < n;
+                        const uint32_t to = base + row * (D * 2) + ((chunk ^ (row & 7)) << 4);
+                        pa_cp_async(to, read ? kp + i * ROWS_PER_LOAD * p.k_token : reinterpret_cast<const T*>(p.k), read);
+                        pa_cp_async(to + PA_WARP_TOKENS * D * 2, read ? vp + i * ROWS_PER_LOAD * p.v_token : reinterpret_cast<const T*>(p.v), read);
+                    }
+                }
+            } else {
+                const int32_t t = t0 + (lane & 15), slot = t - page_number(t) * p.page_size;
+                const bool in = page >= 0;
+                const int64_t k_off = in ? page * p.k_page + head * p.k_head + slot * p.k_token : 0;
+                const int64_t v_off = in ? page * p.v_page + head * p.v_head + slot * p.v_token : 0;
+                const uint32_t mask = __ballot_sync(FULL_MASK, in) & 0xFFFFu;
+                if (lane == 0) s_mask[warp][load_stage] = mask;
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) {
+                    const int row = i * ROWS_PER_LOAD + row0;
+                    const int64_t ko = __shfl_sync(FULL_MASK, k_off, row), vo = __shfl_sync(FULL_MASK, v_off, row);
+                    const bool read = chunk_in && (mask >> row & 1);
+                    const uint32_t to = base + row * (D * 2) + ((chunk ^ (row & 7)) << 4);
+                    pa_cp_async(to, reinterpret_cast<const T*>(p.k) + ko + (read ? chunk * 8 : 0), read);
+                    pa_cp_async(to + PA_WARP_TOKENS * D * 2, reinterpret_cast<const T*>(p.v) + vo + (read ? chunk * 8 : 0), read);
+                }
+            }
             ++loaded;
             load.next(p, streams);
-            if (loaded < count) page = page_of(load);                         // ready by the next call
-            const uint32_t base = ring + load_stage * Shape::STAGE_BYTES;
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int row = i * ROWS_PER_LOAD + row0;
-                const int64_t ko = __shfl_sync(FULL_MASK, k_off, row), vo = __shfl_sync(FULL_MASK, v_off, row);
-                const bool read = chunk_in && (mask >> row & 1);
-                const uint32_t to = base + row * (D * 2) + ((chunk ^ (row & 7)) << 4);
-                pa_cp_async(to, reinterpret_cast<const T*>(p.k) + ko + (read ? chunk * 8 : 0), read);
-                pa_cp_async(to + PA_WARP_TOKENS * D * 2, reinterpret_cast<const T*>(p.v) + vo + (read ? chunk * 8 : 0), read);
+            if (loaded < count) {
+                page = page_of(load);                                         // ready by the next call
+                if (load.tile == 0) {                                         // the queries of a stream that begins
+                    const int32_t h = (load.stream / p.blocks) * p.group + (load.stream % p.blocks) * p.rows + lane;
+                    if (lane < p.rows && h < p.heads)
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const T*>(p.q) + load.seq * p.q_seq + h * p.q_head));
+                }
             }
         }
         pa_cp_commit();
@@ -237,8 +288,8 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
     for (int s = 0; s < STAGES - 1; ++s) load_tile();
 
     const float c = p.scale * LOG2E;
-    uint32_t qf[KSTEPS][4];
-    float o[NT][4], m[2], l[2];
+    uint32_t qf[N8][KSTEPS][2];
+    float o[MT][N8][4], m[N8][2], l[N8][2];                                   // of heads 8 n + 2 quad and + 1
     bool fresh = true, whole = work.tile == 0;                                // a new stream begins / it began in this share
     int stage = 0;
     PaMeta meta{-1, 0, 0, 0};
@@ -248,84 +299,97 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
         const int32_t rows = min(p.rows, (work.stream / p.blocks + 1) * p.group - head0);
         if (fresh) {
             fresh = false;
-            m[0] = m[1] = LOWEST;
-            l[0] = l[1] = 0.f;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
             const T* q = reinterpret_cast<const T*>(p.q) + work.seq * p.q_seq + head0 * p.q_head;
 #pragma unroll
-            for (int ks = 0; ks < KSTEPS; ++ks)
+            for (int n = 0; n < N8; ++n) {
+                m[n][0] = m[n][1] = LOWEST;
+                l[n][0] = l[n][1] = 0.f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = g + (i & 1) * 8, col = ks * 16 + quad * 2 + (i >> 1) * 8;
-                    qf[ks][i] = r < rows && col < p.dim ? *reinterpret_cast<const uint32_t*>(q + r * p.q_head + col) : 0u;
-                }
+                for (int mt = 0; mt < MT; ++mt) o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < KSTEPS; ++ks)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int r = n * 8 + g, col = ks * 16 + i * 8 + quad * 2;
+                        qf[n][ks][i] = r < rows && col < p.dim ? *reinterpret_cast<const uint32_t*>(q + r * p.q_head + col) : 0u;
+                    }
+            }
         }
         pa_cp_wait<STAGES - 1>();
         __syncwarp();
         const uint32_t kb = ring + stage * Shape::STAGE_BYTES, vb = kb + PA_WARP_TOKENS * D * 2;
-        // scores: 16 heads x 16 tokens
-        float s[2][4] = {};
+        // scores: 16 tokens x 8 N8 heads
+        float s[N8][4] = {};
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) {
-            const int row = (lane & 7) + ((lane >> 4) << 3), ch = ks * 2 + ((lane >> 3) & 1);
-            uint32_t b[4];
-            pa_ldmatrix(b, kb + row * (D * 2) + ((ch ^ (row & 7)) << 4));
-            pa_mma<T>(s[0], qf[ks], b[0], b[1]);
-            pa_mma<T>(s[1], qf[ks], b[2], b[3]);
+            const int row = lane & 15, ch = ks * 2 + (lane >> 4);
+            uint32_t a[4];
+            pa_ldmatrix(a, kb + row * (D * 2) + ((ch ^ (row & 7)) << 4));
+#pragma unroll
+            for (int n = 0; n < N8; ++n) pa_mma<T>(s[n], a, qf[n][ks][0], qf[n][ks][1]);
         }
         const uint32_t mask = s_mask[warp][stage];
         if (mask != 0xFFFFu) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int n = 0; n < N8; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (!(mask >> (n * 8 + quad * 2 + (i & 1)) & 1)) s[n][i] = -INFINITY;
+                    if (!(mask >> (g + (i >> 1) * 8) & 1)) s[n][i] = -INFINITY;
         }
-        // running maximum: of row g (i = 0, 1) and of row g + 8 (i = 2, 3)
-        float top[2];
+        // running maxima of the thread's heads (i & 1), over its two tokens and the eight lanes of the same quad
+        float top[N8][2];
+        bool higher = false;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            top[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
-            top[h] = fmaxf(top[h], __shfl_xor_sync(FULL_MASK, top[h], 1));
-            top[h] = fmaxf(top[h], __shfl_xor_sync(FULL_MASK, top[h], 2));
-        }
-        if (__any_sync(FULL_MASK, top[0] > m[0] || top[1] > m[1])) {
+        for (int n = 0; n < N8; ++n)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float to = fmaxf(m[h], top[h]), f = exp2_approx((m[h] - to) * c);
-                m[h] = to;
-                l[h] *= f;
-#pragma unroll
-                for (int n = 0; n < NT; ++n) { o[n][2 * h] *= f; o[n][2 * h + 1] *= f; }
+                float t = fmaxf(s[n][h], s[n][2 + h]);
+                t = fmaxf(t, __shfl_xor_sync(FULL_MASK, t, 4));
+                t = fmaxf(t, __shfl_xor_sync(FULL_MASK, t, 8));
+                t = fmaxf(t, __shfl_xor_sync(FULL_MASK, t, 16));
+                top[n][h] = t;
+                higher = higher || t > m[n][h];
             }
+        if (__any_sync(FULL_MASK, higher)) {
+#pragma unroll
+            for (int n = 0; n < N8; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float to = fmaxf(m[n][h], top[n][h]), f = exp2_approx((m[n][h] - to) * c);
+                    m[n][h] = to;
+                    l[n][h] *= f;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) { o[mt][n][h] *= f; o[mt][n][2 + h] *= f; }
+                }
         }
-        float e[2][4];
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e[n][i] = exp2_approx((s[n][i] - m[i >> 1]) * c);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) l[h] += (e[0][2 * h] + e[0][2 * h + 1]) + (e[1][2 * h] + e[1][2 * h + 1]);
         // The probabilities enter the second product as two numbers of the cache's type, the rounded one and what the
         // rounding left off: one alone would add an error as large as the rounding of the output.
-        uint32_t hi[4], lo[4];
+        uint32_t hi[N8][2], lo[N8][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float a = e[i >> 1][(i & 1) * 2], b = e[i >> 1][(i & 1) * 2 + 1];
-            hi[i] = pa_pack<T>(a, b);
-            const float2 r = pa_unpack<T>(hi[i]);
-            lo[i] = pa_pack<T>(a - r.x, b - r.y);
+        for (int n = 0; n < N8; ++n) {
+            float e[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = exp2_approx((s[n][i] - m[n][i & 1]) * c);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) l[n][h] += e[h] + e[2 + h];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t w = pa_pack<T>(e[2 * i], e[2 * i + 1]);
+                const float2 r = pa_unpack<T>(w);
+                hi[n][i] = pa_transpose(w);
+                lo[n][i] = pa_transpose(pa_pack<T>(e[2 * i] - r.x, e[2 * i + 1] - r.y));
+            }
         }
 #pragma unroll
-        for (int n = 0; n < NT; n += 2) {
-            const int row = lane & 15, ch = n + (lane >> 4);
-            uint32_t b[4];
-            pa_ldmatrix_trans(b, vb + row * (D * 2) + ((ch ^ (row & 7)) << 4));
-            pa_mma<T>(o[n], hi, b[0], b[1]);
-            pa_mma<T>(o[n + 1], hi, b[2], b[3]);
-            pa_mma<T>(o[n], lo, b[0], b[1]);
-            pa_mma<T>(o[n + 1], lo, b[2], b[3]);
+        for (int mt = 0; mt < MT; ++mt) {
+            const int row = (lane & 7) + ((lane >> 4) << 3), ch = mt * 2 + ((lane >> 3) & 1);
+            uint32_t a[4];
+            pa_ldmatrix_trans(a, vb + row * (D * 2) + ((ch ^ (row & 7)) << 4));
+#pragma unroll
+            for (int n = 0; n < N8; ++n) {
+                pa_mma<T>(o[mt][n], a, hi[n][0], hi[n][1]);
+                pa_mma<T>(o[mt][n], a, lo[n][0], lo[n][1]);
+            }
         }
         __syncwarp();                                                         // the stage may be filled again
         stage = stage + 1 == STAGES ? 0 : stage + 1;
@@ -334,41 +398,45 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
         if (stream_ends || done + 1 == count) {
             // join the four warps
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                l[h] += __shfl_xor_sync(FULL_MASK, l[h], 1);
-                l[h] += __shfl_xor_sync(FULL_MASK, l[h], 2);
-                if (quad == 0) { s_max[warp][g + 8 * h] = m[h]; s_sum[warp][g + 8 * h] = l[h]; }
-            }
+            for (int n = 0; n < N8; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float t = l[n][h];
+                    t += __shfl_xor_sync(FULL_MASK, t, 4);
+                    t += __shfl_xor_sync(FULL_MASK, t, 8);
+                    t += __shfl_xor_sync(FULL_MASK, t, 16);
+                    if (g == 0) { s_max[warp][n * 8 + quad * 2 + h] = m[n][h]; s_sum[warp][n * 8 + quad * 2 + h] = t; }
+                }
             const bool final = whole && stream_ends;
             float* part = p.parts + ((int64_t)blockIdx.x * 2 + (whole ? 1 : 0)) * Shape::SLOT;
             const int64_t out_row = (int64_t)work.seq * p.heads + head0;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (h * 8 >= rows) break;
+            for (int n = 0; n < N8; ++n) {
+                if (n * 8 >= rows) break;
 #pragma unroll
                 for (int half = 0; half < D / PA_MERGE_COLS; ++half) {
 #pragma unroll
-                    for (int n = 0; n < PA_MERGE_COLS / 8; ++n) {
-                        const int nn = half * (PA_MERGE_COLS / 8) + n;
-                        *reinterpret_cast<float2*>(&s_merge[warp][g][n * 8 + quad * 2]) = make_float2(o[nn][2 * h], o[nn][2 * h + 1]);
-                    }
+                    for (int q = 0; q < PA_MERGE_COLS / 16; ++q)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            s_merge[warp][quad * 2 + (i & 1)][q * 16 + g + (i >> 1) * 8] = o[half * (PA_MERGE_COLS / 16) + q][n][i];
                     __syncthreads();
-                    const int r = tid / 16, col = (tid % 16) * 4, row = h * 8 + r, at = half * PA_MERGE_COLS + col;
-                    float top_row = LOWEST, sum = 0.f;
-                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                    for (int w = 0; w < PA_WARPS; ++w) top_row = fmaxf(top_row, s_max[w][row]);
-#pragma unroll
-                    for (int w = 0; w < PA_WARPS; ++w) {
-                        const float f = exp2_approx((s_max[w][row] - top_row) * c);
-                        const float4 x = *reinterpret_cast<const float4*>(&s_merge[w][r][col]);
-                        sum = fmaf(f, s_sum[w][row], sum);
-                        acc.x = fmaf(f, x.x, acc.x);
-                        acc.y = fmaf(f, x.y, acc.y);
-                        acc.z = fmaf(f, x.z, acc.z);
-                        acc.w = fmaf(f, x.w, acc.w);
-                    }
+                    const int r = tid / 16, col = (tid % 16) * 4, row = n * 8 + r, at = half * PA_MERGE_COLS + col;
                     if (row < rows) {
+                        float top_row = LOWEST, sum = 0.f;
+                        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (int w = 0; w < PA_WARPS; ++w) top_row = fmaxf(top_row, s_max[w][row]);
+#pragma unroll
+                        for (int w = 0; w < PA_WARPS; ++w) {
+                            const float f = exp2_approx((s_max[w][row] - top_row) * c);
+                            const float4 x = *reinterpret_cast<const float4*>(&s_merge[w][r][col]);
+                            sum = fmaf(f, s_sum[w][row], sum);
+                            acc.x = fmaf(f, x.x, acc.x);
+                            acc.y = fmaf(f, x.y, acc.y);
+                            acc.z = fmaf(f, x.z, acc.z);
+                            acc.w = fmaf(f, x.w, acc.w);
+                        }
                         if (final) {
                             if (at < p.dim) {
                                 const float inv = sum == 0.f ? 0.f : 1.f / sum;      // nothing held a token: zeros
@@ -397,67 +465,66 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
     if (tid == 0) p.meta[blockIdx.x] = meta;
 }
 
-// Joins the parts of one head of a stream that several CTAs share.  grid: (CTAs of the first kernel, PA_ROWS).
-constexpr int PJ_THREADS = 256;
+// Joins the parts of a stream that several CTAs share, one warp per head; where they are many, one CTA per head.
+// grid: (CTAs of the first kernel, heads per pass).
+constexpr int PJ_THREADS = 128;
+constexpr int PJ_MANY = 16;                                                   // more parts than this are split among warps
 template <typename T, int D>
 __global__ void __launch_bounds__(PJ_THREADS) paged_attention_join_kernel(const PaParams p) {
     using Shape = PaShape<D>;
-    constexpr int LANES = D / 4, GROUPS = PJ_THREADS / LANES;                 // threads per part, parts at a time
-    __shared__ __align__(16) float s_acc[GROUPS][D];
-    __shared__ float s_red[16];
+    constexpr int WARPS = PJ_THREADS / 32, COLS = D / 32;                     // columns per lane: 2, 4 or 8
+    __shared__ __align__(16) float s_acc[WARPS][D];
+    __shared__ float s_sum[WARPS];
     pdl_wait();
     pdl_launch_dependents();
     const PaMeta meta = p.meta[blockIdx.x];
     if (meta.seq < 0) return;
     const int32_t head0 = (meta.stream / p.blocks) * p.group + (meta.stream % p.blocks) * p.rows;
-    const int row = blockIdx.y, tid = threadIdx.x;
-    if (row >= min(p.rows, (meta.stream / p.blocks + 1) * p.group - head0)) return;
+    const int32_t rows = min(p.rows, (meta.stream / p.blocks + 1) * p.group - head0);
     const int32_t first = blockIdx.x, n = meta.last - first + 1;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const bool many = n > PJ_MANY;
+    const int row = many ? (int)blockIdx.y : (int)blockIdx.y * WARPS + warp;
+    if (row >= rows) return;                                                  // (many: the whole CTA)
     auto slot = [&](int32_t i) { return p.parts + ((int64_t)(first + i) * 2 + (i == 0 ? 1 : 0)) * Shape::SLOT; };
     const float c = p.scale * LOG2E;
-    float top = LOWEST;
-    for (int32_t i = tid; i < n; i += PJ_THREADS) top = fmaxf(top, slot(i)[PA_ROWS * D + row]);
+    float top = LOWEST, sum = 0.f, acc[COLS];
+    for (int32_t i = lane; i < n; i += 32) top = fmaxf(top, slot(i)[PA_ROWS * D + row]);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, d));
-    if ((tid & 31) == 0) s_red[tid >> 5] = top;
-    __syncthreads();
-    for (int w = 0; w < PJ_THREADS / 32; ++w) top = fmaxf(top, s_red[w]);
-    const int group = tid / LANES, col = (tid % LANES) * 4;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-    for (int32_t i = group; i < n; i += GROUPS) {
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) acc[j] = 0.f;
+#pragma unroll 4
+    for (int32_t i = many ? warp : 0; i < n; i += many ? WARPS : 1) {
         const float* s = slot(i);
         const float f = exp2_approx((s[PA_ROWS * D + row] - top) * c);
-        const float4 x = *reinterpret_cast<const float4*>(s + row * D + col);
         sum = fmaf(f, s[PA_ROWS * (D + 1) + row], sum);
-        acc.x = fmaf(f, x.x, acc.x);
-        acc.y = fmaf(f, x.y, acc.y);
-        acc.z = fmaf(f, x.z, acc.z);
-        acc.w = fmaf(f, x.w, acc.w);
-    }
-    *reinterpret_cast<float4*>(&s_acc[group][col]) = acc;
-    __syncthreads();
-    if (col == 0) s_red[group] = sum;                                         // (GROUPS <= 16; top has been read)
-    __syncthreads();
-    if (tid < LANES) {
-        float total = 0.f;
-        acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int q = 0; q < GROUPS; ++q) {
-            const float4 x = *reinterpret_cast<const float4*>(&s_acc[q][col]);
-            total += s_red[q];
-            acc.x += x.x;
-            acc.y += x.y;
-            acc.z += x.z;
-            acc.w += x.w;
-        }
-        const int64_t out_row = (int64_t)meta.seq * p.heads + head0 + row;
-        const float inv = total == 0.f ? 0.f : 1.f / total;
-        if (col < p.dim)
-            *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.out) + out_row * p.dim + col) =
-                make_uint2(pa_pack<T>(acc.x * inv, acc.y * inv), pa_pack<T>(acc.z * inv, acc.w * inv));
-        if (tid == 0) p.lse[out_row] = total == 0.f ? -INFINITY : fmaf(top, p.scale, logf(total));
+        for (int j = 0; j < COLS; ++j) acc[j] = fmaf(f, s[row * D + j * 32 + lane], acc[j]);
     }
+    if (many) {
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) s_acc[warp][j * 32 + lane] = acc[j];
+        if (lane == 0) s_sum[warp] = sum;
+        __syncthreads();
+        if (warp > 0) return;
+        sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) acc[j] = 0.f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            sum += s_sum[w];
+#pragma unroll
+            for (int j = 0; j < COLS; ++j) acc[j] += s_acc[w][j * 32 + lane];
+        }
+    }
+    const int64_t out_row = (int64_t)meta.seq * p.heads + head0 + row;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    T* out = reinterpret_cast<T*>(p.out) + out_row * p.dim;
+#pragma unroll
+    for (int j = 0; j < COLS; ++j)
+        if (j * 32 + lane < p.dim) out[j * 32 + lane] = Logit<T>::from_float(acc[j] * inv);
+    if (lane == 0) p.lse[out_row] = sum == 0.f ? -INFINITY : fmaf(top, p.scale, logf(sum));
 }
 
 }  // namespace profk
