@@ -33,7 +33,7 @@ template <int D> struct PaShape {
     static constexpr int SLOT = PA_ROWS * (D + 2);      // floats of a part: output, maxima, sums
 };
 
-struct PaMeta { int32_t seq, stream, last, unused; };   // the parts of (seq, stream): this CTA's to CTA `last`'s; seq < 0: none
+struct PaMeta { int32_t seq, head, heads, last; };      // the parts of `heads` heads of seq: this CTA's to CTA `last`'s; seq < 0: none
 
 struct PaParams {
     const void* q;
@@ -108,21 +108,25 @@ __device__ __forceinline__ int32_t pa_length(const PaParams& p, int32_t seq) {
     return (int32_t)max((int64_t)0, min((int64_t)p.lengths[seq], room));
 }
 
-// A place in the list of tiles.
+// A place in the list of tiles: sequence by sequence, head by head (and pass by pass), tile by tile.
 struct PaCursor {
-    int32_t seq, stream, tile, tiles, len;
-    // To the first tile of the next (sequence, head), past empty sequences.
-    __device__ __forceinline__ void next(const PaParams& p, int32_t streams) {
+    int32_t seq, head, block, tile, tiles, len;
+    // To the next tile, past empty sequences.
+    __device__ __forceinline__ void next(const PaParams& p) {
         if (++tile < tiles) return;
         tile = 0;
-        if (++stream < streams) return;
-        stream = 0;
+        if (++block < p.blocks) return;
+        block = 0;
+        if (++head < p.kv_heads) return;
+        head = 0;
         do {
             if (++seq >= p.seqs) { tiles = 0; return; }
             len = pa_length(p, seq);
             tiles = (len + PA_TILE - 1) / PA_TILE;
         } while (tiles == 0);
     }
+    __device__ __forceinline__ int32_t first_head(const PaParams& p) const { return head * p.group + block * p.rows; }
+    __device__ __forceinline__ int32_t heads(const PaParams& p) const { return min(p.rows, p.group - block * p.rows); }
 };
 
 // Transposes an 8 x 8 matrix of 16-bit numbers held by the warp (lane 4 r + q: row r, columns 2 q and 2 q + 1).
@@ -139,7 +143,7 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
     constexpr int STAGES = Shape::STAGES, CH = D / 8, KSTEPS = D / 16, MT = D / 16;
     constexpr int ROWS_PER_LOAD = 32 / CH;                                   // token rows that one warp-wide copy covers
     constexpr int LOADS = PA_WARP_TOKENS / ROWS_PER_LOAD;
-    extern __shared__ __align__(128) unsigned char pa_dyn[];
+    extern __shared__ __align__(512) unsigned char pa_dyn[];           // (512: the longest row; see the exclusive ors below)
     __shared__ __align__(16) float s_merge[PA_WARPS][8][PA_MERGE_STRIDE];
     __shared__ float s_max[PA_WARPS][PA_ROWS], s_sum[PA_WARPS][PA_ROWS];
     __shared__ uint32_t s_mask[PA_WARPS][STAGES];
@@ -201,8 +205,10 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
     work.seq = s_seq;
     work.len = pa_length(p, work.seq);
     work.tiles = (work.len + PA_TILE - 1) / PA_TILE;
-    work.stream = (int32_t)((u0 - s_start) / work.tiles);
-    work.tile = (int32_t)((u0 - s_start) % work.tiles);
+    const int32_t stream0 = (int32_t)((u0 - s_start) / work.tiles);
+    work.tile = (int32_t)(u0 - s_start - (long long)stream0 * work.tiles);
+    work.head = stream0 / p.blocks;
+    work.block = stream0 - work.head * p.blocks;
     const uint32_t count = (uint32_t)(u1 - u0);
 
     // loading side
@@ -224,7 +230,7 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
     int32_t page = page_of(load);
     auto load_tile = [&]() {
         if (loaded < count) {
-            const int32_t t0 = load.tile * PA_TILE + warp * PA_WARP_TOKENS, head = load.stream / p.blocks;
+            const int32_t t0 = load.tile * PA_TILE + warp * PA_WARP_TOKENS, head = load.head;
             const uint32_t base = ring + load_stage * Shape::STAGE_BYTES;
             if (p.one_page) {
                 const int32_t slot = t0 - page_number(t0) * p.page_size;
@@ -271,13 +277,12 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
                 }
             }
             ++loaded;
-            load.next(p, streams);
+            load.next(p);
             if (loaded < count) {
                 page = page_of(load);                                         // ready by the next call
                 if (load.tile == 0) {                                         // the queries of a stream that begins
-                    const int32_t h = (load.stream / p.blocks) * p.group + (load.stream % p.blocks) * p.rows + lane;
-                    if (lane < p.rows && h < p.heads)
-                        asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const T*>(p.q) + load.seq * p.q_seq + h * p.q_head));
+                    if (lane < load.heads(p))
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const T*>(p.q) + load.seq * p.q_seq + (load.first_head(p) + lane) * p.q_head));
                 }
             }
         }
@@ -288,6 +293,10 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
     for (int s = 0; s < STAGES - 1; ++s) load_tile();
 
     const float c = p.scale * LOG2E;
+    // where the lane's rows of the matrices lie in a stage: tokens lane & 15 of the keys, (lane & 7) + 8 (lane >> 4) of the values
+    const uint32_t k_lane = (lane & 15) * (D * 2) + (((lane >> 4) ^ (lane & 7)) << 4);
+    const uint32_t v_lane = ((lane & 7) + ((lane >> 4) << 3)) * (D * 2) + ((((lane >> 3) & 1) ^ (lane & 7)) << 4);
+    const float far = 8.f / c;                                                // the reference of the exponents lags the maximum by up to 2^8
     uint32_t qf[N8][KSTEPS][2];
     float o[MT][N8][4], m[N8][2], l[N8][2];                                   // of heads 8 n + 2 quad and + 1
     bool fresh = true, whole = work.tile == 0;                                // a new stream begins / it began in this share
@@ -295,10 +304,9 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
     PaMeta meta{-1, 0, 0, 0};
     for (uint32_t done = 0; done < count; ++done) {
         load_tile();
-        const int32_t head0 = (work.stream / p.blocks) * p.group + (work.stream % p.blocks) * p.rows;
-        const int32_t rows = min(p.rows, (work.stream / p.blocks + 1) * p.group - head0);
         if (fresh) {
             fresh = false;
+            const int32_t head0 = work.first_head(p), rows = work.heads(p);
             const T* q = reinterpret_cast<const T*>(p.q) + work.seq * p.q_seq + head0 * p.q_head;
 #pragma unroll
             for (int n = 0; n < N8; ++n) {
@@ -318,13 +326,12 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
         pa_cp_wait<STAGES - 1>();
         __syncwarp();
         const uint32_t kb = ring + stage * Shape::STAGE_BYTES, vb = kb + PA_WARP_TOKENS * D * 2;
-        // scores: 16 tokens x 8 N8 heads
+        // scores: 16 tokens x 8 N8 heads (a stage begins at a multiple of a row's bytes, so that a step is an exclusive or)
         float s[N8][4] = {};
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) {
-            const int row = lane & 15, ch = ks * 2 + (lane >> 4);
             uint32_t a[4];
-            pa_ldmatrix(a, kb + row * (D * 2) + ((ch ^ (row & 7)) << 4));
+            pa_ldmatrix(a, (kb + k_lane) ^ (ks << 5));
 #pragma unroll
             for (int n = 0; n < N8; ++n) pa_mma<T>(s[n], a, qf[n][ks][0], qf[n][ks][1]);
         }
@@ -348,9 +355,9 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
                 t = fmaxf(t, __shfl_xor_sync(FULL_MASK, t, 8));
                 t = fmaxf(t, __shfl_xor_sync(FULL_MASK, t, 16));
                 top[n][h] = t;
-                higher = higher || t > m[n][h];
+                higher = higher || t > m[n][h] + far;
             }
-        if (__any_sync(FULL_MASK, higher)) {
+        if (__any_sync(FULL_MASK, higher)) {                                  // (rare after a stream's first tile)
 #pragma unroll
             for (int n = 0; n < N8; ++n)
 #pragma unroll
@@ -382,9 +389,8 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            const int row = (lane & 7) + ((lane >> 4) << 3), ch = mt * 2 + ((lane >> 3) & 1);
             uint32_t a[4];
-            pa_ldmatrix_trans(a, vb + row * (D * 2) + ((ch ^ (row & 7)) << 4));
+            pa_ldmatrix_trans(a, (vb + v_lane) ^ (mt << 5));
 #pragma unroll
             for (int n = 0; n < N8; ++n) {
                 pa_mma<T>(o[mt][n], a, hi[n][0], hi[n][1]);
@@ -408,6 +414,7 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
                     if (g == 0) { s_max[warp][n * 8 + quad * 2 + h] = m[n][h]; s_sum[warp][n * 8 + quad * 2 + h] = t; }
                 }
             const bool final = whole && stream_ends;
+            const int32_t head0 = work.first_head(p), rows = work.heads(p);
             float* part = p.parts + ((int64_t)blockIdx.x * 2 + (whole ? 1 : 0)) * Shape::SLOT;
             const int64_t out_row = (int64_t)work.seq * p.heads + head0;
 #pragma unroll
@@ -455,11 +462,11 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
             if (whole && !stream_ends) {
                 // the stream goes on in the next CTA's share: this one names the parts
                 const long long end = u0 + done + (work.tiles - work.tile);   // the first unit behind the stream
-                meta = PaMeta{work.seq, work.stream, (int32_t)((end * ctas + total - 1) / total - 1), 0};
+                meta = PaMeta{work.seq, head0, rows, (int32_t)((end * ctas + total - 1) / total - 1)};
             }
             fresh = whole = true;
         }
-        work.next(p, streams);
+        work.next(p);
     }
     pa_cp_wait<0>();
     if (tid == 0) p.meta[blockIdx.x] = meta;
@@ -479,13 +486,11 @@ __global__ void __launch_bounds__(PJ_THREADS) paged_attention_join_kernel(const 
     pdl_launch_dependents();
     const PaMeta meta = p.meta[blockIdx.x];
     if (meta.seq < 0) return;
-    const int32_t head0 = (meta.stream / p.blocks) * p.group + (meta.stream % p.blocks) * p.rows;
-    const int32_t rows = min(p.rows, (meta.stream / p.blocks + 1) * p.group - head0);
     const int32_t first = blockIdx.x, n = meta.last - first + 1;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const bool many = n > PJ_MANY;
     const int row = many ? (int)blockIdx.y : (int)blockIdx.y * WARPS + warp;
-    if (row >= rows) return;                                                  // (many: the whole CTA)
+    if (row >= meta.heads) return;                                               // (many: the whole CTA)
     auto slot = [&](int32_t i) { return p.parts + ((int64_t)(first + i) * 2 + (i == 0 ? 1 : 0)) * Shape::SLOT; };
     const float c = p.scale * LOG2E;
     float top = LOWEST, sum = 0.f, acc[COLS];
@@ -518,7 +523,7 @@ __global__ void __launch_bounds__(PJ_THREADS) paged_attention_join_kernel(const 
             for (int j = 0; j < COLS; ++j) acc[j] += s_acc[w][j * 32 + lane];
         }
     }
-    const int64_t out_row = (int64_t)meta.seq * p.heads + head0 + row;
+    const int64_t out_row = (int64_t)meta.seq * p.heads + meta.head + row;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     T* out = reinterpret_cast<T*>(p.out) + out_row * p.dim;
 #pragma unroll
