@@ -152,11 +152,15 @@ int lp_backward(const T* logits, int64_t rows, int64_t V, int64_t row_stride, do
 constexpr int PA_MAX_DIM = 256;
 
 int pa_tile_dim(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
-unsigned pa_ctas(int64_t dim, int sms) { return (unsigned)sms * (pa_tile_dim(dim) == 256 ? PaShape<256>::CTAS : PaShape<128>::CTAS); }
-size_t pa_meta_bytes(unsigned ctas) { return ((size_t)ctas * sizeof(PaMeta) + 255) / 256 * 256; }
+size_t pa_meta_bytes(int sms) { return ((size_t)sms * sizeof(PaMeta) + 255) / 256 * 256; }
 size_t pa_workspace(int64_t dim, int sms) {
-    const unsigned ctas = pa_ctas(dim, sms);
-    return pa_meta_bytes(ctas) + (size_t)ctas * 2 * PA_ROWS * (pa_tile_dim(dim) + 2) * sizeof(float);
+    const int d = pa_tile_dim(dim);
+    const size_t slots = d == 64 ? PaShape<64>::SLOTS : d == 128 ? PaShape<128>::SLOTS : PaShape<256>::SLOTS;
+    return pa_meta_bytes(sms) + (size_t)sms * slots * PA_ROWS * (d + 2) * sizeof(float);
+}
+int pa_warps(int64_t dim) {
+    const int d = pa_tile_dim(dim);
+    return d == 64 ? PaShape<64>::WARPS : d == 128 ? PaShape<128>::WARPS : PaShape<256>::WARPS;
 }
 
 template <typename T, int D, int N8>
@@ -164,7 +168,7 @@ int pa_launch(const PaParams& p, unsigned ctas, void* stream) {
     static uint64_t done = 0;
     static std::mutex mutex;
     DEC_TRY(prepare_kernel(paged_attention_kernel<T, D, N8>, PaShape<D>::SMEM, false, &done, &mutex));
-    Launch l(ctas, PA_THREADS, PaShape<D>::SMEM, stream);
+    Launch l(ctas, PaShape<D>::THREADS, PaShape<D>::SMEM, stream);
     DEC_TRY(cudaLaunchKernelEx(&l.cfg, paged_attention_kernel<T, D, N8>, p));
     Launch j(ctas, PJ_THREADS, 0, stream);
     j.cfg.gridDim.y = (unsigned)p.rows;
@@ -181,6 +185,8 @@ int32_t log2_of(int64_t n) {      // -1: no power of two
     while ((int64_t)1 << s < n) ++s;
     return (int64_t)1 << s == n ? s : -1;
 }
+// Whether a page's tokens lie within 2^32 bytes (of two-byte elements) behind the first.
+bool spans_32_bits(int64_t page_size, int64_t token) { return token >= 0 && token <= (0xFFFFFFFFll / 2) / (page_size + PA_TILE); }
 bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 template <typename T>
@@ -194,18 +200,20 @@ int pa_run(const T* q, int64_t q_seq, int64_t q_head, const T* k, const T* v, co
         return PROFK_EINVAL;
     for (const profk_page_strides_t* s : {ks, vs})
         if (s->page % 8 != 0 || s->head % 8 != 0 || s->token % 8 != 0) return PROFK_EINVAL;
+    if ((width * page_size / PA_TILE + 1) * kv_heads * ((heads / kv_heads + PA_ROWS - 1) / PA_ROWS) > 0x7FFFFFFFll) return PROFK_EINVAL;   // tiles of a sequence
     const int sms = sm_count();
     if (sms < 1) return PROFK_ECUDA;
     const size_t need = pa_workspace(dim, sms);
     if (!workspace || workspace_bytes < need || !aligned_to(workspace, 256)) return PROFK_EWORKSPACE;
     const int32_t group = (int32_t)(heads / kv_heads), blocks = (group + PA_ROWS - 1) / PA_ROWS;
-    // no more CTAs than there can be tiles, or sequences without any
-    const int64_t most = std::max<int64_t>(seqs, seqs * kv_heads * blocks * ((width * page_size + PA_TILE - 1) / PA_TILE));
-    const unsigned ctas = (unsigned)std::min<int64_t>(pa_ctas(dim, sms), most);
+    // no more warps than there can be shares, or sequences without tokens
+    const int64_t tiles = seqs * kv_heads * blocks * ((width * page_size + PA_TILE - 1) / PA_TILE);
+    const int64_t most = std::max<int64_t>(seqs, tiles), warps = pa_warps(dim);
+    const unsigned ctas = (unsigned)std::min<int64_t>(sms, (most + warps - 1) / warps);
     PaParams p{q, k, v, q_seq, q_head, ks->page, ks->head, ks->token, vs->page, vs->head, vs->token, tables, table_stride, lengths,
                (int32_t)seqs, (int32_t)heads, (int32_t)kv_heads, group, (int32_t)dim, (int32_t)page_size, (int32_t)pages, (int32_t)width,
-               blocks, (group + blocks - 1) / blocks, log2_of(page_size), page_size % PA_WARP_TOKENS == 0, (float)scale, out, lse,
-               reinterpret_cast<float*>(static_cast<char*>(workspace) + pa_meta_bytes(pa_ctas(dim, sms))), static_cast<PaMeta*>(workspace)};
+               blocks, (group + blocks - 1) / blocks, log2_of(page_size), page_size % PA_TILE == 0 && spans_32_bits(page_size, ks->token) && spans_32_bits(page_size, vs->token), (float)scale, out, lse,
+               reinterpret_cast<float*>(static_cast<char*>(workspace) + pa_meta_bytes(sms)), static_cast<PaMeta*>(workspace)};
     switch (pa_tile_dim(dim)) {
         case 64: return pa_launch<T, 64>(p, ctas, stream);
         case 128: return pa_launch<T, 128>(p, ctas, stream);

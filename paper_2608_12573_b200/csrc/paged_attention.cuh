@@ -3,34 +3,35 @@
 //
 // The cache is read once and every key meets the few query heads that share it, so the kernel is bound by HBM (4 dim
 // bytes and 4 dim G operations per token and key-value head).  The work is the list of (sequence, key-value head, tile of
-// 64 tokens), cut into one contiguous share per CTA whatever the lengths; a CTA that holds only part of a (sequence,
-// head) leaves its running maximum, sum and unnormalised output for a second, small kernel that joins the parts in order.
+// 16 tokens), cut into one contiguous share per warp whatever the lengths.  A warp that holds only part of a (sequence,
+// head) leaves its running maximum, sum and unnormalised output in scratch memory; at its end a CTA joins the parts of its
+// own warps, and a second, small kernel those of several CTAs, always in order.  A barrier every few tiles keeps the warps
+// of an SM together: left to themselves some finished their equal shares in two thirds of the others' time (200 sequences of
+// 17 to 700 tokens: 42 us against 75), and the SM was half idle in the end.
 //
-// Inside a CTA each of four warps takes 16 tokens of a tile through a ring of its own in shared memory (cp.async; no
-// barrier until the (sequence, head) ends), and multiplies with the warp-level matrix instruction, tokens (and then
-// dimensions) along its 16 rows and query heads along its 8 columns: K Q^T, then V^T P^T.  The few heads that share a key
-// are the narrow side of the product, far below the 128 rows that a tcgen05 tile wants, and the tensor pipe is not what
-// bounds it.
+// A warp works by itself: its tiles come through a ring of its own in shared memory (cp.async, no barrier), and it
+// multiplies with the warp-level matrix instruction, tokens (and then dimensions) along its 16 rows and query heads along
+// its 8 columns: K Q^T, then V^T P^T.  The few heads that share a key are the narrow side of the product, far below the 128
+// rows that a tcgen05 tile wants, and the tensor pipe is not what bounds it.
 #pragma once
 
 #include "logits.cuh"
 
 namespace profk {
 
-constexpr int PA_WARPS = 4;
-constexpr int PA_THREADS = PA_WARPS * 32;
-constexpr int PA_WARP_TOKENS = 16;
-constexpr int PA_TILE = PA_WARPS * PA_WARP_TOKENS;      // tokens per tile
+constexpr int PA_TILE = 16;                             // tokens per tile
 constexpr int PA_ROWS = 16;                             // most query heads per pass over a key-value head
-constexpr int PA_MERGE_COLS = 64;
-constexpr int PA_MERGE_STRIDE = PA_MERGE_COLS + 4;      // floats; 4 row pairs x 8 columns then fall on 32 banks
+constexpr int PA_PACE = 4;                              // tiles between two barriers of a CTA
 
 template <int D> struct PaShape {
-    static constexpr int STAGES = D == 64 ? 6 : 3;      // of the ring: 96 KB per CTA up to D = 128, 192 KB for 256
-    static constexpr int CTAS = D == 256 ? 1 : 2;       // per SM
-    static constexpr int STAGE_BYTES = PA_WARP_TOKENS * D * 2 * 2;                       // keys, then values, of a warp
-    static constexpr size_t SMEM = (size_t)PA_WARPS * STAGES * STAGE_BYTES;
+    // One CTA per SM, 192 KB of rings.
+    static constexpr int WARPS = D == 64 ? 12 : D == 128 ? 8 : 4;
+    static constexpr int THREADS = WARPS * 32;
+    static constexpr int STAGES = D == 64 ? 4 : 3;      // of a warp's ring
+    static constexpr int STAGE_BYTES = PA_TILE * D * 2 * 2;                              // keys, then values
+    static constexpr size_t SMEM = (size_t)WARPS * STAGES * STAGE_BYTES;
     static constexpr int SLOT = PA_ROWS * (D + 2);      // floats of a part: output, maxima, sums
+    static constexpr int SLOTS = 2 * WARPS + 2;         // of a CTA: for each warp, then for the CTA, its first and its last stream
 };
 
 struct PaMeta { int32_t seq, head, heads, last; };      // the parts of `heads` heads of seq: this CTA's to CTA `last`'s; seq < 0: none
@@ -51,7 +52,7 @@ struct PaParams {
     float scale;
     void* out;                                          // seqs x heads x dim
     float* lse;                                         // seqs x heads
-    float* parts;                                       // two slots per CTA: of the share's first and of its last stream
+    float* parts;                                       // SLOTS slots per CTA
     PaMeta* meta;                                       // one per CTA
 };
 
@@ -129,6 +130,14 @@ struct PaCursor {
     __device__ __forceinline__ int32_t heads(const PaParams& p) const { return min(p.rows, p.group - block * p.rows); }
 };
 
+// What the parts of a warp's share are, for the join at the CTA's end.
+struct PaShare {
+    int32_t first;                                      // its first stream began in an earlier share: heads of that stream, else 0
+    int32_t first_ends;                                 // ... and ended in this one
+    int32_t seq, head, heads;                           // the stream that began here and goes on behind it; heads 0: none
+    int32_t last;                                       // the share that stream ends in
+};
+
 // Transposes an 8 x 8 matrix of 16-bit numbers held by the warp (lane 4 r + q: row r, columns 2 q and 2 q + 1).
 __device__ __forceinline__ uint32_t pa_transpose(uint32_t x) {
     uint32_t y;
@@ -137,31 +146,49 @@ __device__ __forceinline__ uint32_t pa_transpose(uint32_t x) {
 }
 
 // N8: groups of eight query heads per pass (rows <= 8 N8).
+// A list of `total` tiles in `shares` shares of equal length, the first `more` of them one tile longer.
+struct PaShares {
+    long long each;
+    int32_t more, n;
+    __device__ __forceinline__ PaShares(long long total, int32_t warps) {
+        n = (int32_t)max(1LL, min((long long)warps, total));
+        each = total < 0x7FFFFFFF ? (long long)((uint32_t)total / (uint32_t)n) : total / n;
+        more = (int32_t)(total - each * n);
+    }
+    __device__ __forceinline__ long long begin(int32_t i) const { return i < n ? each * i + min(i, more) : each * n + more; }
+    __device__ __forceinline__ int32_t of(long long unit) const {             // the share that holds a tile
+        const long long longer = (each + 1) * more;
+        return (int32_t)(unit < longer ? unit / (each + 1) : more + (unit - longer) / each);
+    }
+};
+
+// N8: groups of eight query heads per pass (rows <= 8 N8).
 template <typename T, int D, int N8>
-__global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_kernel(const PaParams p) {
+__global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel(const PaParams p) {
     using Shape = PaShape<D>;
-    constexpr int STAGES = Shape::STAGES, CH = D / 8, KSTEPS = D / 16, MT = D / 16;
+    constexpr int STAGES = Shape::STAGES, CH = D / 8, KSTEPS = D / 16, MT = D / 16, WARPS = Shape::WARPS, THREADS = Shape::THREADS;
     constexpr int ROWS_PER_LOAD = 32 / CH;                                   // token rows that one warp-wide copy covers
-    constexpr int LOADS = PA_WARP_TOKENS / ROWS_PER_LOAD;
+    constexpr int LOADS = PA_TILE / ROWS_PER_LOAD;
     extern __shared__ __align__(512) unsigned char pa_dyn[];           // (512: the longest row; see the exclusive ors below)
-    __shared__ __align__(16) float s_merge[PA_WARPS][8][PA_MERGE_STRIDE];
-    __shared__ float s_max[PA_WARPS][PA_ROWS], s_sum[PA_WARPS][PA_ROWS];
-    __shared__ uint32_t s_mask[PA_WARPS][STAGES];
-    __shared__ long long s_scan[PA_WARPS];
-    __shared__ long long s_start;
-    __shared__ int32_t s_seq;
+    __shared__ uint32_t s_mask[WARPS][STAGES];
+    __shared__ long long s_scan[WARPS], s_start[WARPS];
+    __shared__ int32_t s_seq[WARPS];
+    __shared__ PaShare s_share[WARPS];
+    __shared__ float s_max[WARPS][2][PA_ROWS], s_sum[WARPS][2][PA_ROWS];      // of the warps' parts
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, quad = lane & 3;
     const int32_t streams = p.kv_heads * p.blocks;
+    const float c = p.scale * LOG2E;
     pdl_wait();
     pdl_launch_dependents();
 
     // where the sequences' tiles begin in the list: each thread sums a run of sequences
-    const int32_t per = (p.seqs + PA_THREADS - 1) / PA_THREADS;
+    const int32_t per = (p.seqs + THREADS - 1) / THREADS;
     const int32_t run0 = min(p.seqs, tid * per), run1 = min(p.seqs, run0 + per);
+    auto tiles_of = [&](int32_t s) { return (long long)((pa_length(p, s) + PA_TILE - 1) / PA_TILE) * streams; };
     long long mine = 0;
-    for (int32_t s = run0; s < run1; ++s) mine += (long long)((pa_length(p, s) + PA_TILE - 1) / PA_TILE) * streams;
+    for (int32_t s = run0; s < run1; ++s) mine += tiles_of(s);
     long long incl = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -172,43 +199,45 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
     __syncthreads();
     long long total = 0;
 #pragma unroll
-    for (int w = 0; w < PA_WARPS; ++w) {
+    for (int w = 0; w < WARPS; ++w) {
         if (w < warp) incl += s_scan[w];
         total += s_scan[w];
     }
-    // sequences without tokens
-    for (int32_t s = blockIdx.x; s < p.seqs; s += gridDim.x) {
-        if (pa_length(p, s) > 0) continue;
-        T* o = reinterpret_cast<T*>(p.out) + (int64_t)s * p.heads * p.dim;
-        for (int32_t i = tid; i < p.heads * p.dim; i += PA_THREADS) o[i] = Logit<T>::from_float(0.f);
-        for (int32_t i = tid; i < p.heads; i += PA_THREADS) p.lse[(int64_t)s * p.heads + i] = -INFINITY;
-    }
-    const long long ctas = min((long long)gridDim.x, total);                  // every share then has a tile
-    if ((long long)blockIdx.x >= ctas) {
-        if (tid == 0) p.meta[blockIdx.x] = PaMeta{-1, 0, 0, 0};
-        return;
-    }
-    const long long u0 = total * blockIdx.x / ctas, u1 = total * (blockIdx.x + 1) / ctas;
-    if (incl - mine <= u0 && u0 < incl) {
-        long long at = incl - mine;
-        int32_t s = run0;
-        for (;; ++s) {
-            const long long n = (long long)((pa_length(p, s) + PA_TILE - 1) / PA_TILE) * streams;
-            if (u0 < at + n) break;
-            at += n;
+    const PaShares shares(total, gridDim.x * WARPS);
+    const int32_t me = blockIdx.x * WARPS + warp;
+    // who begins where: the threads whose run of sequences holds the first tile of one of the CTA's shares say so
+    const long long cta0 = shares.begin(blockIdx.x * WARPS), cta1 = shares.begin((blockIdx.x + 1) * WARPS);
+    if (incl - mine < cta1 && incl > cta0) {
+        for (int w = 0; w < WARPS; ++w) {
+            const long long u = shares.begin(blockIdx.x * WARPS + w);
+            if (u < incl - mine || u >= incl) continue;
+            long long at = incl - mine;
+            int32_t s = run0;
+            for (;; ++s) {
+                const long long n = per > 1 ? tiles_of(s) : mine;
+                if (u < at + n) break;
+                at += n;
+            }
+            s_seq[w] = s;
+            s_start[w] = at;
         }
-        s_seq = s;
-        s_start = at;
     }
     __syncthreads();
+    const long long u0 = shares.begin(me), u1 = shares.begin(me + 1);
+    // barriers of the CTA, the same number for all of its warps
+    const int32_t turns = (int32_t)((shares.begin(blockIdx.x * WARPS + 1) - cta0) / PA_PACE);
+    int32_t turn = 0;
+    PaShare share{0, 0, 0, 0, 0, 0};
+    float* const slots = p.parts + (int64_t)blockIdx.x * Shape::SLOTS * Shape::SLOT;
+    if (u0 < u1) {
     PaCursor work;
-    work.seq = s_seq;
+    work.seq = s_seq[warp];
     work.len = pa_length(p, work.seq);
     work.tiles = (work.len + PA_TILE - 1) / PA_TILE;
-    const int32_t stream0 = (int32_t)((u0 - s_start) / work.tiles);
-    work.tile = (int32_t)(u0 - s_start - (long long)stream0 * work.tiles);
-    work.head = stream0 / p.blocks;
-    work.block = stream0 - work.head * p.blocks;
+    const uint32_t in_seq = (uint32_t)(u0 - s_start[warp]), stream0 = in_seq / (uint32_t)work.tiles;   // (a sequence's tiles: less than 2^32)
+    work.tile = (int32_t)(in_seq - stream0 * (uint32_t)work.tiles);
+    work.head = (int32_t)stream0 / p.blocks;
+    work.block = (int32_t)stream0 - work.head * p.blocks;
     const uint32_t count = (uint32_t)(u1 - u0);
 
     // loading side
@@ -220,34 +249,58 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
     const bool chunk_in = chunk * 8 < p.dim;
     const uint32_t to0 = row0 * (D * 2) + ((chunk ^ (row0 & 7)) << 4);
     auto page_number = [&](int32_t t) { return p.page_shift >= 0 ? t >> p.page_shift : t / p.page_size; };
+    // of the sequence and head that is being loaded: its row of the table, and the lane's place in page 0, token 0
+    const int32_t* table = nullptr;
+    const char* k_base = nullptr;
+    const char* v_base = nullptr;
+    auto new_stream = [&]() {
+        table = p.tables + load.seq * p.table_stride;
+        const int32_t in = chunk_in ? chunk * 8 : 0;
+        k_base = reinterpret_cast<const char*>(reinterpret_cast<const T*>(p.k) + load.head * p.k_head + row0 * p.k_token + in);
+        v_base = reinterpret_cast<const char*>(reinterpret_cast<const T*>(p.v) + load.head * p.v_head + row0 * p.v_token + in);
+    };
+    new_stream();
+    const int64_t k_page = p.k_page * 2, v_page = p.v_page * 2;               // bytes
+    const uint32_t k_token = (uint32_t)p.k_token * 2, v_token = (uint32_t)p.v_token * 2;    // (one_page: a page's tokens span less than 2^32 bytes)
     // page of the lane's token (one_page: of the warp's first token); -1: no token, or no page
     auto page_of = [&](const PaCursor& c) -> int32_t {
-        const int32_t t = c.tile * PA_TILE + warp * PA_WARP_TOKENS + (p.one_page ? 0 : (lane & 15));
+        const int32_t t = c.tile * PA_TILE + (p.one_page ? 0 : (lane & 15));
         if (t >= c.len) return -1;
-        const int32_t page = p.tables[c.seq * p.table_stride + page_number(t)];
+        const int32_t page = table[page_number(t)];
         return page >= 0 && page < p.pages ? page : -1;
     };
     int32_t page = page_of(load);
     auto load_tile = [&]() {
         if (loaded < count) {
-            const int32_t t0 = load.tile * PA_TILE + warp * PA_WARP_TOKENS, head = load.head;
+            const int32_t t0 = load.tile * PA_TILE;
             const uint32_t base = ring + load_stage * Shape::STAGE_BYTES;
             if (p.one_page) {
                 const int32_t slot = t0 - page_number(t0) * p.page_size;
-                const int32_t n = page < 0 ? 0 : min(PA_WARP_TOKENS, load.len - t0);
-                const T* kp = reinterpret_cast<const T*>(p.k);
-                const T* vp = reinterpret_cast<const T*>(p.v);
-                if (n > 0 && chunk_in) {
-                    kp += page * p.k_page + head * p.k_head + (slot + row0) * p.k_token + chunk * 8;
-                    vp += page * p.v_page + head * p.v_head + (slot + row0) * p.v_token + chunk * 8;
-                }
+                const int32_t n = page < 0 ? 0 : min(PA_TILE, load.len - t0);
+                const uint32_t at = n > 0 ? (uint32_t)page : 0u, behind = n > 0 ? (uint32_t)slot : 0u;
+                const char* kp = k_base + at * k_page + behind * k_token;
+                const char* vp = v_base + at * v_page + behind * v_token;
                 if (lane == 0) s_mask[warp][load_stage] = (1u << n) - 1u;
-                if (n == PA_WARP_TOKENS && chunk_in) {
+                if (n == PA_TILE && chunk_in) {
+                    // (a stage begins at a multiple of a row's bytes, and rows i ROWS_PER_LOAD + row0 differ from row0 in other
+                    // bits of the swizzle only; tokens that lie together need no address arithmetic)
+                    if (p.k_token == D && p.v_token == D) {
 #pragma unroll
-                    for (int i = 0; i < LOADS; ++i) {
-                        const uint32_t to = base + ((to0 ^ ((i * ROWS_PER_LOAD & 7) << 4)) + i * ROWS_PER_LOAD * (D * 2));
-                        pa_cp_async(to, kp + i * ROWS_PER_LOAD * p.k_token, true);
-                        pa_cp_async(to + PA_WARP_TOKENS * D * 2, vp + i * ROWS_PER_LOAD * p.v_token, true);
+                        for (int i = 0; i < LOADS; ++i) {
+                            const uint32_t to = ((base + to0) ^ ((i * ROWS_PER_LOAD & 7) << 4)) + i * ROWS_PER_LOAD * (D * 2);
+                            pa_cp_async(to, kp + i * ROWS_PER_LOAD * D * 2, true);
+                            pa_cp_async(to + PA_TILE * D * 2, vp + i * ROWS_PER_LOAD * D * 2, true);
+                        }
+                    } else {
+                        const uint32_t k_step = ROWS_PER_LOAD * k_token, v_step = ROWS_PER_LOAD * v_token;
+#pragma unroll
+                        for (int i = 0; i < LOADS; ++i) {
+                            const uint32_t to = ((base + to0) ^ ((i * ROWS_PER_LOAD & 7) << 4)) + i * ROWS_PER_LOAD * (D * 2);
+                            pa_cp_async(to, kp, true);
+                            pa_cp_async(to + PA_TILE * D * 2, vp, true);
+                            kp += k_step;
+                            vp += v_step;
+                        }
                     }
                 } else {
 #pragma unroll
@@ -255,15 +308,15 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
                         const int row = i * ROWS_PER_LOAD + row0;
                         const bool read = chunk_in && row < n;
                         const uint32_t to = base + row * (D * 2) + ((chunk ^ (row & 7)) << 4);
-                        pa_cp_async(to, read ? kp + i * ROWS_PER_LOAD * p.k_token : reinterpret_cast<const T*>(p.k), read);
-                        pa_cp_async(to + PA_WARP_TOKENS * D * 2, read ? vp + i * ROWS_PER_LOAD * p.v_token : reinterpret_cast<const T*>(p.v), read);
+                        pa_cp_async(to, read ? kp + i * ROWS_PER_LOAD * k_token : reinterpret_cast<const char*>(p.k), read);
+                        pa_cp_async(to + PA_TILE * D * 2, read ? vp + i * ROWS_PER_LOAD * v_token : reinterpret_cast<const char*>(p.v), read);
                     }
                 }
             } else {
                 const int32_t t = t0 + (lane & 15), slot = t - page_number(t) * p.page_size;
                 const bool in = page >= 0;
-                const int64_t k_off = in ? page * p.k_page + head * p.k_head + slot * p.k_token : 0;
-                const int64_t v_off = in ? page * p.v_page + head * p.v_head + slot * p.v_token : 0;
+                const int64_t k_off = in ? page * p.k_page + load.head * p.k_head + slot * p.k_token : 0;
+                const int64_t v_off = in ? page * p.v_page + load.head * p.v_head + slot * p.v_token : 0;
                 const uint32_t mask = __ballot_sync(FULL_MASK, in) & 0xFFFFu;
                 if (lane == 0) s_mask[warp][load_stage] = mask;
 #pragma unroll
@@ -273,17 +326,18 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
                     const bool read = chunk_in && (mask >> row & 1);
                     const uint32_t to = base + row * (D * 2) + ((chunk ^ (row & 7)) << 4);
                     pa_cp_async(to, reinterpret_cast<const T*>(p.k) + ko + (read ? chunk * 8 : 0), read);
-                    pa_cp_async(to + PA_WARP_TOKENS * D * 2, reinterpret_cast<const T*>(p.v) + vo + (read ? chunk * 8 : 0), read);
+                    pa_cp_async(to + PA_TILE * D * 2, reinterpret_cast<const T*>(p.v) + vo + (read ? chunk * 8 : 0), read);
                 }
             }
             ++loaded;
             load.next(p);
             if (loaded < count) {
-                page = page_of(load);                                         // ready by the next call
-                if (load.tile == 0) {                                         // the queries of a stream that begins
+                if (load.tile == 0) {                                         // a stream begins: its queries will be wanted
+                    new_stream();
                     if (lane < load.heads(p))
                         asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const T*>(p.q) + load.seq * p.q_seq + (load.first_head(p) + lane) * p.q_head));
                 }
+                page = page_of(load);                                         // ready by the next call
             }
         }
         pa_cp_commit();
@@ -292,7 +346,6 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) load_tile();
 
-    const float c = p.scale * LOG2E;
     // where the lane's rows of the matrices lie in a stage: tokens lane & 15 of the keys, (lane & 7) + 8 (lane >> 4) of the values
     const uint32_t k_lane = (lane & 15) * (D * 2) + (((lane >> 4) ^ (lane & 7)) << 4);
     const uint32_t v_lane = ((lane & 7) + ((lane >> 4) << 3)) * (D * 2) + ((((lane >> 3) & 1) ^ (lane & 7)) << 4);
@@ -301,7 +354,7 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
     float o[MT][N8][4], m[N8][2], l[N8][2];                                   // of heads 8 n + 2 quad and + 1
     bool fresh = true, whole = work.tile == 0;                                // a new stream begins / it began in this share
     int stage = 0;
-    PaMeta meta{-1, 0, 0, 0};
+    if (!whole) share.first = work.heads(p);
     for (uint32_t done = 0; done < count; ++done) {
         load_tile();
         if (fresh) {
@@ -325,16 +378,24 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
         }
         pa_cp_wait<STAGES - 1>();
         __syncwarp();
-        const uint32_t kb = ring + stage * Shape::STAGE_BYTES, vb = kb + PA_WARP_TOKENS * D * 2;
+        const uint32_t kb = ring + stage * Shape::STAGE_BYTES, vb = kb + PA_TILE * D * 2;
         // scores: 16 tokens x 8 N8 heads (a stage begins at a multiple of a row's bytes, so that a step is an exclusive or)
-        float s[N8][4] = {};
+        float s[N8][4] = {}, odd[N8][4] = {};                                 // two chains, for the latency of a product
 #pragma unroll
-        for (int ks = 0; ks < KSTEPS; ++ks) {
-            uint32_t a[4];
+        for (int ks = 0; ks < KSTEPS; ks += 2) {
+            uint32_t a[4], b[4];
             pa_ldmatrix(a, (kb + k_lane) ^ (ks << 5));
+            pa_ldmatrix(b, (kb + k_lane) ^ ((ks + 1) << 5));
 #pragma unroll
-            for (int n = 0; n < N8; ++n) pa_mma<T>(s[n], a, qf[n][ks][0], qf[n][ks][1]);
+            for (int n = 0; n < N8; ++n) {
+                pa_mma<T>(s[n], a, qf[n][ks][0], qf[n][ks][1]);
+                pa_mma<T>(odd[n], b, qf[n][ks + 1][0], qf[n][ks + 1][1]);
+            }
         }
+#pragma unroll
+        for (int n = 0; n < N8; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[n][i] += odd[n][i];
         const uint32_t mask = s_mask[warp][stage];
         if (mask != 0xFFFFu) {
 #pragma unroll
@@ -388,13 +449,16 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
             }
         }
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            uint32_t a[4];
-            pa_ldmatrix_trans(a, (vb + v_lane) ^ (mt << 5));
+        for (int m0 = 0; m0 < MT; m0 += 4) {
+            uint32_t a[4][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pa_ldmatrix_trans(a[i], (vb + v_lane) ^ ((m0 + i) << 5));
 #pragma unroll
             for (int n = 0; n < N8; ++n) {
-                pa_mma<T>(o[mt][n], a, hi[n][0], hi[n][1]);
-                pa_mma<T>(o[mt][n], a, lo[n][0], lo[n][1]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pa_mma<T>(o[m0 + i][n], a[i], hi[n][0], hi[n][1]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pa_mma<T>(o[m0 + i][n], a[i], lo[n][0], lo[n][1]);
             }
         }
         __syncwarp();                                                         // the stage may be filled again
@@ -402,73 +466,130 @@ __global__ void __launch_bounds__(PA_THREADS, PaShape<D>::CTAS) paged_attention_
 
         const bool stream_ends = work.tile + 1 == work.tiles;
         if (stream_ends || done + 1 == count) {
-            // join the four warps
-#pragma unroll
-            for (int n = 0; n < N8; ++n)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float t = l[n][h];
-                    t += __shfl_xor_sync(FULL_MASK, t, 4);
-                    t += __shfl_xor_sync(FULL_MASK, t, 8);
-                    t += __shfl_xor_sync(FULL_MASK, t, 16);
-                    if (g == 0) { s_max[warp][n * 8 + quad * 2 + h] = m[n][h]; s_sum[warp][n * 8 + quad * 2 + h] = t; }
-                }
             const bool final = whole && stream_ends;
             const int32_t head0 = work.first_head(p), rows = work.heads(p);
-            float* part = p.parts + ((int64_t)blockIdx.x * 2 + (whole ? 1 : 0)) * Shape::SLOT;
             const int64_t out_row = (int64_t)work.seq * p.heads + head0;
+            float* part = slots + (2 * warp + (whole ? 1 : 0)) * Shape::SLOT;
 #pragma unroll
             for (int n = 0; n < N8; ++n) {
-                if (n * 8 >= rows) break;
+                float inv[2];
 #pragma unroll
-                for (int half = 0; half < D / PA_MERGE_COLS; ++half) {
-#pragma unroll
-                    for (int q = 0; q < PA_MERGE_COLS / 16; ++q)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            s_merge[warp][quad * 2 + (i & 1)][q * 16 + g + (i >> 1) * 8] = o[half * (PA_MERGE_COLS / 16) + q][n][i];
-                    __syncthreads();
-                    const int r = tid / 16, col = (tid % 16) * 4, row = n * 8 + r, at = half * PA_MERGE_COLS + col;
-                    if (row < rows) {
-                        float top_row = LOWEST, sum = 0.f;
-                        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                        for (int w = 0; w < PA_WARPS; ++w) top_row = fmaxf(top_row, s_max[w][row]);
-#pragma unroll
-                        for (int w = 0; w < PA_WARPS; ++w) {
-                            const float f = exp2_approx((s_max[w][row] - top_row) * c);
-                            const float4 x = *reinterpret_cast<const float4*>(&s_merge[w][r][col]);
-                            sum = fmaf(f, s_sum[w][row], sum);
-                            acc.x = fmaf(f, x.x, acc.x);
-                            acc.y = fmaf(f, x.y, acc.y);
-                            acc.z = fmaf(f, x.z, acc.z);
-                            acc.w = fmaf(f, x.w, acc.w);
-                        }
-                        if (final) {
-                            if (at < p.dim) {
-                                const float inv = sum == 0.f ? 0.f : 1.f / sum;      // nothing held a token: zeros
-                                const uint2 w2 = make_uint2(pa_pack<T>(acc.x * inv, acc.y * inv), pa_pack<T>(acc.z * inv, acc.w * inv));
-                                *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.out) + (out_row + row) * p.dim + at) = w2;
-                            }
-                            if (at == 0) p.lse[out_row + row] = sum == 0.f ? -INFINITY : fmaf(top_row, p.scale, logf(sum));
-                        } else {
-                            *reinterpret_cast<float4*>(part + row * D + at) = acc;
-                            if (at == 0) { part[PA_ROWS * D + row] = top_row; part[PA_ROWS * (D + 1) + row] = sum; }
-                        }
+                for (int h = 0; h < 2; ++h) {
+                    float sum = l[n][h];
+                    sum += __shfl_xor_sync(FULL_MASK, sum, 4);
+                    sum += __shfl_xor_sync(FULL_MASK, sum, 8);
+                    sum += __shfl_xor_sync(FULL_MASK, sum, 16);
+                    inv[h] = sum == 0.f ? 0.f : 1.f / sum;                    // nothing held a token: zeros
+                    const int row = n * 8 + quad * 2 + h;
+                    if (g == 0 && row < rows) {
+                        if (final) p.lse[out_row + row] = sum == 0.f ? -INFINITY : fmaf(m[n][h], p.scale, logf(sum));
+                        else { s_max[warp][whole ? 1 : 0][row] = m[n][h]; s_sum[warp][whole ? 1 : 0][row] = sum; }
                     }
-                    __syncthreads();
+                }
+                if (final) {
+                    // rows of the transposed matrix are heads: lane 4 g + quad gets dimensions 2 quad and + 1 of head 8 n + g
+                    T* out = reinterpret_cast<T*>(p.out) + (out_row + n * 8 + g) * p.dim;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t w = pa_transpose(pa_pack<T>(o[mt][n][2 * i] * inv[0], o[mt][n][2 * i + 1] * inv[1]));
+                            const int at = mt * 16 + i * 8 + quad * 2;
+                            if (n * 8 + g < rows && at < p.dim) *reinterpret_cast<uint32_t*>(out + at) = w;
+                        }
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int row = n * 8 + quad * 2 + h;
+                        if (row < rows)
+#pragma unroll
+                            for (int mt = 0; mt < MT; ++mt) {
+                                part[row * D + mt * 16 + g] = o[mt][n][h];
+                                part[row * D + mt * 16 + 8 + g] = o[mt][n][2 + h];
+                            }
+                    }
                 }
             }
+            if (!whole) share.first_ends = stream_ends;
             if (whole && !stream_ends) {
-                // the stream goes on in the next CTA's share: this one names the parts
                 const long long end = u0 + done + (work.tiles - work.tile);   // the first unit behind the stream
-                meta = PaMeta{work.seq, head0, rows, (int32_t)((end * ctas + total - 1) / total - 1)};
+                share.seq = work.seq;
+                share.head = head0;
+                share.heads = rows;
+                share.last = shares.of(end - 1);
             }
             fresh = whole = true;
         }
         work.next(p);
+        if ((done + 1) % PA_PACE == 0 && turn < turns) {
+            ++turn;
+            __syncthreads();
+        }
     }
     pa_cp_wait<0>();
+    }
+    for (; turn < turns; ++turn) __syncthreads();
+    // sequences without tokens
+    for (int32_t s = blockIdx.x; s < p.seqs; s += gridDim.x) {
+        if (pa_length(p, s) > 0) continue;
+        T* o = reinterpret_cast<T*>(p.out) + (int64_t)s * p.heads * p.dim;
+        for (int32_t i = tid; i < p.heads * p.dim; i += THREADS) o[i] = Logit<T>::from_float(0.f);
+        for (int32_t i = tid; i < p.heads; i += THREADS) p.lse[(int64_t)s * p.heads + i] = -INFINITY;
+    }
+    // The parts of the CTA's warps, chain by chain: a chain begins with a stream that goes on behind a warp's share, or with
+    // the CTA's first stream where that began in an earlier CTA; it is an output if it lies within the CTA, else a part.
+    if (lane == 0) s_share[warp] = share;
+    __syncthreads();
+    PaMeta meta{-1, 0, 0, 0};
+    int32_t from = -1, heads = 0, last = -1;                                  // the chain's first warp (-1: no chain), heads, last warp
+    bool inside = false;                                                      // it began in this CTA
+    auto close = [&](bool ends) {
+        const bool final = inside && ends;
+        float* part = slots + (2 * WARPS + (inside ? 1 : 0)) * Shape::SLOT;
+        const int64_t out_row = inside ? (int64_t)s_share[from].seq * p.heads + s_share[from].head : 0;
+        for (int32_t i = tid; i < heads * (D / 4); i += THREADS) {
+            const int32_t row = i / (D / 4), at = i % (D / 4) * 4;
+            float top = LOWEST, sum = 0.f;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int w = from; w <= last; ++w) top = fmaxf(top, s_max[w][inside && w == from][row]);
+#pragma unroll 4
+            for (int w = from; w <= last; ++w) {
+                const int which = inside && w == from;
+                const float f = exp2_approx((s_max[w][which][row] - top) * c);
+                const float4 x = *reinterpret_cast<const float4*>(slots + (2 * w + which) * Shape::SLOT + row * D + at);
+                sum = fmaf(f, s_sum[w][which][row], sum);
+                acc.x = fmaf(f, x.x, acc.x);
+                acc.y = fmaf(f, x.y, acc.y);
+                acc.z = fmaf(f, x.z, acc.z);
+                acc.w = fmaf(f, x.w, acc.w);
+            }
+            if (final) {
+                if (at < p.dim) {
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    const uint2 w2 = make_uint2(pa_pack<T>(acc.x * inv, acc.y * inv), pa_pack<T>(acc.z * inv, acc.w * inv));
+                    *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.out) + (out_row + row) * p.dim + at) = w2;
+                }
+                if (at == 0) p.lse[out_row + row] = sum == 0.f ? -INFINITY : fmaf(top, p.scale, logf(sum));
+            } else {
+                *reinterpret_cast<float4*>(part + row * D + at) = acc;
+                if (at == 0) { part[PA_ROWS * D + row] = top; part[PA_ROWS * (D + 1) + row] = sum; }
+            }
+        }
+        from = -1;
+    };
+    for (int w = 0; w < WARPS; ++w) {
+        const PaShare s = s_share[w];
+        if (s.first > 0) {
+            if (from < 0) { from = w; heads = s.first; inside = false; }
+            last = w;
+            if (s.first_ends) close(true);
+        }
+        if (s.heads > 0) { from = last = w; heads = s.heads; inside = true; }
+    }
+    if (from >= 0) {
+        if (inside) meta = PaMeta{s_share[from].seq, s_share[from].head, s_share[from].heads, s_share[from].last / WARPS};
+        close(false);
+    }
     if (tid == 0) p.meta[blockIdx.x] = meta;
 }
 
@@ -491,7 +612,7 @@ __global__ void __launch_bounds__(PJ_THREADS) paged_attention_join_kernel(const 
     const bool many = n > PJ_MANY;
     const int row = many ? (int)blockIdx.y : (int)blockIdx.y * WARPS + warp;
     if (row >= meta.heads) return;                                               // (many: the whole CTA)
-    auto slot = [&](int32_t i) { return p.parts + ((int64_t)(first + i) * 2 + (i == 0 ? 1 : 0)) * Shape::SLOT; };
+    auto slot = [&](int32_t i) { return p.parts + ((int64_t)(first + i) * Shape::SLOTS + 2 * Shape::WARPS + (i == 0 ? 1 : 0)) * Shape::SLOT; };
     const float c = p.scale * LOG2E;
     float top = LOWEST, sum = 0.f, acc[COLS];
     for (int32_t i = lane; i < n; i += 32) top = fmaxf(top, slot(i)[PA_ROWS * D + row]);
