@@ -186,7 +186,7 @@ int32_t log2_of(int64_t n) {      // -1: no power of two
     return (int64_t)1 << s == n ? s : -1;
 }
 // Whether a page's tokens lie within 2^32 bytes (of two-byte elements) behind the first.
-bool spans_32_bits(int64_t page_size, int64_t token) { return token >= 0 && token <= (0xFFFFFFFFll / 2) / (page_size + PA_TILE); }
+bool spans_32_bits(int64_t page_size, int64_t token) { return token >= 0 && token <= (0xFFFFFFFFll / 2) / (page_size + PA_SUB); }
 bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 template <typename T>
@@ -200,19 +200,19 @@ int pa_run(const T* q, int64_t q_seq, int64_t q_head, const T* k, const T* v, co
         return PROFK_EINVAL;
     for (const profk_page_strides_t* s : {ks, vs})
         if (s->page % 8 != 0 || s->head % 8 != 0 || s->token % 8 != 0) return PROFK_EINVAL;
-    if ((width * page_size / PA_TILE + 1) * kv_heads * ((heads / kv_heads + PA_ROWS - 1) / PA_ROWS) > 0x7FFFFFFFll) return PROFK_EINVAL;   // tiles of a sequence
+    if ((width * page_size / PA_SUB + 1) * kv_heads * ((heads / kv_heads + PA_ROWS - 1) / PA_ROWS) > 0x7FFFFFFFll) return PROFK_EINVAL;   // tiles of a sequence
     const int sms = sm_count();
     if (sms < 1) return PROFK_ECUDA;
     const size_t need = pa_workspace(dim, sms);
     if (!workspace || workspace_bytes < need || !aligned_to(workspace, 256)) return PROFK_EWORKSPACE;
     const int32_t group = (int32_t)(heads / kv_heads), blocks = (group + PA_ROWS - 1) / PA_ROWS;
     // no more warps than there can be shares, or sequences without tokens
-    const int64_t tiles = seqs * kv_heads * blocks * ((width * page_size + PA_TILE - 1) / PA_TILE);
+    const int64_t tiles = seqs * kv_heads * blocks * ((width * page_size + PA_SUB - 1) / PA_SUB);
     const int64_t most = std::max<int64_t>(seqs, tiles), warps = pa_warps(dim);
     const unsigned ctas = (unsigned)std::min<int64_t>(sms, (most + warps - 1) / warps);
     PaParams p{q, k, v, q_seq, q_head, ks->page, ks->head, ks->token, vs->page, vs->head, vs->token, tables, table_stride, lengths,
                (int32_t)seqs, (int32_t)heads, (int32_t)kv_heads, group, (int32_t)dim, (int32_t)page_size, (int32_t)pages, (int32_t)width,
-               blocks, (group + blocks - 1) / blocks, log2_of(page_size), page_size % PA_TILE == 0 && spans_32_bits(page_size, ks->token) && spans_32_bits(page_size, vs->token), (float)scale, out, lse,
+               blocks, (group + blocks - 1) / blocks, log2_of(page_size), page_size % PA_SUB == 0 && spans_32_bits(page_size, ks->token) && spans_32_bits(page_size, vs->token), (float)scale, out, lse,
                reinterpret_cast<float*>(static_cast<char*>(workspace) + pa_meta_bytes(sms)), static_cast<PaMeta*>(workspace)};
     switch (pa_tile_dim(dim)) {
         case 64: return pa_launch<T, 64>(p, ctas, stream);

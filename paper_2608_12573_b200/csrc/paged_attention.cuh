@@ -19,16 +19,20 @@
 
 namespace profk {
 
-constexpr int PA_TILE = 16;                             // tokens per tile
+constexpr int PA_SUB = 16;                              // tokens per step of the matrix instruction
 constexpr int PA_ROWS = 16;                             // most query heads per pass over a key-value head
 constexpr int PA_PACE = 4;                              // tiles between two barriers of a CTA
 
 template <int D> struct PaShape {
-    // One CTA per SM, 192 KB of rings.
-    static constexpr int WARPS = D == 64 ? 12 : D == 128 ? 8 : 4;
+    // One CTA per SM, 192 KB of rings.  A tile is 8 KB of keys and values or more: with 16 tokens of 64 dimensions at a time
+    // the arithmetic around them held the stream to 5.5 TB/s.
+    static constexpr int SUBS = D == 64 ? 2 : 1;        // steps per tile
+    static constexpr int TILE = PA_SUB * SUBS;          // tokens per tile
+    static constexpr int WARPS = D == 256 ? 4 : 8;
     static constexpr int THREADS = WARPS * 32;
-    static constexpr int STAGES = D == 64 ? 4 : 3;      // of a warp's ring
-    static constexpr int STAGE_BYTES = PA_TILE * D * 2 * 2;                              // keys, then values
+    static constexpr int STAGES = 3;                    // of a warp's ring
+    static constexpr int SUB_BYTES = PA_SUB * D * 2 * 2;                                 // keys, then values
+    static constexpr int STAGE_BYTES = SUB_BYTES * SUBS;
     static constexpr size_t SMEM = (size_t)WARPS * STAGES * STAGE_BYTES;
     static constexpr int SLOT = PA_ROWS * (D + 2);      // floats of a part: output, maxima, sums
     static constexpr int SLOTS = 2 * WARPS + 2;         // of a CTA: for each warp, then for the CTA, its first and its last stream
@@ -110,6 +114,7 @@ __device__ __forceinline__ int32_t pa_length(const PaParams& p, int32_t seq) {
 }
 
 // A place in the list of tiles: sequence by sequence, head by head (and pass by pass), tile by tile.
+template <int TILE>
 struct PaCursor {
     int32_t seq, head, block, tile, tiles, len;
     // To the next tile, past empty sequences.
@@ -123,7 +128,7 @@ struct PaCursor {
         do {
             if (++seq >= p.seqs) { tiles = 0; return; }
             len = pa_length(p, seq);
-            tiles = (len + PA_TILE - 1) / PA_TILE;
+            tiles = (len + TILE - 1) / TILE;
         } while (tiles == 0);
     }
     __device__ __forceinline__ int32_t first_head(const PaParams& p) const { return head * p.group + block * p.rows; }
@@ -137,6 +142,9 @@ struct PaShare {
     int32_t seq, head, heads;                           // the stream that began here and goes on behind it; heads 0: none
     int32_t last;                                       // the share that stream ends in
 };
+
+// Parts of consecutive warps that belong to one stream; `before`: heads of the chains before it.
+struct PaChain { int32_t from, last, heads, before; bool inside, final; };
 
 // Transposes an 8 x 8 matrix of 16-bit numbers held by the warp (lane 4 r + q: row r, columns 2 q and 2 q + 1).
 __device__ __forceinline__ uint32_t pa_transpose(uint32_t x) {
@@ -166,27 +174,38 @@ struct PaShares {
 template <typename T, int D, int N8>
 __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel(const PaParams p) {
     using Shape = PaShape<D>;
-    constexpr int STAGES = Shape::STAGES, CH = D / 8, KSTEPS = D / 16, MT = D / 16, WARPS = Shape::WARPS, THREADS = Shape::THREADS;
+    constexpr int STAGES = Shape::STAGES, CH = D / 8, KSTEPS = D / 16, MT = D / 16, WARPS = Shape::WARPS, THREADS = Shape::THREADS,
+                  SUBS = Shape::SUBS, TILE = Shape::TILE;
     constexpr int ROWS_PER_LOAD = 32 / CH;                                   // token rows that one warp-wide copy covers
-    constexpr int LOADS = PA_TILE / ROWS_PER_LOAD;
+    constexpr int LOADS = PA_SUB / ROWS_PER_LOAD;
     extern __shared__ __align__(512) unsigned char pa_dyn[];           // (512: the longest row; see the exclusive ors below)
-    __shared__ uint32_t s_mask[WARPS][STAGES];
+    __shared__ uint32_t s_mask[WARPS][STAGES][SUBS];
     __shared__ long long s_scan[WARPS], s_start[WARPS];
     __shared__ int32_t s_seq[WARPS];
     __shared__ PaShare s_share[WARPS];
+    __shared__ PaChain s_chain[WARPS + 1];
     __shared__ float s_max[WARPS][2][PA_ROWS], s_sum[WARPS][2][PA_ROWS];      // of the warps' parts
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, quad = lane & 3;
     const int32_t streams = p.kv_heads * p.blocks;
     const float c = p.scale * LOG2E;
+    // Lengths and page tables on their way into L2 while the kernel before this one ends (a prefetch reads nothing).
+    {
+        const int64_t lines = ((int64_t)p.seqs * 4 + 127) / 128, row_lines = ((int64_t)p.width * 4 + 127) / 128;
+        for (int64_t i = (int64_t)blockIdx.x * THREADS + tid; i < lines + p.seqs * row_lines && i < (1 << 20); i += (int64_t)gridDim.x * THREADS) {
+            const char* at = i < lines ? reinterpret_cast<const char*>(p.lengths) + i * 128
+                                       : reinterpret_cast<const char*>(p.tables + (i - lines) / row_lines * p.table_stride) + (i - lines) % row_lines * 128;
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+        }
+    }
     pdl_wait();
     pdl_launch_dependents();
 
     // where the sequences' tiles begin in the list: each thread sums a run of sequences
     const int32_t per = (p.seqs + THREADS - 1) / THREADS;
     const int32_t run0 = min(p.seqs, tid * per), run1 = min(p.seqs, run0 + per);
-    auto tiles_of = [&](int32_t s) { return (long long)((pa_length(p, s) + PA_TILE - 1) / PA_TILE) * streams; };
+    auto tiles_of = [&](int32_t s) { return (long long)((pa_length(p, s) + TILE - 1) / TILE) * streams; };
     long long mine = 0;
     for (int32_t s = run0; s < run1; ++s) mine += tiles_of(s);
     long long incl = mine;
@@ -230,10 +249,10 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
     PaShare share{0, 0, 0, 0, 0, 0};
     float* const slots = p.parts + (int64_t)blockIdx.x * Shape::SLOTS * Shape::SLOT;
     if (u0 < u1) {
-    PaCursor work;
+    PaCursor<TILE> work;
     work.seq = s_seq[warp];
     work.len = pa_length(p, work.seq);
-    work.tiles = (work.len + PA_TILE - 1) / PA_TILE;
+    work.tiles = (work.len + TILE - 1) / TILE;
     const uint32_t in_seq = (uint32_t)(u0 - s_start[warp]), stream0 = in_seq / (uint32_t)work.tiles;   // (a sequence's tiles: less than 2^32)
     work.tile = (int32_t)(in_seq - stream0 * (uint32_t)work.tiles);
     work.head = (int32_t)stream0 / p.blocks;
@@ -241,7 +260,7 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
     const uint32_t count = (uint32_t)(u1 - u0);
 
     // loading side
-    PaCursor load = work;
+    PaCursor<TILE> load = work;
     uint32_t loaded = 0;
     int load_stage = 0;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(pa_dyn) + warp * STAGES * Shape::STAGE_BYTES;
@@ -262,71 +281,76 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
     new_stream();
     const int64_t k_page = p.k_page * 2, v_page = p.v_page * 2;               // bytes
     const uint32_t k_token = (uint32_t)p.k_token * 2, v_token = (uint32_t)p.v_token * 2;    // (one_page: a page's tokens span less than 2^32 bytes)
-    // page of the lane's token (one_page: of the warp's first token); -1: no token, or no page
-    auto page_of = [&](const PaCursor& c) -> int32_t {
-        const int32_t t = c.tile * PA_TILE + (p.one_page ? 0 : (lane & 15));
-        if (t >= c.len) return -1;
+    // page of the lane's token of a step (one_page: of the step's first token); -1: no token, or no page
+    auto page_of = [&](const PaCursor<TILE>& at, int sub) -> int32_t {
+        const int32_t t = at.tile * TILE + sub * PA_SUB + (p.one_page ? 0 : (lane & 15));
+        if (t >= at.len) return -1;
         const int32_t page = table[page_number(t)];
         return page >= 0 && page < p.pages ? page : -1;
     };
-    int32_t page = page_of(load);
+    int32_t page[SUBS];
+#pragma unroll
+    for (int sub = 0; sub < SUBS; ++sub) page[sub] = page_of(load, sub);
     auto load_tile = [&]() {
         if (loaded < count) {
-            const int32_t t0 = load.tile * PA_TILE;
-            const uint32_t base = ring + load_stage * Shape::STAGE_BYTES;
-            if (p.one_page) {
-                const int32_t slot = t0 - page_number(t0) * p.page_size;
-                const int32_t n = page < 0 ? 0 : min(PA_TILE, load.len - t0);
-                const uint32_t at = n > 0 ? (uint32_t)page : 0u, behind = n > 0 ? (uint32_t)slot : 0u;
-                const char* kp = k_base + at * k_page + behind * k_token;
-                const char* vp = v_base + at * v_page + behind * v_token;
-                if (lane == 0) s_mask[warp][load_stage] = (1u << n) - 1u;
-                if (n == PA_TILE && chunk_in) {
-                    // (a stage begins at a multiple of a row's bytes, and rows i ROWS_PER_LOAD + row0 differ from row0 in other
-                    // bits of the swizzle only; tokens that lie together need no address arithmetic)
-                    if (p.k_token == D && p.v_token == D) {
 #pragma unroll
-                        for (int i = 0; i < LOADS; ++i) {
-                            const uint32_t to = ((base + to0) ^ ((i * ROWS_PER_LOAD & 7) << 4)) + i * ROWS_PER_LOAD * (D * 2);
-                            pa_cp_async(to, kp + i * ROWS_PER_LOAD * D * 2, true);
-                            pa_cp_async(to + PA_TILE * D * 2, vp + i * ROWS_PER_LOAD * D * 2, true);
+            for (int sub = 0; sub < SUBS; ++sub) {
+                const int32_t t0 = load.tile * TILE + sub * PA_SUB;
+                const uint32_t base = ring + load_stage * Shape::STAGE_BYTES + sub * Shape::SUB_BYTES;
+                if (p.one_page) {
+                    const int32_t slot = t0 - page_number(t0) * p.page_size;
+                    const int32_t n = page[sub] < 0 ? 0 : min(PA_SUB, load.len - t0);
+                    const uint32_t at = n > 0 ? (uint32_t)page[sub] : 0u, behind = n > 0 ? (uint32_t)slot : 0u;
+                    const char* kp = k_base + at * k_page + behind * k_token;
+                    const char* vp = v_base + at * v_page + behind * v_token;
+                    if (lane == 0) s_mask[warp][load_stage][sub] = (1u << n) - 1u;
+                    if (n == PA_SUB && chunk_in) {
+                        // (a stage begins at a multiple of a row's bytes, and rows i ROWS_PER_LOAD + row0 differ from row0 in
+                        // other bits of the swizzle only; tokens that lie together need no address arithmetic)
+                        if (p.k_token == D && p.v_token == D) {
+#pragma unroll
+                            for (int i = 0; i < LOADS; ++i) {
+                                const uint32_t to = ((base + to0) ^ ((i * ROWS_PER_LOAD & 7) << 4)) + i * ROWS_PER_LOAD * (D * 2);
+                                pa_cp_async(to, kp + i * ROWS_PER_LOAD * D * 2, true);
+                                pa_cp_async(to + PA_SUB * D * 2, vp + i * ROWS_PER_LOAD * D * 2, true);
+                            }
+                        } else {
+                            const uint32_t k_step = ROWS_PER_LOAD * k_token, v_step = ROWS_PER_LOAD * v_token;
+#pragma unroll
+                            for (int i = 0; i < LOADS; ++i) {
+                                const uint32_t to = ((base + to0) ^ ((i * ROWS_PER_LOAD & 7) << 4)) + i * ROWS_PER_LOAD * (D * 2);
+                                pa_cp_async(to, kp, true);
+                                pa_cp_async(to + PA_SUB * D * 2, vp, true);
+                                kp += k_step;
+                                vp += v_step;
+                            }
                         }
                     } else {
-                        const uint32_t k_step = ROWS_PER_LOAD * k_token, v_step = ROWS_PER_LOAD * v_token;
 #pragma unroll
                         for (int i = 0; i < LOADS; ++i) {
-                            const uint32_t to = ((base + to0) ^ ((i * ROWS_PER_LOAD & 7) << 4)) + i * ROWS_PER_LOAD * (D * 2);
-                            pa_cp_async(to, kp, true);
-                            pa_cp_async(to + PA_TILE * D * 2, vp, true);
-                            kp += k_step;
-                            vp += v_step;
+                            const int row = i * ROWS_PER_LOAD + row0;
+                            const bool read = chunk_in && row < n;
+                            const uint32_t to = base + row * (D * 2) + ((chunk ^ (row & 7)) << 4);
+                            pa_cp_async(to, read ? kp + i * ROWS_PER_LOAD * k_token : reinterpret_cast<const char*>(p.k), read);
+                            pa_cp_async(to + PA_SUB * D * 2, read ? vp + i * ROWS_PER_LOAD * v_token : reinterpret_cast<const char*>(p.v), read);
                         }
                     }
                 } else {
+                    const int32_t t = t0 + (lane & 15), slot = t - page_number(t) * p.page_size;
+                    const bool in = page[sub] >= 0;
+                    const int64_t k_off = in ? page[sub] * p.k_page + load.head * p.k_head + slot * p.k_token : 0;
+                    const int64_t v_off = in ? page[sub] * p.v_page + load.head * p.v_head + slot * p.v_token : 0;
+                    const uint32_t mask = __ballot_sync(FULL_MASK, in) & 0xFFFFu;
+                    if (lane == 0) s_mask[warp][load_stage][sub] = mask;
 #pragma unroll
                     for (int i = 0; i < LOADS; ++i) {
                         const int row = i * ROWS_PER_LOAD + row0;
-                        const bool read = chunk_in && row < n;
+                        const int64_t ko = __shfl_sync(FULL_MASK, k_off, row), vo = __shfl_sync(FULL_MASK, v_off, row);
+                        const bool read = chunk_in && (mask >> row & 1);
                         const uint32_t to = base + row * (D * 2) + ((chunk ^ (row & 7)) << 4);
-                        pa_cp_async(to, read ? kp + i * ROWS_PER_LOAD * k_token : reinterpret_cast<const char*>(p.k), read);
-                        pa_cp_async(to + PA_TILE * D * 2, read ? vp + i * ROWS_PER_LOAD * v_token : reinterpret_cast<const char*>(p.v), read);
+                        pa_cp_async(to, reinterpret_cast<const T*>(p.k) + ko + (read ? chunk * 8 : 0), read);
+                        pa_cp_async(to + PA_SUB * D * 2, reinterpret_cast<const T*>(p.v) + vo + (read ? chunk * 8 : 0), read);
                     }
-                }
-            } else {
-                const int32_t t = t0 + (lane & 15), slot = t - page_number(t) * p.page_size;
-                const bool in = page >= 0;
-                const int64_t k_off = in ? page * p.k_page + load.head * p.k_head + slot * p.k_token : 0;
-                const int64_t v_off = in ? page * p.v_page + load.head * p.v_head + slot * p.v_token : 0;
-                const uint32_t mask = __ballot_sync(FULL_MASK, in) & 0xFFFFu;
-                if (lane == 0) s_mask[warp][load_stage] = mask;
-#pragma unroll
-                for (int i = 0; i < LOADS; ++i) {
-                    const int row = i * ROWS_PER_LOAD + row0;
-                    const int64_t ko = __shfl_sync(FULL_MASK, k_off, row), vo = __shfl_sync(FULL_MASK, v_off, row);
-                    const bool read = chunk_in && (mask >> row & 1);
-                    const uint32_t to = base + row * (D * 2) + ((chunk ^ (row & 7)) << 4);
-                    pa_cp_async(to, reinterpret_cast<const T*>(p.k) + ko + (read ? chunk * 8 : 0), read);
-                    pa_cp_async(to + PA_TILE * D * 2, reinterpret_cast<const T*>(p.v) + vo + (read ? chunk * 8 : 0), read);
                 }
             }
             ++loaded;
@@ -337,7 +361,8 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
                     if (lane < load.heads(p))
                         asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const T*>(p.q) + load.seq * p.q_seq + (load.first_head(p) + lane) * p.q_head));
                 }
-                page = page_of(load);                                         // ready by the next call
+#pragma unroll
+                for (int sub = 0; sub < SUBS; ++sub) page[sub] = page_of(load, sub);          // ready by the next call
             }
         }
         pa_cp_commit();
@@ -378,40 +403,47 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
         }
         pa_cp_wait<STAGES - 1>();
         __syncwarp();
-        const uint32_t kb = ring + stage * Shape::STAGE_BYTES, vb = kb + PA_TILE * D * 2;
-        // scores: 16 tokens x 8 N8 heads (a stage begins at a multiple of a row's bytes, so that a step is an exclusive or)
-        float s[N8][4] = {}, odd[N8][4] = {};                                 // two chains, for the latency of a product
+        const uint32_t kb = ring + stage * Shape::STAGE_BYTES, vb = kb + PA_SUB * D * 2;
+        // scores: 16 tokens x 8 N8 heads a step (a stage begins at a multiple of a row's bytes, so that 32 dimensions on is
+        // an exclusive or); two chains of products, for their latency
+        float s[SUBS][N8][4];
 #pragma unroll
-        for (int ks = 0; ks < KSTEPS; ks += 2) {
-            uint32_t a[4], b[4];
-            pa_ldmatrix(a, (kb + k_lane) ^ (ks << 5));
-            pa_ldmatrix(b, (kb + k_lane) ^ ((ks + 1) << 5));
+        for (int sub = 0; sub < SUBS; ++sub) {
+            float even[N8][4] = {}, odd[N8][4] = {};
 #pragma unroll
-            for (int n = 0; n < N8; ++n) {
-                pa_mma<T>(s[n], a, qf[n][ks][0], qf[n][ks][1]);
-                pa_mma<T>(odd[n], b, qf[n][ks + 1][0], qf[n][ks + 1][1]);
+            for (int ks = 0; ks < KSTEPS; ks += 2) {
+                uint32_t a[4], b[4];
+                pa_ldmatrix(a, (kb + sub * Shape::SUB_BYTES + k_lane) ^ (ks << 5));
+                pa_ldmatrix(b, (kb + sub * Shape::SUB_BYTES + k_lane) ^ ((ks + 1) << 5));
+#pragma unroll
+                for (int n = 0; n < N8; ++n) {
+                    pa_mma<T>(even[n], a, qf[n][ks][0], qf[n][ks][1]);
+                    pa_mma<T>(odd[n], b, qf[n][ks + 1][0], qf[n][ks + 1][1]);
+                }
             }
-        }
-#pragma unroll
-        for (int n = 0; n < N8; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[n][i] += odd[n][i];
-        const uint32_t mask = s_mask[warp][stage];
-        if (mask != 0xFFFFu) {
+            const uint32_t mask = s_mask[warp][stage][sub];
 #pragma unroll
             for (int n = 0; n < N8; ++n)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (!(mask >> (g + (i >> 1) * 8) & 1)) s[n][i] = -INFINITY;
+                for (int i = 0; i < 4; ++i) s[sub][n][i] = even[n][i] + odd[n][i];
+            if (mask != 0xFFFFu) {
+#pragma unroll
+                for (int n = 0; n < N8; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!(mask >> (g + (i >> 1) * 8) & 1)) s[sub][n][i] = -INFINITY;
+            }
         }
-        // running maxima of the thread's heads (i & 1), over its two tokens and the eight lanes of the same quad
+        // running maxima of the thread's heads (i & 1), over its tokens and the eight lanes of the same quad
         float top[N8][2];
         bool higher = false;
 #pragma unroll
         for (int n = 0; n < N8; ++n)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                float t = fmaxf(s[n][h], s[n][2 + h]);
+                float t = fmaxf(s[0][n][h], s[0][n][2 + h]);
+#pragma unroll
+                for (int sub = 1; sub < SUBS; ++sub) t = fmaxf(t, fmaxf(s[sub][n][h], s[sub][n][2 + h]));
                 t = fmaxf(t, __shfl_xor_sync(FULL_MASK, t, 4));
                 t = fmaxf(t, __shfl_xor_sync(FULL_MASK, t, 8));
                 t = fmaxf(t, __shfl_xor_sync(FULL_MASK, t, 16));
@@ -432,35 +464,39 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
         }
         // The probabilities enter the second product as two numbers of the cache's type, the rounded one and what the
         // rounding left off: one alone would add an error as large as the rounding of the output.
-        uint32_t hi[N8][2], lo[N8][2];
+        uint32_t hi[SUBS][N8][2], lo[SUBS][N8][2];
 #pragma unroll
-        for (int n = 0; n < N8; ++n) {
-            float e[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = exp2_approx((s[n][i] - m[n][i & 1]) * c);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) l[n][h] += e[h] + e[2 + h];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t w = pa_pack<T>(e[2 * i], e[2 * i + 1]);
-                const float2 r = pa_unpack<T>(w);
-                hi[n][i] = pa_transpose(w);
-                lo[n][i] = pa_transpose(pa_pack<T>(e[2 * i] - r.x, e[2 * i + 1] - r.y));
-            }
-        }
-#pragma unroll
-        for (int m0 = 0; m0 < MT; m0 += 4) {
-            uint32_t a[4][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pa_ldmatrix_trans(a[i], (vb + v_lane) ^ ((m0 + i) << 5));
+        for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
             for (int n = 0; n < N8; ++n) {
+                float e[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) pa_mma<T>(o[m0 + i][n], a[i], hi[n][0], hi[n][1]);
+                for (int i = 0; i < 4; ++i) e[i] = exp2_approx((s[sub][n][i] - m[n][i & 1]) * c);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) pa_mma<T>(o[m0 + i][n], a[i], lo[n][0], lo[n][1]);
+                for (int h = 0; h < 2; ++h) l[n][h] += e[h] + e[2 + h];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t w = pa_pack<T>(e[2 * i], e[2 * i + 1]);
+                    const float2 r = pa_unpack<T>(w);
+                    hi[sub][n][i] = pa_transpose(w);
+                    lo[sub][n][i] = pa_transpose(pa_pack<T>(e[2 * i] - r.x, e[2 * i + 1] - r.y));
+                }
             }
-        }
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+            for (int m0 = 0; m0 < MT; m0 += 4) {
+                uint32_t a[4][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pa_ldmatrix_trans(a[i], (vb + sub * Shape::SUB_BYTES + v_lane) ^ ((m0 + i) << 5));
+#pragma unroll
+                for (int n = 0; n < N8; ++n) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) pa_mma<T>(o[m0 + i][n], a[i], hi[sub][n][0], hi[sub][n][1]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) pa_mma<T>(o[m0 + i][n], a[i], lo[sub][n][0], lo[sub][n][1]);
+                }
+            }
         __syncwarp();                                                         // the stage may be filled again
         stage = stage + 1 == STAGES ? 0 : stage + 1;
 
@@ -540,41 +576,15 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
     // the CTA's first stream where that began in an earlier CTA; it is an output if it lies within the CTA, else a part.
     if (lane == 0) s_share[warp] = share;
     __syncthreads();
+    // (every thread makes the list of chains; the work on all of them is then one loop)
     PaMeta meta{-1, 0, 0, 0};
     int32_t from = -1, heads = 0, last = -1;                                  // the chain's first warp (-1: no chain), heads, last warp
     bool inside = false;                                                      // it began in this CTA
+    int32_t before = 0, chains = 0;
     auto close = [&](bool ends) {
-        const bool final = inside && ends;
-        float* part = slots + (2 * WARPS + (inside ? 1 : 0)) * Shape::SLOT;
-        const int64_t out_row = inside ? (int64_t)s_share[from].seq * p.heads + s_share[from].head : 0;
-        for (int32_t i = tid; i < heads * (D / 4); i += THREADS) {
-            const int32_t row = i / (D / 4), at = i % (D / 4) * 4;
-            float top = LOWEST, sum = 0.f;
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int w = from; w <= last; ++w) top = fmaxf(top, s_max[w][inside && w == from][row]);
-#pragma unroll 4
-            for (int w = from; w <= last; ++w) {
-                const int which = inside && w == from;
-                const float f = exp2_approx((s_max[w][which][row] - top) * c);
-                const float4 x = *reinterpret_cast<const float4*>(slots + (2 * w + which) * Shape::SLOT + row * D + at);
-                sum = fmaf(f, s_sum[w][which][row], sum);
-                acc.x = fmaf(f, x.x, acc.x);
-                acc.y = fmaf(f, x.y, acc.y);
-                acc.z = fmaf(f, x.z, acc.z);
-                acc.w = fmaf(f, x.w, acc.w);
-            }
-            if (final) {
-                if (at < p.dim) {
-                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                    const uint2 w2 = make_uint2(pa_pack<T>(acc.x * inv, acc.y * inv), pa_pack<T>(acc.z * inv, acc.w * inv));
-                    *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.out) + (out_row + row) * p.dim + at) = w2;
-                }
-                if (at == 0) p.lse[out_row + row] = sum == 0.f ? -INFINITY : fmaf(top, p.scale, logf(sum));
-            } else {
-                *reinterpret_cast<float4*>(part + row * D + at) = acc;
-                if (at == 0) { part[PA_ROWS * D + row] = top; part[PA_ROWS * (D + 1) + row] = sum; }
-            }
-        }
+        if (tid == 0) s_chain[chains] = PaChain{from, last, heads, before, inside, inside && ends};
+        before += heads;
+        ++chains;
         from = -1;
     };
     for (int w = 0; w < WARPS; ++w) {
@@ -591,6 +601,41 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
         close(false);
     }
     if (tid == 0) p.meta[blockIdx.x] = meta;
+    __syncthreads();
+    int chain = 0;
+    for (int32_t i = tid; i < before * (D / 4); i += THREADS) {
+        const int32_t at = i % (D / 4) * 4;
+        while (chain + 1 < chains && i / (D / 4) >= s_chain[chain + 1].before) ++chain;
+        const PaChain k = s_chain[chain];
+        const int32_t row = i / (D / 4) - k.before;
+        float top = LOWEST, sum = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = k.from; w <= k.last; ++w) top = fmaxf(top, s_max[w][k.inside && w == k.from][row]);
+#pragma unroll 4
+        for (int w = k.from; w <= k.last; ++w) {
+            const int which = k.inside && w == k.from;
+            const float f = exp2_approx((s_max[w][which][row] - top) * c);
+            const float4 x = *reinterpret_cast<const float4*>(slots + (2 * w + which) * Shape::SLOT + row * D + at);
+            sum = fmaf(f, s_sum[w][which][row], sum);
+            acc.x = fmaf(f, x.x, acc.x);
+            acc.y = fmaf(f, x.y, acc.y);
+            acc.z = fmaf(f, x.z, acc.z);
+            acc.w = fmaf(f, x.w, acc.w);
+        }
+        if (k.final) {
+            const int64_t out_row = (int64_t)s_share[k.from].seq * p.heads + s_share[k.from].head + row;
+            if (at < p.dim) {
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                const uint2 w2 = make_uint2(pa_pack<T>(acc.x * inv, acc.y * inv), pa_pack<T>(acc.z * inv, acc.w * inv));
+                *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.out) + out_row * p.dim + at) = w2;
+            }
+            if (at == 0) p.lse[out_row] = sum == 0.f ? -INFINITY : fmaf(top, p.scale, logf(sum));
+        } else {
+            float* part = slots + (2 * WARPS + (k.inside ? 1 : 0)) * Shape::SLOT;
+            *reinterpret_cast<float4*>(part + row * D + at) = acc;
+            if (at == 0) { part[PA_ROWS * D + row] = top; part[PA_ROWS * (D + 1) + row] = sum; }
+        }
+    }
 }
 
 // Joins the parts of a stream that several CTAs share, one warp per head; where they are many, one CTA per head.
@@ -602,46 +647,72 @@ __global__ void __launch_bounds__(PJ_THREADS) paged_attention_join_kernel(const 
     using Shape = PaShape<D>;
     constexpr int WARPS = PJ_THREADS / 32, COLS = D / 32;                     // columns per lane: 2, 4 or 8
     __shared__ __align__(16) float s_acc[WARPS][D];
-    __shared__ float s_sum[WARPS];
+    __shared__ float s_sum[WARPS], s_top[WARPS];
     pdl_wait();
     pdl_launch_dependents();
-    const PaMeta meta = p.meta[blockIdx.x];
-    if (meta.seq < 0) return;
-    const int32_t first = blockIdx.x, n = meta.last - first + 1;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const bool many = n > PJ_MANY;
-    const int row = many ? (int)blockIdx.y : (int)blockIdx.y * WARPS + warp;
-    if (row >= meta.heads) return;                                               // (many: the whole CTA)
+    const int32_t first = blockIdx.x;
     auto slot = [&](int32_t i) { return p.parts + ((int64_t)(first + i) * Shape::SLOTS + 2 * Shape::WARPS + (i == 0 ? 1 : 0)) * Shape::SLOT; };
     const float c = p.scale * LOG2E;
     float top = LOWEST, sum = 0.f, acc[COLS];
-    for (int32_t i = lane; i < n; i += 32) top = fmaxf(top, slot(i)[PA_ROWS * D + row]);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, d));
 #pragma unroll
     for (int j = 0; j < COLS; ++j) acc[j] = 0.f;
-#pragma unroll 4
-    for (int32_t i = many ? warp : 0; i < n; i += many ? WARPS : 1) {
+    struct Part { float m, l, o[COLS]; };
+    auto read = [&](int32_t i, int32_t row) {
         const float* s = slot(i);
-        const float f = exp2_approx((s[PA_ROWS * D + row] - top) * c);
-        sum = fmaf(f, s[PA_ROWS * (D + 1) + row], sum);
+        Part x;
+        x.m = s[PA_ROWS * D + row];
+        x.l = s[PA_ROWS * (D + 1) + row];
 #pragma unroll
-        for (int j = 0; j < COLS; ++j) acc[j] = fmaf(f, s[row * D + j * 32 + lane], acc[j]);
+        for (int j = 0; j < COLS; ++j) x.o[j] = s[row * D + j * 32 + lane];
+        return x;
+    };
+    auto add = [&](const Part& x) {
+        const float to = fmaxf(top, x.m), f = exp2_approx((top - to) * c), e = exp2_approx((x.m - to) * c);
+        top = to;
+        sum = fmaf(e, x.l, f * sum);
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) acc[j] = fmaf(e, x.o[j], f * acc[j]);
+    };
+    // Most streams have two parts, this CTA's and the next one's: they are read along with what says so (and thrown away if
+    // it does not; scratch memory holds them in any case).
+    const int guess = (int)blockIdx.y * WARPS + warp;
+    Part own, next;
+    const bool guessed = guess < p.rows && first + 1 < (int32_t)gridDim.x;
+    if (guessed) { own = read(0, guess); next = read(1, guess); }
+    const PaMeta meta = p.meta[blockIdx.x];
+    if (meta.seq < 0) return;
+    const int32_t n = meta.last - first + 1;
+    const bool many = n > PJ_MANY;
+    const int row = many ? (int)blockIdx.y : guess;
+    if (row >= meta.heads) return;                                            // (many: the whole CTA)
+    if (!many) {
+        add(own);                                                             // (two parts at least, so that they were read)
+        add(next);
+#pragma unroll 4
+        for (int32_t i = 2; i < n; ++i) add(read(i, row));
+    } else {
+#pragma unroll 4
+        for (int32_t i = warp; i < n; i += WARPS) add(read(i, row));
     }
     if (many) {
 #pragma unroll
         for (int j = 0; j < COLS; ++j) s_acc[warp][j * 32 + lane] = acc[j];
-        if (lane == 0) s_sum[warp] = sum;
+        if (lane == 0) { s_sum[warp] = sum; s_top[warp] = top; }
         __syncthreads();
         if (warp > 0) return;
+        top = LOWEST;
         sum = 0.f;
 #pragma unroll
         for (int j = 0; j < COLS; ++j) acc[j] = 0.f;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
-            sum += s_sum[w];
+            Part x;
+            x.m = s_top[w];
+            x.l = s_sum[w];
 #pragma unroll
-            for (int j = 0; j < COLS; ++j) acc[j] += s_acc[w][j * 32 + lane];
+            for (int j = 0; j < COLS; ++j) x.o[j] = s_acc[w][j * 32 + lane];
+            add(x);
         }
     }
     const int64_t out_row = (int64_t)meta.seq * p.heads + meta.head + row;
