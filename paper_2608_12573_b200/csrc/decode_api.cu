@@ -75,39 +75,63 @@ struct Launch {
 
 // ---- log probabilities -----------------------------------------------------------------------
 
-constexpr unsigned LP_MAX_PARTS = 16;
-
 size_t lp_smem(unsigned parts, uint32_t k) {
-    return LP_TEAMS * sizeof(LpTeamMemory) + 2 * (size_t)parts * ((k ? k + LP_SLACK : 0) * sizeof(uint64_t) + sizeof(LpStats));
+    return LP_TEAMS * sizeof(LpTeamMemory) + 2 * (size_t)parts * ((k ? k + LP_SLACK : 0) * sizeof(uint64_t) + sizeof(LpStats) + 2 * sizeof(float));
 }
 
-// Teams per row: as many as load the device's two teams per SM evenly, with a fixed cost per row and part that is the
-// time of some 16 KB.
-unsigned lp_parts(int64_t rows, int64_t V, size_t elem, int sms) {
-    const double slots = (double)LP_TEAMS * sms, fixed = 16384.0, bytes = (double)V * elem;
+// Clusters of `shares` CTAs (each with an SM to itself) that run at a time: the SMs of a cluster lie in one part of the
+// chip, and not every part holds a multiple of them.
+template <typename K>
+int lp_clusters(K* kernel, unsigned shares, size_t smem, int sms) {
+    if (shares == 1) return sms;
+    static int known[MAX_DEVICES][5];                    // by log2 of the shares; the same for all builds of the kernel
+    static std::mutex mutex;
+    int dev = 0, log2 = 0, n = 0;
+    while ((1u << log2) < shares) ++log2;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 1;
+    std::lock_guard<std::mutex> lock(mutex);
+    if (known[dev][log2] == 0) {
+        Launch l(shares, LP_THREADS, smem, nullptr, shares);
+        if (cudaOccupancyMaxActiveClusters(&n, kernel, &l.cfg) != cudaSuccess || n < 1) { (void)cudaGetLastError(); n = std::max(1, sms / (int)shares); }
+        known[dev][log2] = n;
+    }
+    return known[dev][log2];
+}
+
+// Teams per row.  The time of a row and part is that of its bytes at a team's share of the bandwidth plus a fixed latency
+// (in bytes of that stream, 22 GB/s: 1 us is 22 KB), and rows beyond what runs at a time wait: the number of parts with the
+// least of it.  The fixed part was read off calls with one row per team: 3 us without alternatives, 6 with them (most of
+// it behind the stream, and hidden behind the next row's), and 2 more for parts that meet.
+template <typename K>
+unsigned lp_parts(K* kernel, int64_t rows, int64_t V, size_t elem, bool top, int sms) {
+    const double us = 22000.0, bytes = (double)V * elem;
     unsigned best = 1;
     double best_cost = 0;
     for (unsigned parts = 1; parts <= LP_MAX_PARTS; parts *= 2) {
-        if (parts > 1 && bytes / parts < 8192.0) break;
-        const double rounds = std::ceil((double)rows * parts / slots);
-        const double cost = rounds * (bytes / parts + fixed + (parts > 1 ? fixed : 0.0));
+        if (parts > 1 && bytes / parts < 4096.0) break;
+        const unsigned shares = std::max(1u, parts / LP_TEAMS);
+        const double at_a_time = (double)lp_clusters(kernel, shares, lp_smem(LP_MAX_PARTS, LP_MAX_K), sms) * shares * LP_TEAMS / parts;
+        const double rounds = std::ceil((double)rows / at_a_time);
+        const double open = (top ? 1.5 : 0.5) * us + (parts > 1 ? (top ? 2.0 : 1.0) * us : 0.0), close = (top ? 4.5 : 2.5) * us;
+        const double cost = rounds * (bytes / parts + open) + close;
         if (parts == 1 || cost < best_cost) { best = parts; best_cost = cost; }
     }
     return best;
 }
 
 template <typename T, bool ENT, bool TOPK>
-int lp_launch(LpParams p, unsigned parts, int sms, void* stream) {
+int lp_launch(LpParams p, int sms, void* stream) {
     static uint64_t done = 0;
     static std::mutex mutex;
-    DEC_TRY(prepare_kernel(logprobs_kernel<T, ENT, TOPK>, lp_smem(LP_MAX_PARTS, LP_MAX_K), false, &done, &mutex));
-    p.parts = parts;
-    for (p.parts_log2 = 0; (1u << p.parts_log2) < parts; ++p.parts_log2) {}
-    const unsigned shares = std::max(1u, parts / LP_TEAMS);
-    const int64_t most = std::max<int64_t>(1, sms / shares);
-    const int64_t groups = std::min<int64_t>(parts > 1 ? p.rows : (p.rows + LP_TEAMS - 1) / LP_TEAMS, most);
-    Launch l((unsigned)(groups * shares), LP_THREADS, lp_smem(parts, p.k), stream, shares);
-    DEC_TRY(cudaLaunchKernelEx(&l.cfg, logprobs_kernel<T, ENT, TOPK>, p));
+    auto* kernel = logprobs_kernel<T, ENT, TOPK>;
+    DEC_TRY(prepare_kernel(kernel, lp_smem(LP_MAX_PARTS, LP_MAX_K), false, &done, &mutex));
+    p.parts = lp_parts(kernel, p.rows, p.V, sizeof(T), TOPK, sms);
+    for (p.parts_log2 = 0; (1u << p.parts_log2) < p.parts; ++p.parts_log2) {}
+    const unsigned shares = std::max(1u, p.parts / LP_TEAMS);
+    const int64_t most = lp_clusters(kernel, shares, lp_smem(LP_MAX_PARTS, LP_MAX_K), sms);
+    const int64_t groups = std::min<int64_t>(p.parts > 1 ? p.rows : (p.rows + LP_TEAMS - 1) / LP_TEAMS, most);
+    Launch l((unsigned)(groups * shares), LP_THREADS, lp_smem(p.parts, p.k), stream, shares);
+    DEC_TRY(cudaLaunchKernelEx(&l.cfg, kernel, p));
     return PROFK_OK;
 }
 
@@ -122,9 +146,8 @@ int lp_forward(const T* logits, int64_t rows, int64_t V, int64_t row_stride, con
     const int sms = sm_count();
     if (sms < 1) return PROFK_ECUDA;
     LpParams p{logits, rows, row_stride, (uint32_t)V, (uint32_t)k, 1u, 0u, (float)(1.0 / temperature), tokens, logprob, lse, lse_rest, entropy, top_logprobs, top_tokens};
-    const unsigned parts = lp_parts(rows, V, sizeof(T), sms);
-    if (entropy) return k ? lp_launch<T, true, true>(p, parts, sms, stream) : lp_launch<T, true, false>(p, parts, sms, stream);
-    return k ? lp_launch<T, false, true>(p, parts, sms, stream) : lp_launch<T, false, false>(p, parts, sms, stream);
+    if (entropy) return k ? lp_launch<T, true, true>(p, sms, stream) : lp_launch<T, true, false>(p, sms, stream);
+    return k ? lp_launch<T, false, true>(p, sms, stream) : lp_launch<T, false, false>(p, sms, stream);
 }
 
 template <typename T>

@@ -22,6 +22,8 @@
 
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "logits.cuh"
 
 namespace profk {
@@ -39,6 +41,7 @@ constexpr uint32_t LP_STEP = LP_STREAM * LP_UNROLL;     // vectors per batch
 constexpr uint32_t LP_NOTES = 2048;       // vectors the list holds
 constexpr uint32_t LP_FIN = 512;          // elements the finishing warp holds; more than half of them it cuts back to the k best
 constexpr uint32_t LP_MAX_K = 128;        // most alternatives
+constexpr uint32_t LP_MAX_PARTS = 16;     // most teams that share a row
 constexpr uint32_t LP_SLACK = 32;         // a selection may stop with up to k + LP_SLACK records in hand
 
 struct LpParams {
@@ -78,6 +81,7 @@ struct LpShared {
     LpRow row[2];
     uint64_t fin[LP_FIN];                 // records, of the finishing warp
     float slot[LP_STREAM];                // largest logits seen by a group of lanes
+    float half[LP_STREAM / 16];           // ... by half a warp
 };
 
 // Named barriers of a team: among its streaming warps; a row is ready for the finishing warp; its place may be used again.
@@ -148,37 +152,43 @@ __device__ __forceinline__ uint64_t lp_find_limit(const uint64_t* a, uint32_t n,
 
 // Lanes that share a slot: the coarser the slots the cheaper the bound, the finer the tighter (the k-th largest of n slots
 // has about n ln(n / (n - k)) elements above it).
+constexpr uint32_t LP_RANKED = LP_MAX_K + LP_SLACK;     // records that are ranked against one another
 constexpr uint32_t LP_FEW_K = 16;         // up to here 22 slots, one per lane of a warp, whose k-th largest is found by counting
 __device__ __forceinline__ uint32_t lp_slot_lanes(uint32_t k) { return k <= LP_FEW_K ? 16 : k <= 64 ? 4 : 1; }
 
+// Both kinds of slots; the coarser ones serve alone for few alternatives (slot_lanes 16).
 __device__ __forceinline__ void lp_write_slot(float seen, uint32_t tid, uint32_t lanes, LpShared& sh) {
-    if (lanes >= 4) {
-        seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 1));
-        seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 2));
-    }
-    if (lanes == 16) {
-        seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 4));
-        seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 8));
-    }
-    if ((tid & (lanes - 1)) == 0) sh.slot[tid / lanes] = seen;
+    if (lanes == 1) sh.slot[tid] = seen;
+    seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 1));
+    seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 2));
+    if (lanes == 4 && (tid & 3) == 0) sh.slot[tid / 4] = seen;
+    seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 4));
+    seen = fmaxf(seen, __shfl_xor_sync(FULL_MASK, seen, 8));
+    if ((tid & 15) == 0) sh.half[tid / 16] = seen;
 }
 
 // A count that is near enough: at least k values reach the bound, and not many more.
 __device__ __forceinline__ uint32_t lp_enough(uint32_t k) { return k + k / 8 + 1; }
 
+// By any warp: the k-th largest of the half warps' slots, k <= LP_FEW_K, by counting.
+__device__ __forceinline__ float lp_half_bound(uint32_t k, const LpShared& sh) {
+    constexpr uint32_t N = LP_STREAM / 16;
+    const uint32_t lane = lane_id();
+    const volatile float* slot = sh.half;
+    const float mine = lane < N ? slot[lane] : -INFINITY;
+    uint32_t above = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) above += __shfl_sync(FULL_MASK, mine, i) > mine;
+    // of the slots with fewer than k larger ones the smallest: at least k slots reach it
+    const uint32_t key = above < k && lane < N ? key_from_bits32(float_bits_exact(mine)) : 0xFFFFFFFFu;
+    return __uint_as_float(bits32_from_key(__reduce_min_sync(FULL_MASK, key)));
+}
+
 // By one warp: a bound from the slots that is no lower than `bound`.
 __device__ __forceinline__ float lp_slot_bound(float bound, uint32_t k, uint32_t lanes, const LpShared& sh) {
+    if (lanes == 16) return fmaxf(bound, lp_half_bound(k, sh));
     const uint32_t n = LP_STREAM / lanes, lane = lane_id();
     const volatile float* slot = sh.slot;
-    if (lanes == 16) {
-        const float mine = lane < n ? slot[lane] : -INFINITY;
-        uint32_t above = 0;
-#pragma unroll
-        for (int i = 0; i < LP_STREAM / 16; ++i) above += __shfl_sync(FULL_MASK, mine, i) > mine;
-        // of the slots with fewer than k larger ones the smallest: at least k slots reach it
-        const uint32_t key = above < k && lane < n ? key_from_bits32(float_bits_exact(mine)) : 0xFFFFFFFFu;
-        return fmaxf(bound, __uint_as_float(bits32_from_key(__reduce_min_sync(FULL_MASK, key))));
-    }
     uint32_t top = 0, reach = 0;
     uint32_t lo = key_from_bits32(float_bits_exact(bound));
     for (uint32_t at = lane; at < n; at += 32) {
@@ -204,13 +214,13 @@ __device__ __forceinline__ float lp_slot_bound(float bound, uint32_t k, uint32_t
     return __uint_as_float(bits32_from_key(lo));
 }
 
-// By the streaming warps: (nearly) the k-th largest of the logits `seen` by their threads, by halving the interval of their
-// order keys.  They are LOWEST at least, and so is the bound: -inf is never noted on the way.
-__device__ __forceinline__ float lp_first_bound(float seen, uint32_t k, uint32_t lanes, uint32_t tid, LpShared& sh, const LpBarriers& bar) {
-    if (lanes == 16) {
-        lp_write_slot(seen, tid, lanes, sh);
+// By the streaming warps: (nearly) the k-th largest of the logits `seen` by their threads: of half warps' for few, else by
+// halving the interval of their order keys.  They are LOWEST at least, and so is the bound: -inf is never noted on the
+// way.  The slots must be written; a barrier lies within.
+__device__ __forceinline__ float lp_first_bound(float seen, uint32_t k, LpShared& sh, const LpBarriers& bar) {
+    if (k <= LP_FEW_K) {
         bar.count(true);
-        return lp_slot_bound(LOWEST, k, lanes, sh);
+        return lp_half_bound(k, sh);
     }
     const uint32_t key = key_from_bits32(float_bits_exact(seen));
     uint32_t lo = key_from_bits32(0xFF7FFFFFu), hi = key_from_bits32(0x7F800000u) + 1u;
@@ -305,11 +315,11 @@ __device__ __forceinline__ uint32_t lp_fin_vector(uint32_t n, bool has, const ui
     return n;
 }
 
-// The candidates of a row's share, at most k + LP_SLACK of them, the k best of the share among them.
+// The candidates of a row's share, at most `most` (>= k) of them, the k best of the row among them as far as they lie here.
 template <typename T>
-__device__ __forceinline__ uint32_t lp_fin_select(const LpShare<T> mine, uint32_t k, bool first, bool last, uint32_t V, const LpRow& r, LpShared& sh) {
+__device__ __forceinline__ uint32_t lp_fin_select(const LpShare<T> mine, uint32_t k, uint32_t most, bool first, bool last, uint32_t V, const LpRow& r, LpShared& sh) {
     constexpr int VEC = Logit<T>::VEC;
-    const uint32_t lane = lane_id(), lim = k + LP_SLACK;
+    const uint32_t lane = lane_id();
     uint32_t n = 0;
     float bound = r.bound;
     const uint32_t notes = r.count, tail = mine.head + mine.nvec * VEC;
@@ -342,11 +352,13 @@ __device__ __forceinline__ uint32_t lp_fin_select(const LpShare<T> mine, uint32_
         }
     }
     n = lp_fin_add(n, tx >= bound, tx, tail + lane, sh);
-    // Masked tokens (-inf) fill the places that nothing else takes, lowest indices first.
+    // Masked tokens (-inf) fill the places that nothing else takes, lowest indices first.  (A bound above LOWEST says that
+    // the row has k others; of a part it may have fewer.)
+    const bool short_of = r.bound == LOWEST;
     const uint32_t e1 = last ? V : mine.head + mine.v1 * VEC;
-    for (uint32_t e = (first ? 0 : mine.head + mine.v0 * VEC); n < k && e < e1; e += 32)
+    for (uint32_t e = (first ? 0 : mine.head + mine.v0 * VEC); short_of && n < k && e < e1; e += 32)
         n = lp_fin_add(n, e + lane < e1 && Logit<T>::to_float(mine.x[e + lane]) == -INFINITY, -INFINITY, e + lane, sh);
-    if (n > lim) n = lp_fin_drop(n, lp_find_limit(sh.fin, n, k, lim), sh);
+    if (n > most) n = lp_fin_drop(n, lp_find_limit(sh.fin, n, k, most), sh);
     return n;
 }
 
@@ -374,8 +386,12 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t parts = p.parts, part = parts > 1 ? cluster.block_rank() * LP_TEAMS + team : 0;
     // what the parts of a row hand to the first of them: two sets, used in turn
-    uint64_t* in_recs = reinterpret_cast<uint64_t*>(lp_dyn + LP_TEAMS * sizeof(LpTeamMemory));              // [2][parts][lim]
+    uint64_t* in_recs = reinterpret_cast<uint64_t*>(lp_dyn + LP_TEAMS * sizeof(LpTeamMemory));              // [2][parts * lim]
     LpStats* in_stats = reinterpret_cast<LpStats*>(in_recs + 2 * (size_t)parts * lim);                     // [2][parts]
+    float* in_bounds = reinterpret_cast<float*>(in_stats + 2 * parts);                                     // [2][2][parts], in every CTA
+    __shared__ uint32_t in_found[2];                                              // records in the list
+    if (threadIdx.x < 2) in_found[threadIdx.x] = 0;
+    if (parts > 1) __syncthreads();
 
     const uint32_t shares = parts > 1 ? parts / LP_TEAMS : 1;                     // CTAs per row
     const int32_t rows = (int32_t)p.rows;
@@ -400,6 +416,11 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
             const int64_t token = p.tokens ? p.tokens[row] : -1;
             float token_x = 0.f;
             if (token >= 0 && token < (int64_t)p.V) token_x = Logit<T>::to_float((reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.row_stride)[token]);
+            if constexpr (TOPK)
+                if (parts > 1) {                                                  // the streaming warps exchange bounds, see there
+                    cluster.sync();
+                    if (__any_sync(FULL_MASK, lane < parts && in_bounds[turn * 2 * parts + lane] == LOWEST)) cluster.sync();
+                }
             bar.full_sync(turn);
             LpRow& r = sh.row[turn];
             // join the warps' statistics, in a fixed order; every lane gets the result
@@ -418,13 +439,16 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
             if constexpr (TOPK) {
                 LpShare<T> mine;
                 mine.set(p, row, part);
-                found = lp_fin_select<T>(mine, p.k, part == 0, part == parts - 1, p.V, r, sh);
+                found = lp_fin_select<T>(mine, p.k, parts > 1 ? lim : LP_RANKED, part == 0, part == parts - 1, p.V, r, sh);
             }
             if (parts > 1) {
                 // hand statistics and records to the cluster's first CTA
                 if constexpr (TOPK) {
-                    uint64_t* to_recs = cluster.map_shared_rank(in_recs, 0) + ((size_t)turn * parts + part) * lim;
-                    for (uint32_t i = lane; i < lim; i += 32) to_recs[i] = i < found ? sh.fin[i] : ~0ull;
+                    uint32_t at = 0;
+                    if (lane == 0 && found > 0) at = atomicAdd(cluster.map_shared_rank(in_found, 0) + turn, found);
+                    at = __shfl_sync(FULL_MASK, at, 0);
+                    uint64_t* to_recs = cluster.map_shared_rank(in_recs, 0) + (size_t)turn * parts * lim + at;
+                    for (uint32_t i = lane; i < found; i += 32) to_recs[i] = sh.fin[i];
                 }
                 if (lane == 0) *(cluster.map_shared_rank(in_stats, 0) + turn * parts + part) = all;
                 cluster.sync();
@@ -432,15 +456,17 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
                     all = join_lanes(lane % 16 < parts ? in_stats[turn * parts + lane % 16] : LpStats{LOWEST, 0.f, 0.f}, 16);
                     if constexpr (TOPK) {
                         const uint64_t* recs = in_recs + (size_t)turn * parts * lim;
-                        const uint64_t limit = lp_find_limit(recs, parts * lim, p.k, lim);
+                        const uint32_t n = in_found[turn];
+                        const uint64_t limit = n > LP_RANKED ? lp_find_limit(recs, n, p.k, LP_RANKED) : ~0ull;
                         found = 0;
-                        for (uint32_t i0 = 0; i0 < parts * lim; i0 += 32) {
-                            const uint64_t rec = i0 + lane < parts * lim ? recs[i0 + lane] : ~0ull;
-                            const unsigned who = __ballot_sync(FULL_MASK, rec <= limit);
-                            if (rec <= limit) sh.fin[found + __popc(who & ((1u << lane) - 1u))] = rec;
+                        for (uint32_t i0 = 0; i0 < n; i0 += 32) {
+                            const bool keep = i0 + lane < n && recs[i0 + lane] <= limit;
+                            const unsigned who = __ballot_sync(FULL_MASK, keep);
+                            if (keep) sh.fin[found + __popc(who & ((1u << lane) - 1u))] = recs[i0 + lane];
                             found += __popc(who);
                         }
                         __syncwarp();
+                        if (lane == 0) in_found[turn] = 0;
                     }
                 }
             }
@@ -462,35 +488,40 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
                     }
                 }
                 if constexpr (TOPK) {
-                    constexpr int PER = (LP_MAX_K + LP_SLACK) / 32;
-                    uint64_t rec[PER];
-                    uint32_t rank[PER];
+                    auto rank_and_write = [&](auto regs) {
+                        constexpr int PER = decltype(regs)::value;                // records per lane
+                        uint64_t rec[PER];
+                        uint32_t rank[PER];
 #pragma unroll
-                    for (int i = 0; i < PER; ++i) {
-                        const uint32_t at = i * 32 + lane;
-                        rec[i] = at < found ? sh.fin[at] : ~0ull;
-                        rank[i] = at < found ? 0 : at;
-                    }
-#pragma unroll 2
-                    for (uint32_t q = 0; q < found; ++q) {
-                        const uint64_t other = sh.fin[q];
-#pragma unroll
-                        for (int i = 0; i < PER; ++i)
-                            if (i * 32 < found) rank[i] += other < rec[i] && i * 32 + lane < found;
-                    }
-#pragma unroll
-                    for (int i = 0; i < PER; ++i) {
-                        if (rank[i] >= p.k) continue;
-                        float lp = NAN;                                           // fewer than k elements that are no NaN
-                        int64_t at = -1;
-                        if (rec[i] != ~0ull) {
-                            const float x = __uint_as_float(bits32_from_key(record_key(rec[i])));
-                            lp = empty ? -INFINITY : (x - all.m) * p.scale - log_s;
-                            at = (int64_t)record_idx(rec[i]);
+                        for (int i = 0; i < PER; ++i) {
+                            const uint32_t at = i * 32 + lane;
+                            rec[i] = at < found ? sh.fin[at] : ~0ull;
+                            rank[i] = at < found ? 0 : at - found;                // (behind all that are valid)
                         }
-                        p.top_logprobs[(int64_t)row * p.k + rank[i]] = lp;
-                        p.top_tokens[(int64_t)row * p.k + rank[i]] = at;
-                    }
+#pragma unroll 4
+                        for (uint32_t q = 0; q < found; ++q) {
+                            const uint64_t other = sh.fin[q];
+#pragma unroll
+                            for (int i = 0; i < PER; ++i) rank[i] += other < rec[i];
+                        }
+#pragma unroll
+                        for (int i = 0; i < PER; ++i) {
+                            if (rank[i] >= p.k) continue;
+                            float lp = NAN;                                       // fewer than k elements that are no NaN
+                            int64_t at = -1;
+                            if (rec[i] != ~0ull) {
+                                const float x = __uint_as_float(bits32_from_key(record_key(rec[i])));
+                                lp = empty ? -INFINITY : (x - all.m) * p.scale - log_s;
+                                at = (int64_t)record_idx(rec[i]);
+                            }
+                            p.top_logprobs[(int64_t)row * p.k + rank[i]] = lp;
+                            p.top_tokens[(int64_t)row * p.k + rank[i]] = at;
+                        }
+                    };
+                    const uint32_t places = max(found, p.k);
+                    if (places <= 32) rank_and_write(std::integral_constant<int, 1>{});
+                    else if (places <= 64) rank_and_write(std::integral_constant<int, 2>{});
+                    else rank_and_write(std::integral_constant<int, LP_RANKED / 32>{});
                 }
             }
             __syncwarp();
@@ -538,6 +569,20 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
         };
 #pragma unroll
         for (int s = 0; s < LP_STAGES - 1; ++s) load_batch();
+
+        // The least (or the largest) of the parts' bounds; the finishing warps take part in the barrier.
+        auto lp_exchange = [&](float mine, bool largest) {
+            const uint32_t set = (turn * 2 + (largest ? 1 : 0)) * parts;
+            if (tid < shares) cluster.map_shared_rank(in_bounds, tid)[set + part] = mine;
+            cluster.sync();
+            float b = lane < parts ? in_bounds[set + lane] : largest ? LOWEST : INFINITY;
+#pragma unroll
+            for (int d = LP_MAX_PARTS / 2; d > 0; d >>= 1) {
+                const float o = __shfl_xor_sync(FULL_MASK, b, d);
+                b = largest ? fmaxf(b, o) : fminf(b, o);
+            }
+            return __shfl_sync(FULL_MASK, b, 0);
+        };
 
         int stage = 0;
         for (int32_t row = first; row < rows; row += stride) {
@@ -661,7 +706,15 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
                 if constexpr (TOPK) {
                     volatile float* bound_at = &r.bound;
                     if (batch == 0) {
-                        bound = lp_first_bound(seen, p.k, slot_lanes, tid, sh, bar);
+                        lp_write_slot(seen, tid, slot_lanes, sh);                 // (all slots of the row before anyone reads one)
+                        if (parts == 1) {
+                            bound = lp_first_bound(seen, p.k, sh, bar);
+                        } else {
+                            // k of the row's elements reach the least of the parts' (k / parts)-th largest, a much better
+                            // bound than a part's own k-th unless some part is masked: then the best of those instead.
+                            bound = lp_exchange(lp_first_bound(seen, (p.k + parts - 1) >> p.parts_log2, sh, bar), false);
+                            if (bound == LOWEST) bound = lp_exchange(lp_first_bound(seen, p.k, sh, bar), true);
+                        }
                         if (tid == 0) *bound_at = bound;                          // (nobody else writes it before two more batches)
 #pragma unroll
                         for (int u = 0; u < U; ++u)
@@ -669,7 +722,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
                         __syncwarp();
                     }
                     ++batch;
-                    if ((batch & (batch - 1)) == 0) {
+                    if (batch > 1 && (batch & (batch - 1)) == 0) {
                         lp_write_slot(seen, tid, slot_lanes, sh);
                     } else if (batch == raise_at) {                               // one warp, a batch later: the slots are written
                         const float higher = lp_slot_bound(*bound_at, p.k, slot_lanes, sh);
