@@ -267,7 +267,6 @@ bool fork_sizes_ok(int64_t n_old, int64_t n, int64_t pages, int64_t page_size, i
     return n_old >= 0 && n >= 0 && n_old <= (1 << 24) && n <= (1 << 24) && pages >= 1 && pages <= 0x7FFF0000ll && page_size >= 1 && page_size <= (1 << 24) &&
            grow >= 0 && grow <= (1 << 24) && n * (1 + (grow + page_size - 1) / page_size) <= 0x7FFF0000ll;
 }
-constexpr unsigned PG_CTAS_PER_SM = 6;
 
 }  // namespace
 
@@ -359,7 +358,7 @@ int profk_pages_fork(const profk_pool_t* pool, const int32_t* tables, int64_t n_
     const unsigned copiers = (unsigned)std::min<int64_t>(sms, (pages + PG_PLAN_THREADS - 1) / PG_PLAN_THREADS);
     Launch plan(1 + copiers, PG_PLAN_THREADS, 0, stream);
     DEC_TRY(cudaLaunchKernelEx(&plan.cfg, pages_fork_plan_kernel, p));
-    Launch work((unsigned)sms * PG_CTAS_PER_SM, PG_THREADS, 0, stream);
+    Launch work((unsigned)sms * PG_CTAS_PIECES, PG_THREADS, 0, stream);
     DEC_TRY(cudaLaunchKernelEx(&work.cfg, pages_fork_kernel, p));
     return PROFK_OK;
 }
@@ -383,7 +382,7 @@ int profk_pages_compact(const profk_pool_t* pool, const int32_t* tables, int64_t
                       static_cast<PgPlanHead*>(workspace), reinterpret_cast<PgMove*>(static_cast<char*>(workspace) + 256), pg_pool(pool, 1)};
     Launch plan(1, PG_PLAN_THREADS, 0, stream);
     DEC_TRY(cudaLaunchKernelEx(&plan.cfg, pages_compact_plan_kernel, p));
-    Launch work((unsigned)sms * PG_CTAS_PER_SM, PG_THREADS, 0, stream);
+    Launch work((unsigned)sms * PG_CTAS_PAGES, PG_THREADS, 0, stream);
     DEC_TRY(cudaLaunchKernelEx(&work.cfg, pages_compact_kernel, p));
     return PROFK_OK;
 }
@@ -394,7 +393,7 @@ int profk_pages_copy(const profk_pool_t* pool, int64_t pages, const int32_t* src
     const int sms = sm_count();
     if (sms < 1) return PROFK_ECUDA;
     PgCopyParams p{src, dst, (int32_t)n, (int32_t)pages, pg_pool(pool, pool->page_size)};
-    Launch l((unsigned)std::min<int64_t>((int64_t)sms * PG_CTAS_PER_SM, n * 2 * pool->layers), PG_THREADS, 0, stream);
+    Launch l((unsigned)std::min<int64_t>((int64_t)sms * PG_CTAS_PAGES, n * 2 * pool->layers), PG_THREADS, 0, stream);
     DEC_TRY(cudaLaunchKernelEx(&l.cfg, pages_copy_kernel, p));
     return PROFK_OK;
 }

@@ -6,13 +6,16 @@
 // device then writes tables and counts and moves the pages' bytes.
 #pragma once
 
-#include "select_sort.cuh"
+#include "common.cuh"
 
 namespace profk {
 
 constexpr int PG_PLAN_THREADS = 1024;
 constexpr int PG_THREADS = 256;
-constexpr int PG_UNROLL = 4;              // 16-byte vectors per thread in flight
+// 16-byte vectors per thread in flight, and CTAs per SM.  Whole pages: fewer CTAs with more in flight each (1 GB moved: 171 us
+// against 179); the shorter pieces that a fork copies: more CTAs (86 MB: 24 us against 28).
+constexpr int PG_UNROLL_PAGES = 8, PG_CTAS_PAGES = 4;
+constexpr int PG_UNROLL_PIECES = 4, PG_CTAS_PIECES = 6;
 
 // Where a pool's bytes lie; strides in bytes, all multiples of 16.
 struct PgPool {
@@ -58,10 +61,13 @@ __device__ __forceinline__ int32_t pg_length(const int32_t* lengths, int32_t s, 
 }
 __device__ __forceinline__ int32_t pg_ceil(int64_t tokens, int32_t page_size) { return (int32_t)((tokens + page_size - 1) / page_size); }
 
+constexpr int PG_NEAR = 4096;             // old sequences whose children are counted in shared memory
+
 struct PgChild {
     int32_t parent, old, length, have, want, fill, beyond;   // parent < 0: an empty sequence; beyond: pages past the table
     bool copy;
-    __device__ __forceinline__ PgChild(const PgForkParams& p, int32_t i) {
+    __device__ __forceinline__ PgChild(const PgForkParams& p, int32_t i) : PgChild(p, i, p.first) {}
+    __device__ __forceinline__ PgChild(const PgForkParams& p, int32_t i, const int32_t* first) {
         parent = p.parents[i];
         if (parent < 0 || parent >= p.n_old) parent = -1;
         old = parent >= 0 ? pg_length(p.lengths, parent, p.width, p.page_size) : 0;
@@ -71,20 +77,27 @@ struct PgChild {
         want = pg_ceil(length, p.page_size);
         beyond = pg_ceil(wanted, p.page_size) - want;
         fill = old % p.page_size;
-        copy = parent >= 0 && fill > 0 && p.first[parent] != i;
+        copy = parent >= 0 && fill > 0 && first[parent] != i;
     }
     __device__ __forceinline__ int32_t fresh_from() const { return have - (copy ? 1 : 0); }   // columns from here on are fresh
 };
 
 // Block-wide sum of the numbers before this thread's, and of all of them (1024 threads).
 __device__ __forceinline__ uint32_t pg_scan(uint32_t v, uint32_t* warp_sums, uint32_t* total) {
-    const uint32_t incl = block_scan_any(v, warp_sums);
-    __shared__ uint32_t s_total;
-    if (threadIdx.x == PG_PLAN_THREADS - 1) s_total = incl;
+    const uint32_t lane = lane_id(), warp = threadIdx.x >> 5;
+    uint32_t incl = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t up = __shfl_up_sync(FULL_MASK, incl, d);
+        if (lane >= (uint32_t)d) incl += up;
+    }
+    if (lane == 31) warp_sums[warp] = incl;
     __syncthreads();
-    *total = s_total;
-    __syncthreads();
-    return incl - v;
+    const uint32_t w = warp_sums[lane];                  // (32 warps)
+    *total = __reduce_add_sync(FULL_MASK, w);
+    const uint32_t before = __reduce_add_sync(FULL_MASK, lane < warp ? w : 0u);
+    __syncthreads();                                     // warp_sums may be used again
+    return before + incl - v;
 }
 
 // Block 0 plans; the others copy the counts, which the second kernel then changes.
@@ -99,24 +112,30 @@ __global__ void __launch_bounds__(PG_PLAN_THREADS) pages_fork_plan_kernel(const 
             p.out_refs[i] = p.refs[i];
         return;
     }
+    __shared__ int32_t s_first[PG_NEAR], s_kids[PG_NEAR];
+    const bool near = p.n_old <= PG_NEAR;
+    int32_t* first = near ? s_first : p.first;
+    int32_t* kids = near ? s_kids : p.kids;
     if (tid == 0) s_moves = 0;
-    for (int32_t s = tid; s < p.n_old; s += PG_PLAN_THREADS) { p.first[s] = p.n; p.kids[s] = 0; }
+    for (int32_t s = tid; s < p.n_old; s += PG_PLAN_THREADS) { first[s] = p.n; kids[s] = 0; }
     __syncthreads();
     for (int32_t i = tid; i < p.n; i += PG_PLAN_THREADS) {
         const int32_t parent = p.parents[i];
         if (parent >= 0 && parent < p.n_old) {
-            atomicMin(&p.first[parent], i);
-            atomicAdd(&p.kids[parent], 1);
+            atomicMin(&first[parent], i);
+            atomicAdd(&kids[parent], 1);
         }
     }
     __syncthreads();
+    if (near)
+        for (int32_t s = tid; s < p.n_old; s += PG_PLAN_THREADS) { p.first[s] = first[s]; p.kids[s] = kids[s]; }
     // how many fresh pages each new sequence needs, numbered through
     uint32_t total = 0, beyond = 0;
     for (int32_t i0 = 0; i0 < p.n; i0 += PG_PLAN_THREADS) {
         const int32_t i = i0 + tid;
         uint32_t mine = 0, sum = 0;
         if (i < p.n) {
-            const PgChild c(p, i);
+            const PgChild c(p, i, first);
             mine = (uint32_t)(c.want - c.fresh_from());
             beyond += (uint32_t)c.beyond;
             p.out_lengths[i] = c.length;
@@ -149,7 +168,7 @@ __global__ void __launch_bounds__(PG_PLAN_THREADS) pages_fork_plan_kernel(const 
     __syncthreads();
     // the partly filled pages that are copied
     for (int32_t i = tid; i < p.n; i += PG_PLAN_THREADS) {
-        const PgChild c(p, i);
+        const PgChild c(p, i, first);
         if (!c.copy) continue;
         const int32_t src = p.tables[c.parent * p.table_stride + c.have - 1], number = p.need[i];
         if (number < (int32_t)found && src >= 0 && src < p.pages) {
@@ -166,6 +185,7 @@ __global__ void __launch_bounds__(PG_PLAN_THREADS) pages_fork_plan_kernel(const 
 }
 
 // One page of one layer's keys or values, by the whole CTA: `tokens` tokens of every head.
+template <int PG_UNROLL>
 __device__ __forceinline__ void pg_copy(const PgPool& pool, int32_t src, int32_t dst, int32_t tokens, int32_t plane) {
     char* base = pool.base + (plane >> 1) * pool.layer + (plane & 1) * pool.kv;
     const char* from = base + src * pool.page;
@@ -203,12 +223,13 @@ __device__ __forceinline__ void pg_copy(const PgPool& pool, int32_t src, int32_t
 }
 
 // The copies of a plan; no page is both read and written by them.
+template <int PG_UNROLL>
 __device__ __forceinline__ void pg_copy_all(const PgPool& pool, const PgMove* moves, int32_t n) {
     if (!pool.base) return;
     const int32_t planes = 2 * pool.layers;
     for (int64_t unit = blockIdx.x; unit < (int64_t)n * planes; unit += gridDim.x) {
         const PgMove m = moves[unit / planes];
-        pg_copy(pool, m.src, m.dst, m.tokens, (int32_t)(unit % planes));
+        pg_copy<PG_UNROLL>(pool, m.src, m.dst, m.tokens, (int32_t)(unit % planes));
     }
 }
 
@@ -247,7 +268,7 @@ __global__ void __launch_bounds__(PG_THREADS) pages_fork_kernel(const PgForkPara
         const int32_t page = p.tables[s * p.table_stride + col];
         if (page >= 0 && page < p.pages) atomicAdd(&p.out_refs[page], change);
     }
-    pg_copy_all(p.pool, p.moves, head.moves);
+    pg_copy_all<PG_UNROLL_PIECES>(p.pool, p.moves, head.moves);
 }
 
 // ---- compaction ------------------------------------------------------------------------------
@@ -322,7 +343,7 @@ __global__ void __launch_bounds__(PG_THREADS) pages_compact_kernel(const PgCompa
         const int32_t page = p.tables[e / p.width * p.table_stride + e % p.width];
         p.out_tables[e] = page >= 0 && page < p.pages ? p.page_map[page] : -1;
     }
-    pg_copy_all(p.pool, p.moves, p.head->moves);
+    pg_copy_all<PG_UNROLL_PAGES>(p.pool, p.moves, p.head->moves);
 }
 
 // ---- copying given pages, appending tokens -----------------------------------------------------
@@ -341,7 +362,7 @@ __global__ void __launch_bounds__(PG_THREADS) pages_copy_kernel(const PgCopyPara
     for (int64_t unit = blockIdx.x; unit < (int64_t)p.n * planes; unit += gridDim.x) {
         const int32_t src = p.src[unit / planes], dst = p.dst[unit / planes];
         if (src < 0 || src >= p.pages || dst < 0 || dst >= p.pages || src == dst) continue;
-        pg_copy(p.pool, src, dst, p.pool.page_size, (int32_t)(unit % planes));
+        pg_copy<PG_UNROLL_PAGES>(p.pool, src, dst, p.pool.page_size, (int32_t)(unit % planes));
     }
 }
 
