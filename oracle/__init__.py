@@ -22,6 +22,8 @@ philox    Philox4x32-10 and the stratified sample-index recipe.
 stages    the four stages (sample, threshold, filter, refine/fallback) run
           literally on a NumPy array.                     (Section 3)
 mc        Monte Carlo estimates of the two failure events.
+decode    the decoding operators (log probabilities, their gradient, attention
+          over a paged cache, its pages) in 64 bits, from their definitions.
 
 Parity pins: see each module's header.  For `plan.plan_guarded` in relaxed-recall
 mode (recall < 1) the paper prints no formula; that mode is pinned by Lemma 1's

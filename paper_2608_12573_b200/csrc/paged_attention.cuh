@@ -686,14 +686,24 @@ __global__ void __launch_bounds__(PJ_THREADS) paged_attention_join_kernel(const 
     const bool many = n > PJ_MANY;
     const int row = many ? (int)blockIdx.y : guess;
     if (row >= meta.heads) return;                                            // (many: the whole CTA)
+    auto add_all = [&](int32_t begin, int32_t step) {                         // eight parts' loads in flight at a time
+        constexpr int AT_ONCE = D == 256 ? 4 : 8;
+        for (int32_t i0 = begin; i0 < n; i0 += AT_ONCE * step) {
+            Part x[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u)
+                if (i0 + u * step < n) x[u] = read(i0 + u * step, row);
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u)
+                if (i0 + u * step < n) add(x[u]);
+        }
+    };
     if (!many) {
         add(own);                                                             // (two parts at least, so that they were read)
         add(next);
-#pragma unroll 4
-        for (int32_t i = 2; i < n; ++i) add(read(i, row));
+        add_all(2, 1);
     } else {
-#pragma unroll 4
-        for (int32_t i = warp; i < n; i += WARPS) add(read(i, row));
+        add_all(warp, WARPS);
     }
     if (many) {
 #pragma unroll

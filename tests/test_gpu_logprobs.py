@@ -131,6 +131,28 @@ def test_orders_that_refill_the_candidate_list(order, dtype):
             _near(r.lse.cpu(), np.full(rows, want["lse"]), 3e-5, 2.0 ** -22, "lse")
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows,masked", [(1, "none"), (2, "front"), (3, "middle"), (300, "none")])
+def test_long_rows_and_masked_stretches(dtype, rows, masked):
+    """Many batches per part (the bound is renewed on the way), and whole parts of a row without any token."""
+    vocab = 1_500_007 if rows < 100 else 200_003
+    x, _ = _logits(rows, vocab, dtype, rows)
+    if masked == "front":
+        x[:, :vocab // 2] = -float("inf")
+    elif masked == "middle":
+        x[:, vocab // 5:vocab - 100] = -float("inf")
+    for k in (3, 30, 100):
+        r = profk.logprobs(x, k=k)
+        for i in {0, rows - 1}:
+            host = x[i].float().cpu().numpy()
+            order = np.argsort(-host, kind="stable")[:k]              # (no zeros of either sign are near the largest)
+            np.testing.assert_array_equal(r.top_tokens[i].cpu().numpy(), order)
+            z = host[np.isfinite(host)].astype(np.float64)
+            lse = z.max() + np.log(np.exp(z - z.max()).sum())
+            _near(r.lse[i].cpu(), lse, 3e-5, 2.0 ** -22, "lse")
+            _near(r.top_logprobs[i].cpu(), host[order] - lse, 3e-5, 2.0 ** -22, "top_logprobs")
+
+
 def test_strides_offsets_and_leading_dimensions():
     base = torch.randn(6, 2100, device="cuda").to(torch.bfloat16)
     for off, vocab in ((0, 2000), (1, 2003), (3, 777), (7, 2093)):
