@@ -166,7 +166,9 @@ int lp_backward(const T* logits, int64_t rows, int64_t V, int64_t row_stride, do
     LpGradParams p{logits, grad, rows, row_stride, grad_row_stride, (uint32_t)V, grad_top ? (uint32_t)k : 0u, (uint32_t)chunks, chunk,
                    (float)(1.0 / temperature), tokens, lse, lse_rest, entropy, grad_logprob, grad_entropy, grad_lse, top_tokens, grad_top};
     Launch l((unsigned)(rows * chunks), LG_THREADS, 0, stream);
-    DEC_TRY(cudaLaunchKernelEx(&l.cfg, logprobs_grad_kernel<T>, p));
+    const bool shifted = (reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(grad)) % 16 != 0 ||
+                         (rows > 1 && (row_stride - grad_row_stride) * (int64_t)sizeof(T) % 16 != 0);
+    DEC_TRY(shifted ? cudaLaunchKernelEx(&l.cfg, logprobs_grad_kernel<T, true>, p) : cudaLaunchKernelEx(&l.cfg, logprobs_grad_kernel<T, false>, p));
     return PROFK_OK;
 }
 

@@ -161,7 +161,9 @@ __device__ __forceinline__ uint64_t lp_find_limit(const uint64_t* a, uint32_t n,
 // Lanes that share a slot: the coarser the slots the cheaper the bound, the finer the tighter (the k-th largest of n slots
 // has about n ln(n / (n - k)) elements above it).
 constexpr uint32_t LP_RANKED = LP_MAX_K + LP_SLACK;     // records that are ranked against one another
-constexpr uint32_t LP_FEW_K = 16;         // up to here 22 slots, one per lane of a warp, whose k-th largest is found by counting
+// Up to here 22 slots, one per lane of a warp, whose k-th largest is found by counting: 2368 rows of 131072 bf16, k = 8: 135 us,
+// with the bisection over all threads that larger k take 154; 4 rows, k = 16: 11.2 against 12.9.
+constexpr uint32_t LP_FEW_K = 16;
 __device__ __forceinline__ uint32_t lp_slot_lanes(uint32_t k) { return k <= LP_FEW_K ? 16 : k <= 64 ? 4 : 1; }
 
 // Both kinds of slots; the coarser ones serve alone for few alternatives (slot_lanes 16).
@@ -638,6 +640,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
             if (part == 0 && tid < mine.head) one(Logit<T>::to_float(mine.x[tid]));
             bar.empty_sync(turn);                                                 // the finishing warp is done with this place
             int32_t left = (int32_t)(mine.v1 - mine.v0);                          // vectors of the share from this batch on
+            uint32_t event = 2;                                                   // batches until the next event of the bound
             uint32_t v = mine.v0 + tid, batch = 0;                                // this thread's first vector of the batch
             const uint32_t raise_at = (2u << warp) + 1u;                          // the warp's turn to renew the bound
             float bound = NAN;                                                    // (none yet: nothing is noted)
@@ -731,14 +734,20 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
                             if (Logit<T>::value(tops[u]) >= bound) note(v + u * LP_STREAM);
                         __syncwarp();
                     }
-                    ++batch;
-                    if (batch > 1 && (batch & (batch - 1)) == 0) {
-                        lp_write_slot(seen, tid, slot_lanes, sh);
-                    } else if (batch == raise_at) {                               // one warp, a batch later: the slots are written
-                        const float higher = lp_slot_bound(*bound_at, p.k, slot_lanes, sh);
-                        if (lane == 0 && higher > *bound_at) *bound_at = higher;
+                    // After 2, 4, 8, ... batches the slots are written again, and a batch later one warp renews the bound.
+                    if (++batch == event) {
+                        if (batch & 1) {
+                            if (batch == raise_at) {
+                                const float higher = lp_slot_bound(*bound_at, p.k, slot_lanes, sh);
+                                if (lane == 0 && higher > *bound_at) *bound_at = higher;
+                            }
+                            event = 2 * (batch - 1);
+                        } else {
+                            lp_write_slot(seen, tid, slot_lanes, sh);
+                            event = batch + 1;
+                        }
+                        if (batch > 2) bound = *bound_at;
                     }
-                    if (batch > 2) bound = *bound_at;
                 }
                 stage = stage + 1 == LP_STAGES ? 0 : stage + 1;
                 v += LP_STEP;
@@ -810,7 +819,9 @@ __device__ __forceinline__ float lg_dense(float x, const LgRow& r, float scale) 
     return -q * fmaf(r.g_h, fmaxf(a, FAR_BELOW), r.whole);
 }
 
-template <typename T>
+// SHIFTED: the logits' rows start at other offsets within 16 bytes than the gradient's (a build of its own: its registers
+// would cost the other one an eighth of its threads, 2048 x 131072 bf16 175 us instead of 164).
+template <typename T, bool SHIFTED>
 __global__ void __launch_bounds__(LG_THREADS) logprobs_grad_kernel(const LpGradParams p) {
     constexpr int VEC = Logit<T>::VEC, U = LG_UNROLL;
     __shared__ float s_sum[LG_THREADS / 32];
@@ -845,32 +856,57 @@ __global__ void __launch_bounds__(LG_THREADS) logprobs_grad_kernel(const LpGradP
     const bool empty = r.lse == -INFINITY;                 // nothing but -inf in the row: no gradient
 
     const uint32_t e0 = chunk * p.chunk, e1 = min(p.V, e0 + p.chunk);
-    const uint32_t mis = (uint32_t)(reinterpret_cast<uintptr_t>(x + e0) & 15u);
-    const bool aligned = mis == (uint32_t)(reinterpret_cast<uintptr_t>(y + e0) & 15u);
+    // Vectors are those of the gradient's rows; where the logits' rows start at another offset, each is put together from two
+    // of theirs (2048 x 131072 bf16, logits one element off: 190 us, and 771 element by element).
+    const uint32_t mis = (uint32_t)(reinterpret_cast<uintptr_t>(y + e0) & 15u);
     auto scalar = [&](uint32_t i) { y[i] = Logit<T>::from_float(empty ? 0.f : lg_dense(Logit<T>::to_float(x[i]), r, scale)); };
-    if (aligned) {
-        const uint32_t head = min(e1, e0 + (mis ? (16u - mis) / (uint32_t)sizeof(T) : 0u));
-        const uint32_t nvec = (e1 - head) / VEC, tail = head + nvec * VEC;
-        if (e0 + tid < head) scalar(e0 + tid);
-        if (tail + tid < e1) scalar(tail + tid);
+    const uint32_t head = min(e1, e0 + (mis ? (16u - mis) / (uint32_t)sizeof(T) : 0u));
+    const uint32_t nvec = (e1 - head) / VEC, tail = head + nvec * VEC;
+    if (e0 + tid < head) scalar(e0 + tid);
+    if (tail + tid < e1) scalar(tail + tid);
+    auto put = [&](uint32_t v, const uint4& in) {
+        float f[VEC];
+        Logit<T>::unpack(in, f);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) f[j] = empty ? 0.f : lg_dense(f[j], r, scale);
+        st_stream_u4(y + head + (size_t)v * VEC, Logit<T>::pack(f));
+    };
+    if constexpr (!SHIFTED) {
         for (uint32_t v = tid; v < nvec; v += LG_THREADS * U) {
             uint4 in[U];
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (v + u * LG_THREADS < nvec) in[u] = ld_stream_u4(x + head + (size_t)(v + u * LG_THREADS) * VEC);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (v + u * LG_THREADS < nvec) {
-                    float f[VEC];
-                    Logit<T>::unpack(in[u], f);
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) f[j] = empty ? 0.f : lg_dense(f[j], r, scale);
-                    st_stream_u4(y + head + (size_t)(v + u * LG_THREADS) * VEC, Logit<T>::pack(f));
-                }
-            }
+            for (int u = 0; u < U; ++u)
+                if (v + u * LG_THREADS < nvec) put(v + u * LG_THREADS, in[u]);
         }
-    } else {                                               // gradient rows that start at another offset than the logits'
-        for (uint32_t i = e0 + tid; i < e1; i += LG_THREADS) scalar(i);
+    } else {
+        // (the 16 bytes in which an element of the row lies can be read whole)
+        const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(x + head) & ~(uintptr_t)15u);
+        const uint32_t shift = (uint32_t)(reinterpret_cast<uintptr_t>(x + head) & 15u);
+        const uint32_t words = shift >> 2, bits = (shift & 3u) * 8u, more = shift ? 1u : 0u;
+        for (uint32_t v = tid; v < nvec; v += LG_THREADS * U) {
+            uint4 lo[U], hi[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (v + u * LG_THREADS < nvec) {
+                    lo[u] = __ldg(from + v + u * LG_THREADS);
+                    hi[u] = __ldg(from + v + u * LG_THREADS + more);
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (v + u * LG_THREADS < nvec) {
+                    const uint32_t w[8] = {lo[u].x, lo[u].y, lo[u].z, lo[u].w, hi[u].x, hi[u].y, hi[u].z, hi[u].w};
+                    uint32_t a[6], b[5];
+#pragma unroll
+                    for (int j = 0; j < 6; ++j) a[j] = words & 2u ? w[j + 2] : w[j];
+#pragma unroll
+                    for (int j = 0; j < 5; ++j) b[j] = words & 1u ? a[j + 1] : a[j];
+                    put(v + u * LG_THREADS, make_uint4(__funnelshift_r(b[0], b[1], bits), __funnelshift_r(b[1], b[2], bits),
+                                                       __funnelshift_r(b[2], b[3], bits), __funnelshift_r(b[3], b[4], bits)));
+                }
+        }
     }
     if (empty || (!given && !p.g_top)) return;
     __syncthreads();

@@ -256,6 +256,21 @@ def test_gradient_of_strided_logits():
     _check_gradient(x, torch.arange(5, device="cuda"), up, None, 1.0, 0, "bf16")
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("offset", [1, 2, 3, 5, 7])
+def test_gradient_of_logits_at_another_alignment(dtype, offset):
+    """Every offset of the logits within 16 bytes against the same values in rows of their own: the same bits."""
+    for vocab, pad in ((5003, 9), (4096, 8), (2049, 11)):
+        base = torch.randn(7, vocab + pad, device="cuda").to(DTYPES[dtype])
+        x = base[:, offset:offset + vocab]
+        tokens = torch.arange(7, device="cuda")
+        r = profk.logprobs(x, tokens, k=3)
+        g = torch.randn(7, device="cuda")
+        args = dict(entropy=r.entropy, grad_entropy=g, top_tokens=r.top_tokens, grad_top=torch.randn(7, 3, device="cuda"))
+        got = profk.logprobs_backward(x, r.lse, tokens, g, **args)
+        assert torch.equal(got, profk.logprobs_backward(x.contiguous(), r.lse, tokens, g, **args))
+
+
 def test_gradient_against_differences():
     rows, vocab, k, t = 3, 41, 5, 0.8
     x, tokens, up, g_top = _gradient_case(rows, vocab, "f32", k, 21)
