@@ -255,9 +255,13 @@ bool pg_pool_ok(const profk_pool_t* pool) {
            pool->kv % 16 == 0 && pool->page % 16 == 0 && pool->head % 16 == 0 && pool->token % 16 == 0 &&
            pool->kv_heads * pool->page_size * (pool->row_bytes / 16) <= (1 << 30);
 }
-PgPool pg_pool(const profk_pool_t* pool, int64_t page_size) {
-    if (!pool) return PgPool{nullptr, 0, 0, (int32_t)page_size, 0, 0, 0, 0, 0, 0};
-    return PgPool{static_cast<char*>(pool->base), (int32_t)pool->layers, (int32_t)pool->kv_heads, (int32_t)pool->page_size, (int32_t)pool->row_bytes,
+// `unroll`: vectors per thread that are in flight at a time; a plane is copied by as few threads as hold it so.
+PgPool pg_pool(const profk_pool_t* pool, int64_t page_size, int unroll) {
+    if (!pool) return PgPool{nullptr, 0, 0, (int32_t)page_size, 0, PG_THREADS, 0, 0, 0, 0, 0};
+    const int64_t vectors = pool->kv_heads * pool->page_size * (pool->row_bytes / 16);
+    int team = 32;
+    while (team < PG_THREADS && team * unroll < vectors) team *= 2;
+    return PgPool{static_cast<char*>(pool->base), (int32_t)pool->layers, (int32_t)pool->kv_heads, (int32_t)pool->page_size, (int32_t)pool->row_bytes, team,
                   pool->layer, pool->kv, pool->page, pool->head, pool->token};
 }
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
@@ -356,7 +360,7 @@ int profk_pages_fork(const profk_pool_t* pool, const int32_t* tables, int64_t n_
     p.fresh_cap = (int32_t)fork_fresh(n, pages, page_size, grow);
     p.fresh = reinterpret_cast<int32_t*>(take((size_t)p.fresh_cap * 4));
     p.moves = reinterpret_cast<PgMove*>(take((size_t)n * sizeof(PgMove)));
-    p.pool = pg_pool(pool, page_size);
+    p.pool = pg_pool(pool, page_size, PG_UNROLL_PIECES);
     const unsigned copiers = (unsigned)std::min<int64_t>(sms, (pages + PG_PLAN_THREADS - 1) / PG_PLAN_THREADS);
     Launch plan(1 + copiers, PG_PLAN_THREADS, 0, stream);
     DEC_TRY(cudaLaunchKernelEx(&plan.cfg, pages_fork_plan_kernel, p));
@@ -365,9 +369,11 @@ int profk_pages_fork(const profk_pool_t* pool, const int32_t* tables, int64_t n_
     return PROFK_OK;
 }
 
+static size_t compact_workspace(int64_t pages) { return 256 + up((size_t)pages * 4) + up((size_t)(pages / 2 + 1) * sizeof(PgMove)); }
+
 int profk_pages_compact_workspace_bytes(int64_t pages, size_t* bytes) {
     if (!bytes || pages < 1 || pages > 0x7FFF0000ll) return PROFK_EINVAL;
-    *bytes = 256 + up((size_t)(pages / 2 + 1) * sizeof(PgMove));
+    *bytes = compact_workspace(pages);
     return PROFK_OK;
 }
 
@@ -377,12 +383,15 @@ int profk_pages_compact(const profk_pool_t* pool, const int32_t* tables, int64_t
     if (n < 0 || n > (1 << 24) || width < 1 || width > 0x7FFFFF00ll || table_stride < 0 || pages < 1 || pages > 0x7FFF0000ll || !refs || !out_refs ||
         refs == out_refs || !out_page_map || !out_live || (n > 0 && (!tables || !out_tables || tables == out_tables)) || !pg_pool_ok(pool))
         return PROFK_EINVAL;
-    if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < 256 + up((size_t)(pages / 2 + 1) * sizeof(PgMove))) return PROFK_EWORKSPACE;
+    if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < compact_workspace(pages)) return PROFK_EWORKSPACE;
     const int sms = sm_count();
     if (sms < 1) return PROFK_ECUDA;
+    char* w = static_cast<char*>(workspace) + 256;
+    const int64_t step = 4 * PG_PLAN_THREADS, steps = (pages + step - 1) / step, share = (steps + sms - 1) / sms * step;
     PgCompactParams p{tables, table_stride, refs, (int32_t)n, (int32_t)width, (int32_t)pages, out_tables, out_refs, out_page_map, out_live,
-                      static_cast<PgPlanHead*>(workspace), reinterpret_cast<PgMove*>(static_cast<char*>(workspace) + 256), pg_pool(pool, 1)};
-    Launch plan(1, PG_PLAN_THREADS, 0, stream);
+                      static_cast<PgPlanHead*>(workspace), reinterpret_cast<int32_t*>(w), (int32_t)share,
+                      reinterpret_cast<PgMove*>(w + up((size_t)pages * 4)), pg_pool(pool, 1, PG_UNROLL_PAGES)};
+    Launch plan((unsigned)((pages + share - 1) / share), PG_PLAN_THREADS, 0, stream);
     DEC_TRY(cudaLaunchKernelEx(&plan.cfg, pages_compact_plan_kernel, p));
     Launch work((unsigned)sms * PG_CTAS_PAGES, PG_THREADS, 0, stream);
     DEC_TRY(cudaLaunchKernelEx(&work.cfg, pages_compact_kernel, p));
@@ -394,7 +403,7 @@ int profk_pages_copy(const profk_pool_t* pool, int64_t pages, const int32_t* src
     if (n == 0) return PROFK_OK;
     const int sms = sm_count();
     if (sms < 1) return PROFK_ECUDA;
-    PgCopyParams p{src, dst, (int32_t)n, (int32_t)pages, pg_pool(pool, pool->page_size)};
+    PgCopyParams p{src, dst, (int32_t)n, (int32_t)pages, pg_pool(pool, pool->page_size, PG_UNROLL_PAGES)};
     Launch l((unsigned)std::min<int64_t>((int64_t)sms * PG_CTAS_PAGES, n * 2 * pool->layers), PG_THREADS, 0, stream);
     DEC_TRY(cudaLaunchKernelEx(&l.cfg, pages_copy_kernel, p));
     return PROFK_OK;

@@ -22,6 +22,7 @@ struct PgPool {
     char* base;                           // null: no pool, tables and counts only
     int32_t layers, kv_heads, page_size;
     int32_t row_bytes;                    // of one token and head
+    int32_t team;                         // threads that copy one plane of a page (a power of two, 32 .. PG_THREADS)
     int64_t layer, kv, page, head, token;
 };
 
@@ -184,9 +185,11 @@ __global__ void __launch_bounds__(PG_PLAN_THREADS) pages_fork_plan_kernel(const 
     }
 }
 
-// One page of one layer's keys or values, by the whole CTA: `tokens` tokens of every head.
+// One page of one layer's keys or values: `tokens` tokens of every head, by `pool.team` threads.  A whole CTA for each would
+// idle on small ones (20,000 planes of 1.5 KB, 32 MB: 73 us with the plan, a warp for each 28; 160,000 of 4 KB: 310 us, 115).
 template <int PG_UNROLL>
 __device__ __forceinline__ void pg_copy(const PgPool& pool, int32_t src, int32_t dst, int32_t tokens, int32_t plane) {
+    const uint32_t team = (uint32_t)pool.team, rank = threadIdx.x & (team - 1);
     char* base = pool.base + (plane >> 1) * pool.layer + (plane & 1) * pool.kv;
     const char* from = base + src * pool.page;
     char* to = base + dst * pool.page;
@@ -205,12 +208,12 @@ __device__ __forceinline__ void pg_copy(const PgPool& pool, int32_t src, int32_t
         const uint32_t r = i / run, o = r / runs;
         return (int64_t)o * outer_stride + (int64_t)(r - o * runs) * run_stride + (int64_t)(i - r * run) * 16;
     };
-    for (uint32_t i0 = threadIdx.x; i0 < n; i0 += PG_THREADS * PG_UNROLL) {
+    for (uint32_t i0 = rank; i0 < n; i0 += team * PG_UNROLL) {
         uint4 x[PG_UNROLL];
         int64_t at[PG_UNROLL];
 #pragma unroll
         for (int u = 0; u < PG_UNROLL; ++u) {
-            const uint32_t i = i0 + u * PG_THREADS;
+            const uint32_t i = i0 + u * team;
             if (i < n) {
                 at[u] = offset(i);
                 x[u] = *reinterpret_cast<const uint4*>(from + at[u]);
@@ -218,16 +221,20 @@ __device__ __forceinline__ void pg_copy(const PgPool& pool, int32_t src, int32_t
         }
 #pragma unroll
         for (int u = 0; u < PG_UNROLL; ++u)
-            if (i0 + u * PG_THREADS < n) *reinterpret_cast<uint4*>(to + at[u]) = x[u];
+            if (i0 + u * team < n) *reinterpret_cast<uint4*>(to + at[u]) = x[u];
     }
 }
+
+// The thread's team among all teams of the grid, and their number.
+__device__ __forceinline__ int64_t pg_team(const PgPool& pool) { return ((int64_t)blockIdx.x * PG_THREADS + threadIdx.x) / pool.team; }
+__device__ __forceinline__ int64_t pg_teams(const PgPool& pool) { return (int64_t)gridDim.x * (PG_THREADS / pool.team); }
 
 // The copies of a plan; no page is both read and written by them.
 template <int PG_UNROLL>
 __device__ __forceinline__ void pg_copy_all(const PgPool& pool, const PgMove* moves, int32_t n) {
     if (!pool.base) return;
     const int32_t planes = 2 * pool.layers;
-    for (int64_t unit = blockIdx.x; unit < (int64_t)n * planes; unit += gridDim.x) {
+    for (int64_t unit = pg_team(pool); unit < (int64_t)n * planes; unit += pg_teams(pool)) {
         const PgMove m = moves[unit / planes];
         pg_copy<PG_UNROLL>(pool, m.src, m.dst, m.tokens, (int32_t)(unit % planes));
     }
@@ -273,6 +280,8 @@ __global__ void __launch_bounds__(PG_THREADS) pages_fork_kernel(const PgForkPara
 
 // ---- compaction ------------------------------------------------------------------------------
 
+constexpr int32_t PG_FREE = -1, PG_STAYS = -2;
+
 struct PgCompactParams {
     const int32_t* tables;
     int64_t table_stride;
@@ -283,53 +292,66 @@ struct PgCompactParams {
     int32_t* page_map;
     int32_t* out_live;
     PgPlanHead* head;
+    int32_t* to;                          // pages: PG_FREE, PG_STAYS, or the number of the move that takes the page
+    int32_t share;                        // pages that a planning CTA settles
     PgMove* moves;                        // pages / 2
     PgPool pool;
 };
 
+// Live pages among [from, to), block-wide.
+__device__ __forceinline__ uint32_t pg_live(const int32_t* refs, int64_t from, int64_t to, uint32_t* warp_sums) {
+    uint32_t mine = 0, sum = 0;
+#pragma unroll 8
+    for (int64_t i = from + threadIdx.x; i < to; i += PG_PLAN_THREADS) mine += refs[i] > 0;
+    pg_scan(mine, warp_sums, &sum);
+    return sum;
+}
+
+// Live pages behind the first `live` go to the free ones among them, both in ascending order.  Every CTA settles a share of
+// the pages and counts for itself what lies before it: reading all counts again (4 bytes per page, from L2) costs less than a
+// walk by one CTA with a prefix sum per step (100,000 pages, half of them free,
+// with the copies: 52 us, with the walk 140), and nothing waits for another CTA.
 __global__ void __launch_bounds__(PG_PLAN_THREADS) pages_compact_plan_kernel(const PgCompactParams p) {
     __shared__ uint32_t warp_sums[32];
     const int tid = threadIdx.x;
     pdl_wait();
     pdl_launch_dependents();
-    uint32_t mine = 0, live = 0;
-    for (int32_t i = tid; i < p.pages; i += PG_PLAN_THREADS) mine += p.refs[i] > 0;
-    pg_scan(mine, warp_sums, &live);
-    // live pages behind the first `live` go to the free ones among them, both in ascending order
-    uint32_t holes = 0, movers = 0;
-    for (int32_t c0 = 0; c0 < p.pages; c0 += 4 * PG_PLAN_THREADS) {
-        const int32_t at = c0 + 4 * tid;
+    const int64_t from = (int64_t)blockIdx.x * p.share, to = min((int64_t)p.pages, from + p.share);
+    const uint32_t before = pg_live(p.refs, 0, from, warp_sums);
+    const uint32_t live = before + pg_live(p.refs, from, p.pages, warp_sums);
+    uint32_t holes = from <= live ? (uint32_t)from - before : 0;               // (behind `live` there are none to number)
+    uint32_t movers = from > live ? pg_live(p.refs, live, from, warp_sums) : 0;
+    for (int64_t c0 = from; c0 < to; c0 += 4 * PG_PLAN_THREADS) {
+        const int64_t at = c0 + 4 * tid;
         uint32_t n_holes = 0, n_movers = 0, sum_holes = 0, sum_movers = 0;
         int32_t ref[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            ref[j] = at + j < p.pages ? p.refs[at + j] : 0;
-            const bool held = ref[j] > 0, low = at + j < (int32_t)live;
-            n_holes += low && !held;
+            ref[j] = at + j < to ? p.refs[at + j] : 0;
+            const bool held = ref[j] > 0, low = at + j < live;
+            n_holes += low && !held && at + j < to;
             n_movers += !low && held;
-            if (at + j < p.pages) {
-                p.out_refs[at + j] = low && held ? ref[j] : 0;
-                p.page_map[at + j] = held ? at + j : -1;
-            }
         }
         uint32_t hole = holes + pg_scan(n_holes, warp_sums, &sum_holes), mover = movers + pg_scan(n_movers, warp_sums, &sum_movers);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const bool held = ref[j] > 0, low = at + j < (int32_t)live;
-            if (low && !held) p.moves[hole++].dst = at + j;
-            if (!low && held) p.moves[mover++].src = at + j;
+            if (at + j >= to) break;
+            const int32_t page = (int32_t)(at + j);
+            const bool held = ref[j] > 0, low = at + j < live;
+            p.out_refs[page] = low && held ? ref[j] : 0;
+            p.page_map[page] = low && held ? page : -1;
+            p.to[page] = !held ? PG_FREE : low ? PG_STAYS : (int32_t)mover;
+            if (low && !held) p.moves[hole++].dst = page;
+            if (!low && held) {
+                p.moves[mover].src = page;
+                p.moves[mover++].tokens = p.pool.page_size;
+            }
         }
         holes += sum_holes;
         movers += sum_movers;
     }
-    __syncthreads();
-    for (uint32_t i = tid; i < movers; i += PG_PLAN_THREADS) {
-        const int32_t src = p.moves[i].src, dst = p.moves[i].dst;
-        p.moves[i].tokens = p.pool.page_size;
-        p.page_map[src] = dst;
-        p.out_refs[dst] = p.refs[src];
-    }
-    if (tid == 0) {
+    if (tid == 0 && to == p.pages) {
+        // as many movers as holes: the live pages that do not lie among the first `live`
         *p.head = PgPlanHead{(int32_t)movers, (int32_t)live, 0, 0};
         *p.out_live = (int32_t)live;
     }
@@ -338,12 +360,19 @@ __global__ void __launch_bounds__(PG_PLAN_THREADS) pages_compact_plan_kernel(con
 __global__ void __launch_bounds__(PG_THREADS) pages_compact_kernel(const PgCompactParams p) {
     pdl_wait();
     pdl_launch_dependents();
+    const int32_t moves = p.head->moves;
     const int64_t step = (int64_t)gridDim.x * PG_THREADS, me = (int64_t)blockIdx.x * PG_THREADS + threadIdx.x;
+    for (int64_t i = me; i < moves; i += step) {
+        const PgMove m = p.moves[i];
+        p.page_map[m.src] = m.dst;
+        p.out_refs[m.dst] = p.refs[m.src];
+    }
     for (int64_t e = me; e < (int64_t)p.n * p.width; e += step) {
         const int32_t page = p.tables[e / p.width * p.table_stride + e % p.width];
-        p.out_tables[e] = page >= 0 && page < p.pages ? p.page_map[page] : -1;
+        const int32_t to = page >= 0 && page < p.pages ? p.to[page] : PG_FREE;
+        p.out_tables[e] = to >= 0 ? p.moves[to].dst : to == PG_STAYS ? page : -1;
     }
-    pg_copy_all<PG_UNROLL_PAGES>(p.pool, p.moves, p.head->moves);
+    pg_copy_all<PG_UNROLL_PAGES>(p.pool, p.moves, moves);
 }
 
 // ---- copying given pages, appending tokens -----------------------------------------------------
@@ -359,7 +388,7 @@ __global__ void __launch_bounds__(PG_THREADS) pages_copy_kernel(const PgCopyPara
     pdl_wait();
     pdl_launch_dependents();
     const int32_t planes = 2 * p.pool.layers;
-    for (int64_t unit = blockIdx.x; unit < (int64_t)p.n * planes; unit += gridDim.x) {
+    for (int64_t unit = pg_team(p.pool); unit < (int64_t)p.n * planes; unit += pg_teams(p.pool)) {
         const int32_t src = p.src[unit / planes], dst = p.dst[unit / planes];
         if (src < 0 || src >= p.pages || dst < 0 || dst >= p.pages || src == dst) continue;
         pg_copy<PG_UNROLL_PAGES>(p.pool, src, dst, p.pool.page_size, (int32_t)(unit % planes));

@@ -227,3 +227,32 @@ def test_refusals():
             pytest.fail(f"call {i} was not refused")
     torch.cuda.synchronize()
     np.testing.assert_array_equal(_host(pool), bits)
+
+
+@pytest.mark.parametrize("page,kv_heads,dim", [(1, 1, 8), (8, 1, 96), (16, 2, 64), (16, 8, 128), (64, 4, 64)])
+def test_pages_of_every_size_move_whole(page, kv_heads, dim):
+    """From one vector per page and layer to thousands: the threads that share a page's copy differ."""
+    rng = np.random.default_rng(page * dim)
+    pages, live = 300, 140
+    refs = np.zeros(pages, dtype=np.int32)
+    refs[rng.permutation(pages)[:live]] = 1
+    tables = rng.integers(0, pages, (3, 30)).astype(np.int32)
+    pool = _pool(3, pages, kv_heads, page, dim, 9)
+    before = _host(pool)
+    got = profk.pages_compact(pool, _int32(tables), _int32(refs))
+    want = oracle.compact(before, tables, refs)
+    np.testing.assert_array_equal(got.tables.cpu().numpy(), want[0])
+    np.testing.assert_array_equal(_host(pool), before)
+
+
+@pytest.mark.parametrize("pages", [4096, 4097, 200_000, 700_000])
+@pytest.mark.parametrize("held", [0.02, 0.5, 0.98])
+def test_compact_plans_in_shares(pages, held):
+    rng = np.random.default_rng(pages)
+    refs = (rng.random(pages) < held).astype(np.int32) * rng.integers(1, 5, pages).astype(np.int32)
+    tables = rng.integers(-1, pages + 1, (7, 500)).astype(np.int32)
+    got = profk.pages_compact(None, _int32(tables), _int32(refs))
+    want = oracle.compact(np.zeros((1, 2, pages, 1, 1, 1), dtype=np.uint8), tables, refs)
+    for g, w in zip(got[:3], want[:3]):
+        np.testing.assert_array_equal(g.cpu().numpy(), w)
+    assert int(got.live) == want[3]
