@@ -46,8 +46,9 @@ constexpr int LP_THREADS = LP_TEAMS * LP_TEAM;
 constexpr int LP_UNROLL = 4;              // 16-byte vectors per thread and batch
 constexpr int LP_STAGES = 3;              // batches in flight or in hand per thread
 constexpr uint32_t LP_STEP = LP_STREAM * LP_UNROLL;     // vectors per batch
-constexpr uint32_t LP_NOTES = 2048;       // vectors the list holds
-constexpr uint32_t LP_FIN = 512;          // elements the finishing warp holds; more than half of them it cuts back to the k best
+constexpr uint32_t LP_NOTES = 2560;       // vectors the list holds (k = 128 of 131072 fp32: 1570 on average, 2420 at most in 1184 rows)
+constexpr uint32_t LP_READ = 128;         // ... of which the finishing warp reads so many at a time
+constexpr uint32_t LP_FIN = 512;          // elements the finishing warp holds; more than half of them it cuts back
 constexpr uint32_t LP_MAX_K = 128;        // most alternatives
 constexpr uint32_t LP_MAX_PARTS = 16;     // most teams that share a row
 constexpr uint32_t LP_SLACK = 32;         // a part of a row hands on up to k + LP_SLACK records
@@ -78,8 +79,11 @@ __device__ __forceinline__ LpStats lp_join(const LpStats& a, const LpStats& b, f
 }
 
 // What the streaming warps leave of a row for the finishing one; two of them, used in turn.
+// Bits that the number of any of the row's vectors takes.
+template <typename T> __device__ __forceinline__ uint32_t lp_note_bits(uint32_t V) { return 32 - __clz(V / Logit<T>::VEC | 1); }
+
 struct LpRow {
-    uint32_t note[LP_NOTES];              // numbers of vectors
+    uint32_t note[LP_NOTES];              // vectors: numbers in the low `lp_note_bits`, above them the head of the largest element's order key
     LpStats stats[LP_STREAM_WARPS];
     uint32_t count;
     float bound;                          // elements below it are no longer of interest
@@ -294,8 +298,8 @@ __device__ __forceinline__ uint32_t lp_fin_add(uint32_t n, bool has, float x, ui
     __syncwarp();
     return n + __popc(who);
 }
-// The elements of one vector per lane (`has`) that reach the bound; cuts back to the k best before the room runs out, and
-// then raises the bound above the worst of them where what follows has higher indices only (`ascending`).
+// The elements of one vector per lane (`has`) that reach the bound; cuts back to the k best and some before the room runs out,
+// and then raises the bound above the worst of them where what follows has higher indices only (`ascending`).
 template <typename T>
 __device__ __forceinline__ uint32_t lp_fin_vector(uint32_t n, bool has, const uint4& vec, uint32_t at, float& bound, bool ascending, uint32_t k, LpShared& sh) {
     has = has && Logit<T>::vec_max(vec) >= bound;
@@ -318,32 +322,70 @@ __device__ __forceinline__ uint32_t lp_fin_vector(uint32_t n, bool has, const ui
     n += __shfl_sync(FULL_MASK, incl, 31);
     __syncwarp();
     if (n > LP_FIN / 2) {
-        const uint64_t limit = lp_find_limit(sh.fin, n, k, k);
+        const uint64_t limit = lp_find_limit(sh.fin, n, k, LP_RANKED);
         n = lp_fin_drop(n, limit, sh);
         if (ascending) bound = __uint_as_float(bits32_from_key(~(uint32_t)(limit >> 32) + 1u));
     }
     return n;
 }
 
+// Drops the notes of vectors that cannot matter, most of them from the start of the row when the bound was low: the k-th largest
+// of the noted vectors' largest elements, rounded down to the bits that a note has of them, is a bound of its own.  Returns how many
+// remain.  (What is left out costs a read by latency each: k = 128 of 131072, 2368 rows bf16 329 -> 216 us, 1184 rows fp32
+// 371 -> 141; fewer notes than LP_READ are read at once, 1981 rows of 5946 bf16, k = 64: 48 us, thinned 56.)
+__device__ __forceinline__ uint32_t lp_fin_thin(uint32_t notes, uint32_t k, uint32_t bits, float& bound, LpRow& r) {
+    uint32_t top = 0;
+    for (uint32_t i = lane_id(); i < notes; i += 32) top = max(top, r.note[i] >> bits);
+    uint32_t lo = key_from_bits32(float_bits_exact(bound)) >> bits, hi = __reduce_max_sync(FULL_MASK, top) + 1u;
+    while (lo + 1 < hi) {                                                         // (the first `lo` is the bound of the slots)
+        const uint32_t mid = (lo + hi) >> 1;
+        uint32_t c = 0;
+#pragma unroll 4
+        for (uint32_t i = lane_id(); i < notes; i += 32) c += r.note[i] >> bits >= mid;
+        c = __reduce_add_sync(FULL_MASK, c);
+        if (c >= k) {
+            lo = mid;
+            if (c <= lp_enough(k)) break;
+        } else {
+            hi = mid;
+        }
+    }
+    bound = fmaxf(bound, __uint_as_float(bits32_from_key(lo << bits)));
+    uint32_t kept = 0;
+    for (uint32_t i0 = 0; i0 < notes; i0 += 32) {
+        const uint32_t i = i0 + lane_id();
+        const uint32_t w = i < notes ? r.note[i] : 0u;
+        const bool keep = i < notes && w >> bits >= lo;
+        const unsigned who = __ballot_sync(FULL_MASK, keep);
+        if (keep) r.note[kept + __popc(who & ((1u << lane_id()) - 1u))] = w;      // (at or before i0 + lane: read already)
+        kept += __popc(who);
+        __syncwarp();
+    }
+    return kept;
+}
+
 // The candidates of a row's share, at most `most` (>= k) of them, the k best of the row among them as far as they lie here.
 template <typename T>
-__device__ __forceinline__ uint32_t lp_fin_select(const LpShare<T> mine, uint32_t k, uint32_t most, bool first, bool last, uint32_t V, const LpRow& r, LpShared& sh) {
+__device__ __forceinline__ uint32_t lp_fin_select(const LpShare<T> mine, uint32_t k, uint32_t most, bool first, bool last, uint32_t V, LpRow& r, LpShared& sh) {
     constexpr int VEC = Logit<T>::VEC;
     const uint32_t lane = lane_id();
     uint32_t n = 0;
     float bound = r.bound;
-    const uint32_t notes = r.count, tail = mine.head + mine.nvec * VEC;
+    uint32_t notes = r.count;
+    const uint32_t bits = lp_note_bits<T>(V);
+    const uint32_t tail = mine.head + mine.nvec * VEC;
     const bool in_head = first && lane < mine.head, in_tail = last && tail + lane < V;
     const float hx = in_head ? Logit<T>::to_float(mine.x[lane]) : -INFINITY, tx = in_tail ? Logit<T>::to_float(mine.x[tail + lane]) : -INFINITY;
     n = lp_fin_add(n, hx >= bound, hx, lane, sh);
     if (notes <= LP_NOTES) {
-        for (uint32_t i0 = 0; i0 < notes; i0 += 128) {
+        if (notes > LP_READ && notes >= k) notes = lp_fin_thin(notes, k, bits, bound, r);
+        for (uint32_t i0 = 0; i0 < notes; i0 += LP_READ) {
             uint32_t w[4];
             uint4 vec[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const uint32_t i = i0 + u * 32 + lane;
-                w[u] = i < notes ? r.note[i] : 0u;
+                w[u] = i < notes ? r.note[i] & ((1u << bits) - 1u) : 0u;
                 if (i < notes) vec[u] = *reinterpret_cast<const uint4*>(mine.vec(w[u]));
             }
 #pragma unroll
@@ -532,6 +574,8 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
                     const uint32_t places = max(found, p.k);
                     if (places <= 32) rank_and_write(std::integral_constant<int, 1>{});
                     else if (places <= 64) rank_and_write(std::integral_constant<int, 2>{});
+                    else if (places <= 96) rank_and_write(std::integral_constant<int, 3>{});
+                    else if (places <= 128) rank_and_write(std::integral_constant<int, 4>{});
                     else rank_and_write(std::integral_constant<int, LP_RANKED / 32>{});
                 }
             }
@@ -644,9 +688,9 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
             uint32_t v = mine.v0 + tid, batch = 0;                                // this thread's first vector of the batch
             const uint32_t raise_at = (2u << warp) + 1u;                          // the warp's turn to renew the bound
             float bound = NAN;                                                    // (none yet: nothing is noted)
-            auto note = [&](uint32_t w) {
-                const uint32_t pos = atomicAdd(&r.count, 1u);
-                if (pos < LP_NOTES) r.note[pos] = w;
+            auto note = [&](uint32_t w, float top) {
+                const uint32_t pos = atomicAdd(&r.count, 1u), bits = lp_note_bits<T>(p.V);
+                if (pos < LP_NOTES) r.note[pos] = key_from_bits32(float_bits_exact(top)) >> bits << bits | w;
             };
             do {                                                                  // (an empty share still takes its batch)
                 load_batch();
@@ -675,7 +719,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
                     if (__any_sync(FULL_MASK, top >= bound)) {
 #pragma unroll
                         for (int u = 0; u < U; ++u)
-                            if (Logit<T>::value(tops[u]) >= bound) note(v + u * LP_STREAM);
+                            if (Logit<T>::value(tops[u]) >= bound) note(v + u * LP_STREAM, Logit<T>::value(tops[u]));
                         __syncwarp();
                     }
                 }
@@ -731,7 +775,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
                         if (tid == 0) *bound_at = bound;                          // (nobody else writes it before two more batches)
 #pragma unroll
                         for (int u = 0; u < U; ++u)
-                            if (Logit<T>::value(tops[u]) >= bound) note(v + u * LP_STREAM);
+                            if (Logit<T>::value(tops[u]) >= bound) note(v + u * LP_STREAM, Logit<T>::value(tops[u]));
                         __syncwarp();
                     }
                     // After 2, 4, 8, ... batches the slots are written again, and a batch later one warp renews the bound.
@@ -746,8 +790,8 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
                             lp_write_slot(seen, tid, slot_lanes, sh);
                             event = batch + 1;
                         }
-                        if (batch > 2) bound = *bound_at;
                     }
+                    if (batch > 2) bound = *bound_at;
                 }
                 stage = stage + 1 == LP_STAGES ? 0 : stage + 1;
                 v += LP_STEP;

@@ -153,6 +153,24 @@ def test_long_rows_and_masked_stretches(dtype, rows, masked):
             _near(r.top_logprobs[i].cpu(), host[order] - lse, 3e-5, 2.0 ** -22, "top_logprobs")
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows,vocab,k,levels", [(2, 131072, 128, 0), (300, 131075, 128, 0), (300, 40001, 100, 0), (2, 200001, 17, 0), (300, 60001, 128, 500), (2, 60001, 64, 40)])
+def test_many_alternatives_of_long_rows(dtype, rows, vocab, k, levels):
+    """More noted vectors than are read at a time; with `levels`, values that many elements share (lowest index first)."""
+    x, _ = _logits(rows, vocab, dtype, vocab + k)
+    if levels:
+        x = (torch.round(x.float() * (levels / 30)) * (30 / levels) + 0.0).to(x.dtype)
+    x[0, 100:vocab - 100] = -float("inf")
+    r = profk.logprobs(x, k=k)
+    torch.cuda.synchronize()
+    for i in sorted({0, 1, rows // 2, rows - 1}):
+        host = x[i].double().cpu().numpy()
+        order = np.argsort(-host, kind="stable")[:k]
+        np.testing.assert_array_equal(r.top_tokens[i].cpu().numpy(), order)
+        lse = host.max() + np.log(np.exp(host - host.max()).sum())
+        _near(r.top_logprobs[i].cpu(), host[order] - lse, 3e-5, 2.0 ** -22, "top_logprobs")
+
+
 def test_strides_offsets_and_leading_dimensions():
     base = torch.randn(6, 2100, device="cuda").to(torch.bfloat16)
     for off, vocab in ((0, 2000), (1, 2003), (3, 777), (7, 2093)):
