@@ -19,7 +19,7 @@
 // shared memory; the k-th largest slot is a bound that k elements of the row reach, so that only vectors whose maximum
 // reaches the bound can matter.  Their numbers are noted in a list, a few times k of them for a row in any ordinary order;
 // the bound is renewed whenever the number of batches has doubled, without a barrier: a stale slot only makes it lower.
-// At the end of the row the noted vectors are read once more and their elements above the last bound are ordered.  Where
+// At the end of the row those that still matter are read once more and their elements above the last bound are ordered.  Where
 // the list overflows all the same (ascending order, a flood of equal values) the whole row is read once more instead.
 //
 // A CTA holds the whole SM and is two teams of twelve warps, each with rows of its own (or a part of a row each).  Eleven
