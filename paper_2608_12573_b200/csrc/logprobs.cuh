@@ -449,6 +449,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
     const int32_t rows = (int32_t)p.rows;
     const int32_t first = parts > 1 ? (int32_t)(blockIdx.x / shares) : (int32_t)(blockIdx.x * LP_TEAMS + team);
     const int32_t stride = parts > 1 ? (int32_t)(gridDim.x / shares) : (int32_t)(gridDim.x * LP_TEAMS);
+    auto row_after = [&](int32_t row) { return row > rows - stride ? rows : row + stride; };     // (rows may be 2^31 - 1: row + stride would wrap)
     const float c = p.scale * LOG2E;
     pdl_wait();
     pdl_launch_dependents();
@@ -464,7 +465,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
         };
         if (first < rows) make_empty(0);
         if (stride < rows - first) make_empty(1);
-        for (int32_t row = first; row < rows; row += stride) {
+        for (int32_t row = first; row < rows; row = row_after(row)) {
             const int64_t token = p.tokens ? p.tokens[row] : -1;
             float token_x = 0.f;
             if (token >= 0 && token < (int64_t)p.V) token_x = Logit<T>::to_float((reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.row_stride)[token]);
@@ -615,7 +616,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
                 load_at += LP_STEP * VEC;
                 load_left -= (int32_t)LP_STEP;
                 if (load_left <= 0) {
-                    load_row = load_row > rows - stride ? rows : load_row + stride;
+                    load_row = row_after(load_row);
                     load_from();
                 }
             }
@@ -641,7 +642,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
         };
 
         int stage = 0;
-        for (int32_t row = first; row < rows; row += stride) {
+        for (int32_t row = first; row < rows; row = row_after(row)) {
             LpShare<T> mine;
             mine.set(p, row, part);
             LpRow& r = sh.row[turn];
