@@ -63,6 +63,19 @@ struct PaParams {
     PaMeta* meta;                                       // one per CTA
 };
 
+// Weights are e^(score - reference) 2^SHIFT, and the reference may lag the largest score so far by up to 2^LAG.  fp16 ends at
+// 2^-24: the pair of numbers that a weight is split into for the second product is off by up to 2^-25 of it, so that the
+// weights are lifted as far as 65504 allows, and each is off by 2^-39 of the largest at most, or by 2^-22 of itself (unlifted
+// and with a lag of 2^8, tokens 2^-24.4 below a sink counted a third too much and those from 2^-25 on not at all).  bf16 has
+// fp32's range.
+template <typename T> struct PaWeights { static constexpr float LAG = 8.f, SHIFT = 0.f, UNIT = 1.f; };
+template <> struct PaWeights<__half> { static constexpr float LAG = 1.f, SHIFT = 14.f, UNIT = 16384.f; };      // UNIT = 2^SHIFT
+// lse of a reference and a sum of weights.
+template <typename T>
+__device__ __forceinline__ float pa_lse(float m, float sum, float scale) {
+    return sum == 0.f ? -INFINITY : fmaf(m, scale, logf(sum * (1.f / PaWeights<T>::UNIT)));
+}
+
 template <typename T>
 __device__ __forceinline__ void pa_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
 template <>
@@ -178,7 +191,7 @@ template <typename T, int D, int N8>
 __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel(const PaParams p) {
     using Shape = PaShape<D>;
     constexpr int STAGES = Shape::STAGES, CH = D / 8, KSTEPS = D / 16, MT = D / 16, WARPS = Shape::WARPS, THREADS = Shape::THREADS,
-                  SUBS = Shape::SUBS, TILE = Shape::TILE;
+                  SUBS = Shape::SUBS, TILE = Shape::TILE, AT_ONCE = D > 64 && N8 == 2 ? 2 : 4;
     constexpr int ROWS_PER_LOAD = 32 / CH;                                   // token rows that one warp-wide copy covers
     constexpr int LOADS = PA_SUB / ROWS_PER_LOAD;
     extern __shared__ __align__(512) unsigned char pa_dyn[];           // (512: the longest row; see the exclusive ors below)
@@ -377,9 +390,11 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
     // where the lane's rows of the matrices lie in a stage: tokens lane & 15 of the keys, (lane & 7) + 8 (lane >> 4) of the values
     const uint32_t k_lane = (lane & 15) * (D * 2) + (((lane >> 4) ^ (lane & 7)) << 4);
     const uint32_t v_lane = ((lane & 7) + ((lane >> 4) << 3)) * (D * 2) + ((((lane >> 3) & 1) ^ (lane & 7)) << 4);
-    const float far = 8.f / c;                                                // the reference of the exponents lags the maximum by up to 2^8
+    const float far = PaWeights<T>::LAG / c;                                  // how far the reference of the exponents may lag the maximum
     uint32_t qf[N8][KSTEPS][2];
-    float o[MT][N8][4], m[N8][2], l[N8][2];                                   // of heads 8 n + 2 quad and + 1
+    // of heads 8 n + 2 quad and + 1.  The sums of weights are compensated: a lane that holds a sink would round thousands of
+    // small weights to its sum's 2^-24 (14000 tokens 2^-25 below: lse off by 4e-5)
+    float o[MT][N8][4], m[N8][2], l[N8][2], l_over[N8][2];
     bool fresh = true, whole = work.tile == 0;                                // a new stream begins / it began in this share
     int stage = 0;
     if (!whole) share.first = work.heads(p);
@@ -392,7 +407,7 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
 #pragma unroll
             for (int n = 0; n < N8; ++n) {
                 m[n][0] = m[n][1] = LOWEST;
-                l[n][0] = l[n][1] = 0.f;
+                l[n][0] = l[n][1] = l_over[n][0] = l_over[n][1] = 0.f;
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.f;
 #pragma unroll
@@ -461,6 +476,7 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
                     const float to = fmaxf(m[n][h], top[n][h]), f = exp2_approx((m[n][h] - to) * c);
                     m[n][h] = to;
                     l[n][h] *= f;
+                    l_over[n][h] *= f;
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) { o[mt][n][h] *= f; o[mt][n][2 + h] *= f; }
                 }
@@ -474,9 +490,13 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
             for (int n = 0; n < N8; ++n) {
                 float e[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = exp2_approx((s[sub][n][i] - m[n][i & 1]) * c);
+                for (int i = 0; i < 4; ++i) e[i] = exp2_approx(fmaf(s[sub][n][i] - m[n][i & 1], c, PaWeights<T>::SHIFT));
 #pragma unroll
-                for (int h = 0; h < 2; ++h) l[n][h] += e[h] + e[2 + h];
+                for (int h = 0; h < 2; ++h) {
+                    const float add = e[h] + e[2 + h] - l_over[n][h], to = l[n][h] + add;
+                    l_over[n][h] = (to - l[n][h]) - add;
+                    l[n][h] = to;
+                }
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const uint32_t w = pa_pack<T>(e[2 * i], e[2 * i + 1]);
@@ -485,21 +505,31 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
                     lo[sub][n][i] = pa_transpose(pa_pack<T>(e[2 * i] - r.x, e[2 * i + 1] - r.y));
                 }
             }
+        // A tile's products are summed by themselves and then added: the matrix unit cuts off what lies below its accumulator's
+        // last bit, which beside a sink's value would be a part of every further tile (14000 tokens: 2^-13 of the output).
 #pragma unroll
-        for (int sub = 0; sub < SUBS; ++sub)
+        for (int m0 = 0; m0 < MT; m0 += AT_ONCE) {
+            float acc[AT_ONCE][N8][4] = {};
 #pragma unroll
-            for (int m0 = 0; m0 < MT; m0 += 4) {
-                uint32_t a[4][4];
+            for (int sub = 0; sub < SUBS; ++sub) {
+                uint32_t a[AT_ONCE][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) pa_ldmatrix_trans(a[i], (vb + sub * Shape::SUB_BYTES + v_lane) ^ ((m0 + i) << 5));
+                for (int i = 0; i < AT_ONCE; ++i) pa_ldmatrix_trans(a[i], (vb + sub * Shape::SUB_BYTES + v_lane) ^ ((m0 + i) << 5));
 #pragma unroll
                 for (int n = 0; n < N8; ++n) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) pa_mma<T>(o[m0 + i][n], a[i], hi[sub][n][0], hi[sub][n][1]);
+                    for (int i = 0; i < AT_ONCE; ++i) pa_mma<T>(acc[i][n], a[i], hi[sub][n][0], hi[sub][n][1]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) pa_mma<T>(o[m0 + i][n], a[i], lo[sub][n][0], lo[sub][n][1]);
+                    for (int i = 0; i < AT_ONCE; ++i) pa_mma<T>(acc[i][n], a[i], lo[sub][n][0], lo[sub][n][1]);
                 }
             }
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+                for (int n = 0; n < N8; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[m0 + i][n][j] += acc[i][n][j];
+        }
         __syncwarp();                                                         // the stage may be filled again
         stage = stage + 1 == STAGES ? 0 : stage + 1;
 
@@ -521,7 +551,7 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
                     inv[h] = sum == 0.f ? 0.f : 1.f / sum;                    // nothing held a token: zeros
                     const int row = n * 8 + quad * 2 + h;
                     if (g == 0 && row < rows) {
-                        if (final) p.lse[out_row + row] = sum == 0.f ? -INFINITY : fmaf(m[n][h], p.scale, logf(sum));
+                        if (final) p.lse[out_row + row] = pa_lse<T>(m[n][h], sum, p.scale);
                         else { s_max[warp][whole ? 1 : 0][row] = m[n][h]; s_sum[warp][whole ? 1 : 0][row] = sum; }
                     }
                 }
@@ -632,7 +662,7 @@ __global__ void __launch_bounds__(PaShape<D>::THREADS, 1) paged_attention_kernel
                 const uint2 w2 = make_uint2(pa_pack<T>(acc.x * inv, acc.y * inv), pa_pack<T>(acc.z * inv, acc.w * inv));
                 *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.out) + out_row * p.dim + at) = w2;
             }
-            if (at == 0) p.lse[out_row] = sum == 0.f ? -INFINITY : fmaf(top, p.scale, logf(sum));
+            if (at == 0) p.lse[out_row] = pa_lse<T>(top, sum, p.scale);
         } else {
             float* part = slots + (2 * WARPS + (k.inside ? 1 : 0)) * Shape::SLOT;
             *reinterpret_cast<float4*>(part + row * D + at) = acc;
@@ -736,7 +766,7 @@ __global__ void __launch_bounds__(PJ_THREADS) paged_attention_join_kernel(const 
 #pragma unroll
     for (int j = 0; j < COLS; ++j)
         if (j * 32 + lane < p.dim) out[j * 32 + lane] = Logit<T>::from_float(acc[j] * inv);
-    if (lane == 0) p.lse[out_row] = sum == 0.f ? -INFINITY : fmaf(top, p.scale, logf(sum));
+    if (lane == 0) p.lse[out_row] = pa_lse<T>(top, sum, p.scale);
 }
 
 }  // namespace profk
