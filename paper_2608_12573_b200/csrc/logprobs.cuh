@@ -878,8 +878,8 @@ __global__ void __launch_bounds__(LG_THREADS) logprobs_grad_kernel(const LpGradP
     const T* x = reinterpret_cast<const T*>(p.logits) + row * p.row_stride;
     T* y = reinterpret_cast<T*>(p.grad) + row * p.grad_stride;
     const int64_t token = p.tokens ? p.tokens[row] : -1;
-    const bool given = token >= 0 && token < (int64_t)p.V;
-    const float g_lp = p.g_logprob && given ? p.g_logprob[row] : 0.f;
+    const bool given = p.g_logprob && token >= 0 && token < (int64_t)p.V;      // there is something to add to the token's entry
+    const float g_lp = given ? p.g_logprob[row] : 0.f;
     const float scale = p.scale;
     float g_sum = 0.f;
     if (p.g_top) {

@@ -1,4 +1,6 @@
 """Log probabilities and their gradient where sizes, values and buffers reach the limits of what is accepted."""
+import ctypes
+
 import pytest
 import torch
 
@@ -28,3 +30,34 @@ def test_as_many_rows_as_are_accepted():
     lse = profk.logprobs(x, entropy=False).lse
     for r in range(0, rows, step):
         assert torch.equal(lse[r:r + step], x[r:r + step, 0].float())
+
+
+# --- gradient in place of the logits ---------------------------------------------------------------------------------
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def _backward(x, grad, lse, rest=None, tokens=None, g_logprob=None, entropy=None, g_entropy=None, g_lse=None, top=None, g_top=None):
+    """The C call on (rows, V) tensors of any row stride; its status."""
+    at = lambda t: ctypes.c_void_p(None if t is None else t.data_ptr())  # noqa: E731
+    call = getattr(profk.lib(), "profk_logprobs_backward_" + {d: n for n, d in DTYPES.items()}[x.dtype])
+    rows, vocab = x.shape
+    return call(at(x), ctypes.c_int64(rows), ctypes.c_int64(vocab), ctypes.c_int64(x.stride(0)), ctypes.c_double(1.0), at(lse), at(rest), at(tokens),
+                at(g_logprob), at(entropy), at(g_entropy), at(g_lse), ctypes.c_int64(0 if top is None else top.shape[1]), at(top), at(g_top),
+                ctypes.c_void_p(torch.cuda.current_stream().cuda_stream), at(grad), ctypes.c_int64(grad.stride(0)))
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("vocab,pad", [(1, 0), (7, 1), (5003, 0), (40000, 24)])
+def test_gradient_in_place_of_the_logits(dtype, vocab, pad):
+    """Allowed where no entry is picked out; the tokens and alternatives of the forward call may be there all the same.  The
+    same bits as in rows of their own."""
+    x = (torch.randn(9, vocab + pad, device="cuda") * 3).to(DTYPES[dtype])[:, :vocab]
+    k = min(3, vocab)
+    r = profk.logprobs(x, torch.arange(9, device="cuda") % vocab, k=k)
+    up = torch.randn(2, 9, device="cuda")
+    args = dict(rest=r.lse_rest, tokens=torch.arange(9, device="cuda") % vocab, entropy=r.entropy, g_entropy=up[0].contiguous(), g_lse=up[1].contiguous(), top=r.top_tokens)
+    want = torch.empty_like(x)
+    assert _backward(x, want, r.lse, **args) == 0
+    assert _backward(x, x, r.lse, **args) == 0
+    assert torch.equal(x, want)
