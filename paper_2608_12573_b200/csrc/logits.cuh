@@ -139,6 +139,12 @@ __device__ __forceinline__ F32x2 f2_fma(F32x2 a, F32x2 b, F32x2 c) {
     return r;
 }
 __device__ __forceinline__ uint4 ld_stream_u4(const void* p) { return ld_stream(reinterpret_cast<const uint4*>(p)); }
+// ... of memory that the same kernel may write (not through the read-only path).
+__device__ __forceinline__ uint4 ld_once_u4(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
 __device__ __forceinline__ void st_stream_u4(void* p, const uint4& v) {
     asm volatile("st.global.L1::no_allocate.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }

@@ -917,11 +917,12 @@ __global__ void __launch_bounds__(LG_THREADS) logprobs_grad_kernel(const LpGradP
         st_stream_u4(y + head + (size_t)v * VEC, Logit<T>::pack(f));
     };
     if constexpr (!SHIFTED) {
+        // (the gradient may take the logits' place, so that these are not read through the read-only path)
         for (uint32_t v = tid; v < nvec; v += LG_THREADS * U) {
             uint4 in[U];
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (v + u * LG_THREADS < nvec) in[u] = ld_stream_u4(x + head + (size_t)(v + u * LG_THREADS) * VEC);
+                if (v + u * LG_THREADS < nvec) in[u] = ld_once_u4(x + head + (size_t)(v + u * LG_THREADS) * VEC);
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (v + u * LG_THREADS < nvec) put(v + u * LG_THREADS, in[u]);
