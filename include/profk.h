@@ -436,7 +436,7 @@ int profk_logprobs_f16(const void* logits, int64_t rows, int64_t V, int64_t row_
  *   lse, lse_rest, entropy, tokens, top_tokens   what the forward call took and gave (lse_rest may be NULL: 0)
  *   grad_logprob (needs tokens), grad_entropy (needs entropy), grad_lse, grad_top (needs top_tokens)   each may be NULL: 0
  *   grad_logits   [device] rows x V elements of the logits' type, row stride grad_row_stride; may be `logits` itself only
- *                 if grad_row_stride == row_stride and neither grad_logprob nor grad_top is given
+ *                 if grad_row_stride == row_stride and neither grad_logprob nor grad_top is given (refused otherwise)
  * The sum is taken in fp32 and rounded once.  Rows with lse = -inf get zeros; tokens outside [0, V) get nothing.
  * Errors: PROFK_EINVAL, PROFK_ECUDA.
  */

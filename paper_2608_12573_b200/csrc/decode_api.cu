@@ -159,6 +159,7 @@ int lp_backward(const T* logits, int64_t rows, int64_t V, int64_t row_stride, do
         (reinterpret_cast<uintptr_t>(logits) % sizeof(T)) != 0 || (reinterpret_cast<uintptr_t>(grad) % sizeof(T)) != 0 ||
         (grad_logprob && !tokens) || (grad_entropy && !entropy) || (grad_top && (!top_tokens || k < 1)))
         return PROFK_EINVAL;
+    if (grad == logits && (grad_logprob || grad_top || (rows > 1 && grad_row_stride != row_stride))) return PROFK_EINVAL;
     const uint32_t most = LG_THREADS * LG_UNROLL * 2 * Logit<T>::VEC;
     const uint32_t chunk = (uint32_t)std::min<int64_t>(most, (V + 15) / 16 * 16);
     const int64_t chunks = (V + chunk - 1) / chunk;
