@@ -405,7 +405,7 @@ int profk_topk_noalloc_f32(const float* in, int64_t rows, int64_t N, int64_t k, 
  *                 (log probability 0), a token >= V gives NaN
  *   k             0 <= k <= min(V, 128): alternatives per row, ordered by logit descending, equal logits by index
  *                 ascending (profk_topk_* selects more of them)
- *   temperature   > 0, finite
+ *   temperature   > 0; 1 / temperature and its product with log2(e) normal fp32 numbers (4.3e-39 to 8.5e37)
  *   logprob, lse  [device] rows floats (logprob NULL iff tokens is)
  *   lse_rest      [device] rows floats, or NULL: what the rounding of lse to fp32 left off.  The backward call takes the
  *                 probabilities from lse + lse_rest: beside a large maximum one float alone loses ln s
@@ -526,7 +526,7 @@ int profk_pages_append(const void* k, const void* v, const int64_t* k_strides, c
  *   q            [device] seqs x heads rows of dim elements; strides in elements, even
  *   k_pages, v_pages   [device] 16-byte aligned; strides in elements, multiples of 8
  *   dim          a multiple of 8, up to 256
- *   scale        > 0, finite
+ *   scale        > 0; it and its product with log2(e) normal fp32 numbers
  *   out          [device] seqs x heads x dim, dense, of the cache's type;  lse  [device] seqs x heads floats
  *   workspace    [device] profk_paged_attention_workspace_bytes(dim), 256-byte aligned
  * Statistics and sums are kept in fp32.  A sequence without tokens gets out = 0, lse = -inf.  The same call gives the same

@@ -2,6 +2,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <mutex>
@@ -21,6 +22,14 @@ namespace {
     } while (0)
 
 constexpr int MAX_DEVICES = 64;
+
+// Whether the kernels can work with a factor of the exponents: it and its product with log2(e) are normal fp32 numbers (a
+// factor of zero would make masked elements NaN, an infinite one all that equal the maximum).
+bool factor_ok(double factor) {
+    const float f = (float)factor;
+    return f >= FLT_MIN && std::isfinite(f * LOG2E);
+}
+bool temperature_ok(double temperature) { return temperature > 0 && std::isfinite(temperature) && factor_ok(1.0 / temperature); }
 
 // Streaming multiprocessors of the current device; 0 on an error.
 int sm_count() {
@@ -139,8 +148,7 @@ template <typename T>
 int lp_forward(const T* logits, int64_t rows, int64_t V, int64_t row_stride, const int64_t* tokens, int64_t k, double temperature,
                void* stream, float* logprob, float* lse, float* lse_rest, float* entropy, float* top_logprobs, int64_t* top_tokens) {
     if (!logits || !lse || rows < 1 || rows > 0x7FFFFFFFll || V < 1 || V > 0x7FFFFFFFll || rows > (1ll << 40) / V || (rows > 1 && row_stride < V) || k < 0 ||
-        k > LP_MAX_K || k > V || !(temperature > 0) || !std::isfinite(temperature) || !std::isfinite(1.0 / temperature) ||
-        (reinterpret_cast<uintptr_t>(logits) % sizeof(T)) != 0 || (k > 0) != (top_logprobs != nullptr) ||
+        k > LP_MAX_K || k > V || !temperature_ok(temperature) || (reinterpret_cast<uintptr_t>(logits) % sizeof(T)) != 0 || (k > 0) != (top_logprobs != nullptr) ||
         (k > 0) != (top_tokens != nullptr) || (tokens != nullptr) != (logprob != nullptr))
         return PROFK_EINVAL;
     const int sms = sm_count();
@@ -155,7 +163,7 @@ int lp_backward(const T* logits, int64_t rows, int64_t V, int64_t row_stride, do
                 const float* grad_logprob, const float* entropy, const float* grad_entropy, const float* grad_lse, int64_t k,
                 const int64_t* top_tokens, const float* grad_top, void* stream, T* grad, int64_t grad_row_stride) {
     if (!logits || !grad || !lse || rows < 1 || V < 1 || V > 0x7FFFFFFFll || rows > (1ll << 40) / V || (rows > 1 && (row_stride < V || grad_row_stride < V)) ||
-        k < 0 || k > LP_MAX_K || k > V || !(temperature > 0) || !std::isfinite(temperature) || !std::isfinite(1.0 / temperature) ||
+        k < 0 || k > LP_MAX_K || k > V || !temperature_ok(temperature) ||
         (reinterpret_cast<uintptr_t>(logits) % sizeof(T)) != 0 || (reinterpret_cast<uintptr_t>(grad) % sizeof(T)) != 0 ||
         (grad_logprob && !tokens) || (grad_entropy && !entropy) || (grad_top && (!top_tokens || k < 1)))
         return PROFK_EINVAL;
@@ -221,7 +229,7 @@ int pa_run(const T* q, int64_t q_seq, int64_t q_head, const T* k, const T* v, co
            int64_t page_size, int64_t pages, int64_t width, double scale, void* workspace, size_t workspace_bytes, void* stream, T* out, float* lse) {
     if (!q || !k || !v || !ks || !vs || !tables || !lengths || !out || !lse || seqs < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0 ||
         dim < 8 || dim > PA_MAX_DIM || dim % 8 != 0 || page_size < 1 || pages < 1 || width < 1 || seqs > (1 << 24) || heads > (1 << 16) ||
-        page_size > (1 << 24) || pages > 0x7FFFFFFFll || width * page_size > 0x7FFFFF00ll || table_stride < 0 || !(scale > 0) || !std::isfinite(scale) ||
+        page_size > (1 << 24) || pages > 0x7FFFFFFFll || width * page_size > 0x7FFFFF00ll || table_stride < 0 || !factor_ok(scale) ||
         !aligned_to(q, 4) || q_seq % 2 != 0 || q_head % 2 != 0 || !aligned_to(k, 16) || !aligned_to(v, 16) || !aligned_to(out, 16))
         return PROFK_EINVAL;
     for (const profk_page_strides_t* s : {ks, vs})

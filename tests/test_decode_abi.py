@@ -33,3 +33,29 @@ def test_gradient_in_place_is_refused_where_it_cannot_be_right(lib, dtype):
     assert _backward(lib, grad=P, g_logprob=P, dtype=dtype) == EINVAL
     assert _backward(lib, grad=P, k=2, top=P, g_top=P, dtype=dtype) == EINVAL
     assert _backward(lib, grad=P, stride=104, dtype=dtype) == EINVAL
+
+
+# --- factors of the exponents, which the kernels hold in fp32 ---------------------------------------------------------
+
+BEYOND_FP32 = [2e38, 1e60, 1e-39, 1e-46, 1e-300]          # their reciprocals or they themselves are no normal fp32 numbers (or overflow times log2 e)
+
+
+def _forward(lib, temperature, dtype="f32"):
+    return getattr(lib, "profk_logprobs_" + dtype)(P, I(4), I(100), I(100), NULL, I(0), ctypes.c_double(temperature), NULL, NULL, P, NULL, NULL, NULL, NULL)
+
+
+@pytest.mark.parametrize("temperature", [0.0, -1.0, float("nan"), float("inf")] + BEYOND_FP32)
+def test_temperatures_that_fp32_cannot_hold_are_refused(lib, temperature):
+    assert _forward(lib, temperature) == EINVAL and _forward(lib, temperature, "bf16") == EINVAL
+    assert _backward(lib, temperature=temperature) == EINVAL
+
+
+def _attention(lib, scale=0.125, dtype="bf16", width=8, page_size=16, workspace=P):
+    strides = (I * 3)(2048, 1024, 64)
+    return getattr(lib, "profk_paged_attention_" + dtype)(P, I(256), I(64), P, P, strides, strides, P, I(width), P, I(2), I(4), I(2), I(64), I(page_size), I(10), I(width),
+                                                          ctypes.c_double(scale), workspace, ctypes.c_size_t(1 << 40), NULL, P, P)
+
+
+@pytest.mark.parametrize("scale", [0.0, -1.0, float("nan"), float("inf"), 3e38, 1e39, 1e-39, 1e-46, 1e-300])
+def test_scales_that_fp32_cannot_hold_are_refused(lib, scale):
+    assert _attention(lib, scale) == EINVAL and _attention(lib, scale, "f16") == EINVAL
