@@ -22,6 +22,10 @@ namespace {
     } while (0)
 
 constexpr int MAX_DEVICES = 64;
+constexpr int64_t MAX_PAGE_SIZE = 1 << 24, MAX_TOKENS = 0x7FFFFF00ll;      // of a page, of a sequence
+
+// Whether a table of `width` entries and pages of `page_size` tokens are within what the kernels count (no product wraps).
+bool table_ok(int64_t width, int64_t page_size) { return page_size >= 1 && page_size <= MAX_PAGE_SIZE && width >= 1 && width <= MAX_TOKENS / page_size; }
 
 // Whether the kernels can work with a factor of the exponents: it and its product with log2(e) are normal fp32 numbers (a
 // factor of zero would make masked elements NaN, an infinite one all that equal the maximum).
@@ -228,8 +232,8 @@ int pa_run(const T* q, int64_t q_seq, int64_t q_head, const T* k, const T* v, co
            const int32_t* tables, int64_t table_stride, const int32_t* lengths, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t dim,
            int64_t page_size, int64_t pages, int64_t width, double scale, void* workspace, size_t workspace_bytes, void* stream, T* out, float* lse) {
     if (!q || !k || !v || !ks || !vs || !tables || !lengths || !out || !lse || seqs < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0 ||
-        dim < 8 || dim > PA_MAX_DIM || dim % 8 != 0 || page_size < 1 || pages < 1 || width < 1 || seqs > (1 << 24) || heads > (1 << 16) ||
-        page_size > (1 << 24) || pages > 0x7FFFFFFFll || width * page_size > 0x7FFFFF00ll || table_stride < 0 || !factor_ok(scale) ||
+        dim < 8 || dim > PA_MAX_DIM || dim % 8 != 0 || !table_ok(width, page_size) || pages < 1 || seqs > (1 << 24) || heads > (1 << 16) ||
+        pages > 0x7FFFFFFFll || table_stride < 0 || !factor_ok(scale) ||
         !aligned_to(q, 4) || q_seq % 2 != 0 || q_head % 2 != 0 || !aligned_to(k, 16) || !aligned_to(v, 16) || !aligned_to(out, 16))
         return PROFK_EINVAL;
     for (const profk_page_strides_t* s : {ks, vs})
@@ -260,7 +264,7 @@ int pa_run(const T* q, int64_t q_seq, int64_t q_head, const T* k, const T* v, co
 bool pg_pool_ok(const profk_pool_t* pool) {
     if (!pool) return true;
     return pool->base && aligned_to(pool->base, 16) && pool->layers >= 1 && pool->layers <= (1 << 20) && pool->kv_heads >= 1 && pool->kv_heads <= (1 << 16) &&
-           pool->page_size >= 1 && pool->row_bytes >= 16 && pool->row_bytes <= (1 << 20) && pool->row_bytes % 16 == 0 && pool->layer % 16 == 0 &&
+           pool->page_size >= 1 && pool->page_size <= MAX_PAGE_SIZE && pool->row_bytes >= 16 && pool->row_bytes <= (1 << 20) && pool->row_bytes % 16 == 0 && pool->layer % 16 == 0 &&
            pool->kv % 16 == 0 && pool->page % 16 == 0 && pool->head % 16 == 0 && pool->token % 16 == 0 &&
            pool->kv_heads * pool->page_size * (pool->row_bytes / 16) <= (1 << 30);
 }
@@ -279,7 +283,7 @@ size_t fork_workspace(int64_t n_old, int64_t n, int64_t pages, int64_t page_size
     return 256 + 2 * up((size_t)n_old * 4) + up((size_t)n * 4) + up((size_t)fork_fresh(n, pages, page_size, grow) * 4) + up((size_t)n * sizeof(PgMove));
 }
 bool fork_sizes_ok(int64_t n_old, int64_t n, int64_t pages, int64_t page_size, int64_t grow) {
-    return n_old >= 0 && n >= 0 && n_old <= (1 << 24) && n <= (1 << 24) && pages >= 1 && pages <= 0x7FFF0000ll && page_size >= 1 && page_size <= (1 << 24) &&
+    return n_old >= 0 && n >= 0 && n_old <= (1 << 24) && n <= (1 << 24) && pages >= 1 && pages <= 0x7FFF0000ll && page_size >= 1 && page_size <= MAX_PAGE_SIZE &&
            grow >= 0 && grow <= (1 << 24) && n * (1 + (grow + page_size - 1) / page_size) <= 0x7FFF0000ll;
 }
 
@@ -337,7 +341,7 @@ int profk_pages_fork_workspace_bytes(int64_t n_old, int64_t n, int64_t pages, in
 int profk_pages_fork(const profk_pool_t* pool, const int32_t* tables, int64_t n_old, int64_t width, int64_t table_stride, const int32_t* lengths,
                      const int32_t* refs, int64_t pages, const int32_t* parents, int64_t n, int64_t page_size, int64_t grow, void* workspace,
                      size_t workspace_bytes, void* stream, int32_t* out_tables, int32_t* out_lengths, int32_t* out_refs, int32_t* out_missing) {
-    if (!fork_sizes_ok(n_old, n, pages, page_size, grow) || width < 1 || width * page_size > 0x7FFFFF00ll || table_stride < 0 || !refs || !out_refs ||
+    if (!fork_sizes_ok(n_old, n, pages, page_size, grow) || !table_ok(width, page_size) || table_stride < 0 || !refs || !out_refs ||
         out_refs == refs || !out_missing || (n_old > 0 && (!tables || !lengths)) || (n > 0 && (!parents || !out_tables || !out_lengths)) ||
         (n > 0 && (out_tables == tables || out_lengths == lengths)) || !pg_pool_ok(pool) || (pool && pool->page_size != page_size))
         return PROFK_EINVAL;
@@ -423,8 +427,8 @@ int profk_pages_append(const void* k, const void* v, const int64_t* k_strides, c
                        const int32_t* lengths, int64_t seqs, int64_t tokens, int64_t kv_heads, int64_t row_bytes, int64_t page_size,
                        int64_t pages, int64_t width, void* stream) {
     if (!k || !v || !k_strides || !v_strides || !k_pages || !v_pages || !kp || !vp || !tables || !lengths || seqs < 1 || seqs > (1 << 24) || tokens < 1 ||
-        kv_heads < 1 || kv_heads > (1 << 16) || row_bytes < 16 || row_bytes > (1 << 20) || row_bytes % 16 != 0 || page_size < 1 || pages < 1 ||
-        pages > 0x7FFFFFFFll || width < 1 || width * page_size > 0x7FFFFF00ll || tokens > width * page_size || table_stride < 0 || !aligned_to(k, 16) ||
+        kv_heads < 1 || kv_heads > (1 << 16) || row_bytes < 16 || row_bytes > (1 << 20) || row_bytes % 16 != 0 || !table_ok(width, page_size) || pages < 1 ||
+        pages > 0x7FFFFFFFll || tokens > width * page_size || table_stride < 0 || !aligned_to(k, 16) ||
         !aligned_to(v, 16) || !aligned_to(k_pages, 16) || !aligned_to(v_pages, 16))
         return PROFK_EINVAL;
     for (const int64_t x : {k_strides[0], k_strides[1], k_strides[2], v_strides[0], v_strides[1], v_strides[2], kp->page, kp->head, kp->token, vp->page,
