@@ -412,7 +412,9 @@ int profk_topk_noalloc_f32(const float* in, int64_t rows, int64_t N, int64_t k, 
  *   entropy       [device] rows floats, or NULL: not computed
  *   top_logprobs, top_tokens   [device] rows x k floats / int64; NULL iff k = 0
  * All statistics are kept in fp32, sums relative to the row's largest logit.  -inf masks a token: probability 0, no part
- * in the entropy.  A row of nothing but -inf has lse = -inf, log probabilities -inf, entropy 0.  A NaN or +inf anywhere in
+ * in the entropy.  A row of nothing but -inf has lse = -inf, log probabilities -inf, entropy 0.  Where the largest logit /
+ * temperature passes fp32's range (a row masked with its lowest value, at a temperature below 1) lse is infinite, too, while
+ * log probabilities and entropy are what they should be; such rows have no gradient.  A NaN or +inf anywhere in
  * a row makes its lse, log probabilities and entropy NaN; a NaN is never among the alternatives (places that nothing else
  * fills get token -1, log probability NaN).
  * The result does not depend on how a row is cut into parts except in the last bits of the sums; it is the same in every
@@ -437,7 +439,7 @@ int profk_logprobs_f16(const void* logits, int64_t rows, int64_t V, int64_t row_
  *   grad_logprob (needs tokens), grad_entropy (needs entropy), grad_lse, grad_top (needs top_tokens)   each may be NULL: 0
  *   grad_logits   [device] rows x V elements of the logits' type, row stride grad_row_stride; may be `logits` itself only
  *                 if grad_row_stride == row_stride and neither grad_logprob nor grad_top is given (refused otherwise)
- * The sum is taken in fp32 and rounded once.  Rows with lse = -inf get zeros; tokens outside [0, V) get nothing.
+ * The sum is taken in fp32 and rounded once.  Rows with an infinite lse get zeros (see above); tokens outside [0, V) get nothing.
  * Errors: PROFK_EINVAL, PROFK_ECUDA.
  */
 int profk_logprobs_backward_f32(const float* logits, int64_t rows, int64_t V, int64_t row_stride, double temperature,

@@ -900,7 +900,7 @@ __global__ void __launch_bounds__(LG_THREADS) logprobs_grad_kernel(const LpGradP
     const float whole = g_lp + g_sum - (p.g_lse ? p.g_lse[row] : 0.f);
     r.whole = (whole + (p.g_entropy ? g_h * p.entropy[row] : 0.f)) * scale;
     r.g_h = g_h * scale;
-    const bool empty = r.lse == -INFINITY;                 // nothing but -inf in the row: no gradient
+    const bool empty = isinf(r.lse);                       // nothing but -inf in the row, or more than fp32 holds: no gradient
 
     const uint32_t e0 = chunk * p.chunk, e1 = min(p.V, e0 + p.chunk);
     // Vectors are those of the gradient's rows; where the logits' rows start at another offset, each is put together from two

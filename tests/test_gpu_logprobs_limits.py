@@ -61,3 +61,31 @@ def test_gradient_in_place_of_the_logits(dtype, vocab, pad):
     assert _backward(x, want, r.lse, **args) == 0
     assert _backward(x, x, r.lse, **args) == 0
     assert torch.equal(x, want)
+
+
+# --- logits at the ends of fp32's range ------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("temperature", [0.7, 0.5])
+def test_rows_whose_scaled_logits_pass_the_range(dtype, temperature):
+    """Largest logits of the type's lowest and largest values at temperatures below 1: lse is infinite, log probabilities and
+    entropy are those of the tied tokens, the gradient is zero."""
+    import math
+
+    vocab, info = 3001, torch.finfo(DTYPES[dtype])
+    x = torch.full((4, vocab), info.min, dtype=DTYPES[dtype], device="cuda")
+    x[1, 7:] = -float("inf")                           # seven of them
+    x[2] = 0.0
+    x[2, 5:10] = info.max                              # five of the largest value
+    x[3] = torch.randn(vocab, device="cuda")           # an ordinary row beside them
+    tokens = torch.tensor([3, 2, 6, 11], device="cuda")
+    r = profk.logprobs(x, tokens, k=4, temperature=temperature)
+    assert r.lse[:3].tolist() == [-float("inf"), -float("inf"), float("inf")] and torch.isfinite(r.lse[3])
+    want = torch.tensor([-math.log(n) for n in (vocab, 7, 5)], device="cuda")
+    assert (r.logprob[:3] - want).abs().max() < 1e-5 and (r.entropy[:3] + want).abs().max() < 1e-5
+    assert (r.top_logprobs[:3] - want[:, None]).abs().max() < 1e-5
+    assert r.top_tokens.tolist()[:3] == [[0, 1, 2, 3], [0, 1, 2, 3], [5, 6, 7, 8]]
+    one = torch.ones(4, device="cuda")
+    grad = profk.logprobs_backward(x, r.lse, tokens, one, entropy=r.entropy, grad_entropy=one, grad_lse=one, top_tokens=r.top_tokens,
+                                   grad_top=torch.ones(4, 4, device="cuda"), lse_rest=r.lse_rest, temperature=temperature)
+    assert (grad[:3] == 0).all() and (grad[3] != 0).any() and torch.isfinite(grad[3]).all()
