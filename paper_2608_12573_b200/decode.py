@@ -41,6 +41,19 @@ class LogProbs(NamedTuple):
     lse_rest: torch.Tensor                  # (...)    what the rounding of lse left off, for `logprobs_backward`
 
 
+class _LogProbsGradient(torch.autograd.Function):
+    """The gradient as a node of its own, for `create_graph=True`: a second derivative is refused, not left out."""
+    @staticmethod
+    def forward(ctx, *args):
+        return _load().logprobs_backward(*args)
+
+    @staticmethod
+    def backward(ctx, *_):
+        import paper_2608_12573_b200 as package
+
+        raise package.ProfkError("logprobs can be differentiated once only")
+
+
 class _LogProbsFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, tokens, k, temperature, entropy):
@@ -58,9 +71,9 @@ class _LogProbsFunction(torch.autograd.Function):
         def dense(g):
             return None if g is None else g.contiguous()
 
-        grad = logprobs_backward(logits, lse, tokens, dense(g_logprob), entropy=entropy, grad_entropy=dense(g_entropy),
-                                 grad_lse=dense(g_lse), top_tokens=top, grad_top=dense(g_top), lse_rest=rest,
-                                 temperature=ctx.temperature)
+        args = (logits, lse, rest, tokens, dense(g_logprob), entropy, dense(g_entropy), dense(g_lse), top, dense(g_top), ctx.temperature)
+        # (grad mode is on here where a graph of the gradient was asked for)
+        grad = _LogProbsGradient.apply(*args) if torch.is_grad_enabled() else _load().logprobs_backward(*args)
         return grad, None, None, None, None
 
 
@@ -70,7 +83,7 @@ def logprobs(logits, tokens=None, k: int = 0, temperature: float = 1.0, entropy:
 
     logits: CUDA tensor (..., V), float32, bfloat16 or float16, dense rows at any stride.  tokens: int64 (...), negative
     where no token is given.  k <= 128 (`topk` selects more).  Differentiable in the logits (through `logprob`, `lse`,
-    `entropy` and `top_logprobs`); see `profk.h` for masked, empty and NaN rows."""
+    `entropy` and `top_logprobs`), once; see `profk.h` for masked, empty and NaN rows."""
     if isinstance(logits, torch.Tensor) and logits.requires_grad and torch.is_grad_enabled():
         return LogProbs._make(_LogProbsFunction.apply(logits, tokens, k, temperature, bool(entropy)))
     return LogProbs._make((_native or _load()).logprobs(logits, tokens, k, temperature, bool(entropy)))
