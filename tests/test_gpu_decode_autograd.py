@@ -24,3 +24,39 @@ def test_a_second_derivative_is_refused():
     assert (grad - torch.autograd.grad(plain, x)[0]).abs().max() < 1e-5
     with pytest.raises(RuntimeError):
         (loss + (grad ** 2).sum()).backward()              # (a penalty on the gradient: its term would count for nothing)
+
+
+def _cache():
+    pool = torch.randn(1, 2, 6, 2, 16, 64, device="cuda").to(torch.bfloat16)
+    tables = torch.tensor([[0, 1], [2, 3]], dtype=torch.int32, device="cuda")
+    lengths = torch.tensor([20, 30], dtype=torch.int32, device="cuda")
+    refs = torch.tensor([1, 1, 1, 1, 0, 0], dtype=torch.int32, device="cuda")
+    return pool, tables, lengths, refs
+
+
+def test_tangents_are_refused():
+    import torch.autograd.forward_ad as forward
+
+    x, tokens = torch.randn(3, 50, device="cuda"), torch.arange(3, device="cuda")
+    r = profk.logprobs(x, tokens, k=2)
+    one = torch.ones(3, device="cuda")
+    pool, tables, lengths, refs = _cache()
+    k, v = pool[0, 0], pool[0, 1]
+    q, new = torch.randn(2, 4, 64, device="cuda").to(k.dtype), torch.randn(2, 2, 64, device="cuda").to(k.dtype)
+    before = pool.clone()
+    with forward.dual_level():
+        dual = lambda t: forward.make_dual(t, torch.ones_like(t))  # noqa: E731
+        calls = [lambda: profk.logprobs(dual(x), tokens), lambda: profk.logprobs(dual(x.clone().requires_grad_(True)), tokens),
+                 lambda: profk.logprobs_backward(dual(x), r.lse, tokens, one), lambda: profk.logprobs_backward(x, r.lse, tokens, dual(one)),
+                 lambda: profk.logprobs_backward(x, dual(r.lse), tokens, one), lambda: profk.logprobs_backward(x, r.lse, grad_lse=dual(one)),
+                 lambda: profk.paged_attention(dual(q), k, v, tables, lengths), lambda: profk.paged_attention(q, dual(k), v, tables, lengths),
+                 lambda: profk.paged_attention(q, k, dual(v), tables, lengths), lambda: profk.pages_append(k, v, tables, lengths, dual(new), new),
+                 lambda: profk.pages_append(k, v, tables, lengths, new, dual(new)), lambda: profk.pages_append(dual(k), v, tables, lengths, new, new),
+                 lambda: profk.pages_copy(dual(pool), refs[:1], refs[4:5]), lambda: profk.pages_compact(dual(pool), tables, refs),
+                 lambda: profk.pages_fork(dual(pool), tables, lengths, refs, refs[:2], grow=1)]
+        for n, call in enumerate(calls):
+            with pytest.raises(RuntimeError):
+                call()
+                pytest.fail(f"call {n} was not refused")
+        assert torch.equal(profk.logprobs(x, tokens).lse, r.lse)
+    assert torch.equal(pool, before)
