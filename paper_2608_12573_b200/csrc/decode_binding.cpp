@@ -6,6 +6,7 @@
 #include <Python.h>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -77,9 +78,13 @@ PyObject* pack(std::initializer_list<PyObject*> items) {
     return t;
 }
 
-// Refuses a tensor that carries a tangent (forward-mode differentiation): the call would drop it.
-void no_tangent(const at::Tensor* t, const char* what) {
-    if (t && t->_fw_grad(0).defined()) refuse(std::string(what) + " carries a tangent: there is no forward-mode derivative");
+// Refuses a tensor whose derivative the call would drop: one with a tangent (forward mode), or that requires a gradient in
+// grad mode (`logprobs` is differentiable, and calls this module with grad mode off).
+void no_derivative(const at::Tensor* t, const char* what) {
+    if (!t) return;
+    if (t->_fw_grad(0).defined()) refuse(std::string(what) + " carries a tangent: there is no forward-mode derivative");
+    if (t->requires_grad() && at::GradMode::is_enabled())
+        refuse(std::string(what) + " requires a gradient, which this call does not have: detach it, or call under torch.no_grad()");
 }
 
 // Whether consecutive elements of the last dimension lie together.
@@ -138,7 +143,7 @@ PyObject* logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t k = integer(a[2], "k");
         const double temperature = real(a[3], "temperature");
         const bool entropy = a[4] == Py_True;
-        no_tangent(&x, "logits");
+        no_derivative(&x, "logits");
         const Matrix m = matrix(x);
         const int type = dtype_index(x.scalar_type());
         const c10::Device dev = x.device();
@@ -176,9 +181,9 @@ PyObject* logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor* top = optional(a[8], "top_tokens");
         const at::Tensor* g_top = optional(a[9], "grad_top");
         const double temperature = real(a[10], "temperature");
-        no_tangent(&x, "logits");
+        no_derivative(&x, "logits");
         for (const auto& [i, what] : {std::pair{1, "lse"}, {2, "lse_rest"}, {4, "grad_logprob"}, {5, "entropy"}, {6, "grad_entropy"}, {7, "grad_lse"}, {9, "grad_top"}})
-            no_tangent(optional(a[i], what), what);
+            no_derivative(optional(a[i], what), what);
         const Matrix m = matrix(x);
         const int type = dtype_index(x.scalar_type());
         const c10::Device dev = x.device();
@@ -242,7 +247,7 @@ PyObject* pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     return guarded([&]() -> PyObject* {
         need(n_args == 7, "pages_fork takes seven arguments");
         const at::Tensor* pool = optional(a[0], "pool");
-        no_tangent(pool, "pool");
+        no_derivative(pool, "pool");
         const at::Tensor &tables = tensor(a[1], "tables"), &lengths = tensor(a[2], "lengths"), &refs = tensor(a[3], "refs"), &parents = tensor(a[4], "parents");
         const int64_t grow = integer(a[5], "grow");
         int64_t page_size = integer(a[6], "page_size");
@@ -280,7 +285,7 @@ PyObject* pages_compact(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     return guarded([&]() -> PyObject* {
         need(n_args == 3, "pages_compact takes three arguments");
         const at::Tensor* pool = optional(a[0], "pool");
-        no_tangent(pool, "pool");
+        no_derivative(pool, "pool");
         const at::Tensor &tables = tensor(a[1], "tables"), &refs = tensor(a[2], "refs");
         need(refs.is_cuda(), "refs must be a CUDA tensor");
         const c10::Device dev = refs.device();
@@ -310,7 +315,7 @@ PyObject* pages_copy(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     return guarded([&]() -> PyObject* {
         need(n_args == 3, "pages_copy takes three arguments");
         const at::Tensor &pool = tensor(a[0], "pool"), &src = tensor(a[1], "src"), &dst = tensor(a[2], "dst");
-        no_tangent(&pool, "pool");
+        no_derivative(&pool, "pool");
         const profk_pool_t desc = pool_of(pool);
         const c10::Device dev = pool.device();
         const int32_t *src_p = ints(src, "src", 1, dev), *dst_p = ints(dst, "dst", 1, dev);
@@ -336,7 +341,7 @@ PyObject* pages_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         need(n_args == 6, "pages_append takes six arguments");
         const at::Tensor &kp = tensor(a[0], "k_pages"), &vp = tensor(a[1], "v_pages"), &tables = tensor(a[2], "tables"), &lengths = tensor(a[3], "lengths"),
                          &k = tensor(a[4], "k"), &v = tensor(a[5], "v");
-        for (const auto& [t, what] : {std::pair{&kp, "k_pages"}, {&vp, "v_pages"}, {&k, "k"}, {&v, "v"}}) no_tangent(t, what);
+        for (const auto& [t, what] : {std::pair{&kp, "k_pages"}, {&vp, "v_pages"}, {&k, "k"}, {&v, "v"}}) no_derivative(t, what);
         pages_pair(kp, vp);
         const c10::Device dev = kp.device();
         const int64_t stride = table_stride(tables, dev), seqs = tables.size(0), width = tables.size(1), dims = k.dim();
@@ -365,7 +370,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         need(n_args == 6, "paged_attention takes six arguments");
         const at::Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k_pages"), &v = tensor(a[2], "v_pages"), &tables = tensor(a[3], "tables"),
                          &lengths = tensor(a[4], "lengths");
-        for (const auto& [t, what] : {std::pair{&q, "q"}, {&k, "k_pages"}, {&v, "v_pages"}}) no_tangent(t, what);
+        for (const auto& [t, what] : {std::pair{&q, "q"}, {&k, "k_pages"}, {&v, "v_pages"}}) no_derivative(t, what);
         need(q.is_cuda(), "q must be a CUDA tensor");
         pages_pair(k, v);
         need(q.dim() == 3 && q.numel() > 0 && dense_rows(q), "q must be of shape (seqs, heads, dim) with dense rows");

@@ -2,7 +2,8 @@
 gradient), the forking and compaction of the pages of a key-value cache, and attention of one token over them.
 
 Checks, allocation and marshalling are done by the in-tree extension module `_decode` (csrc/decode_binding.cpp), which calls
-the C ABI of `profk.h`; a refusal raises `ProfkError`.  Nothing is synchronised, and scratch memory comes from torch's
+the C ABI of `profk.h`; a refusal raises `ProfkError`.  Of all of them `logprobs` has a derivative; the others refuse tensors
+that require a gradient unless grad mode is off.  Nothing is synchronised, and scratch memory comes from torch's
 allocator on the current stream, so that calls on several streams do not meet.
 """
 from __future__ import annotations

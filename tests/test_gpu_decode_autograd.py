@@ -60,3 +60,30 @@ def test_tangents_are_refused():
                 pytest.fail(f"call {n} was not refused")
         assert torch.equal(profk.logprobs(x, tokens).lse, r.lse)
     assert torch.equal(pool, before)
+
+
+def test_inputs_that_require_a_gradient_are_refused_in_grad_mode():
+    x, tokens = torch.randn(3, 50, device="cuda"), torch.arange(3, device="cuda")
+    r = profk.logprobs(x, tokens, k=2)
+    one = torch.ones(3, device="cuda")
+    pool, tables, lengths, refs = _cache()
+    k, v = pool[0, 0], pool[0, 1]
+    q, new = torch.randn(2, 4, 64, device="cuda").to(k.dtype), torch.randn(2, 2, 64, device="cuda").to(k.dtype)
+    before = pool.clone()
+    leaf = lambda t: t.detach().requires_grad_(True)  # noqa: E731
+    calls = [lambda: profk.logprobs_backward(leaf(x), r.lse, tokens, one), lambda: profk.logprobs_backward(x, r.lse, tokens, leaf(one)),
+             lambda: profk.logprobs_backward(x, leaf(r.lse), tokens, one), lambda: profk.paged_attention(leaf(q), k, v, tables, lengths),
+             lambda: profk.paged_attention(q, leaf(k), v, tables, lengths), lambda: profk.paged_attention(q, k, leaf(v), tables, lengths),
+             lambda: profk.pages_append(k, v, tables, lengths, leaf(new), new), lambda: profk.pages_append(k, v, tables, lengths, new, leaf(new)),
+             lambda: profk.pages_append(leaf(k), v, tables, lengths, new, new), lambda: profk.pages_copy(leaf(pool), refs[:1], refs[4:5]),
+             lambda: profk.pages_compact(leaf(pool), tables, refs), lambda: profk.pages_fork(leaf(pool), tables, lengths, refs, refs[:2], grow=1)]
+    for n, call in enumerate(calls):
+        with pytest.raises(profk.ProfkError):
+            call()
+            pytest.fail(f"call {n} was not refused")
+    assert torch.equal(pool, before)
+    want = profk.paged_attention(q, k, v, tables, lengths)
+    with torch.no_grad():
+        got = profk.paged_attention(leaf(q), k, v, tables, lengths)
+        profk.logprobs_backward(leaf(x), r.lse, tokens, one)
+    assert torch.equal(got[0], want[0])
