@@ -87,6 +87,11 @@ void no_derivative(const at::Tensor* t, const char* what) {
         refuse(std::string(what) + " requires a gradient, which this call does not have: detach it, or call under torch.no_grad()");
 }
 
+// Tells autograd that a tensor was written (inference tensors have no version to raise).
+void written(const at::Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // Whether consecutive elements of the last dimension lie together.
 bool dense_rows(const at::Tensor& t) { return t.size(-1) <= 1 || t.stride(-1) == 1; }
 
@@ -276,6 +281,7 @@ PyObject* pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                                 static_cast<int32_t*>(new_lengths.data_ptr()), static_cast<int32_t*>(new_refs.data_ptr()),
                                 static_cast<int32_t*>(missing.data_ptr())),
                "profk_pages_fork");
+        if (pool) written(*pool);
         return pack({wrap(new_tables), wrap(new_lengths), wrap(new_refs), wrap(missing)});
     });
 }
@@ -306,6 +312,7 @@ PyObject* pages_compact(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                                    static_cast<int32_t*>(new_tables.data_ptr()), static_cast<int32_t*>(new_refs.data_ptr()),
                                    static_cast<int32_t*>(page_map.data_ptr()), static_cast<int32_t*>(live.data_ptr())),
                "profk_pages_compact");
+        if (pool) written(*pool);
         return pack({wrap(new_tables), wrap(new_refs), wrap(page_map), wrap(live)});
     });
 }
@@ -322,6 +329,7 @@ PyObject* pages_copy(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         need(src.size(0) == dst.size(0), "src and dst must have the same length");
         const c10::cuda::CUDAGuard guard(dev);
         status(profk_pages_copy(&desc, pool.size(2), src_p, dst_p, src.size(0), c10::cuda::getCurrentCUDAStream(dev.index()).stream()), "profk_pages_copy");
+        written(pool);
         return none();
     });
 }
@@ -360,6 +368,8 @@ PyObject* pages_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                                   lengths_p, seqs, tokens, kp.size(1), kp.size(3) * b, kp.size(2), kp.size(0), width,
                                   c10::cuda::getCurrentCUDAStream(dev.index()).stream()),
                "profk_pages_append");
+        written(kp);
+        written(vp);
         return none();
     });
 }

@@ -87,3 +87,23 @@ def test_inputs_that_require_a_gradient_are_refused_in_grad_mode():
         got = profk.paged_attention(leaf(q), k, v, tables, lengths)
         profk.logprobs_backward(leaf(x), r.lse, tokens, one)
     assert torch.equal(got[0], want[0])
+
+
+def test_writes_to_a_cache_are_seen_by_autograd():
+    pool, tables, lengths, refs = _cache()
+    new = torch.randn(2, 2, 64, device="cuda").to(pool.dtype)
+    k, v = pool[0, 0], pool[0, 1]
+    calls = [lambda: profk.pages_append(k, v, tables, lengths, new, new), lambda: profk.pages_copy(pool, refs[4:5], refs[:1]),
+             lambda: profk.pages_fork(pool, tables, lengths, refs, torch.zeros(2, dtype=torch.int32, device="cuda"), grow=1), lambda: profk.pages_compact(pool, tables, refs)]
+    for n, call in enumerate(calls):
+        weight = torch.ones((), device="cuda", dtype=pool.dtype, requires_grad=True)
+        kept = weight * k                                        # autograd keeps a view of the cache for the weight's gradient
+        call()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            kept.sum().backward()
+            pytest.fail(f"call {n} was not noticed")
+    with torch.inference_mode():
+        other = pool.clone()
+        profk.pages_append(other[0, 0], other[0, 1], tables, lengths, new, new)
+    with torch.no_grad():                                        # an inference tensor outside of inference mode
+        profk.pages_append(other[0, 0], other[0, 1], tables, lengths, new, new)
