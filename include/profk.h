@@ -461,7 +461,7 @@ int profk_logprobs_backward_f16(const void* logits, int64_t rows, int64_t V, int
  *   tables   n rows of `width` entries, row i at tables + i * table_stride; entry c is the page of the tokens
  *            [c * page_size, (c + 1) * page_size).  Entries at or behind a sequence's length are not read; a number outside
  *            [0, pages) stands for a page that is not there (its tokens take no part, nothing is copied)
- *   lengths  n tokens held, taken into [0, width * page_size]
+ *   lengths  n tokens held, taken into [0, width * page_size] (profk_pages_append takes them as they are)
  *   refs     one per page: how many table entries (or other owners) hold it; <= 0 is free
  */
 
@@ -489,12 +489,22 @@ typedef struct profk_page_strides { int64_t page, head, token; } profk_page_stri
  *                stands in the table in place of each that has room there.  Must not overlap the inputs
  *   workspace    [device] profk_pages_fork_workspace_bytes, 256-byte aligned
  * n = 0 releases all.  Errors: PROFK_EINVAL, PROFK_EWORKSPACE, PROFK_ECUDA.
+ *
+ * A sequence whose table is full gets no longer: of its new tokens, out_missing is the only sign, and profk_pages_append with
+ * that length writes over its last ones, in a page that its siblings hold.  With PROFK_FORK_PAST_ROOM (profk_pages_fork_ex)
+ * out_lengths go on counting past the table's end instead, and profk_pages_append passes the tokens over that lie there; all
+ * other calls take such lengths for a full table's.
  */
 int profk_pages_fork_workspace_bytes(int64_t n_old, int64_t n, int64_t pages, int64_t page_size, int64_t grow, size_t* bytes /* [host] */);
 int profk_pages_fork(const profk_pool_t* pool /* [host] */, const int32_t* tables, int64_t n_old, int64_t width, int64_t table_stride,
                      const int32_t* lengths, const int32_t* refs, int64_t pages, const int32_t* parents, int64_t n, int64_t page_size,
                      int64_t grow, void* workspace, size_t workspace_bytes, void* stream, int32_t* out_tables, int32_t* out_lengths,
                      int32_t* out_refs, int32_t* out_missing);
+#define PROFK_FORK_PAST_ROOM 1
+int profk_pages_fork_ex(const profk_pool_t* pool /* [host] */, const int32_t* tables, int64_t n_old, int64_t width, int64_t table_stride,
+                        const int32_t* lengths, const int32_t* refs, int64_t pages, const int32_t* parents, int64_t n, int64_t page_size,
+                        int64_t grow, int flags, void* workspace, size_t workspace_bytes, void* stream, int32_t* out_tables,
+                        int32_t* out_lengths, int32_t* out_refs, int32_t* out_missing);
 
 /*
  * Moves the L live pages (refs > 0) to the pages [0, L): live pages at or behind L go to the free ones in front of it, both
@@ -515,8 +525,8 @@ int profk_pages_copy(const profk_pool_t* pool /* [host] */, int64_t pages, const
 
 /* Writes the keys and values of the last `tokens` tokens of every sequence (positions length - tokens .. length - 1) to
  * their places in one layer's pages.  k, v: [device] (seqs, tokens, kv_heads) rows of row_bytes; *_strides [host] three
- * strides each; kp, vp: those of the pages; all strides in bytes, multiples of 16.  Tokens before position 0 or on a page
- * that is not there are passed over.  No two sequences may write to one page.  Errors: PROFK_EINVAL, PROFK_ECUDA. */
+ * strides each; kp, vp: those of the pages; all strides in bytes, multiples of 16.  Tokens before position 0, at or behind
+ * width * page_size or on a page that is not there are passed over.  No two sequences may write to one page.  Errors: PROFK_EINVAL, PROFK_ECUDA. */
 int profk_pages_append(const void* k, const void* v, const int64_t* k_strides, const int64_t* v_strides, void* k_pages, void* v_pages,
                        const profk_page_strides_t* kp, const profk_page_strides_t* vp, const int32_t* tables, int64_t table_stride,
                        const int32_t* lengths, int64_t seqs, int64_t tokens, int64_t kv_heads, int64_t row_bytes, int64_t page_size,

@@ -104,8 +104,9 @@ def paged_attention(q, k_pages, v_pages, tables, lengths, scale):
 
 # --- pages ----------------------------------------------------------------------------------------------------------
 
-def fork(pool, tables, lengths, refs, parents, grow):
-    """pool (layers, 2, pages, kv_heads, page_size, dim) is changed in place; returns (tables, lengths, refs, missing)."""
+def fork(pool, tables, lengths, refs, parents, grow, past_room=False):
+    """pool (layers, 2, pages, kv_heads, page_size, dim) is changed in place; returns (tables, lengths, refs, missing).  With
+    `past_room` lengths count what was wanted, not what the table holds."""
     n_old, width = tables.shape
     pages, page = pool.shape[2], pool.shape[4]
     held = [min(max(int(n), 0), width * page) for n in lengths]
@@ -123,7 +124,7 @@ def fork(pool, tables, lengths, refs, parents, grow):
         old = held[parent] if known else 0
         wanted = old + grow
         length = min(wanted, width * page)
-        new_lengths[i] = length
+        new_lengths[i] = wanted if past_room else length
         have, fill = -(-old // page), old % page
         copy = known and fill > 0 and parent in kept
         if known:

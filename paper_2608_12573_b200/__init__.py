@@ -29,7 +29,7 @@ EXPORTS = [
     "profk_logprobs_f32", "profk_logprobs_bf16", "profk_logprobs_f16", "profk_logprobs_backward_f32",
     "profk_logprobs_backward_bf16", "profk_logprobs_backward_f16",
     "profk_paged_attention_workspace_bytes", "profk_paged_attention_bf16", "profk_paged_attention_f16",
-    "profk_pages_fork_workspace_bytes", "profk_pages_fork", "profk_pages_compact_workspace_bytes", "profk_pages_compact",
+    "profk_pages_fork_workspace_bytes", "profk_pages_fork", "profk_pages_fork_ex", "profk_pages_compact_workspace_bytes", "profk_pages_compact",
     "profk_pages_copy", "profk_pages_append",
 ]
 

@@ -341,7 +341,14 @@ int profk_pages_fork_workspace_bytes(int64_t n_old, int64_t n, int64_t pages, in
 int profk_pages_fork(const profk_pool_t* pool, const int32_t* tables, int64_t n_old, int64_t width, int64_t table_stride, const int32_t* lengths,
                      const int32_t* refs, int64_t pages, const int32_t* parents, int64_t n, int64_t page_size, int64_t grow, void* workspace,
                      size_t workspace_bytes, void* stream, int32_t* out_tables, int32_t* out_lengths, int32_t* out_refs, int32_t* out_missing) {
-    if (!fork_sizes_ok(n_old, n, pages, page_size, grow) || !table_ok(width, page_size) || table_stride < 0 || !refs || !out_refs ||
+    return profk_pages_fork_ex(pool, tables, n_old, width, table_stride, lengths, refs, pages, parents, n, page_size, grow, 0, workspace, workspace_bytes, stream,
+                               out_tables, out_lengths, out_refs, out_missing);
+}
+
+int profk_pages_fork_ex(const profk_pool_t* pool, const int32_t* tables, int64_t n_old, int64_t width, int64_t table_stride, const int32_t* lengths,
+                        const int32_t* refs, int64_t pages, const int32_t* parents, int64_t n, int64_t page_size, int64_t grow, int flags, void* workspace,
+                        size_t workspace_bytes, void* stream, int32_t* out_tables, int32_t* out_lengths, int32_t* out_refs, int32_t* out_missing) {
+    if ((flags & ~PROFK_FORK_PAST_ROOM) != 0 || !fork_sizes_ok(n_old, n, pages, page_size, grow) || !table_ok(width, page_size) || table_stride < 0 || !refs || !out_refs ||
         out_refs == refs || !out_missing || (n_old > 0 && (!tables || !lengths)) || (n > 0 && (!parents || !out_tables || !out_lengths)) ||
         (n > 0 && (out_tables == tables || out_lengths == lengths)) || !pg_pool_ok(pool) || (pool && pool->page_size != page_size))
         return PROFK_EINVAL;
@@ -362,6 +369,7 @@ int profk_pages_fork(const profk_pool_t* pool, const int32_t* tables, int64_t n_
     p.pages = (int32_t)pages;
     p.page_size = (int32_t)page_size;
     p.grow = (int32_t)grow;
+    p.past_room = (flags & PROFK_FORK_PAST_ROOM) != 0;
     p.out_tables = out_tables;
     p.out_lengths = out_lengths;
     p.out_refs = out_refs;

@@ -247,10 +247,10 @@ profk_pool_t pool_of(const at::Tensor& t) {
     return profk_pool_t{t.data_ptr(), t.size(0), t.size(3), t.size(4), t.size(5) * b, t.stride(0) * b, t.stride(1) * b, t.stride(2) * b, t.stride(3) * b, t.stride(4) * b};
 }
 
-// (pool, tables, lengths, refs, parents, grow, page_size) -> (tables, lengths, refs, missing); page_size < 0: the pool's
+// (pool, tables, lengths, refs, parents, grow, page_size, past_room) -> (tables, lengths, refs, missing); page_size < 0: the pool's
 PyObject* pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     return guarded([&]() -> PyObject* {
-        need(n_args == 7, "pages_fork takes seven arguments");
+        need(n_args == 8, "pages_fork takes eight arguments");
         const at::Tensor* pool = optional(a[0], "pool");
         no_derivative(pool, "pool");
         const at::Tensor &tables = tensor(a[1], "tables"), &lengths = tensor(a[2], "lengths"), &refs = tensor(a[3], "refs"), &parents = tensor(a[4], "parents");
@@ -276,8 +276,8 @@ PyObject* pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         const at::Tensor ws = fresh({(int64_t)bytes}, at::kByte, dev), new_tables = fresh({n, width}, at::kInt, dev), new_lengths = fresh({n}, at::kInt, dev),
                          new_refs = fresh({pages}, at::kInt, dev), missing = fresh({}, at::kInt, dev);
         void* stream = c10::cuda::getCurrentCUDAStream(dev.index()).stream();
-        status(profk_pages_fork(pool ? &desc : nullptr, static_cast<const int32_t*>(tables.data_ptr()), n_old, width, stride, lengths_p, refs_p, pages, parents_p, n,
-                                page_size, grow, ws.data_ptr(), bytes, stream, static_cast<int32_t*>(new_tables.data_ptr()),
+        status(profk_pages_fork_ex(pool ? &desc : nullptr, static_cast<const int32_t*>(tables.data_ptr()), n_old, width, stride, lengths_p, refs_p, pages, parents_p, n,
+                                page_size, grow, a[7] == Py_True ? PROFK_FORK_PAST_ROOM : 0, ws.data_ptr(), bytes, stream, static_cast<int32_t*>(new_tables.data_ptr()),
                                 static_cast<int32_t*>(new_lengths.data_ptr()), static_cast<int32_t*>(new_refs.data_ptr()),
                                 static_cast<int32_t*>(missing.data_ptr())),
                "profk_pages_fork");

@@ -42,6 +42,7 @@ struct PgForkParams {
     const int32_t* refs;
     const int32_t* parents;
     int32_t n_old, n, width, pages, page_size, grow;
+    bool past_room;                       // lengths go on behind the table's end
     int32_t* out_tables;                  // n x width
     int32_t* out_lengths;
     int32_t* out_refs;
@@ -65,7 +66,7 @@ __device__ __forceinline__ int32_t pg_ceil(int64_t tokens, int32_t page_size) { 
 constexpr int PG_NEAR = 4096;             // old sequences whose children are counted in shared memory
 
 struct PgChild {
-    int32_t parent, old, length, have, want, fill, beyond;   // parent < 0: an empty sequence; beyond: pages past the table
+    int32_t parent, old, length, counted, have, want, fill, beyond;   // parent < 0: an empty sequence; beyond: pages past the table
     bool copy;
     __device__ __forceinline__ PgChild(const PgForkParams& p, int32_t i) : PgChild(p, i, p.first) {}
     __device__ __forceinline__ PgChild(const PgForkParams& p, int32_t i, const int32_t* first) {
@@ -74,6 +75,7 @@ struct PgChild {
         old = parent >= 0 ? pg_length(p.lengths, parent, p.width, p.page_size) : 0;
         const int64_t wanted = (int64_t)old + p.grow;
         length = (int32_t)min(wanted, (int64_t)p.width * p.page_size);
+        counted = p.past_room ? (int32_t)min(wanted, (int64_t)0x7FFFFFFF) : length;
         have = pg_ceil(old, p.page_size);
         want = pg_ceil(length, p.page_size);
         beyond = pg_ceil(wanted, p.page_size) - want;
@@ -139,7 +141,7 @@ __global__ void __launch_bounds__(PG_PLAN_THREADS) pages_fork_plan_kernel(const 
             const PgChild c(p, i, first);
             mine = (uint32_t)(c.want - c.fresh_from());
             beyond += (uint32_t)c.beyond;
-            p.out_lengths[i] = c.length;
+            p.out_lengths[i] = c.counted;
         }
         const uint32_t before = pg_scan(mine, warp_sums, &sum);
         if (i < p.n) p.need[i] = (int32_t)(total + before);
@@ -395,7 +397,9 @@ __global__ void __launch_bounds__(PG_THREADS) pages_copy_kernel(const PgCopyPara
     }
 }
 
-// Keys and values of the last `tokens` tokens of every sequence go to their places.
+// Keys and values of the last `tokens` tokens of every sequence go to their places.  Lengths are taken as they are: the tokens
+// of a sequence that has outgrown its table have none (taken into the table, they would overwrite its last tokens, in pages that
+// other sequences may hold).
 struct PgAppendParams {
     const char* k;                        // seqs x tokens x kv_heads rows; strides in bytes
     const char* v;
@@ -420,8 +424,9 @@ __global__ void __launch_bounds__(PG_THREADS) pages_append_kernel(const PgAppend
         const int32_t head = (int32_t)(rest % p.kv_heads);
         rest /= p.kv_heads;
         const int32_t tok = (int32_t)(rest % p.tokens), seq = (int32_t)(rest / p.tokens);
-        const int32_t at = pg_length(p.lengths, seq, p.width, p.page_size) - p.tokens + tok;
-        if (at < 0) continue;
+        const int64_t place = (int64_t)p.lengths[seq] - p.tokens + tok;
+        if (place < 0 || place >= (int64_t)p.width * p.page_size) continue;
+        const int32_t at = (int32_t)place;
         const int32_t page = p.tables[seq * p.table_stride + at / p.page_size], slot = at % p.page_size;
         if (page < 0 || page >= p.pages) continue;
         const uint4 k = *reinterpret_cast<const uint4*>(p.k + seq * p.k_seq + tok * p.k_tok + head * p.k_head + vec * 16);

@@ -115,13 +115,17 @@ class PagesCompacted(NamedTuple):
     live: torch.Tensor         # () int32
 
 
-def pages_fork(pool, tables, lengths, refs, parents, grow: int = 0, page_size: Optional[int] = None) -> PagesForked:
+def pages_fork(pool, tables, lengths, refs, parents, grow: int = 0, page_size: Optional[int] = None, past_room: bool = False) -> PagesForked:
     """`profk_pages_fork` on the current stream: new sequence i continues old sequence `parents[i]` (a negative number: an
     empty one) with room for `grow` more tokens.  Full pages are shared, a partly filled one stays with the first child and
     is copied for the others, sequences without a child are released.  Copies are made in `pool` ((layers, 2, pages,
     kv_heads, page_size, dim), any strides with dense rows; None with `page_size`: tables and counts only); tables, lengths
-    and counts come back new.  tables (n_old, width), lengths (n_old,), refs (pages,), parents (n,): int32."""
-    return PagesForked._make((_native or _load()).pages_fork(pool, tables, lengths, refs, parents, grow, -1 if page_size is None else page_size))
+    and counts come back new.  tables (n_old, width), lengths (n_old,), refs (pages,), parents (n,): int32.
+
+    A sequence whose table is full gets no longer, and appending to it all the same would write over its last tokens, which its
+    siblings share.  Where that can happen, `past_room=True` lets the lengths go on past the table's end, so that
+    `pages_append` passes over what has no place."""
+    return PagesForked._make((_native or _load()).pages_fork(pool, tables, lengths, refs, parents, grow, -1 if page_size is None else page_size, bool(past_room)))
 
 
 def pages_compact(pool, tables, refs) -> PagesCompacted:
@@ -138,7 +142,8 @@ def pages_copy(pool, src, dst) -> None:
 def pages_append(k_pages, v_pages, tables, lengths, k, v) -> None:
     """`profk_pages_append` on the current stream: writes `k`, `v` ((seqs, kv_heads, dim), or (seqs, tokens, kv_heads, dim)),
     the keys and values of every sequence's last token(s), to their places in one layer's pages (pages, kv_heads, page_size,
-    dim).  `lengths` counts the new tokens already (`pages_fork(grow=...)`)."""
+    dim).  `lengths` counts the new tokens already (`pages_fork(grow=...)`; with `past_room=True` where a table may be full);
+    tokens behind the table's end or on a page that is not there are passed over."""
     (_native or _load()).pages_append(k_pages, v_pages, tables, lengths, k, v)
 
 
