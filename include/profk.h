@@ -439,7 +439,8 @@ int profk_logprobs_f16(const void* logits, int64_t rows, int64_t V, int64_t row_
  *   grad_logprob (needs tokens), grad_entropy (needs entropy), grad_lse, grad_top (needs top_tokens)   each may be NULL: 0
  *   grad_logits   [device] rows x V elements of the logits' type, row stride grad_row_stride; may be `logits` itself only
  *                 if grad_row_stride == row_stride and neither grad_logprob nor grad_top is given (refused otherwise)
- * The sum is taken in fp32 and rounded once.  Rows with an infinite lse get zeros (see above); tokens outside [0, V) get nothing.
+ * The sum is taken in fp32 and rounded once.  Rows with an infinite lse get zeros (see above).  Tokens and alternatives
+ * outside [0, V) take no part, nor do their gradients (a list of alternatives may be filled up with -1).
  * Errors: PROFK_EINVAL, PROFK_ECUDA.
  */
 int profk_logprobs_backward_f32(const float* logits, int64_t rows, int64_t V, int64_t row_stride, double temperature,

@@ -58,6 +58,7 @@ def logprobs_gradient_row(x, temperature, token, g_lp, g_h, g_lse, top, g_top):
     if r["lse"] == NEG:
         return np.zeros(x.size), np.zeros(x.size)
     given = token is not None and 0 <= token < x.size
+    g_top = np.array([g if 0 <= i < x.size else 0.0 for i, g in zip(top, g_top)])     # a place without a token has no gradient
     g = (g_lp if given else 0.0) + float(np.sum(g_top)) - g_lse
     a = r["logp"]
     p = np.exp(a)

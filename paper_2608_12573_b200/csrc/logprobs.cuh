@@ -886,7 +886,10 @@ __global__ void __launch_bounds__(LG_THREADS) logprobs_grad_kernel(const LpGradP
     float g_sum = 0.f;
     if (p.g_top) {
         float g = 0.f;
-        for (uint32_t j = tid; j < p.k; j += LG_THREADS) g += p.g_top[row * p.k + j];
+        for (uint32_t j = tid; j < p.k; j += LG_THREADS) {
+            const int64_t i = p.top_tokens[row * p.k + j];
+            if (i >= 0 && i < (int64_t)p.V) g += p.g_top[row * p.k + j];           // (a place without a token has no gradient)
+        }
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) g += __shfl_xor_sync(FULL_MASK, g, d);
         if ((tid & 31) == 0) s_sum[tid >> 5] = g;

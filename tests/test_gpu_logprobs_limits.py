@@ -89,3 +89,25 @@ def test_rows_whose_scaled_logits_pass_the_range(dtype, temperature):
     grad = profk.logprobs_backward(x, r.lse, tokens, one, entropy=r.entropy, grad_entropy=one, grad_lse=one, top_tokens=r.top_tokens,
                                    grad_top=torch.ones(4, 4, device="cuda"), lse_rest=r.lse_rest, temperature=temperature)
     assert (grad[:3] == 0).all() and (grad[3] != 0).any() and torch.isfinite(grad[3]).all()
+
+
+# --- alternatives that are none --------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("k", [1, 3, 128])
+def test_gradient_of_places_without_a_token(dtype, k):
+    """A list of alternatives that is filled up with -1 (or names tokens outside the vocabulary): the same bits as with
+    gradients of zero there."""
+    vocab = 517
+    x = torch.randn(5, vocab, device="cuda").to(DTYPES[dtype])
+    r = profk.logprobs(x, k=k)
+    top, g_top = r.top_tokens.clone(), torch.randn(5, k, device="cuda")
+    none = torch.rand(5, k, device="cuda") < 0.4
+    none[0], none[1] = True, False
+    top[none] = -1
+    top[2][none[2]] = vocab
+    top[3][none[3]] = 1 << 40
+    zeroed = torch.where(none, torch.zeros_like(g_top), g_top)
+    got = profk.logprobs_backward(x, r.lse, top_tokens=top, grad_top=g_top, lse_rest=r.lse_rest)
+    want = profk.logprobs_backward(x, r.lse, top_tokens=r.top_tokens, grad_top=zeroed, lse_rest=r.lse_rest)
+    assert torch.equal(got, want) and (got[0] == 0).all() and (got[1] != 0).any()
