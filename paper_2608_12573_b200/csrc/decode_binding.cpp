@@ -13,6 +13,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <initializer_list>
+#include <stdexcept>
 #include <string>
 #include <utility>
 
@@ -21,6 +22,7 @@
 namespace {
 
 PyObject* g_error = nullptr;      // ProfkError
+PyObject* g_no_memory = nullptr;  // torch.OutOfMemoryError
 
 struct Refusal { std::string what; };
 [[noreturn]] void refuse(const std::string& what) { throw Refusal{what}; }
@@ -39,7 +41,7 @@ PyObject* guarded(F&& f) {
     } catch (const Refusal& r) {
         PyErr_SetString(g_error, r.what.c_str());
     } catch (const c10::OutOfMemoryError& e) {
-        PyErr_SetString(PyExc_MemoryError, e.what_without_backtrace());
+        PyErr_SetString(g_no_memory, e.what_without_backtrace());
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
     }
@@ -405,15 +407,21 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     });
 }
 
-PyObject* set_error(PyObject*, PyObject* type) {
-    Py_XINCREF(type);
-    Py_XSETREF(g_error, type);
-    Py_RETURN_NONE;
+// (ProfkError, torch.OutOfMemoryError): the exceptions to raise
+PyObject* set_errors(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (n != 2) throw std::invalid_argument("set_errors takes two arguments");
+        Py_INCREF(a[0]);
+        Py_XSETREF(g_error, a[0]);
+        Py_INCREF(a[1]);
+        Py_XSETREF(g_no_memory, a[1]);
+        return none();
+    });
 }
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {FAST(logprobs), FAST(logprobs_backward), FAST(pages_fork), FAST(pages_compact), FAST(pages_copy), FAST(pages_append), FAST(paged_attention),
-                           {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                           FAST(set_errors), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_decode", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

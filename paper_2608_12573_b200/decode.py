@@ -27,7 +27,7 @@ def _load():
         except ImportError as e:
             raise package.ProfkError(f"the extension module _decode cannot be loaded ({e}): run "
                                      "paper_2608_12573_b200._build.build() (there is no fallback implementation)") from e
-        _decode.set_error(package.ProfkError)
+        _decode.set_errors(package.ProfkError, torch.OutOfMemoryError)
         _native = _decode
     return _native
 
