@@ -27,6 +27,13 @@ def nvcc_command(extra: list[str] | None = None) -> list[str]:
     return cmd + (extra or []) + os.environ.get("PROFK_NVCC_FLAGS", "").split()
 
 
+def binding_for() -> str:
+    """What the binding is built against: it loads into this interpreter and this torch only."""
+    from importlib.metadata import version
+
+    return f"_decode for torch {version('torch')}, {sys.implementation.cache_tag}"
+
+
 def binding_command() -> list[str]:
     """g++ -> paper_2608_12573_b200/_decode.so, the CPython binding of the decoding operators over torch's tensors."""
     import sysconfig
@@ -35,6 +42,7 @@ def binding_command() -> list[str]:
     from torch.utils.cpp_extension import include_paths, library_paths
 
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f'-DPROFK_BINDING_FOR="{binding_for()}"',
            "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"]]
     cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
     cmd += [f"-I{p}" for p in include_paths() + [os.path.join(cuda, "include")]]
@@ -43,9 +51,16 @@ def binding_command() -> list[str]:
     return cmd
 
 
-def _build_binding(force: bool) -> None:
+def _binding_current() -> bool:
     deps = [BINDING_SOURCE, os.path.join(ROOT, "include", "profk.h")]
-    if not force and os.path.exists(BINDING_PATH) and os.path.getmtime(BINDING_PATH) >= max(os.path.getmtime(d) for d in deps):
+    if not os.path.exists(BINDING_PATH) or os.path.getmtime(BINDING_PATH) < max(os.path.getmtime(d) for d in deps):
+        return False
+    with open(BINDING_PATH, "rb") as f:
+        return binding_for().encode() + b"\0" in f.read()
+
+
+def _build_binding(force: bool) -> None:
+    if not force and _binding_current():
         return
     res = subprocess.run(binding_command(), capture_output=True, text=True)
     if res.returncode != 0:

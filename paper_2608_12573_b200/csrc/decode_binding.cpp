@@ -426,4 +426,8 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_decode", nullptr, -1, g_methods
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__decode(void) { return PyModule_Create(&g_module); }
+PyMODINIT_FUNC PyInit__decode(void) {
+    PyObject* m = PyModule_Create(&g_module);
+    if (m && PyModule_AddStringConstant(m, "built_for", PROFK_BINDING_FOR) != 0) Py_CLEAR(m);      // (the build looks for it in the file)
+    return m;
+}
