@@ -49,18 +49,17 @@ int sm_count() {
     return counts[dev];
 }
 
-// Allows `kernel` its dynamic shared memory (and clusters beyond 8 CTAs where asked) once per device.
+// Allows `kernel` its dynamic shared memory once per device.
 template <typename K>
-cudaError_t prepare_kernel(K* kernel, size_t smem, bool wide_cluster, uint64_t* done_mask, std::mutex* mutex) {
+cudaError_t prepare_kernel(K* kernel, size_t smem, uint64_t* done_mask, std::mutex* mutex) {
     int dev = 0;
     cudaError_t err = cudaGetDevice(&dev);
     if (err != cudaSuccess) return err;
     std::lock_guard<std::mutex> lock(*mutex);
     if (*done_mask >> dev & 1) return cudaSuccess;
     err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    // all of the SM's memory as shared memory: two CTAs have to fit
+    // all of the SM's memory as shared memory: its one CTA takes most of it
     if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-    if (err == cudaSuccess && wide_cluster) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (err == cudaSuccess) *done_mask |= 1ull << dev;
     return err;
 }
@@ -137,7 +136,7 @@ int lp_launch(LpParams p, int sms, void* stream) {
     static uint64_t done = 0;
     static std::mutex mutex;
     auto* kernel = logprobs_kernel<T, ENT, TOPK>;
-    DEC_TRY(prepare_kernel(kernel, lp_smem(LP_MAX_PARTS, LP_MAX_K), false, &done, &mutex));
+    DEC_TRY(prepare_kernel(kernel, lp_smem(LP_MAX_PARTS, LP_MAX_K), &done, &mutex));
     p.parts = lp_parts(kernel, p.rows, p.V, sizeof(T), TOPK, sms);
     for (p.parts_log2 = 0; (1u << p.parts_log2) < p.parts; ++p.parts_log2) {}
     const unsigned shares = std::max(1u, p.parts / LP_TEAMS);
@@ -205,7 +204,7 @@ template <typename T, int D, int N8>
 int pa_launch(const PaParams& p, unsigned ctas, void* stream) {
     static uint64_t done = 0;
     static std::mutex mutex;
-    DEC_TRY(prepare_kernel(paged_attention_kernel<T, D, N8>, PaShape<D>::SMEM, false, &done, &mutex));
+    DEC_TRY(prepare_kernel(paged_attention_kernel<T, D, N8>, PaShape<D>::SMEM, &done, &mutex));
     Launch l(ctas, PaShape<D>::THREADS, PaShape<D>::SMEM, stream);
     DEC_TRY(cudaLaunchKernelEx(&l.cfg, paged_attention_kernel<T, D, N8>, p));
     Launch j(ctas, PJ_THREADS, 0, stream);
@@ -378,8 +377,7 @@ int profk_pages_fork_ex(const profk_pool_t* pool, const int32_t* tables, int64_t
     p.first = reinterpret_cast<int32_t*>(take((size_t)n_old * 4));
     p.kids = reinterpret_cast<int32_t*>(take((size_t)n_old * 4));
     p.need = reinterpret_cast<int32_t*>(take((size_t)n * 4));
-    p.fresh_cap = (int32_t)fork_fresh(n, pages, page_size, grow);
-    p.fresh = reinterpret_cast<int32_t*>(take((size_t)p.fresh_cap * 4));
+    p.fresh = reinterpret_cast<int32_t*>(take((size_t)fork_fresh(n, pages, page_size, grow) * 4));
     p.moves = reinterpret_cast<PgMove*>(take((size_t)n * sizeof(PgMove)));
     p.pool = pg_pool(pool, page_size, PG_UNROLL_PIECES);
     const unsigned copiers = (unsigned)std::min<int64_t>(sms, (pages + PG_PLAN_THREADS - 1) / PG_PLAN_THREADS);

@@ -106,7 +106,6 @@ template <> struct Logit<__half> {
 };
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LN2 = 0.6931471805599453f;
 constexpr float LOWEST = -3.402823466e38f;      // start of a running maximum: finite, so that -inf - LOWEST is no NaN
 constexpr float FAR_BELOW = -1e28f;             // stands in for differences of -inf where they meet a factor of zero (times 2^31 still finite)
 

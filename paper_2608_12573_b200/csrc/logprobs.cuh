@@ -80,10 +80,10 @@ __device__ __forceinline__ LpStats lp_join(const LpStats& a, const LpStats& b, f
     return LpStats{m, fa * a.s + fb * b.s, fa * fmaf(da, a.s, a.t) + fb * fmaf(db, b.s, b.t)};
 }
 
-// What the streaming warps leave of a row for the finishing one; two of them, used in turn.
 // Bits that the number of any of the row's vectors takes.
 template <typename T> __device__ __forceinline__ uint32_t lp_note_bits(uint32_t V) { return 32 - __clz(V / Logit<T>::VEC | 1); }
 
+// What the streaming warps leave of a row for the finishing one; two of them, used in turn.
 struct LpRow {
     uint32_t note[LP_NOTES];              // vectors: numbers in the low `lp_note_bits`, above them the head of the largest element's order key
     LpStats stats[LP_STREAM_WARPS];
@@ -292,7 +292,7 @@ __device__ __forceinline__ uint32_t lp_fin_drop(uint32_t n, uint64_t limit, LpSh
     }
     return kept;
 }
-// Adds each lane's element if it has one; cuts back to the k best before the room runs out.
+// Adds each lane's element if it has one (lp_fin_vector leaves room for it).
 __device__ __forceinline__ uint32_t lp_fin_add(uint32_t n, bool has, float x, uint32_t idx, LpShared& sh) {
     const unsigned who = __ballot_sync(FULL_MASK, has);
     if (who == 0) return n;

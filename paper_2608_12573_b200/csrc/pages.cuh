@@ -52,7 +52,6 @@ struct PgForkParams {
     int32_t* kids;                        // n_old
     int32_t* need;                        // n: number of the sequence's first fresh page
     int32_t* fresh;                       // lowest free pages, ascending
-    int32_t fresh_cap;
     PgMove* moves;                        // n
     PgPool pool;
 };
