@@ -418,7 +418,8 @@ int profk_topk_noalloc_f32(const float* in, int64_t rows, int64_t N, int64_t k, 
  * a row makes its lse, log probabilities and entropy NaN; a NaN is never among the alternatives (places that nothing else
  * fills get token -1, log probability NaN).
  * The result does not depend on how a row is cut into parts except in the last bits of the sums; it is the same in every
- * call with the same arguments.  Errors: PROFK_EINVAL, PROFK_ECUDA.
+ * call with the same arguments.  Time with alternatives depends on the rows' order: rows in ascending order or of equal values
+ * are read a second time, by few threads (up to 30 times slower).  Errors: PROFK_EINVAL, PROFK_ECUDA.
  */
 int profk_logprobs_f32(const float* logits, int64_t rows, int64_t V, int64_t row_stride, const int64_t* tokens, int64_t k,
                        double temperature, void* stream, float* logprob, float* lse, float* lse_rest, float* entropy, float* top_logprobs,
@@ -542,7 +543,9 @@ int profk_pages_append(const void* k, const void* v, const int64_t* k_strides, c
  *   scale        > 0; it and its product with log2(e) normal fp32 numbers
  *   out          [device] seqs x heads x dim, dense, of the cache's type;  lse  [device] seqs x heads floats
  *   workspace    [device] profk_paged_attention_workspace_bytes(dim), 256-byte aligned
- * Statistics and sums are kept in fp32.  A sequence without tokens gets out = 0, lse = -inf.  The same call gives the same
+ * Statistics and sums are kept in fp32; weights enter the product with the values as two numbers of the cache's type (bf16: off by
+ * 2^-16 of each; fp16: by 2^-22 of it or 2^-39 of the largest).  More than 16 query heads to a key read the cache once for each
+ * 16.  A sequence without tokens gets out = 0, lse = -inf.  The same call gives the same
  * bits every time.  Errors: PROFK_EINVAL, PROFK_EWORKSPACE, PROFK_ECUDA.
  */
 int profk_paged_attention_workspace_bytes(int64_t dim, size_t* bytes /* [host] */);

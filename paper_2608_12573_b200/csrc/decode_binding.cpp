@@ -1,6 +1,6 @@
 // CPython binding of the decoding operators' C ABI (profk.h).  A decoding step makes these calls on small tensors, where
 // the caller's time is mostly argument handling: through ctypes and Python checks a call took 17-32 us on the host for
-// 8 us of device time, through this module 4-7.  It checks and marshals arguments and allocates outputs, nothing else;
+// 8 us of device time, through this module 7-10 with the Python call around it.  It checks and marshals arguments and allocates outputs, nothing else;
 // refusals are raised as the package's ProfkError.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>

@@ -10,19 +10,22 @@
 // by up to 2^32 and moved less often takes 1 % off the time of scoring, and 1e-6 of accuracy.)  T only enters as a factor of the
 // exponent: e^(z - m) = 2^((x - mx) log2(e) / T).
 //
-// What bounds it: fp32 the stream from HBM (2368 rows of 131072: 6.6 TB/s without alternatives, 6.5 with five); 16-bit types
-// have twice the exponentials per byte, and the unit that takes them (16 per SM and cycle) is 70 % busy at 5.8 TB/s, the
-// issue slots as much, whence the packed arithmetic, the one look per batch and thread, and everything rare out of the way.
-// The alternatives cost 28 % there for five of them, 60 % for twenty: the barrier of a row's first bound, and notes.  Steps on
-// the way for 2368 rows of bf16 with five: a barrier and a look at every element per batch 254 us, notes 158, one CTA per SM
-// 154, one look per batch 142, no 64-bit divisions 139, half warps' slots 137.
+// What bounds it: fp32 the stream from HBM (1184 rows of 131072: 98 us, 6.3 TB/s without alternatives, 6.1 with five); 16-bit
+// types have twice the exponentials per byte, and without alternatives the unit that takes them (16 per SM and cycle) is 70 %
+// busy (2368 rows of bf16: 105 us, 5.9 TB/s), the issue slots as much, whence the packed arithmetic, the one look per batch and
+// thread, and everything rare out of the way.  With five alternatives the same rows take 135 us, with twenty 168, and nothing is
+// saturated (unit 52 %, issue slots 65 %, DRAM 51 %): the warps wait for the barrier of each row's first bound, and notes.  Steps
+// on the way for five: a barrier and a look at every element per batch 254 us, notes 158, one CTA per SM 154, one look per batch
+// 142, no 64-bit divisions 139, half warps' slots 137.
 //
 // The k largest logits are found on the way.  Groups of lanes keep the largest logit that they have seen in a slot of
 // shared memory; the k-th largest slot is a bound that k elements of the row reach, so that only vectors whose maximum
 // reaches the bound can matter.  Their numbers are noted in a list, a few times k of them for a row in any ordinary order;
 // the bound is renewed whenever the number of batches has doubled, without a barrier: a stale slot only makes it lower.
 // At the end of the row those that still matter are read once more and their elements above the last bound are ordered.  Where
-// the list overflows all the same (ascending order, a flood of equal values) the whole row is read once more instead.
+// the list overflows all the same (ascending order, a flood of equal values, a hundred alternatives of a million tokens) the whole
+// row is read once more instead, by one warp, while the others wait: right, and slow (2368 rows of bf16 with five: 870 us where all
+// values are equal, 3000 in ascending order; 592 rows of 1048576 with 128: 945, with five 236).
 //
 // A CTA holds the whole SM and is two teams of twelve warps, each with rows of its own (or a part of a row each).  Eleven
 // warps of a team stream; the first, which the scheduler prefers, finishes rows (joins the statistics, orders the list,
@@ -48,7 +51,7 @@ constexpr int LP_THREADS = LP_TEAMS * LP_TEAM;
 constexpr int LP_UNROLL = 4;              // 16-byte vectors per thread and batch
 constexpr int LP_STAGES = 3;              // batches in flight or in hand per thread
 constexpr uint32_t LP_STEP = LP_STREAM * LP_UNROLL;     // vectors per batch
-constexpr uint32_t LP_NOTES = 2560;       // vectors the list holds (k = 128 of 131072 fp32: 1570 on average, 2420 at most in 1184 rows)
+constexpr uint32_t LP_NOTES = 2560;       // vectors the list holds (k = 128 of 131072 fp32, normal: 1570 on average, 2420 at most in 1184 rows)
 constexpr uint32_t LP_READ = 128;         // ... of which the finishing warp reads so many at a time
 constexpr uint32_t LP_FIN = 512;          // elements the finishing warp holds; more than half of them it cuts back
 constexpr uint32_t LP_MAX_K = 128;        // most alternatives
@@ -334,7 +337,7 @@ __device__ __forceinline__ uint32_t lp_fin_vector(uint32_t n, bool has, const ui
 // Drops the notes of vectors that cannot matter, most of them from the start of the row when the bound was low: the k-th largest
 // of the noted vectors' largest elements, rounded down to the bits that a note has of them, is a bound of its own.  Returns how many
 // remain.  (What is left out costs a read by latency each: k = 128 of 131072, 2368 rows bf16 329 -> 216 us, 1184 rows fp32
-// 371 -> 141; fewer notes than LP_READ are read at once, 1981 rows of 5946 bf16, k = 64: 48 us, thinned 56.)
+// 371 -> 141 to 171; fewer notes than LP_READ are read at once, 1981 rows of 5946 bf16, k = 64: 48 us, thinned 56.)
 __device__ __forceinline__ uint32_t lp_fin_thin(uint32_t notes, uint32_t k, uint32_t bits, float& bound, LpRow& r) {
     uint32_t top = 0;
     for (uint32_t i = lane_id(); i < notes; i += 32) top = max(top, r.note[i] >> bits);
@@ -835,7 +838,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
 // Gradient.  With upstream gradients g_lp (of the token's log probability), g_H, g_lse and g_j (of the alternatives'),
 //   dL/dx_v = (1/T) [ -p_v (G + g_H (ln p_v + H)) + g_lp 1[v = token] + sum_j g_j 1[v = i_j] ],   G = g_lp + sum_j g_j - g_lse,
 // p_v = e^(x_v / T - lse): one read and one write of the matrix; the picked entries are written again behind a barrier.
-// Bound by HBM: 4096 x 131072 bf16 (2.1 GB) in 334 us, 6.4 TB/s, a copy's rate; 256 threads with 64 bytes each in flight, a
+// Bound by HBM: 4096 x 131072 bf16 (2.1 GB) in 344 to 358 us, 6.0 to 6.2 TB/s, 0.92 to 0.95 of a copy's rate; 256 threads with 64 bytes each in flight, a
 // grid over chunks of rows.
 struct LpGradParams {
     const void* logits;

@@ -11,7 +11,9 @@
 //
 // A warp works by itself: its tiles come through a ring of its own in shared memory (cp.async, no barrier), and it
 // multiplies with the warp-level matrix instruction, tokens (and then dimensions) along its 16 rows and query heads along
-// its 8 columns: K Q^T, then V^T P^T.  The few heads that share a key are the narrow side of the product, far below the 128
+// its 8 columns: K Q^T, then V^T P^T.  More than 16 heads to a key take a pass over the key-value head for each 16, as tiles
+// of their own in other warps' shares, so that the cache is read again from L2 or HBM and the arithmetic, not HBM, is the bound
+// (16 sequences of 16384 tokens, one key-value head: 16 heads 50 us, 32 67, 64 108).  The few heads that share a key are the narrow side of the product, far below the 128
 // rows that a tcgen05 tile wants, and the tensor pipe is not what bounds it.
 #pragma once
 
@@ -22,7 +24,8 @@ namespace profk {
 constexpr int PA_SUB = 16;                              // tokens per step of the matrix instruction
 constexpr int PA_ROWS = 16;                             // most query heads per pass over a key-value head
 constexpr int PA_PACE = 4;                              // tiles between two barriers of a CTA, which keep its reads close together
-                                                        // (4 x 131072 tokens: 287 us; every 8, 16, 64 tiles: 292, 295, 301)
+                                                        // (4 x 131072 tokens: 287 us; every 8, 16, 64 tiles: 292, 295, 301;
+                                                        // 290 since a tile's products are summed apart)
 
 template <int D> struct PaShape {
     // One CTA per SM, 192 KB of rings.  A tile is 8 KB of keys and values or more: with 16 tokens of 64 dimensions at a time

@@ -146,7 +146,8 @@ __global__ void __launch_bounds__(PG_PLAN_THREADS) pages_fork_plan_kernel(const 
         if (i < p.n) p.need[i] = (int32_t)(total + before);
         total += sum;
     }
-    // the lowest-numbered free pages
+    // the lowest-numbered free pages, a walk by this CTA that ends with the last one needed (256 sequences: 15 us where the free
+    // pages lie low, 34 where they are the last of 100,000, 210 the last of a million)
     uint32_t found = 0;
     for (int32_t c0 = 0; c0 < p.pages && found < total; c0 += 4 * PG_PLAN_THREADS) {
         const int32_t at = c0 + 4 * tid;

@@ -83,7 +83,7 @@ def logprobs(logits, tokens=None, k: int = 0, temperature: float = 1.0, entropy:
     probable tokens of every row of `logits / temperature`, in one read of the logits.
 
     logits: CUDA tensor (..., V), float32, bfloat16 or float16, dense rows at any stride.  tokens: int64 (...), negative
-    where no token is given.  k <= 128 (`topk` selects more).  Differentiable in the logits (through `logprob`, `lse`,
+    where no token is given.  k <= 128 (`topk` selects more; rows in ascending order or of equal values are slow).  Differentiable in the logits (through `logprob`, `lse`,
     `entropy` and `top_logprobs`), once; see `profk.h` for masked, empty and NaN rows."""
     if isinstance(logits, torch.Tensor) and logits.requires_grad and torch.is_grad_enabled():
         return LogProbs._make(_LogProbsFunction.apply(logits, tokens, k, temperature, bool(entropy)))
@@ -152,5 +152,5 @@ def paged_attention(q, k_pages, v_pages, tables, lengths, scale: Optional[float]
 
     q (seqs, heads, dim), k_pages and v_pages (pages, kv_heads, page_size, dim), bfloat16 or float16, any strides with dense
     rows (a cache laid out tokens first is passed as `.transpose(1, 2)`); tables (seqs, width), lengths (seqs,) int32;
-    scale defaults to dim ** -0.5.  Returns (out (seqs, heads, dim), lse (seqs, heads) float32)."""
+    scale defaults to dim ** -0.5.  The cache is read once for up to 16 query heads to a key.  Returns (out (seqs, heads, dim), lse (seqs, heads) float32)."""
     return (_native or _load()).paged_attention(q, k_pages, v_pages, tables, lengths, scale)
