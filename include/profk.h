@@ -407,8 +407,9 @@ int profk_topk_noalloc_f32(const float* in, int64_t rows, int64_t N, int64_t k, 
  *                 ascending (profk_topk_* selects more of them)
  *   temperature   > 0; 1 / temperature and its product with log2(e) normal fp32 numbers (4.3e-39 to 8.5e37)
  *   logprob, lse  [device] rows floats (logprob NULL iff tokens is)
- *   lse_rest      [device] rows floats, or NULL: what the rounding of lse to fp32 left off.  The backward call takes the
- *                 probabilities from lse + lse_rest: beside a large maximum one float alone loses ln s
+ *   lse_rest      [device] rows floats, or NULL: what the rounding of lse to fp32 left off, for the backward call, which
+ *                 takes the probabilities from both: beside a large maximum one float alone loses ln s (from |lse| = 2^30 on
+ *                 it is ln s and a hint at the maximum, and no longer what lse is to be added to)
  *   entropy       [device] rows floats, or NULL: not computed
  *   top_logprobs, top_tokens   [device] rows x k floats / int64; NULL iff k = 0
  * All statistics are kept in fp32, sums relative to the row's largest logit.  -inf masks a token: probability 0, no part

@@ -34,6 +34,8 @@ bool factor_ok(double factor) {
     return f >= FLT_MIN && std::isfinite(f * LOG2E);
 }
 bool temperature_ok(double temperature) { return temperature > 0 && std::isfinite(temperature) && factor_ok(1.0 / temperature); }
+float scale_of(double temperature) { return (float)(1.0 / temperature); }
+float unscale_of(double temperature) { return (float)(1.0 / (double)scale_of(temperature)); }
 
 // Streaming multiprocessors of the current device; 0 on an error.
 int sm_count() {
@@ -156,7 +158,7 @@ int lp_forward(const T* logits, int64_t rows, int64_t V, int64_t row_stride, con
         return PROFK_EINVAL;
     const int sms = sm_count();
     if (sms < 1) return PROFK_ECUDA;
-    LpParams p{logits, rows, row_stride, (uint32_t)V, (uint32_t)k, 1u, 0u, (float)(1.0 / temperature), tokens, logprob, lse, lse_rest, entropy, top_logprobs, top_tokens};
+    LpParams p{logits, rows, row_stride, (uint32_t)V, (uint32_t)k, 1u, 0u, scale_of(temperature), unscale_of(temperature), tokens, logprob, lse, lse_rest, entropy, top_logprobs, top_tokens};
     if (entropy) return k ? lp_launch<T, true, true>(p, sms, stream) : lp_launch<T, true, false>(p, sms, stream);
     return k ? lp_launch<T, false, true>(p, sms, stream) : lp_launch<T, false, false>(p, sms, stream);
 }
@@ -176,7 +178,7 @@ int lp_backward(const T* logits, int64_t rows, int64_t V, int64_t row_stride, do
     const int64_t chunks = (V + chunk - 1) / chunk;
     if (rows * chunks > 0x7FFFFFFFll) return PROFK_EINVAL;
     LpGradParams p{logits, grad, rows, row_stride, grad_row_stride, (uint32_t)V, grad_top ? (uint32_t)k : 0u, (uint32_t)chunks, chunk,
-                   (float)(1.0 / temperature), tokens, lse, lse_rest, entropy, grad_logprob, grad_entropy, grad_lse, top_tokens, grad_top};
+                   scale_of(temperature), unscale_of(temperature), tokens, lse, lse_rest, entropy, grad_logprob, grad_entropy, grad_lse, top_tokens, grad_top};
     Launch l((unsigned)(rows * chunks), LG_THREADS, 0, stream);
     const bool shifted = (reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(grad)) % 16 != 0 ||
                          (rows > 1 && (row_stride - grad_row_stride) * (int64_t)sizeof(T) % 16 != 0);

@@ -63,7 +63,7 @@ struct LpParams {
     int64_t rows, row_stride;
     uint32_t V, k;
     uint32_t parts, parts_log2;           // teams that share a row: 1, or twice the CTAs of a cluster (a power of two)
-    float scale;                          // 1 / T
+    float scale, unscale;                 // 1 / T, and its reciprocal
     const int64_t* tokens;                // may be null
     float* logprob;
     float* lse;
@@ -74,6 +74,21 @@ struct LpParams {
 };
 
 struct LpStats { float m, s, t; };
+
+// lse in two floats.  `near` is its rounding, `rest` what that left off.  From 2^30 on that would be two things, the rounding of
+// max / T and ln s, and a float that holds the first (2^-24 of max / T) has no place for the second.  There rest is ln s, and its
+// last three bits say which float around near T the row's largest logit is (as many floats on as these bits, less 3), from which
+// the gradient then takes the exponents.  near T is off by three roundings and ln s, which is 3 floats at most.
+constexpr float LP_HUGE = 1073741824.f;
+__device__ __forceinline__ float lp_rest(float near, float m, float log_s, float scale, float unscale) {
+    if (isinf(near)) return 0.f;
+    if (!(fabsf(near) >= LP_HUGE)) return fmaf(m, scale, -near) + log_s;
+    const int on = __float_as_int(m) - __float_as_int(near * unscale);
+    return __int_as_float((__float_as_int(log_s) & ~7) | (min(max(on, -3), 3) + 3));
+}
+__device__ __forceinline__ float lp_max_of(float near, float rest, float unscale) {
+    return __int_as_float(__float_as_int(near * unscale) + (__float_as_int(rest) & 7) - 3);
+}
 
 // Both parts moved to the larger maximum; c = log2(e) / T.
 __device__ __forceinline__ LpStats lp_join(const LpStats& a, const LpStats& b, float c) {
@@ -537,7 +552,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) logprobs_kernel(const LpParams 
                     // lowest value), and with it the probabilities that the gradient takes from it
                     const float near = empty ? -INFINITY : fmaf(all.m, p.scale, log_s);
                     p.lse[row] = near;
-                    if (p.lse_rest) p.lse_rest[row] = isinf(near) ? 0.f : fmaf(all.m, p.scale, -near) + log_s;
+                    if (p.lse_rest) p.lse_rest[row] = lp_rest(near, all.m, log_s, p.scale, p.unscale);
                     if constexpr (ENT) p.entropy[row] = empty ? 0.f : log_s - p.scale * (all.t / all.s);
                     if (p.logprob) {
                         float lp = 0.f;                                           // no token given
@@ -846,7 +861,7 @@ struct LpGradParams {
     int64_t rows, row_stride, grad_stride;
     uint32_t V, k, chunks;               // chunks per row
     uint32_t chunk;                      // elements per chunk
-    float scale;
+    float scale, unscale;                // 1 / T, and its reciprocal
     const int64_t* tokens;               // the pointers below may be null, except lse
     const float* lse;
     const float* lse_rest;
@@ -861,18 +876,20 @@ struct LpGradParams {
 constexpr int LG_THREADS = 256;
 constexpr int LG_UNROLL = 4;
 
-struct LgRow { float lse, rest, whole, g_h; };      // lse in two floats; (G + g_H H) / T; g_H / T
+// ln p = (x - from) / T - lse - rest, and of that -rest log2(e); (G + g_H (H - rest)) / T; g_H / T
+struct LgRow { float from, lse, rest2, whole, g_h; };
 
 __device__ __forceinline__ float lg_dense(float x, const LgRow& r, float scale) {
-    const float a = fmaf(x, scale, -r.lse) - r.rest;
-    const float q = exp2_approx(a * LOG2E);
+    const float a = fmaf(x - r.from, scale, -r.lse);
+    const float q = exp2_approx(fmaf(a, LOG2E, r.rest2));
     return -q * fmaf(r.g_h, fmaxf(a, FAR_BELOW), r.whole);
 }
 
 // SHIFTED: the logits' rows start at other offsets within 16 bytes than the gradient's (a build of its own: its registers
-// would cost the other one an eighth of its threads, 2048 x 131072 bf16 175 us instead of 164).
+// would cost the other one an eighth of its threads, 2048 x 131072 bf16 175 us instead of 164; four CTAs of it to an SM, 1024 x
+// 131072 bf16 100 us, three 112).
 template <typename T, bool SHIFTED>
-__global__ void __launch_bounds__(LG_THREADS) logprobs_grad_kernel(const LpGradParams p) {
+__global__ void __launch_bounds__(LG_THREADS, SHIFTED ? 4 : 5) logprobs_grad_kernel(const LpGradParams p) {
     constexpr int VEC = Logit<T>::VEC, U = LG_UNROLL;
     __shared__ float s_sum[LG_THREADS / 32];
     const unsigned tid = threadIdx.x;
@@ -901,18 +918,23 @@ __global__ void __launch_bounds__(LG_THREADS) logprobs_grad_kernel(const LpGradP
     }
     LgRow r;
     r.lse = p.lse[row];
-    r.rest = p.lse_rest ? p.lse_rest[row] : 0.f;
+    float rest = p.lse_rest ? p.lse_rest[row] : 0.f;
     const float g_h = p.g_entropy ? p.g_entropy[row] : 0.f;
     const float whole = g_lp + g_sum - (p.g_lse ? p.g_lse[row] : 0.f);
-    r.whole = (whole + (p.g_entropy ? g_h * p.entropy[row] : 0.f)) * scale;
-    r.g_h = g_h * scale;
     const bool empty = isinf(r.lse);                       // nothing but -inf in the row, or more than fp32 holds: no gradient
+    const bool huge = p.lse_rest && fabsf(r.lse) >= LP_HUGE;                      // see lp_rest
+    r.from = huge && !empty ? lp_max_of(r.lse, rest, p.unscale) : 0.f;
+    r.lse = empty ? INFINITY : huge ? rest : r.lse;        // (empty: a is -inf for every element, its exponential and the factors 0)
+    rest = huge ? 0.f : rest;
+    r.rest2 = -rest * LOG2E;
+    r.whole = empty ? 0.f : (whole + (p.g_entropy ? g_h * (p.entropy[row] - rest) : 0.f)) * scale;
+    r.g_h = empty ? 0.f : g_h * scale;
 
     const uint32_t e0 = chunk * p.chunk, e1 = min(p.V, e0 + p.chunk);
     // Vectors are those of the gradient's rows; where the logits' rows start at another offset, each is put together from two
     // of theirs (2048 x 131072 bf16, logits one element off: 190 us, and 771 element by element).
     const uint32_t mis = (uint32_t)(reinterpret_cast<uintptr_t>(y + e0) & 15u);
-    auto scalar = [&](uint32_t i) { y[i] = Logit<T>::from_float(empty ? 0.f : lg_dense(Logit<T>::to_float(x[i]), r, scale)); };
+    auto scalar = [&](uint32_t i) { y[i] = Logit<T>::from_float(lg_dense(Logit<T>::to_float(x[i]), r, scale)); };
     const uint32_t head = min(e1, e0 + (mis ? (16u - mis) / (uint32_t)sizeof(T) : 0u));
     const uint32_t nvec = (e1 - head) / VEC, tail = head + nvec * VEC;
     if (e0 + tid < head) scalar(e0 + tid);
@@ -921,7 +943,7 @@ __global__ void __launch_bounds__(LG_THREADS) logprobs_grad_kernel(const LpGradP
         float f[VEC];
         Logit<T>::unpack(in, f);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) f[j] = empty ? 0.f : lg_dense(f[j], r, scale);
+        for (int j = 0; j < VEC; ++j) f[j] = lg_dense(f[j], r, scale);
         st_stream_u4(y + head + (size_t)v * VEC, Logit<T>::pack(f));
     };
     if constexpr (!SHIFTED) {

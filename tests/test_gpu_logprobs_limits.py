@@ -111,3 +111,72 @@ def test_gradient_of_places_without_a_token(dtype, k):
     got = profk.logprobs_backward(x, r.lse, top_tokens=top, grad_top=g_top, lse_rest=r.lse_rest)
     want = profk.logprobs_backward(x, r.lse, top_tokens=r.top_tokens, grad_top=zeroed, lse_rest=r.lse_rest)
     assert torch.equal(got, want) and (got[0] == 0).all() and (got[1] != 0).any()
+
+
+# --- logits far from zero --------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("temperature", [1.0, 1.3, 5.0, 0.9999])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_gradient_of_logits_far_from_zero(dtype, temperature, offset):
+    """Rows whose largest logits are large and tied: the gradient is that of the tied tokens, at any temperature.  Log
+    probabilities are exact to 2^-22 of themselves here (ln s to three bits less than a float), 12 * 2^-20 at most, and the
+    logits' differences times 1 / temperature to 2^-23 of themselves: 2e-5 of a probability's part, with the entropy's factor of
+    12 besides; and half a unit in the last place."""
+    vocab, info = 5003, torch.finfo(DTYPES[dtype])
+    values = [v for v in (info.min, info.max, -1e30, 3e20, -1e12, 2.5e9, -1.3e9, 9e8, -6e4, 2e3) if info.min <= v <= info.max]
+    if temperature < 1:
+        values = [v for v in values if abs(v) < 1e38]
+    x = torch.empty(len(values), vocab + 1, dtype=DTYPES[dtype], device="cuda")[:, offset:offset + vocab]
+    for row, v in enumerate(values):
+        x[row] = v                                            # everything tied, then a part of it masked or below
+        x[row, 100 + 400 * row:] = -float("inf") if row % 2 or v == info.min else v - abs(v) * 2.0 ** -6
+        x[row, 7:40:3] = -float("inf")
+    rows = len(values)
+    tokens = torch.arange(rows, device="cuda")
+    up = torch.randn(3, rows, device="cuda")
+    k = 3
+    g_top = torch.randn(rows, k, device="cuda")
+    r = profk.logprobs(x, tokens, k=k, temperature=temperature)
+    args = dict(entropy=r.entropy, grad_entropy=up[1].contiguous(), grad_lse=up[2].contiguous(), top_tokens=r.top_tokens, grad_top=g_top, lse_rest=r.lse_rest,
+                temperature=temperature)
+    got = profk.logprobs_backward(x, r.lse, tokens, up[0].contiguous(), **args).double()
+    z = x.double() / temperature
+    d = z - z.amax(1, keepdim=True)
+    logp = d - torch.exp(d).sum(1, keepdim=True).log()
+    p = torch.exp(logp)
+    entropy = torch.special.entr(p).sum(1, keepdim=True)
+    one = torch.zeros_like(z)
+    one[tokens, tokens] += up[0].double()
+    one.scatter_add_(1, r.top_tokens, g_top.double())
+    inner = one.sum(1, keepdim=True) - up[2].double()[:, None]
+    safe = torch.where(p > 0, logp, 0.0)
+    want = (one - p * (inner + up[1].double()[:, None] * (safe + entropy))) / temperature
+    size = p * (up[0].abs() + up[2].abs() + g_top.abs().sum(1) + 12 * up[1].abs()).double()[:, None] / temperature
+    allowed = 2e-5 * size + 2.0 ** -22 * want.abs() + 0.5 * info.eps * want.abs() + (2.0 ** -25 if dtype == "f16" else 1e-38)
+    assert ((got - want).abs() <= allowed).all(), ((got - want).abs() - allowed).amax(1)
+    if temperature == 1.0:                                    # in place of the logits, without picked entries
+        args = dict(rest=r.lse_rest, entropy=r.entropy, g_entropy=up[1].contiguous(), g_lse=up[2].contiguous())
+        out = torch.empty(rows, vocab + 1, dtype=x.dtype, device="cuda")[:, offset:offset + vocab]
+        assert _backward(x, out, r.lse, **args) == 0 and _backward(x, x, r.lse, **args) == 0
+        assert torch.equal(x, out)
+
+
+def test_gradient_of_neighbouring_logits_far_from_zero():
+    """Two fp32 logits that differ in their last bit, 1e13 from zero: the smaller one's probability is 0, whatever the
+    temperature rounds their quotients to."""
+    rng = torch.Generator().manual_seed(5)
+    rows, vocab = 400, 33
+    big = (torch.rand(rows, generator=rng) + 1) * 2.0 ** torch.randint(40, 120, (rows,), generator=rng)
+    big = torch.where(torch.rand(rows, generator=rng) < 0.5, big, -big)
+    x = torch.full((rows, vocab), -float("inf"))
+    x[:, 3], x[:, 20] = big, torch.nextafter(big, torch.full_like(big, -float("inf")))
+    x[:, 30] = big
+    x = x.cuda()
+    g = torch.ones(rows, device="cuda")
+    for temperature in (1.1, 1.7, 3.0, 0.77):
+        r = profk.logprobs(x, temperature=temperature)
+        got = profk.logprobs_backward(x, r.lse, grad_lse=g, lse_rest=r.lse_rest, temperature=temperature)       # the probabilities / temperature
+        want = torch.zeros(rows, vocab, device="cuda")
+        want[:, [3, 30]] = 0.5 / temperature
+        assert (got - want).abs().max() < 1e-5
