@@ -562,6 +562,101 @@ int profk_paged_attention_f16(const void* q, int64_t q_seq_stride, int64_t q_hea
                               void* stream, void* out, float* lse);
 
 /*
+ * PROMPTS AND DRAFTS.  What takes several new tokens of a sequence at a time into the loop above: their positions, their
+ * places in the cache, their attention, and the rules that a sampler lays over the logits behind them.
+ */
+
+/* How heads are turned: pair i of the first 2 * pairs elements (elements i and pairs + i, or 2 i and 2 i + 1 if interleaved) by
+ * position * frequencies[i] radians. */
+typedef struct profk_rotary {
+    const double* frequencies;            /* [device] `pairs` finite numbers, radians per position */
+    int64_t pairs;                        /* 1 .. 512, 2 * pairs <= dim */
+    int interleaved, inverse;             /* inverse: by the negative angle */
+    double magnitude;                     /* times cosine and sine */
+} profk_rotary_t;
+
+/*
+ * Rotary positions:  y_1 = m (x_1 cos a - x_2 sin a),  y_2 = m (x_2 cos a + x_1 sin a);  the rest of a head is copied bit for bit.
+ * Called with `inverse` on the upstream gradient it gives the gradient.
+ *   x            [device] outer x inner rows of `heads` heads of dim <= 1024 elements; strides [host] three, in elements: outer,
+ *                inner, head; any alignment of the elements (16-byte vectors where addresses, strides and parts of a head allow)
+ *   positions    [device] int64, any sign; position_strides [host] two: outer, inner
+ *   out          [device] outer x inner x heads x dim, dense; must not overlap x
+ * Angles are products of 64-bit integers (fractions of a turn), off by |position| * 2^-56 turns; cosine, sine and the sums are fp32,
+ * rounded once.  Errors: PROFK_EINVAL, PROFK_ECUDA.
+ */
+int profk_rotary_f32(const void* x, int64_t outer, int64_t inner, int64_t heads, int64_t dim, const int64_t* strides, const int64_t* positions,
+                     const int64_t* position_strides, const profk_rotary_t* how, void* stream, void* out);
+int profk_rotary_bf16(const void* x, int64_t outer, int64_t inner, int64_t heads, int64_t dim, const int64_t* strides, const int64_t* positions,
+                     const int64_t* position_strides, const profk_rotary_t* how, void* stream, void* out);
+int profk_rotary_f16(const void* x, int64_t outer, int64_t inner, int64_t heads, int64_t dim, const int64_t* strides, const int64_t* positions,
+                     const int64_t* position_strides, const profk_rotary_t* how, void* stream, void* out);
+
+/*
+ * profk_pages_append with the turn on the way: the queries and keys of new tokens are turned, keys and values go to their places
+ * in one layer's pages, queries to out_q.
+ *   q, k, v      [device] rows of `heads` / kv_heads heads of dim elements; *_strides [host] three each, in elements: sequence, token,
+ *                head.  q NULL (then heads = 0 and out_q NULL): keys and values only
+ *   starts       [device] seqs + 1 int32, ascending: sequence s has the rows [starts[s], starts[s + 1]) (the sequence stride is not
+ *                used).  NULL: rows / seqs rows each
+ *   lengths      [device] seqs: tokens held, the new ones among them, which are the last.  As they are: tokens before place 0, at or
+ *                behind width * page_size or on a page that is not there are turned, but have no place
+ *   positions    [device] int64, two strides (sequence, token); NULL: a token's place in its sequence
+ *   kp, vp       [host] strides of the pages, in elements
+ *   out_q        [device] rows x heads x dim, dense.  Rows that no sequence holds come back as zeros
+ * No two sequences may write to one page; outputs must not overlap inputs.  Errors: PROFK_EINVAL, PROFK_ECUDA.
+ */
+int profk_pages_append_rotary_f32(const void* q, const int64_t* q_strides, const void* k, const int64_t* k_strides, const void* v, const int64_t* v_strides,
+                                  void* k_pages, void* v_pages, const profk_page_strides_t* kp, const profk_page_strides_t* vp, const int32_t* tables,
+                                  int64_t table_stride, const int32_t* lengths, const int32_t* starts, int64_t seqs, int64_t rows, int64_t heads,
+                                  int64_t kv_heads, int64_t dim, int64_t page_size, int64_t pages, int64_t width, const int64_t* positions,
+                                  const int64_t* position_strides, const profk_rotary_t* how, void* stream, void* out_q);
+int profk_pages_append_rotary_bf16(const void* q, const int64_t* q_strides, const void* k, const int64_t* k_strides, const void* v, const int64_t* v_strides,
+                                  void* k_pages, void* v_pages, const profk_page_strides_t* kp, const profk_page_strides_t* vp, const int32_t* tables,
+                                  int64_t table_stride, const int32_t* lengths, const int32_t* starts, int64_t seqs, int64_t rows, int64_t heads,
+                                  int64_t kv_heads, int64_t dim, int64_t page_size, int64_t pages, int64_t width, const int64_t* positions,
+                                  const int64_t* position_strides, const profk_rotary_t* how, void* stream, void* out_q);
+int profk_pages_append_rotary_f16(const void* q, const int64_t* q_strides, const void* k, const int64_t* k_strides, const void* v, const int64_t* v_strides,
+                                  void* k_pages, void* v_pages, const profk_page_strides_t* kp, const profk_page_strides_t* vp, const int32_t* tables,
+                                  int64_t table_stride, const int32_t* lengths, const int32_t* starts, int64_t seqs, int64_t rows, int64_t heads,
+                                  int64_t kv_heads, int64_t dim, int64_t page_size, int64_t pages, int64_t width, const int64_t* positions,
+                                  const int64_t* position_strides, const profk_rotary_t* how, void* stream, void* out_q);
+
+/* What is laid over a row of logits.  Strides in elements, between rows; 0: one for all. */
+typedef struct profk_adjust {
+    const int64_t* tokens;                /* [device] rows x history: prompt, then answer; NULL iff history = 0.  Tokens outside [0, V) are passed over */
+    int64_t history, token_stride;        /* history < 2^30 */
+    const int32_t* lengths;               /* [device] rows: how many of them count (taken into [0, history]); NULL: all */
+    const int32_t* prompts;               /* [device] rows: how many of those are prompt; NULL: none */
+    const float* repetition;              /* [device] rows, > 0; NULL: repetition_value */
+    const float* frequency;               /* ... frequency_value */
+    const float* presence;                /* ... presence_value */
+    double repetition_value, frequency_value, presence_value;
+    const int64_t* bias_tokens;           /* [device] rows x biases; NULL iff biases = 0.  Tokens outside [0, V) are passed over */
+    const float* bias_values;
+    int64_t biases;                       /* <= 8192 */
+    int64_t bias_token_stride, bias_value_stride;
+    const uint32_t* mask;                 /* [device] rows x ceil(V / 32): bit (v % 32) of word v / 32 is set iff token v is allowed; NULL: all are */
+    int64_t mask_stride;
+} profk_adjust_t;
+
+/*
+ * Penalties for repeated tokens, biases and masks.  For token v with logit x that occurs c times in the answer:
+ *   y = x > 0 ? x / repetition : x * repetition   if v occurs in prompt or answer, else x;
+ *   y = y - (frequency * c + presence)            if c > 0;
+ *   y = y + (sum of v's biases, in the list's order);   -inf where v is not allowed.
+ *   logits       [device] rows x V elements, row r at logits + r * row_stride (row_stride >= V), any element alignment
+ *   out          [device] likewise; may be `logits` itself (with its stride): only vectors that change are read and written then
+ * In fp32, rounded once; logits that nothing applies to keep their bits.  Same bits in every call.  Errors: PROFK_EINVAL, PROFK_ECUDA.
+ */
+int profk_adjust_logits_f32(const void* logits, int64_t rows, int64_t V, int64_t row_stride, const profk_adjust_t* how, void* stream, void* out,
+                            int64_t out_row_stride);
+int profk_adjust_logits_bf16(const void* logits, int64_t rows, int64_t V, int64_t row_stride, const profk_adjust_t* how, void* stream, void* out,
+                            int64_t out_row_stride);
+int profk_adjust_logits_f16(const void* logits, int64_t rows, int64_t V, int64_t row_stride, const profk_adjust_t* how, void* stream, void* out,
+                            int64_t out_row_stride);
+
+/*
  * Copies the statistics of the last call that used the registered workspace to
  * the host and waits for `stream`.  out: [host] rows entries.  Every wait inside
  * the kernels is bounded (the grid barriers of the exact-selection and large-k

@@ -1,12 +1,8 @@
 // C ABI of the operators around a selection in a decoding loop (see profk.h): argument checks, launch shapes, launches.
-#include <cuda_runtime.h>
-
 #include <algorithm>
-#include <cfloat>
-#include <cmath>
 #include <cstring>
-#include <mutex>
 
+#include "decode_host.cuh"
 #include "logprobs.cuh"
 #include "paged_attention.cuh"
 #include "pages.cuh"
@@ -16,76 +12,9 @@ using namespace profk;
 
 namespace {
 
-#define DEC_TRY(expr)                                                     \
-    do {                                                                  \
-        if ((expr) != cudaSuccess) { (void)cudaGetLastError(); return PROFK_ECUDA; } \
-    } while (0)
-
-constexpr int MAX_DEVICES = 64;
-constexpr int64_t MAX_PAGE_SIZE = 1 << 24, MAX_TOKENS = 0x7FFFFF00ll;      // of a page, of a sequence
-
-// Whether a table of `width` entries and pages of `page_size` tokens are within what the kernels count (no product wraps).
-bool table_ok(int64_t width, int64_t page_size) { return page_size >= 1 && page_size <= MAX_PAGE_SIZE && width >= 1 && width <= MAX_TOKENS / page_size; }
-
-// Whether the kernels can work with a factor of the exponents: it and its product with log2(e) are normal fp32 numbers (a
-// factor of zero would make masked elements NaN, an infinite one all that equal the maximum).
-bool factor_ok(double factor) {
-    const float f = (float)factor;
-    return f >= FLT_MIN && std::isfinite(f * LOG2E);
-}
 bool temperature_ok(double temperature) { return temperature > 0 && std::isfinite(temperature) && factor_ok(1.0 / temperature); }
 float scale_of(double temperature) { return (float)(1.0 / temperature); }
 float unscale_of(double temperature) { return (float)(1.0 / (double)scale_of(temperature)); }
-
-// Streaming multiprocessors of the current device; 0 on an error.
-int sm_count() {
-    static int counts[MAX_DEVICES];
-    static std::mutex mutex;
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) { (void)cudaGetLastError(); return 0; }
-    std::lock_guard<std::mutex> lock(mutex);
-    if (counts[dev] == 0 && cudaDeviceGetAttribute(&counts[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return 0;
-    }
-    return counts[dev];
-}
-
-// Allows `kernel` its dynamic shared memory once per device.
-template <typename K>
-cudaError_t prepare_kernel(K* kernel, size_t smem, uint64_t* done_mask, std::mutex* mutex) {
-    int dev = 0;
-    cudaError_t err = cudaGetDevice(&dev);
-    if (err != cudaSuccess) return err;
-    std::lock_guard<std::mutex> lock(*mutex);
-    if (*done_mask >> dev & 1) return cudaSuccess;
-    err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    // all of the SM's memory as shared memory: its one CTA takes most of it
-    if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-    if (err == cudaSuccess) *done_mask |= 1ull << dev;
-    return err;
-}
-
-struct Launch {
-    cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute attrs[2];
-    Launch(unsigned grid, unsigned block, size_t smem, void* stream, unsigned cluster = 1) {
-        cfg.gridDim = dim3(grid);
-        cfg.blockDim = dim3(block);
-        cfg.dynamicSmemBytes = smem;
-        cfg.stream = (cudaStream_t)stream;
-        attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attrs[0].val.programmaticStreamSerializationAllowed = 1;
-        cfg.attrs = attrs;
-        cfg.numAttrs = 1;
-        if (cluster > 1) {
-            attrs[1].id = cudaLaunchAttributeClusterDimension;
-            attrs[1].val.clusterDim.x = cluster;
-            attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
-            cfg.numAttrs = 2;
-        }
-    }
-};
 
 // ---- log probabilities -----------------------------------------------------------------------
 
@@ -226,7 +155,6 @@ int32_t log2_of(int64_t n) {      // -1: no power of two
 }
 // Whether a page's tokens lie within 2^32 bytes (of two-byte elements) behind the first.
 bool spans_32_bits(int64_t page_size, int64_t token) { return token >= 0 && token <= (0xFFFFFFFFll / 2) / (page_size + PA_SUB); }
-bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 template <typename T>
 int pa_run(const T* q, int64_t q_seq, int64_t q_head, const T* k, const T* v, const profk_page_strides_t* ks, const profk_page_strides_t* vs,

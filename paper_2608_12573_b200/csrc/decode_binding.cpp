@@ -12,6 +12,8 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <array>
+#include <cmath>
 #include <initializer_list>
 #include <stdexcept>
 #include <string>
@@ -407,6 +409,217 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     });
 }
 
+// ---- prompts and drafts ----------------------------------------------------------------------
+
+using Strides3 = std::array<int64_t, 3>;
+
+int64_t stride_of(const at::Tensor& t, int64_t d) { return t.size(d) > 1 ? t.stride(d) : 0; }
+
+const double* frequencies_of(const at::Tensor& t, c10::Device device) {
+    no_derivative(&t, "frequencies");
+    need(t.is_cuda() && t.device() == device && t.scalar_type() == at::kDouble && t.dim() == 1 && t.numel() > 0 && t.is_contiguous(),
+         "frequencies must be a contiguous float64 tensor of one dimension on the same device");
+    return static_cast<const double*>(t.data_ptr());
+}
+
+// (x, positions, frequencies, interleaved, magnitude, inverse) -> turned
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+    return guarded([&]() -> PyObject* {
+        need(n_args == 6, "rotary takes six arguments");
+        const at::Tensor &x = tensor(a[0], "x"), &positions = tensor(a[1], "positions"), &frequencies = tensor(a[2], "frequencies");
+        no_derivative(&x, "x");
+        need(x.is_cuda() && x.dim() >= 2, "x must be a CUDA tensor (..., heads, dim)");
+        const int type = dtype_index(x.scalar_type());
+        const c10::Device dev = x.device();
+        need(x.numel() == 0 || dense_rows(x), "x must have dense heads");
+        need(positions.is_cuda() && positions.device() == dev && positions.scalar_type() == at::kLong && positions.dim() <= x.dim() - 2,
+             "positions must be an int64 tensor that broadcasts to x's leading dimensions, on the same device");
+        const double magnitude = real(a[4], "magnitude");
+        profk_rotary_t how{frequencies_of(frequencies, dev), frequencies.numel(), a[3] == Py_True, a[5] == Py_True, magnitude};
+        // the leading dimensions as two evenly spaced levels, of x and positions alike
+        int64_t sizes[2] = {1, 1}, xs[2] = {0, 0}, ps[2] = {0, 0};
+        int level = 2;
+        for (int64_t d = x.dim() - 3; d >= 0; --d) {
+            const int64_t pd = d - (x.dim() - 2 - positions.dim()), n = x.size(d);
+            need(pd < 0 || positions.size(pd) == n || positions.size(pd) == 1, "positions must be an int64 tensor that broadcasts to x's leading dimensions, on the same device");
+            if (n == 1) continue;
+            const int64_t x_step = x.stride(d), p_step = pd >= 0 && positions.size(pd) > 1 ? positions.stride(pd) : 0;
+            if (level < 2 && x_step == xs[level] * sizes[level] && p_step == ps[level] * sizes[level]) {
+                sizes[level] *= n;
+                continue;
+            }
+            need(--level >= 0, "x: the leading dimensions must be evenly spaced on two levels at most");
+            sizes[level] = n;
+            xs[level] = x_step;
+            ps[level] = p_step;
+        }
+        const c10::cuda::CUDAGuard guard(dev);
+        const at::Tensor out = fresh(x.sizes(), x.scalar_type(), dev);
+        if (x.numel() == 0) return wrap(out);
+        const int64_t strides[3] = {xs[0], xs[1], stride_of(x, x.dim() - 2)};
+        auto* call = type == 0 ? &profk_rotary_f32 : type == 1 ? &profk_rotary_bf16 : &profk_rotary_f16;
+        status(call(x.data_ptr(), sizes[0], sizes[1], x.size(-2), x.size(-1), strides, static_cast<const int64_t*>(positions.data_ptr()), ps, &how,
+                    c10::cuda::getCurrentCUDAStream(dev.index()).stream(), out.data_ptr()),
+               "profk_rotary");
+        return wrap(out);
+    });
+}
+
+// The rows of new tokens: (seqs, [tokens,] heads, dim), or (rows, heads, dim) where `starts` tells the sequences apart.
+struct NewRows {
+    int64_t rows;
+    c10::SmallVector<int64_t, 4> lead;                       // leading dimensions
+    const int32_t* starts;
+};
+NewRows new_rows(const at::Tensor& t, const char* what, const at::Tensor* starts, int64_t seqs, c10::Device device) {
+    if (starts) {
+        need(t.dim() == 3, "with starts, rows of new tokens must be of shape (rows, heads, dim)");
+        const int32_t* p = ints(*starts, "starts", 1, device);
+        need(starts->size(0) == seqs + 1, "starts must have one entry more than there are sequences");
+        return {t.size(0), {t.size(0)}, p};
+    }
+    if (!((t.dim() == 3 || t.dim() == 4) && t.size(0) == seqs)) refuse(std::string(what) + " must be of shape (seqs, [tokens,] heads, dim), one sequence per row of the tables");
+    if (t.dim() == 3) return {seqs, {seqs}, nullptr};
+    return {seqs * t.size(1), {seqs, t.size(1)}, nullptr};
+}
+Strides3 row_strides(const at::Tensor& t, bool ragged) {
+    if (ragged) return {0, stride_of(t, 0), stride_of(t, 1)};
+    if (t.dim() == 3) return {stride_of(t, 0), 0, stride_of(t, 1)};
+    return {stride_of(t, 0), stride_of(t, 1), stride_of(t, 2)};
+}
+
+// (k_pages, v_pages, tables, lengths, q, k, v, frequencies, starts, positions, interleaved, magnitude) -> turned q
+PyObject* pages_append_rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+    return guarded([&]() -> PyObject* {
+        need(n_args == 12, "pages_append_rotary takes twelve arguments");
+        const at::Tensor &kp = tensor(a[0], "k_pages"), &vp = tensor(a[1], "v_pages"), &tables = tensor(a[2], "tables"), &lengths = tensor(a[3], "lengths"),
+                         &k = tensor(a[5], "k"), &v = tensor(a[6], "v"), &frequencies = tensor(a[7], "frequencies");
+        const at::Tensor *q = optional(a[4], "q"), *starts = optional(a[8], "starts"), *positions = optional(a[9], "positions");
+        const double magnitude = real(a[11], "magnitude");
+        for (const auto& [t, what] : {std::pair{&kp, "k_pages"}, {&vp, "v_pages"}, {&k, "k"}, {&v, "v"}}) no_derivative(t, what);
+        no_derivative(q, "q");
+        pages_pair(kp, vp);
+        const c10::Device dev = kp.device();
+        const int type = dtype_index(kp.scalar_type());
+        const int64_t stride = table_stride(tables, dev), seqs = tables.size(0), width = tables.size(1);
+        const int32_t* lengths_p = ints(lengths, "lengths", 1, dev);
+        need(lengths.size(0) == seqs, "tables and lengths must have the same number of sequences");
+        const NewRows rows = new_rows(k, "k", starts, seqs, dev);
+        const int64_t d = k.dim();
+        need(k.sizes() == v.sizes() && k.size(d - 2) == kp.size(1) && k.size(d - 1) == kp.size(3), "k and v must be alike, with the pages' kv_heads and dim");
+        for (const at::Tensor* t : {&k, &v, q}) {
+            if (!t) continue;
+            need(t->scalar_type() == kp.scalar_type() && t->device() == dev && (t->numel() == 0 || dense_rows(*t)), "q, k and v must have the pages' type and device, and dense heads");
+        }
+        if (q) need(q->dim() == d && q->sizes().slice(0, d - 2) == k.sizes().slice(0, d - 2) && q->size(d - 1) == k.size(d - 1) && q->size(d - 2) > 0, "q must have the same tokens and dim as k");
+        const int64_t* pos_p = nullptr;
+        int64_t pos_strides[2] = {0, 0};
+        if (positions) {
+            need(positions->is_cuda() && positions->device() == dev && positions->scalar_type() == at::kLong && positions->sizes() == k.sizes().slice(0, d - 2),
+                 "positions must be an int64 tensor with one value per token, on the pages' device");
+            pos_p = static_cast<const int64_t*>(positions->data_ptr());
+            pos_strides[0] = starts ? 0 : stride_of(*positions, 0);
+            pos_strides[1] = starts ? stride_of(*positions, 0) : d == 4 ? stride_of(*positions, 1) : 0;
+        }
+        profk_rotary_t how{frequencies_of(frequencies, dev), frequencies.numel(), a[10] == Py_True, 0, magnitude};
+        const c10::cuda::CUDAGuard guard(dev);
+        at::Tensor out;
+        if (q) out = fresh(q->sizes(), q->scalar_type(), dev);
+        if (rows.rows > 0) {
+            const Strides3 qs = q ? row_strides(*q, starts) : Strides3{}, ks = row_strides(k, starts), vs = row_strides(v, starts);
+            const profk_page_strides_t kps = strides_of(kp, 1), vps = strides_of(vp, 1);
+            auto* call = type == 0 ? &profk_pages_append_rotary_f32 : type == 1 ? &profk_pages_append_rotary_bf16 : &profk_pages_append_rotary_f16;
+            status(call(q ? q->data_ptr() : nullptr, qs.data(), k.data_ptr(), ks.data(), v.data_ptr(), vs.data(), kp.data_ptr(), vp.data_ptr(), &kps, &vps,
+                        static_cast<const int32_t*>(tables.data_ptr()), stride, lengths_p, rows.starts, seqs, rows.rows, q ? q->size(d - 2) : 0, kp.size(1), kp.size(3),
+                        kp.size(2), kp.size(0), width, pos_p, pos_strides, &how, c10::cuda::getCurrentCUDAStream(dev.index()).stream(),
+                        q ? out.data_ptr() : nullptr),
+                   "profk_pages_append_rotary");
+            written(kp);
+            written(vp);
+        }
+        return q ? wrap(out) : none();
+    });
+}
+
+// Something of n values per row of logits, or (of one dimension) the same for all rows: its stride between rows; null: not given.
+template <typename P>
+const P* beside_rows(const at::Tensor* t, const char* what, at::ScalarType type, at::IntArrayRef lead, c10::Device device, int64_t* n, int64_t* stride) {
+    if (!t) return nullptr;
+    const int64_t d = t->dim();
+    bool ok = t->is_cuda() && t->device() == device && t->scalar_type() == type && d >= 1 && (t->numel() == 0 || dense_rows(*t));
+    ok = ok && (d == 1 || t->sizes().slice(0, d - 1) == lead);
+    if (!ok) refuse(std::string(what) + " must be a " + c10::toString(type) + " tensor with dense rows, one for each row of logits or one for all, on the logits' device");
+    *n = t->size(-1);
+    *stride = 0;
+    int64_t rows = 1;
+    bool first = true;
+    for (int64_t i = d - 2; i >= 0; --i) {
+        if (t->size(i) == 1) continue;
+        if (first) *stride = t->stride(i);
+        else if (t->stride(i) != *stride * rows) refuse(std::string(what) + ": the leading dimensions must be evenly spaced");
+        first = false;
+        rows *= t->size(i);
+    }
+    return static_cast<const P*>(t->data_ptr());
+}
+
+// (logits, tokens, lengths, prompts, repetition, frequency, presence, bias_tokens, bias_values, mask, out) -> adjusted
+PyObject* adjust_logits(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+    return guarded([&]() -> PyObject* {
+        need(n_args == 11, "adjust_logits takes eleven arguments");
+        const at::Tensor& x = tensor(a[0], "logits");
+        const at::Tensor *tokens = optional(a[1], "tokens"), *lengths = optional(a[2], "lengths"), *prompts = optional(a[3], "prompts"), *bias_tokens = optional(a[7], "bias_tokens"),
+                         *bias_values = optional(a[8], "bias_values"), *mask = optional(a[9], "mask"), *given = optional(a[10], "out");
+        no_derivative(&x, "logits");
+        no_derivative(bias_values, "bias_values");
+        no_derivative(given, "out");
+        const int type = dtype_index(x.scalar_type());
+        const c10::Device dev = x.device();
+        need(x.is_cuda() && x.dim() >= 1, "logits must be a CUDA tensor (..., V)");
+        const at::IntArrayRef lead = x.sizes().slice(0, x.dim() - 1);
+        profk_adjust_t how{};
+        int64_t n = 0, words = 0;
+        how.tokens = beside_rows<int64_t>(tokens, "tokens", at::kLong, lead, dev, &how.history, &how.token_stride);
+        need(tokens || (!lengths && !prompts), "lengths and prompts need tokens");
+        how.lengths = of_row<const int32_t>(lengths, "lengths", at::kInt, lead, dev);
+        how.prompts = of_row<const int32_t>(prompts, "prompts", at::kInt, lead, dev);
+        auto number = [&](int i, const char* what, const float** rows, double* value) {
+            if (!THPVariable_Check(a[i])) {
+                *value = real(a[i], what);
+                if (!std::isfinite((float)*value)) refuse(std::string(what) + " must be finite");
+                return;
+            }
+            const at::Tensor& t = THPVariable_Unpack(a[i]);
+            no_derivative(&t, what);
+            *rows = of_row<const float>(&t, what, at::kFloat, lead, dev);
+        };
+        number(4, "repetition", &how.repetition, &how.repetition_value);
+        number(5, "frequency", &how.frequency, &how.frequency_value);
+        number(6, "presence", &how.presence, &how.presence_value);
+        need(how.repetition || (float)how.repetition_value > 0.0f, "repetition must be positive");
+        need((bias_tokens != nullptr) == (bias_values != nullptr), "bias_tokens and bias_values belong together");
+        how.bias_tokens = beside_rows<int64_t>(bias_tokens, "bias_tokens", at::kLong, lead, dev, &how.biases, &how.bias_token_stride);
+        how.bias_values = beside_rows<float>(bias_values, "bias_values", at::kFloat, lead, dev, &n, &how.bias_value_stride);
+        need(n == how.biases, "bias_tokens and bias_values must have the same length");
+        how.mask = beside_rows<uint32_t>(mask, "mask", at::kInt, lead, dev, &words, &how.mask_stride);
+        if (mask) need(words == (x.size(-1) + 31) / 32, "mask must have ceil(V / 32) words");
+        if (given) need(given->is_cuda() && given->device() == dev && given->scalar_type() == x.scalar_type() && given->sizes() == x.sizes(), "out must be like logits");
+        const c10::cuda::CUDAGuard guard(dev);
+        const at::Tensor out = given ? *given : fresh(x.sizes(), x.scalar_type(), dev);
+        if (x.numel() == 0) return wrap(out);
+        const Matrix m = matrix(x), o = given ? matrix(*given) : Matrix{m.rows, m.cols, m.cols};
+        if (given && out.data_ptr() != x.data_ptr()) {
+            const int64_t b = (int64_t)x.element_size();
+            const char *x0 = static_cast<const char*>(x.data_ptr()), *o0 = static_cast<const char*>(out.data_ptr());
+            need(x0 + ((m.rows - 1) * m.stride + m.cols) * b <= o0 || o0 + ((o.rows - 1) * o.stride + o.cols) * b <= x0, "out must be logits itself or not overlap it");
+        }
+        auto* call = type == 0 ? &profk_adjust_logits_f32 : type == 1 ? &profk_adjust_logits_bf16 : &profk_adjust_logits_f16;
+        status(call(x.data_ptr(), m.rows, m.cols, m.stride, &how, c10::cuda::getCurrentCUDAStream(dev.index()).stream(), out.data_ptr(), o.stride), "profk_adjust_logits");
+        if (given) written(out);
+        return wrap(out);
+    });
+}
+
 // (ProfkError, torch.OutOfMemoryError): the exceptions to raise
 PyObject* set_errors(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
@@ -421,7 +634,7 @@ PyObject* set_errors(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {FAST(logprobs), FAST(logprobs_backward), FAST(pages_fork), FAST(pages_compact), FAST(pages_copy), FAST(pages_append), FAST(paged_attention),
-                           FAST(set_errors), {nullptr, nullptr, 0, nullptr}};
+                           FAST(rotary), FAST(pages_append_rotary), FAST(adjust_logits), FAST(set_errors), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_decode", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -8,6 +8,7 @@ allocator on the current stream, so that calls on several streams do not meet.
 """
 from __future__ import annotations
 
+import math
 from typing import NamedTuple, Optional
 
 import torch
@@ -154,3 +155,78 @@ def paged_attention(q, k_pages, v_pages, tables, lengths, scale: Optional[float]
     rows (a cache laid out tokens first is passed as `.transpose(1, 2)`); tables (seqs, width), lengths (seqs,) int32;
     scale defaults to dim ** -0.5.  The cache is read once for up to 16 query heads to a key.  Returns (out (seqs, heads, dim), lse (seqs, heads) float32)."""
     return (_native or _load()).paged_attention(q, k_pages, v_pages, tables, lengths, scale)
+
+
+# --- prompts and drafts -----------------------------------------------------------------------------------------------
+
+def rotary_frequencies(dim: int, base: float = 10000.0, stretch: float = 1.0, context: Optional[int] = None, keep: float = 32.0,
+                       slow: float = 1.0, device="cuda"):
+    """The frequencies of rotary positions over `dim` elements of a head: base ** (-2 i / dim) radians per position, float64.
+
+    For contexts `stretch` times longer than the one a model was trained on: without `context` every frequency is divided by
+    `stretch`.  With it (the trained context's length), pairs that make at least `keep` turns over that length keep their
+    frequency, those that make at most `slow` are divided by `stretch`, and between the two the share that is divided falls
+    linearly with the number of turns.  (Another base is given as such.)"""
+    if dim < 2 or dim % 2 != 0 or not base > 0 or not stretch > 0 or (context is not None and not (context > 0 and keep > slow >= 0)):
+        import paper_2608_12573_b200 as package
+
+        raise package.ProfkError("rotary_frequencies: dim must be even, base, stretch and context positive, keep above slow")
+    f = float(base) ** (-2.0 * torch.arange(dim // 2, dtype=torch.float64) / dim)
+    kept = torch.zeros_like(f) if context is None else ((f * context / (2 * math.pi) - slow) / (keep - slow)).clamp(0, 1)
+    return (f * kept + f / stretch * (1 - kept)).to(device)
+
+
+class _RotaryFunction(torch.autograd.Function):
+    """Linear in x: the transpose of a turn is the turn by the negative angle, so every derivative is this function again."""
+    @staticmethod
+    def forward(ctx, x, positions, frequencies, interleaved, magnitude, inverse):
+        ctx.save_for_backward(positions, frequencies)
+        ctx.how = interleaved, magnitude, inverse
+        return _load().rotary(x, positions, frequencies, interleaved, magnitude, inverse)
+
+    @staticmethod
+    def backward(ctx, g):
+        positions, frequencies = ctx.saved_tensors
+        interleaved, magnitude, inverse = ctx.how
+        # (an upstream gradient may be a broadcast scalar)
+        g = g if g.dim() == 0 or g.stride(-1) == 1 or g.size(-1) <= 1 else g.contiguous()
+        return _RotaryFunction.apply(g, positions, frequencies, interleaved, magnitude, not inverse), None, None, None, None, None
+
+
+def rotary(x, positions, frequencies, *, interleaved: bool = False, magnitude: float = 1.0, inverse: bool = False):
+    """`profk_rotary_*` on the current stream: turns pair i of every head by `positions * frequencies[i]` radians.
+
+    x: CUDA tensor (..., heads, dim), float32, bfloat16 or float16, dense heads, any strides.  positions: int64, broadcast to
+    x's leading dimensions.  frequencies: float64 (pairs,), 2 * pairs <= dim; the rest of a head is left as it is
+    (`rotary_frequencies`).  Pairs are elements i and pairs + i, or 2 i and 2 i + 1 with `interleaved`.  `magnitude` scales what
+    is turned; `inverse` turns back.  Differentiable in x, any number of times."""
+    if isinstance(x, torch.Tensor) and x.requires_grad and torch.is_grad_enabled():
+        return _RotaryFunction.apply(x, positions, frequencies, bool(interleaved), magnitude, bool(inverse))
+    return (_native or _load()).rotary(x, positions, frequencies, bool(interleaved), magnitude, bool(inverse))
+
+
+def pages_append_rotary(k_pages, v_pages, tables, lengths, q, k, v, frequencies, *, starts=None, positions=None, interleaved: bool = False,
+                        magnitude: float = 1.0):
+    """`profk_pages_append_rotary_*` on the current stream: `pages_append` with `rotary` on the way.  Writes the turned keys `k`
+    and the values `v` of every sequence's newest tokens to their places in one layer's pages, and returns the turned queries.
+
+    q (None: no queries, returns None), k, v: (seqs, [tokens,] heads or kv_heads, dim), or with `starts` (seqs + 1,) int32 (rows,
+    heads or kv_heads, dim), where sequence s has the rows starts[s] to starts[s + 1] - 1, any strides with dense heads; float32,
+    bfloat16 or float16, as the pages.  `lengths` counts the new tokens already; a token is turned by its place in its sequence,
+    or by `positions` (int64, one per token).  Tokens without a place (see `pages_append`) are turned only; rows that no
+    sequence holds come back as zeros."""
+    return (_native or _load()).pages_append_rotary(k_pages, v_pages, tables, lengths, q, k, v, frequencies, starts, positions, bool(interleaved), magnitude)
+
+
+def adjust_logits(logits, tokens=None, lengths=None, prompts=None, *, repetition=1.0, frequency=0.0, presence=0.0, bias_tokens=None,
+                  bias_values=None, mask=None, out=None):
+    """`profk_adjust_logits_*` on the current stream: what a sampler lays over logits before `logprobs` or `topk`.
+
+    logits: CUDA tensor (..., V), float32, bfloat16 or float16, dense rows at any stride.  tokens: int64 (..., L), every row's
+    prompt and answer, of which the first `lengths` (int32 (...); None: L) count and the first `prompts` of those (int32; None: 0) are
+    prompt.  For a token that was seen the logit is divided (if positive, else multiplied) by `repetition`; one that occurs c
+    times in the answer loses frequency * c + presence (each a number or a float32 tensor (...)).  Then bias_values (float32 (..., n),
+    n <= 8192) are added at bias_tokens (int64), duplicates summed; what `mask` (int32 (..., ceil(V / 32)), bit v % 32 of word
+    v // 32: token v is allowed) does not allow becomes -inf.  tokens, biases and mask may be of one dimension, for all rows alike.
+    `out` may be `logits`: then only what changes is touched.  Returns the adjusted logits."""
+    return (_native or _load()).adjust_logits(logits, tokens, lengths, prompts, repetition, frequency, presence, bias_tokens, bias_values, mask, out)
