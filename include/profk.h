@@ -622,6 +622,36 @@ int profk_pages_append_rotary_f16(const void* q, const int64_t* q_strides, const
                                   int64_t kv_heads, int64_t dim, int64_t page_size, int64_t pages, int64_t width, const int64_t* positions,
                                   const int64_t* position_strides, const profk_rotary_t* how, void* stream, void* out_q);
 
+/*
+ * Attention of a chunk of new tokens of every sequence over one layer's pages, which hold them already: of n new tokens of a sequence
+ * of length L, number t sees the tokens j <= L - n + t.  out and lse as profk_paged_attention_*, which is the form for one token.
+ *   q            [device] rows x heads rows of dim elements; strides [host] three, in elements: sequence, token, head; any alignment
+ *                (read 16 bytes at a time where address and strides are multiples of 8 elements)
+ *   starts       [device] seqs + 1 int32, ascending: sequence s has the rows [starts[s], starts[s + 1]) (the sequence stride is not
+ *                used).  NULL: rows / seqs rows each
+ *   k_pages, v_pages   [device] 16-byte aligned; strides in elements, multiples of 8
+ *   lengths      [device] seqs: tokens held, the new ones among them.  Places follow from them as they are; tokens behind the table's
+ *                end are not there
+ *   dim          a multiple of 8, up to 256;  rows * heads < 2^31
+ *   workspace    [device] profk_paged_attention_chunk_workspace_bytes(dim), 256-byte aligned
+ *   out          [device] rows x heads x dim, dense, of the cache's type;  lse  [device] rows x heads floats
+ * Products in the cache's type, sums and statistics in fp32; weights are rounded once to the cache's type (bf16: off by 2^-9 of each; fp16:
+ * by 2^-12 of it or 2^-39 of the largest).  A token that sees nothing gets out = 0, lse = -inf; rows that no sequence holds likewise.
+ * What a row does not see does not reach it, whatever its values are.  The same call gives the same bits every time.  Waits inside
+ * the kernel are bounded; should one run out, all outputs are NaN.  Errors: PROFK_EINVAL, PROFK_EWORKSPACE, PROFK_ECUDA.
+ */
+int profk_paged_attention_chunk_workspace_bytes(int64_t dim, size_t* bytes /* [host] */);
+int profk_paged_attention_chunk_bf16(const void* q, const int64_t* q_strides, const void* k_pages, const void* v_pages,
+                                    const profk_page_strides_t* k_strides, const profk_page_strides_t* v_strides, const int32_t* tables, int64_t table_stride,
+                                    const int32_t* lengths, const int32_t* starts, int64_t seqs, int64_t rows, int64_t heads, int64_t kv_heads, int64_t dim,
+                                    int64_t page_size, int64_t pages, int64_t width, double scale, void* workspace, size_t workspace_bytes, void* stream,
+                                    void* out, float* lse);
+int profk_paged_attention_chunk_f16(const void* q, const int64_t* q_strides, const void* k_pages, const void* v_pages,
+                                    const profk_page_strides_t* k_strides, const profk_page_strides_t* v_strides, const int32_t* tables, int64_t table_stride,
+                                    const int32_t* lengths, const int32_t* starts, int64_t seqs, int64_t rows, int64_t heads, int64_t kv_heads, int64_t dim,
+                                    int64_t page_size, int64_t pages, int64_t width, double scale, void* workspace, size_t workspace_bytes, void* stream,
+                                    void* out, float* lse);
+
 /* What is laid over a row of logits.  Strides in elements, between rows; 0: one for all. */
 typedef struct profk_adjust {
     const int64_t* tokens;                /* [device] rows x history: prompt, then answer; NULL iff history = 0.  Tokens outside [0, V) are passed over */

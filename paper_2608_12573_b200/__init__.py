@@ -31,6 +31,7 @@ EXPORTS = [
     "profk_paged_attention_workspace_bytes", "profk_paged_attention_bf16", "profk_paged_attention_f16",
     "profk_pages_fork_workspace_bytes", "profk_pages_fork", "profk_pages_fork_ex", "profk_pages_compact_workspace_bytes", "profk_pages_compact",
     "profk_pages_copy", "profk_pages_append",
+    "profk_paged_attention_chunk_workspace_bytes", "profk_paged_attention_chunk_bf16", "profk_paged_attention_chunk_f16",
     "profk_rotary_f32", "profk_rotary_bf16", "profk_rotary_f16", "profk_pages_append_rotary_f32", "profk_pages_append_rotary_bf16",
     "profk_pages_append_rotary_f16", "profk_adjust_logits_f32", "profk_adjust_logits_bf16", "profk_adjust_logits_f16",
 ]
@@ -455,5 +456,5 @@ def last_launch_count() -> int:
 
 # (behind the names above, which the module uses)
 from .decode import (LogProbs, PagesCompacted, PagesForked, adjust_logits, logprobs, logprobs_backward,  # noqa: E402
-                     paged_attention, pages_append, pages_append_rotary, pages_compact, pages_copy, pages_fork, rotary,
+                     paged_attention, paged_attention_chunk, pages_append, pages_append_rotary, pages_compact, pages_copy, pages_fork, rotary,
                      rotary_frequencies)

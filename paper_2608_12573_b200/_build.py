@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libprofk.so")
 BINDING_PATH = os.path.join(PKG_DIR, "_decode.so")
 BINDING_SOURCE = os.path.join(CSRC, "decode_binding.cpp")
-SOURCES = ["profk_api.cu", "decode_api.cu", "prompt_api.cu", "plan.cpp"]
+SOURCES = ["profk_api.cu", "decode_api.cu", "prompt_api.cu", "chunk_api.cu", "plan.cpp"]
 
 
 def _newest_source_mtime() -> float:

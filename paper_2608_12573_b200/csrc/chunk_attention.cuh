@@ -1,0 +1,998 @@
+// Attention of a chunk of new tokens of every sequence over a paged key-value cache that holds them already:
+//   out_h = sum_j p_j v_j,   p = softmax_j(scale q_h . k_j),   lse_h = ln sum_j e^(scale q_h . k_j),
+// for the new token at place t of its sequence over the tokens j <= t.
+//
+// Prompts are bound by the matrix unit (4 dim operations per query head, new token and seen key), drafts of a few tokens by
+// HBM.  Query heads that share a key-value head are rows of the same tile: row r of a (sequence, key-value head) is the
+// token r / group and the head r % group, so that the cache is read once for all of them.
+//
+// A CTA has an SM to itself.  Two streams of 128 rows (two tiles of queries over every tile of keys; or, where there are no
+// more than 128 rows, one tile of queries whose tiles of keys alternate between the streams) take turns on the matrix unit:
+// while one stream's scores are turned into weights by its four warps, the other's products run.
+//   S = Q K^T   tcgen05.mma, both operands in shared memory, S in tensor memory;
+//   P           a thread owns a row: reads its scores, keeps the running maximum and sum, writes the weights over the scores;
+//   O += P V    tcgen05.mma, P from tensor memory, V from shared memory as it was loaded (its rows run along the product).
+// With dim > 128 there is room for one O only: one stream, whose scores alternate between two places.
+// The exponents' reference is raised only when a score passes it by more than 2^8 (fp16: 2, its weights are lifted by 2^14 so
+// that small ones do not vanish); then the row's own thread scales its O.  Weights are rounded once to the cache's type, as the
+// product with the values needs it: an error of half a step in each, which for values of either sign adds up to no more
+// than the rounding of the output does.  Sums of weights are kept in fp32, unrounded and compensated.
+//
+// The work is the list of (sequence, key-value head, block of rows, tile of keys), cut into one contiguous share per CTA by
+// cost whatever the lengths; items that a cut goes through leave unnormalised parts, which a second kernel joins in order.
+#pragma once
+
+#include "logits.cuh"
+
+namespace profk {
+
+constexpr int CA_ROWS = 128;              // rows of a tile of queries: lanes of the tensor memory
+constexpr int CA_THREADS = 384;           // two warpgroups of weights; three warps that load, one that issues products
+constexpr int CA_LOADERS = 96, CA_LOAD_ROWS = CA_LOADERS / 8;            // eight threads to 128 bytes of a row
+constexpr int CA_OVERHEAD = 3;            // what an item costs beside its tiles, in units of one tile of one stream
+constexpr int CA_MASKS = 8;               // tiles whose masks are kept; loading runs ahead by fewer
+constexpr int CA_ITEMS = 4;               // items whose bad tokens are kept
+constexpr int CA_BAD_TILES = 4;           // tiles of an item that its mask can cut
+constexpr int CA_POLLS = 1 << 22;
+constexpr int CA_MANY_REGISTERS = 208, CA_FEW_REGISTERS = 88;      // of a thread that weighs, and of the others, after the launch
+
+template <int D>
+struct CaShape {
+    static constexpr int STREAMS = D <= 128 ? 2 : 1;
+    static constexpr int KT = D <= 128 ? 128 : 64;                       // tokens of a tile
+    static constexpr int BLOCK = STREAMS * CA_ROWS;                      // rows of an item
+    static constexpr int Q_TILE = CA_ROWS * D * 2, STAGE = KT * D * 2;
+    static constexpr int STAGES = D == 64 ? 8 : 5;
+    static constexpr int O_AT = 256;                                     // columns of the tensor memory: S 0 and 128, O from here
+};
+
+template <typename T>
+struct CaParams {
+    const T* q;
+    int64_t q_seq, q_token, q_head;       // strides in elements
+    const T* k;
+    const T* v;
+    int64_t ks_page, ks_head, ks_token, vs_page, vs_head, vs_token;
+    const int32_t* tables;
+    int64_t table_stride;
+    const int32_t* lengths;
+    const int32_t* starts;                // null: `tokens` rows each
+    int32_t rows, tokens;
+    int32_t seqs, heads, kv_heads, group, dim, page_size, pages, width, page_shift;
+    bool q_wide;                          // rows of q lie on 16-byte vectors
+    float scale;
+    T* out;
+    float* lse;
+    float* parts;                         // (2 per CTA) x BLOCK x D
+    float2* sums;                         // (2 per CTA) x BLOCK: reference, sum
+    struct CaMeta* meta;                  // 2 per CTA
+};
+
+struct CaMeta {
+    int32_t valid, last, failed, rows;    // of this part: whether there is one, whether it ends its item
+    int32_t row0;                         // of the first new token, in q and out
+    int32_t head, first;                  // key-value head; first row of the item
+};
+
+// ---- items -------------------------------------------------------------------------------------
+
+// The new tokens of a sequence: first row, how many, place of the first.  (Rows times heads stay below 2^31.  A place below
+// -2^31 is taken for that: all tokens of such a sequence lie before its beginning.)
+struct CaSeq { int32_t row0, n, base; };
+template <typename T>
+__device__ __forceinline__ CaSeq ca_seq(const CaParams<T>& p, int32_t s) {
+    CaSeq q;
+    if (p.starts) {
+        q.row0 = max(0, min(p.starts[s], p.rows));
+        q.n = max(q.row0, min(p.starts[s + 1], p.rows)) - q.row0;
+    } else {
+        q.row0 = s * p.tokens;
+        q.n = p.tokens;
+    }
+    q.base = (int32_t)max((int64_t)p.lengths[s] - q.n, (int64_t)INT32_MIN);
+    return q;
+}
+
+// Block b of a sequence's rows: its first row, how many; tokens that its last row sees, tiles of them; a tile's weight.
+template <int D>
+struct CaBlock {
+    int32_t first, rows, end, tiles;
+    __device__ __forceinline__ CaBlock(const CaSeq& s, int32_t group, int32_t room, int32_t b) {
+        using S = CaShape<D>;
+        first = b * S::BLOCK;
+        rows = min(S::BLOCK, s.n * group - first);
+        end = (int32_t)max(0ll, min((long long)s.base + (uint32_t)(first + rows - 1) / (uint32_t)group + 1, (long long)room));
+        tiles = (int32_t)(((uint32_t)end + S::KT - 1) / S::KT);
+    }
+    __device__ __forceinline__ int32_t weight() const { return rows > CA_ROWS ? 2 : 1; }
+    __device__ __forceinline__ int32_t cost() const { return CA_OVERHEAD + weight() * tiles; }
+    // tiles in front of unit x of the item
+    __device__ __forceinline__ int32_t tile_of(int32_t x) const { return x <= CA_OVERHEAD ? 0 : min(tiles, (x - CA_OVERHEAD + weight() - 1) / weight()); }
+};
+template <int D>
+__device__ __forceinline__ int32_t ca_blocks(const CaSeq& s, int32_t group) { return (int32_t)(((uint32_t)(s.n * group) + CaShape<D>::BLOCK - 1) / CaShape<D>::BLOCK); }
+template <int D>
+__device__ __forceinline__ int64_t ca_head_cost(const CaSeq& s, int32_t group, int32_t room) {
+    int64_t sum = 0;
+    for (int32_t b = 0, n = ca_blocks<D>(s, group); b < n; ++b) sum += CaBlock<D>(s, group, room, b).cost();
+    return sum;
+}
+
+struct CaPlace {                          // an item, and its first unit
+    int64_t at;
+    int32_t block, seq, head;
+};
+
+// What a share covers, item by item; every warp walks by itself.
+template <typename T, int D>
+struct CaWalk {
+    const CaParams<T>& p;
+    int64_t left;                         // units from the item's first to the share's end
+    int32_t skip;                         // units of the item in front of the share
+    int32_t block_number, seq_number, head;
+    CaSeq seq;
+    int32_t number = -1;                  // of the item, among those with tiles
+    bool begun = false;
+    // the item:
+    CaBlock<D> block;
+    int32_t tile0, tile1;
+    __device__ __forceinline__ CaWalk(const CaParams<T>& params, const CaPlace& start, int64_t from, int64_t to)
+        : p(params), left(from < to ? to - start.at : 0), skip(from < to ? (int32_t)(from - start.at) : 0), block_number(start.block), seq_number(start.seq),
+          head(start.head), seq(ca_seq(params, from < to ? start.seq : 0)), block(seq, params.group, room(), from < to ? start.block : 0), tile0(0), tile1(0) {}
+    __device__ __forceinline__ int32_t room() const { return p.width * p.page_size; }
+    __device__ __forceinline__ bool next() {
+        for (;;) {
+            if (begun) {
+                left -= block.cost();
+                skip -= block.cost();
+                if (left <= 0) return false;
+                if (++block_number >= ca_blocks<D>(seq, p.group)) {
+                    block_number = 0;
+                    if (++head >= p.kv_heads) {
+                        head = 0;
+                        do {
+                            if (++seq_number >= p.seqs) return false;
+                            seq = ca_seq(p, seq_number);
+                        } while (seq.n == 0);
+                    }
+                }
+                block = CaBlock<D>(seq, p.group, room(), block_number);
+            } else {
+                if (left <= 0) return false;
+                begun = true;
+            }
+            tile0 = block.tile_of(max(skip, 0));
+            tile1 = block.tile_of((int32_t)min(left, (int64_t)block.cost()));
+            if (tile1 > tile0 || (block.tiles == 0 && skip <= 0)) {
+                number += tile1 > tile0;
+                return true;
+            }
+        }
+    }
+    __device__ __forceinline__ bool whole() const { return tile0 == 0 && tile1 == block.tiles; }
+};
+
+// ---- instructions ------------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t ca_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void ca_bar_init(uint64_t* bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ca_smem(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void ca_arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(ca_smem(bar)) : "memory");
+}
+__device__ __forceinline__ bool ca_test(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(ca_smem(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Waits for a phase; gives up after a limit, or when another warp has, and then returns false for good.
+__device__ __forceinline__ bool ca_wait(uint64_t* bar, uint32_t parity, volatile int32_t* failed) {
+    for (int32_t i = 0; i < CA_POLLS; ++i) {
+        if (ca_test(bar, parity)) return true;
+        if (*failed) return false;
+    }
+    *failed = 1;
+    return false;
+}
+// Warps meet (the barrier counts them); the wait is limited as all others are.
+__device__ __forceinline__ bool ca_meet(uint64_t* bar, uint32_t& phase, volatile int32_t* failed) {
+    __syncwarp();
+    if ((threadIdx.x & 31u) == 0) ca_arrive(bar);
+    const bool ok = __all_sync(FULL_MASK, ca_wait(bar, phase, failed));
+    phase ^= 1u;
+    return ok;
+}
+
+__device__ __forceinline__ void ca_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(ca_smem(bar)) : "memory");
+}
+__device__ __forceinline__ void ca_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void ca_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// D (128 x N, tensor memory) (+)= A (shared memory or tensor memory) B (shared memory)
+__device__ __forceinline__ void ca_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void ca_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
+}
+// Shared-memory operand in rows of 128 bytes, swizzled in atoms of eight rows; `leading`: between atoms along a transposed
+// operand's rows.
+__device__ __forceinline__ uint64_t ca_operand(uint32_t addr, uint32_t leading) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+template <typename T> struct CaType;
+template <> struct CaType<__nv_bfloat16> {
+    static constexpr uint32_t CODE = 1;
+    static constexpr float RAISE = 8.0f, LIFT = 0.0f;
+    static constexpr uint32_t EXPONENT = 0x7F80u;
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+};
+template <> struct CaType<__half> {
+    static constexpr uint32_t CODE = 0;
+    static constexpr float RAISE = 1.0f, LIFT = 14.0f;
+    static constexpr uint32_t EXPONENT = 0x7C00u;
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {
+        const __half2 h = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+};
+// 128 x N product of 16-bit operands summed in fp32; `transposed`: B's rows run along the summation.
+template <typename T>
+__device__ __forceinline__ constexpr uint32_t ca_product(uint32_t n, bool transposed) {
+    return 1u << 4 | CaType<T>::CODE << 7 | CaType<T>::CODE << 10 | (transposed ? 1u << 16 : 0u) | (n >> 3) << 17 | (128u >> 4) << 24;
+}
+
+__device__ __forceinline__ void ca_tm_load(uint32_t addr, float* r) {
+    uint32_t* u = reinterpret_cast<uint32_t*>(r);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]),
+                   "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]),
+                   "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+                 : "r"(addr));
+}
+__device__ __forceinline__ void ca_tm_store(uint32_t addr, const uint32_t* u) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(u[0]),
+                 "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]),
+                 "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]), "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]),
+                 "r"(u[30]), "r"(u[31]), "r"(addr)
+                 : "memory");
+}
+// The loads have ended; their 32 registers pass through, so that nothing that uses them moves in front.
+__device__ __forceinline__ void ca_tm_loaded(float* r) {
+    uint32_t* u = reinterpret_cast<uint32_t*>(r);
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7]), "+r"(u[8]), "+r"(u[9]), "+r"(u[10]), "+r"(u[11]), "+r"(u[12]),
+                   "+r"(u[13]), "+r"(u[14]), "+r"(u[15]), "+r"(u[16]), "+r"(u[17]), "+r"(u[18]), "+r"(u[19]), "+r"(u[20]), "+r"(u[21]), "+r"(u[22]), "+r"(u[23]), "+r"(u[24]),
+                   "+r"(u[25]), "+r"(u[26]), "+r"(u[27]), "+r"(u[28]), "+r"(u[29]), "+r"(u[30]), "+r"(u[31])
+                 :: "memory");
+}
+__device__ __forceinline__ void ca_tm_store16(uint32_t addr, const uint32_t* u) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]),
+                 "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ void ca_tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// 16 bytes from global to shared memory; zeros where there is nothing to read.
+__device__ __forceinline__ void ca_copy(uint32_t to, const void* from, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16u : 0u) : "memory");
+}
+
+// ---- shared memory -----------------------------------------------------------------------------
+
+template <int D>
+struct CaControl {
+    uint64_t full[CaShape<D>::STAGES], empty[CaShape<D>::STAGES];
+    uint64_t q_full, q_free, s_full[2], p_full[2], o_full[2], o_step, loaders, weighers, drain;
+    uint32_t tensor;                      // address of the tensor memory
+    int32_t failed;
+    int32_t table[2][CaShape<D>::KT];     // pages of two tiles' tokens; -1: nothing there
+    alignas(16) uint32_t mask[CA_MASKS][4];        // which tokens of a tile are there
+    uint32_t bad[CA_ITEMS][CA_BAD_TILES][4];       // tokens whose values are not finite, of the tiles that a mask cuts
+    float2 other[CA_ROWS];                // reference and sum of the second stream, where two share rows
+    CaPlace place[2];
+    int64_t bound[2];
+    int64_t scan[CA_THREADS / 32];
+};
+template <int D>
+constexpr size_t ca_smem_bytes() { return CaShape<D>::STREAMS * CaShape<D>::Q_TILE + CaShape<D>::STAGES * CaShape<D>::STAGE + sizeof(CaControl<D>); }
+static_assert(ca_smem_bytes<128>() <= 232448 && ca_smem_bytes<256>() <= 232448 && ca_smem_bytes<64>() <= 232448, "an SM's shared memory");
+
+// Units of all items, and the share of this CTA: [bound[0], bound[1]) of them, beginning at place[0].  A cut that would leave
+// little of an item on either side is moved to the item's nearer end: parts cost their reading and writing.
+template <typename T, int D>
+__device__ void ca_plan(const CaParams<T>& p, CaControl<D>* ctl) {
+    const int32_t room = p.width * p.page_size;
+    const int32_t tid = (int32_t)threadIdx.x, lane = tid & 31, warp = tid / 32;
+    const int32_t per = (p.seqs + CA_THREADS - 1) / CA_THREADS, s0 = min(p.seqs, tid * per), s1 = min(p.seqs, s0 + per);
+    int64_t mine = 0;
+    for (int32_t s = s0; s < s1; ++s) mine += ca_head_cost<D>(ca_seq(p, s), p.group, room) * p.kv_heads;
+    int64_t upto = mine;
+    for (int d = 1; d < 32; d *= 2) {
+        const int64_t o = __shfl_up_sync(FULL_MASK, upto, d);
+        if (lane >= d) upto += o;
+    }
+    if (lane == 31) ctl->scan[warp] = upto;
+    __syncthreads();
+    int64_t total = 0, before = upto - mine;
+    for (int w = 0; w < CA_THREADS / 32; ++w) {
+        if (w < warp) before += ctl->scan[w];
+        total += ctl->scan[w];
+    }
+    const int64_t shares = min((int64_t)gridDim.x, max((int64_t)1, total / 4));       // (a share within an item holds a tile at least)
+    for (int i = 0; i < 2; ++i) {
+        const int64_t c = (int64_t)blockIdx.x + i;
+        const int64_t x = c >= shares ? total : total / shares * c + total % shares * c / shares;
+        if (tid == 0 && x >= total) ctl->bound[i] = total;
+        if (x < before || x >= before + mine) continue;
+        int64_t at = before;
+        for (int32_t s = s0; s < s1; ++s) {
+            const CaSeq seq = ca_seq(p, s);
+            const int64_t one = ca_head_cost<D>(seq, p.group, room), all = one * p.kv_heads;
+            if (x >= at + all) { at += all; continue; }
+            CaPlace place{at + (x - at) / one * one, 0, s, (int32_t)((x - at) / one)};
+            for (;; ++place.block) {
+                const CaBlock<D> b(seq, p.group, room, place.block);
+                if (x >= place.at + b.cost()) { place.at += b.cost(); continue; }
+                // x lies in this item
+                int64_t cut = x;
+                if (x > place.at && b.cost() <= 4 + b.rows / 16) cut = x - place.at < place.at + b.cost() - x ? place.at : place.at + b.cost();
+                ctl->bound[i] = cut;
+                ctl->place[i] = place;                       // (a cut at the item's end: the walk steps over it)
+                break;
+            }
+            break;
+        }
+    }
+    __syncthreads();
+}
+
+// ---- loading -----------------------------------------------------------------------------------
+
+// What a loading thread has in flight: groups of copies, oldest first, each with the barrier that tells of it.
+template <typename T, int D>
+struct CaLoader {
+    using S = CaShape<D>;
+    static constexpr int DEPTH = 3;
+    CaControl<D>* ctl;
+    uint32_t stages;                      // shared memory
+    uint64_t* pending[DEPTH];
+    int32_t check[DEPTH];                 // values to look through: stage | tile's number << 8 | item's << 16; -1: none
+    int32_t count = 0;
+    int32_t stage = 0;
+    uint32_t phase = 1;                   // of `empty`: the first round waits for nothing
+    // The oldest copies have landed, once no more than `newer` groups are in flight: look through them if asked, tell.
+    __device__ __forceinline__ void retire(int32_t newer) {
+        if (newer == 3) asm volatile("cp.async.wait_group 3;" ::: "memory");
+        else if (newer == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else if (newer == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+        if (check[0] >= 0) look(ctl, stages, check[0] & 255, check[0] >> 8 & 255, check[0] >> 16);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane_id() == 0) ca_arrive(pending[0]);
+#pragma unroll
+        for (int i = 0; i + 1 < DEPTH; ++i) { pending[i] = pending[i + 1]; check[i] = check[i + 1]; }
+        --count;
+    }
+    __device__ __forceinline__ void issued(uint64_t* bar, int32_t what) {
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (count == DEPTH) retire(DEPTH);
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i)
+            if (i == count) { pending[i] = bar; check[i] = what; }
+        ++count;
+    }
+    // Waits until a barrier's phase has passed; what has landed meanwhile is told of.
+    __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
+        while (count > 0) {
+            if (__all_sync(FULL_MASK, ca_test(bar, parity))) return true;
+            retire(count - 1);
+        }
+        return __all_sync(FULL_MASK, ca_wait(bar, parity, &ctl->failed));
+    }
+    __device__ __forceinline__ void flush() {
+        while (count > 0) retire(count - 1);
+    }
+    static __device__ __forceinline__ uint32_t chunk_at(int32_t row, int32_t chunk, int32_t rows) {
+        return (uint32_t)((chunk >> 3) * rows * 128 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4));
+    }
+    // This thread's copies of a tile of values: those that are not finite are taken out, and their tokens noted.
+    static __device__ __noinline__ void look(CaControl<D>* ctl, uint32_t stages, int32_t st, int32_t tile, int32_t item) {
+        const int32_t t = (int32_t)threadIdx.x - 256;
+        char* base = reinterpret_cast<char*>(__cvta_shared_to_generic(stages + st * S::STAGE));
+        for (int i = 0; i < S::KT * (D / 64); i += CA_LOAD_ROWS) {
+            const int32_t both = i + (t >> 3), row = both % S::KT, chunk = (t & 7) + 8 * (both / S::KT);
+            if (both >= S::KT * (D / 64)) break;
+            uint4* at = reinterpret_cast<uint4*>(base + chunk_at(row, chunk, S::KT));
+            const uint4 v = *at;
+            bool bad = false;
+            for (const uint32_t w : {v.x, v.y, v.z, v.w})
+                bad |= (w & CaType<T>::EXPONENT) == CaType<T>::EXPONENT || (w >> 16 & CaType<T>::EXPONENT) == CaType<T>::EXPONENT;
+            if (!bad) continue;
+            *at = make_uint4(0, 0, 0, 0);
+            atomicOr(&ctl->bad[item % CA_ITEMS][tile % CA_BAD_TILES][row / 32], 1u << (row % 32));
+        }
+    }
+    // One tile of keys or values.
+    __device__ __forceinline__ bool tile(const CaParams<T>& p, const T* pages, int64_t page_stride, int64_t token_stride, int32_t buffer, int32_t first, int32_t what) {
+        if (!wait(&ctl->empty[stage], phase)) return false;
+        const int32_t t = (int32_t)threadIdx.x - 256;
+        const uint32_t to = stages + stage * S::STAGE;
+#pragma unroll 4
+        for (int32_t row = t >> 3; row < S::KT; row += CA_LOAD_ROWS) {
+            const int32_t page = ctl->table[buffer][row];
+            const uint32_t token = (uint32_t)(first + row);
+            const uint32_t slot = p.page_shift >= 0 ? token & ((1u << p.page_shift) - 1u) : token % (uint32_t)p.page_size;
+            const T* from = pages + max(page, 0) * page_stride + (page >= 0 ? slot * token_stride : 0);
+#pragma unroll
+            for (int h = 0; h < D / 64; ++h) {
+                const int32_t chunk = (t & 7) + 8 * h;
+                const bool there = page >= 0 && chunk * 8 < p.dim;
+                ca_copy(to + chunk_at(row, chunk, S::KT), there ? from + chunk * 8 : pages, there);
+            }
+        }
+        issued(&ctl->full[stage], what < 0 ? -1 : what | stage);
+        if (++stage == S::STAGES) { stage = 0; phase ^= 1; }
+        return true;
+    }
+};
+
+template <typename T, int D>
+__device__ void ca_load(const CaParams<T>& p, CaControl<D>* ctl, char* queries, char* stages) {
+    using S = CaShape<D>;
+    CaLoader<T, D> load;
+    load.ctl = ctl;
+    load.stages = ca_smem(stages);
+    const uint32_t q_at = ca_smem(queries);
+    const int32_t t = (int32_t)threadIdx.x - 256, warp = t / 32;
+    CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
+    uint32_t q_phase = 1, meeting = 0;
+    int32_t tiles_done = 0;
+    while (walk.next()) {
+        const auto& b = walk.block;
+        const int32_t* table = p.tables + walk.seq_number * p.table_stride;
+        auto page_of = [&](int32_t token) -> int32_t {
+            if (token >= b.end) return -1;
+            const uint32_t c = p.page_shift >= 0 ? (uint32_t)token >> p.page_shift : (uint32_t)token / (uint32_t)p.page_size;
+            const int32_t page = table[c];
+            return page >= 0 && page < p.pages ? page : -1;
+        };
+        if (walk.tile1 == walk.tile0) continue;                          // no token to see
+        // (the tile's tokens to the threads, the last 32 of 128 to the first warp once more)
+        int32_t page = t < S::KT ? page_of(walk.tile0 * S::KT + t) : -1, page2 = t + CA_LOADERS < S::KT ? page_of(walk.tile0 * S::KT + CA_LOADERS + t) : -1;
+        if (t < CA_BAD_TILES * 4) ctl->bad[walk.number % CA_ITEMS][t / 4][t % 4] = 0;
+        // queries: rows of (token, head)
+        if (!load.wait(&ctl->q_free, q_phase)) break;
+        q_phase ^= 1;
+        const T* q = p.q + (p.starts ? (int64_t)walk.seq.row0 * p.q_token : walk.seq_number * p.q_seq) + (int64_t)walk.head * p.group * p.q_head;
+        const int32_t streams = b.rows > CA_ROWS ? 2 : 1;
+        for (int s = 0; s < streams; ++s)
+            for (int32_t row = t >> 3; row < CA_ROWS; row += CA_LOAD_ROWS) {
+                const int32_t r = s * CA_ROWS + row;
+                const bool held = r < b.rows;
+                const uint32_t token = (uint32_t)(b.first + r) / (uint32_t)p.group, g = (uint32_t)(b.first + r) - token * p.group;
+                const T* from = held ? q + token * p.q_token + g * p.q_head : p.q;
+                for (int h = 0; h < D / 64; ++h) {
+                    const int32_t chunk = (t & 7) + 8 * h;
+                    const bool there = held && chunk * 8 < p.dim;
+                    const uint32_t to = q_at + s * S::Q_TILE + CaLoader<T, D>::chunk_at(row, chunk, CA_ROWS);
+                    if (p.q_wide) {
+                        ca_copy(to, there ? from + chunk * 8 : p.q, there);
+                    } else {
+                        uint32_t w[4] = {0, 0, 0, 0};
+                        if (there)
+                            for (int e = 0; e < 8; ++e) w[e / 2] |= (uint32_t)reinterpret_cast<const unsigned short*>(from)[chunk * 8 + e] << (16 * (e % 2));
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                    }
+                }
+            }
+        load.issued(&ctl->q_full, -1);
+        // the first tile that some row does not see all of
+        const int64_t seen = (int64_t)walk.seq.base + (uint32_t)b.first / (uint32_t)p.group + 1;
+        const int32_t cut = (int32_t)(max((int64_t)0, min(seen, (int64_t)b.end)) / S::KT);
+        const T* keys = p.k + walk.head * p.ks_head;
+        const T* values = p.v + walk.head * p.vs_head;
+        bool ok = true;
+        for (int32_t tile = walk.tile0; tile < walk.tile1 && ok; ++tile, ++tiles_done) {
+            const int32_t buffer = tiles_done & 1;
+            const uint32_t there = __ballot_sync(FULL_MASK, page >= 0), there2 = __ballot_sync(FULL_MASK, page2 >= 0);
+            uint32_t* mask = ctl->mask[tiles_done % CA_MASKS];
+            if (t < S::KT) ctl->table[buffer][t] = page;
+            if (t + CA_LOADERS < S::KT) ctl->table[buffer][t + CA_LOADERS] = page2;
+            if (lane_id() == 0) {
+                mask[warp] = warp * 32 < S::KT ? there : ~0u;
+                if (warp == 0) mask[3] = CA_LOADERS < S::KT ? there2 : ~0u;
+            }
+            if (tile + 1 < walk.tile1) {
+                page = t < S::KT ? page_of((tile + 1) * S::KT + t) : -1;
+                page2 = t + CA_LOADERS < S::KT ? page_of((tile + 1) * S::KT + CA_LOADERS + t) : -1;
+            }
+            if (!(ok = ca_meet(&ctl->loaders, meeting, &ctl->failed))) break;
+            const int32_t first = tile * S::KT;
+            ok = load.tile(p, keys, p.ks_page, p.ks_token, buffer, first, -1);
+            ok = ok && load.tile(p, values, p.vs_page, p.vs_token, buffer, first, tile >= cut ? (tile % CA_BAD_TILES) << 8 | (walk.number % CA_ITEMS) << 16 : -1);
+        }
+        if (!ok) break;
+    }
+    load.flush();
+    asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+// ---- products ----------------------------------------------------------------------------------
+
+// One thread issues all products of the CTA.
+template <typename T, int D>
+__device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t queries, uint32_t stages) {
+    using S = CaShape<D>;
+    const uint32_t tm = ctl->tensor;
+    volatile int32_t* failed = &ctl->failed;
+    constexpr uint32_t SCORES = ca_product<T>(S::KT, false), OUTPUT = ca_product<T>(D, true);
+    CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
+    uint32_t q_phase = 0, p_phase[2] = {0, 0};
+    int32_t taken = 0;                    // stages so far: keys of tile i are number 2 i, values 2 i + 1
+    auto bar_full = [&](int32_t n, uint64_t** empty, uint32_t* at) {
+        const int32_t st = n % S::STAGES;
+        *empty = &ctl->empty[st];
+        *at = stages + st * S::STAGE;
+        return ca_wait(&ctl->full[st], (uint32_t)(n / S::STAGES) & 1u, failed);
+    };
+    auto scores = [&](int s, int buffer, uint32_t keys) {
+        const uint32_t q = queries + s * S::Q_TILE;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+            ca_mma_ss(tm + buffer * 128, ca_operand(q + k / 4 * (CA_ROWS * 128) + k % 4 * 32, 16), ca_operand(keys + k / 4 * (S::KT * 128) + k % 4 * 32, 16), SCORES, k > 0);
+    };
+    auto output = [&](int o, int buffer, uint32_t values, bool add) {
+#pragma unroll
+        for (int k = 0; k < S::KT / 16; ++k)
+            ca_mma_ts(tm + S::O_AT + o * D, tm + buffer * 128 + k * 8, ca_operand(values + k * 2048, S::KT * 128), OUTPUT, add || k > 0);
+    };
+    while (walk.next()) {
+        const int32_t n = walk.tile1 - walk.tile0;
+        if (n == 0) continue;
+        if (!ca_wait(&ctl->q_full, q_phase, failed)) return;
+        q_phase ^= 1;
+        uint64_t *k_empty = nullptr, *v_empty = nullptr;
+        uint32_t k_at = 0, v_at = 0;
+        if (S::STREAMS == 2 && walk.block.rows > CA_ROWS) {
+            // both streams over every tile
+            if (!bar_full(taken, &k_empty, &k_at)) return;
+            ca_after_sync();
+            for (int s = 0; s < 2; ++s) {
+                scores(s, s, k_at);
+                ca_commit(&ctl->s_full[s]);
+            }
+            ca_commit(k_empty);
+            if (n == 1) ca_commit(&ctl->q_free);
+            for (int32_t i = 0; i < n; ++i) {
+                if (!bar_full(taken + 2 * i + 1, &v_empty, &v_at)) return;
+                for (int s = 0; s < 2; ++s) {
+                    if (!ca_wait(&ctl->p_full[s], p_phase[s], failed)) return;
+                    p_phase[s] ^= 1;
+                    ca_after_sync();
+                    output(s, s, v_at, i > 0);
+                    if (i + 1 < n) {
+                        if (s == 0 && !bar_full(taken + 2 * i + 2, &k_empty, &k_at)) return;
+                        ca_after_sync();
+                        scores(s, s, k_at);
+                        ca_commit(&ctl->s_full[s]);
+                    } else {
+                        ca_commit(&ctl->o_full[s]);
+                    }
+                }
+                ca_commit(v_empty);
+                if (i + 1 < n) ca_commit(k_empty);
+                if (i + 2 == n) ca_commit(&ctl->q_free);
+            }
+        } else {
+            // tiles alternate between two places of scores (and, with two streams, two of output)
+            if (!bar_full(taken, &k_empty, &k_at)) return;
+            ca_after_sync();
+            scores(0, 0, k_at);
+            ca_commit(&ctl->s_full[0]);
+            ca_commit(k_empty);
+            if (n == 1) ca_commit(&ctl->q_free);
+            for (int32_t i = 0; i < n; ++i) {
+                const int s = i & 1;
+                if (i + 1 < n) {
+                    if (!bar_full(taken + 2 * i + 2, &k_empty, &k_at)) return;
+                    ca_after_sync();
+                    scores(0, s ^ 1, k_at);
+                    ca_commit(&ctl->s_full[s ^ 1]);
+                    ca_commit(k_empty);
+                    if (i + 2 == n) ca_commit(&ctl->q_free);
+                }
+                if (!bar_full(taken + 2 * i + 1, &v_empty, &v_at)) return;
+                if (!ca_wait(&ctl->p_full[s], p_phase[s], failed)) return;
+                p_phase[s] ^= 1;
+                ca_after_sync();
+                output(S::STREAMS == 2 ? s : 0, s, v_at, i >= S::STREAMS);
+                ca_commit(v_empty);
+                if constexpr (S::STREAMS == 2) {
+                    if (i + 2 >= n) ca_commit(&ctl->o_full[s]);
+                } else {
+                    ca_commit(&ctl->o_step);
+                    if (i + 1 == n) ca_commit(&ctl->o_full[0]);
+                }
+            }
+        }
+        taken += 2 * n;
+    }
+}
+
+// ---- weights and output ------------------------------------------------------------------------
+
+// Adds what tokens with values that are not finite contribute to 32 columns of a row's output (their values were left out of
+// the product, where they would have met weights of zero).  Slow, and rare: the token's weight is computed again.
+template <typename T, int D>
+__device__ __noinline__ void ca_add_bad(const CaParams<T>& p, const uint32_t (*bad)[4], const int32_t* table, int32_t head, const T* q, const int32_t tile0, int32_t tile1,
+                                        int32_t seen, float factor, float reference, int32_t column, float* o) {
+    using S = CaShape<D>;
+    for (int32_t tile = max(tile0, tile1 - CA_BAD_TILES); tile < tile1; ++tile)
+        for (int32_t i = 0; i < S::KT; ++i) {
+            const int64_t token = (int64_t)tile * S::KT + i;
+            if (!(bad[tile % CA_BAD_TILES][i / 32] >> (i % 32) & 1u) || token >= seen) continue;
+            const int64_t page = table[token / p.page_size], slot = token % p.page_size;
+            const T* k = p.k + page * p.ks_page + head * p.ks_head + slot * p.ks_token;
+            const T* v = p.v + page * p.vs_page + head * p.vs_head + slot * p.vs_token;
+            float s = 0.0f;
+            for (int32_t d = 0; d < p.dim; ++d) s += Logit<T>::to_float(q[d]) * Logit<T>::to_float(k[d]);
+            const float w = exp2_approx(s * factor - reference);
+            // in vectors of 16 bytes, as they were taken out
+            for (int32_t c = 0; c < 32 && column + c < p.dim; c += 8) {
+                bool out = false;
+                for (int e = 0; e < 8; ++e) out |= !isfinite(Logit<T>::to_float(v[column + c + e]));
+                for (int e = 0; out && e < 8; ++e) o[c + e] += w * Logit<T>::to_float(v[column + c + e]);
+            }
+        }
+}
+
+// A warpgroup's part: a thread to a row.
+template <typename T, int D>
+__device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
+    using S = CaShape<D>;
+    constexpr int KT = S::KT;
+    const int group = (int)threadIdx.x / 128, lane_row = (int)threadIdx.x % 128;          // (stream, row of its tile)
+    const uint32_t lanes = (uint32_t)(lane_row / 32) << 21;                               // this warp's lanes of the tensor memory
+    const uint32_t tm = ctl->tensor + lanes;
+    volatile int32_t* failed = &ctl->failed;
+    const float factor = p.scale * LOG2E;
+    CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
+    uint32_t s_phase[2] = {0, 0}, o_phase = 0, step_phase = 0, meeting = 0;
+    int32_t tiles_done = 0;
+    while (walk.next()) {
+        const auto& b = walk.block;
+        const bool both = S::STREAMS == 2 && b.rows > CA_ROWS;           // streams have rows of their own
+        const int32_t n = walk.tile1 - walk.tile0;
+        const int32_t row = (both ? group * CA_ROWS : 0) + lane_row;     // of the item
+        const bool held = row < b.rows, warp_held = (row & ~31) < b.rows;
+        const uint32_t token = (uint32_t)(b.first + min(row, b.rows - 1)) / (uint32_t)p.group, g = (uint32_t)(b.first + min(row, b.rows - 1)) - token * p.group;
+        const int32_t seen = (int32_t)max(-1ll, min((long long)walk.seq.base + token + 1, (long long)b.end));       // tokens of the row
+        const int32_t first = both || S::STREAMS == 1 ? 0 : group, step = both || S::STREAMS == 1 ? 1 : 2;
+        float reference = LOWEST, sum = 0.0f, lost = 0.0f;
+        bool ok = true;
+        for (int32_t i = first; i < n; i += step) {
+            const int buffer = both ? group : (S::STREAMS == 2 ? group : i & 1);
+            ok = __all_sync(FULL_MASK, ca_wait(&ctl->s_full[buffer], s_phase[buffer], failed));
+            if (!ok) break;
+            s_phase[buffer] ^= 1;
+            ca_after_sync();
+            if (warp_held) {
+                float x[KT];
+#pragma unroll
+                for (int c = 0; c < KT; c += 32) ca_tm_load(tm + buffer * 128 + c, x + c);
+#pragma unroll
+                for (int c = 0; c < KT; c += 32) ca_tm_loaded(x + c);
+                const uint4 mask = *reinterpret_cast<const uint4*>(ctl->mask[(tiles_done + i) % CA_MASKS]);
+                const int32_t left = seen - (walk.tile0 + i) * KT;
+                if (left < KT || (mask.x & mask.y & mask.z & mask.w) != ~0u) {
+                    const int32_t limit = max(0, left);
+                    const uint32_t word[4] = {mask.x, mask.y, mask.z, mask.w};
+#pragma unroll
+                    for (int c = 0; c < KT; ++c)
+                        if (c >= limit || !(word[c / 32] >> (c % 32) & 1u)) x[c] = -INFINITY;
+                }
+                float most[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+                for (int c = 4; c < KT; ++c) most[c % 4] = fmaxf(most[c % 4], x[c]);
+                const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * factor;
+                const bool raise = top > reference + CaType<T>::RAISE;
+                if (__any_sync(FULL_MASK, raise)) {
+                    const float next = raise ? top : reference, by = raise ? exp2_approx(reference - next) : 1.0f;
+                    reference = next;
+                    sum *= by;
+                    lost *= by;
+                    if (i > first) {
+                        if (S::STREAMS == 1) {           // the products of the tile before may still run
+                            ok = __all_sync(FULL_MASK, ca_wait(&ctl->o_step, step_phase ^ 1u, failed));
+                            ca_after_sync();
+                        }
+                        const uint32_t o = tm + S::O_AT + (S::STREAMS == 2 ? group * D : 0);
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 32) {
+                            float y[32];
+                            ca_tm_load(o + c, y);
+                            ca_tm_loaded(y);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) y[e] *= by;
+                            ca_tm_store(o + c, reinterpret_cast<uint32_t*>(y));
+                        }
+                    }
+                }
+                const F32x2 by = f2_make(factor, factor), minus = f2_make(CaType<T>::LIFT - reference, CaType<T>::LIFT - reference);
+                F32x2 part[4];
+#pragma unroll
+                for (int c0 = 0; c0 < KT; c0 += 32) {
+                    uint32_t packed[16];
+#pragma unroll
+                    for (int c = c0; c < c0 + 32; c += 2) {
+                        float u, v;
+                        f2_split(f2_fma(f2_make(x[c], x[c + 1]), by, minus), u, v);
+                        u = exp2_approx(u);
+                        v = exp2_approx(v);
+                        const F32x2 w = f2_make(u, v);
+                        part[c / 2 % 4] = c < 8 ? w : f2_add(part[c / 2 % 4], w);
+                        packed[(c - c0) / 2] = CaType<T>::pack(u, v);
+                    }
+                    ca_tm_store16(tm + buffer * 128 + c0 / 2, packed);
+                }
+                float u, v;
+                f2_split(f2_add(f2_add(part[0], part[1]), f2_add(part[2], part[3])), u, v);
+                const float y = (u + v) - lost, more = sum + y;          // (what a sum loses is taken off the next addend)
+                lost = (more - sum) - y;
+                sum = more;
+                ca_tm_stored();
+            }
+            step_phase ^= 1;
+            ca_before_sync();
+            __syncwarp();
+            if (lane_id() == 0) ca_arrive(&ctl->p_full[buffer]);
+            if (!ok) break;
+        }
+        if (!ok) break;
+        // --- the item's output: this thread's row
+        const bool shared = S::STREAMS == 2 && !both;                    // two streams share rows: the first writes
+        const bool mine = both || group == 0;
+        const int32_t others = shared ? n / 2 : 0;                       // tiles of the second stream
+        if (n > first) {
+            ok = __all_sync(FULL_MASK, ca_wait(&ctl->o_full[S::STREAMS == 2 ? group : 0], o_phase, failed));
+            if (!ok) break;
+            o_phase ^= 1;
+        }
+        float lift = 1.0f, other_lift = 0.0f;
+        if (shared && n > 0) {
+            if (group == 1) ctl->other[lane_row] = make_float2(reference, sum);
+            ca_before_sync();
+            if (!ca_meet(&ctl->weighers, meeting, failed)) break;
+            ca_after_sync();
+            if (mine && others > 0) {
+                const float2 o = ctl->other[lane_row];
+                const float most = fmaxf(reference, o.x);
+                lift = exp2_approx(reference - most);
+                other_lift = exp2_approx(o.x - most);
+                sum = sum * lift + o.y * other_lift;
+                reference = most;
+            }
+        }
+        ca_after_sync();
+        if (mine && warp_held) {
+            const int64_t out_row = (int64_t)(walk.seq.row0 + token) * p.heads + (int64_t)walk.head * p.group + g;
+            const bool whole = walk.whole();
+            const int32_t slot = (int32_t)blockIdx.x * 2 + (walk.tile0 == 0 ? 1 : 0);
+            float* part = whole ? nullptr : p.parts + ((int64_t)slot * S::BLOCK + row) * D;
+            const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+            bool any_bad = false;
+            const uint32_t(*bad)[4] = ctl->bad[max(walk.number, 0) % CA_ITEMS];
+            if (n > 0) {
+                uint32_t seen_bad = 0;
+                for (int i = 0; i < CA_BAD_TILES * 4; ++i) seen_bad |= bad[i / 4][i % 4];
+                any_bad = seen_bad != 0;
+            }
+            const T* q = p.q + (p.starts ? (int64_t)walk.seq.row0 * p.q_token : walk.seq_number * p.q_seq) + token * p.q_token + ((int64_t)walk.head * p.group + g) * p.q_head;
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+                if (c >= p.dim) break;
+                __syncwarp();
+                float y[32];
+                if (n > 0) {
+                    ca_tm_load(tm + S::O_AT + (both ? group * D : 0) + c, y);
+                    ca_tm_loaded(y);
+                    if (others > 0) {
+                        float z[32];
+                        ca_tm_load(tm + S::O_AT + D + c, z);
+                        ca_tm_loaded(z);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) y[e] = y[e] * lift + z[e] * other_lift;
+                    }
+                    if (any_bad && held) {
+                        float z[32];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) z[e] = y[e];
+                        ca_add_bad<T, D>(p, bad, p.tables + walk.seq_number * p.table_stride, walk.head, q, walk.tile0, walk.tile1, seen, factor, reference - CaType<T>::LIFT, c, z);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) y[e] = z[e];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) y[e] = 0.0f;
+                }
+                if (!held) continue;
+                if (part) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(part + c + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        if (c + e >= p.dim) break;
+                        float f[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) f[j] = sum == 0.0f ? 0.0f : y[e + j] * inverse;
+                        *reinterpret_cast<uint4*>(p.out + out_row * p.dim + c + e) = Logit<T>::pack(f);
+                    }
+                }
+            }
+            if (held) {
+                if (whole) p.lse[out_row] = sum == 0.0f ? -INFINITY : (reference - CaType<T>::LIFT + log2f(sum)) * 0.6931471805599453f;
+                else p.sums[(int64_t)slot * S::BLOCK + row] = make_float2(reference, sum);
+            }
+            if (!whole && row == 0) {
+                CaMeta* m = p.meta + slot;
+                m->valid = 1;
+                m->last = walk.tile1 == b.tiles;
+                m->rows = b.rows;
+                m->row0 = walk.seq.row0;
+                m->head = walk.head;
+                m->first = b.first;
+            }
+        }
+        ca_before_sync();
+        if (shared && n > 0 && !ca_meet(&ctl->weighers, meeting, failed)) break;
+        ca_after_sync();
+        tiles_done += n;
+    }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(CA_THREADS, 1) paged_attention_chunk_kernel(const CaParams<T> p) {
+    using S = CaShape<D>;
+    extern __shared__ __align__(1024) char ca_memory[];
+    char* queries = ca_memory;
+    char* stages = ca_memory + S::STREAMS * S::Q_TILE;
+    CaControl<D>* ctl = reinterpret_cast<CaControl<D>*>(stages + S::STAGES * S::STAGE);
+    const int32_t warp = (int32_t)threadIdx.x / 32;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::STAGES; ++i) {
+            ca_bar_init(&ctl->full[i], CA_LOADERS / 32);
+            ca_bar_init(&ctl->empty[i], 1);
+        }
+        ca_bar_init(&ctl->q_full, CA_LOADERS / 32);
+        ca_bar_init(&ctl->q_free, 1);
+        for (int i = 0; i < 2; ++i) {
+            ca_bar_init(&ctl->s_full[i], 1);
+            ca_bar_init(&ctl->p_full[i], 4);
+            ca_bar_init(&ctl->o_full[i], 1);
+        }
+        ca_bar_init(&ctl->o_step, 1);
+        ca_bar_init(&ctl->loaders, CA_LOADERS / 32);
+        ca_bar_init(&ctl->weighers, 8);
+        ca_bar_init(&ctl->drain, 1);
+        ctl->failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 11) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(ca_smem(&ctl->tensor)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        ca_before_sync();
+    }
+    pdl_wait();
+    pdl_launch_dependents();
+    if (threadIdx.x < 2) {
+        CaMeta* m = p.meta + blockIdx.x * 2 + threadIdx.x;
+        m->valid = m->last = m->failed = 0;
+    }
+    ca_plan<T, D>(p, ctl);
+    ca_after_sync();
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(CA_MANY_REGISTERS));
+        if (p.starts) {
+            // rows that no sequence holds
+            const int64_t a = max(0, min(p.starts[0], p.rows)), z = max(a, (int64_t)min(p.starts[p.seqs], p.rows));
+            const int64_t t = (int64_t)blockIdx.x * 256 + (int)threadIdx.x, all = (int64_t)gridDim.x * 256;
+            const int64_t per = (int64_t)p.heads * p.dim / 8, n = a + p.rows - z;
+            for (int64_t i = t; i < n * per; i += all) {
+                const int64_t r = i / per, row = r < a ? r : r - a + z;
+                reinterpret_cast<uint4*>(p.out)[row * per + i % per] = make_uint4(0, 0, 0, 0);
+            }
+            for (int64_t i = t; i < n * p.heads; i += all) {
+                const int64_t r = i / p.heads, row = r < a ? r : r - a + z;
+                p.lse[row * p.heads + i % p.heads] = -INFINITY;
+            }
+            __syncwarp();
+        }
+        if (S::STREAMS == 2 || warp < 4) ca_weigh<T, D>(p, ctl);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CA_FEW_REGISTERS));
+        if (warp < 11) {
+            ca_load<T, D>(p, ctl, queries, stages);
+        } else {
+            if (lane_id() == 0) ca_multiply<T, D>(p, ctl, ca_smem(queries), ca_smem(stages));
+            __syncwarp();
+        }
+    }
+    ca_before_sync();
+    __syncthreads();
+    if (threadIdx.x == 0 && ctl->failed) p.meta[blockIdx.x * 2].failed = 1;
+    if (warp == 11) {
+        if (ctl->failed) {                                               // products may be under way still
+            int32_t ignored = 0;
+            if (lane_id() == 0) {
+                ca_commit(&ctl->drain);
+                (void)ca_wait(&ctl->drain, 0, &ignored);
+            }
+            __syncwarp();
+        }
+        ca_after_sync();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(ctl->tensor));
+    }
+}
+
+// Joins the parts of the item that begins in CTA x's share and goes on in the next ones'; rows are spread over grid.y.
+constexpr int CJ_THREADS = 256;
+template <typename T, int D>
+__global__ void __launch_bounds__(CJ_THREADS) paged_attention_chunk_join_kernel(const CaParams<T> p, int32_t ctas) {
+    using S = CaShape<D>;
+    pdl_wait();
+    pdl_launch_dependents();
+    // (a wait of the first kernel that ran out leaves its outputs unwritten: then none are given)
+    bool failed = false;
+    for (int32_t c = (int32_t)threadIdx.x; c < ctas; c += CJ_THREADS) failed |= p.meta[c * 2].failed != 0;
+    if (__syncthreads_or(failed)) {
+        const int64_t t = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * CJ_THREADS + threadIdx.x, all = (int64_t)gridDim.x * gridDim.y * CJ_THREADS;
+        for (int64_t i = t; i < (int64_t)p.rows * p.heads * p.dim; i += all) p.out[i] = Logit<T>::from_float(NAN);
+        for (int64_t i = t; i < (int64_t)p.rows * p.heads; i += all) p.lse[i] = NAN;
+        return;
+    }
+    const int32_t c0 = (int32_t)blockIdx.x;
+    const CaMeta m = p.meta[c0 * 2 + 1];
+    if (!m.valid) return;
+    const int32_t warp = (int32_t)threadIdx.x / 32, lane = (int32_t)lane_id();
+    int32_t last = c0 + 1;                                               // the CTA with the item's last part
+    for (uint32_t found = 0; last < ctas; last += 32) {
+        found = __ballot_sync(FULL_MASK, last + lane < ctas && p.meta[(last + lane) * 2].last != 0);
+        if (found) { last += __ffs((int)found) - 1; break; }
+    }
+    last = min(last, ctas - 1);
+    auto slot_of = [&](int32_t c) { return (int64_t)(c == c0 ? c0 * 2 + 1 : c * 2); };
+    for (int32_t row = (int32_t)blockIdx.y * (CJ_THREADS / 32) + warp; row < m.rows; row += (int32_t)gridDim.y * (CJ_THREADS / 32)) {
+        float most = LOWEST;
+        for (int32_t c = c0 + lane; c <= last; c += 32) most = fmaxf(most, p.sums[slot_of(c) * S::BLOCK + row].x);
+        for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(FULL_MASK, most, d));
+        float sum = 0.0f, o[D / 32] = {};
+#pragma unroll 4
+        for (int32_t c = c0; c <= last; ++c) {
+            const float2 s = p.sums[slot_of(c) * S::BLOCK + row];
+            const float by = exp2_approx(s.x - most);
+            sum += s.y * by;
+            const float* part = p.parts + (slot_of(c) * S::BLOCK + row) * D;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) o[j] += part[lane + 32 * j] * by;
+        }
+        const uint32_t r = (uint32_t)(m.first + row), token = r / (uint32_t)p.group, g = r - token * p.group;
+        const int64_t out_row = (int64_t)(m.row0 + token) * p.heads + (int64_t)m.head * p.group + g;
+        const float inverse = 1.0f / sum;
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) {
+            if (lane + 32 * j < p.dim) p.out[out_row * p.dim + lane + 32 * j] = Logit<T>::from_float(sum == 0.0f ? 0.0f : o[j] * inverse);
+        }
+        if (lane == 0) p.lse[out_row] = sum == 0.0f ? -INFINITY : (most - CaType<T>::LIFT + log2f(sum)) * 0.6931471805599453f;
+    }
+}
+
+}  // namespace profk

@@ -541,6 +541,45 @@ PyObject* pages_append_rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) 
     });
 }
 
+// (q, k_pages, v_pages, tables, lengths, starts, scale) -> (out, lse); scale None: dim ** -0.5
+PyObject* paged_attention_chunk(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+    return guarded([&]() -> PyObject* {
+        need(n_args == 7, "paged_attention_chunk takes seven arguments");
+        const at::Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k_pages"), &v = tensor(a[2], "v_pages"), &tables = tensor(a[3], "tables"),
+                         &lengths = tensor(a[4], "lengths");
+        const at::Tensor* starts = optional(a[5], "starts");
+        for (const auto& [t, what] : {std::pair{&q, "q"}, {&k, "k_pages"}, {&v, "v_pages"}}) no_derivative(t, what);
+        need(q.is_cuda(), "q must be a CUDA tensor");
+        pages_pair(k, v);
+        const c10::Device dev = q.device();
+        const int64_t stride = table_stride(tables, dev), seqs = tables.size(0), d = q.dim();
+        const int32_t* lengths_p = ints(lengths, "lengths", 1, dev);
+        need(lengths.size(0) == seqs, "tables and lengths must have the same number of sequences");
+        need(starts ? d == 3 : d == 4, "q must be of shape (seqs, tokens, heads, dim), or with starts (rows, heads, dim)");
+        const NewRows rows = new_rows(q, "q", starts, seqs, dev);
+        const int64_t heads = q.size(d - 2), dim = q.size(d - 1);
+        need(q.numel() == 0 || dense_rows(q), "q must have dense heads");
+        need(heads > 0 && k.scalar_type() == q.scalar_type() && k.device() == dev && k.size(3) == dim && heads % k.size(1) == 0,
+             "q and pages do not belong together (type, device, dim or heads differ)");
+        need(q.scalar_type() == at::kBFloat16 || q.scalar_type() == at::kHalf, "unsupported dtype: bfloat16 and float16 only");
+        const double scale = a[6] == Py_None ? 1.0 / std::sqrt((double)dim) : real(a[6], "scale");
+        const c10::cuda::CUDAGuard guard(dev);
+        const at::Tensor out = fresh(q.sizes(), q.scalar_type(), dev), lse = fresh(q.sizes().slice(0, d - 1), at::kFloat, dev);
+        if (rows.rows == 0) return pack({wrap(out), wrap(lse)});
+        size_t bytes = 0;
+        status(profk_paged_attention_chunk_workspace_bytes(dim, &bytes), "profk_paged_attention_chunk");
+        const at::Tensor ws = fresh({(int64_t)bytes}, at::kByte, dev);
+        const Strides3 qs = row_strides(q, starts);
+        const profk_page_strides_t ks = strides_of(k, 1), vs = strides_of(v, 1);
+        auto* call = q.scalar_type() == at::kHalf ? &profk_paged_attention_chunk_f16 : &profk_paged_attention_chunk_bf16;
+        status(call(q.data_ptr(), qs.data(), k.data_ptr(), v.data_ptr(), &ks, &vs, static_cast<const int32_t*>(tables.data_ptr()), stride, lengths_p, rows.starts, seqs,
+                    rows.rows, heads, k.size(1), dim, k.size(2), k.size(0), tables.size(1), scale, ws.data_ptr(), bytes,
+                    c10::cuda::getCurrentCUDAStream(dev.index()).stream(), out.data_ptr(), static_cast<float*>(lse.data_ptr())),
+               "profk_paged_attention_chunk");
+        return pack({wrap(out), wrap(lse)});
+    });
+}
+
 // Something of n values per row of logits, or (of one dimension) the same for all rows: its stride between rows; null: not given.
 template <typename P>
 const P* beside_rows(const at::Tensor* t, const char* what, at::ScalarType type, at::IntArrayRef lead, c10::Device device, int64_t* n, int64_t* stride) {
@@ -634,7 +673,7 @@ PyObject* set_errors(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {FAST(logprobs), FAST(logprobs_backward), FAST(pages_fork), FAST(pages_compact), FAST(pages_copy), FAST(pages_append), FAST(paged_attention),
-                           FAST(rotary), FAST(pages_append_rotary), FAST(adjust_logits), FAST(set_errors), {nullptr, nullptr, 0, nullptr}};
+                           FAST(rotary), FAST(pages_append_rotary), FAST(paged_attention_chunk), FAST(adjust_logits), FAST(set_errors), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_decode", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -218,6 +218,18 @@ def pages_append_rotary(k_pages, v_pages, tables, lengths, q, k, v, frequencies,
     return (_native or _load()).pages_append_rotary(k_pages, v_pages, tables, lengths, q, k, v, frequencies, starts, positions, bool(interleaved), magnitude)
 
 
+def paged_attention_chunk(q, k_pages, v_pages, tables, lengths, *, starts=None, scale: Optional[float] = None):
+    """`profk_paged_attention_chunk_*` on the current stream: attention of several new tokens per sequence (a prompt or a part of it,
+    drafted tokens) over one layer's pages, which hold their keys and values already.  Token t of n new ones of a sequence of
+    length L sees the tokens up to place L - n + t.
+
+    q: (seqs, tokens, heads, dim), or with `starts` (seqs + 1,) int32 (rows, heads, dim), where sequence s has the rows starts[s] to
+    starts[s + 1] - 1; bfloat16 or float16, any strides with dense heads.  Pages, tables, lengths and scale as for
+    `paged_attention`, the form for one token.  Returns (out, of q's shape, lse (..., heads) float32); rows that no sequence
+    holds come back as 0 and -inf."""
+    return (_native or _load()).paged_attention_chunk(q, k_pages, v_pages, tables, lengths, starts, scale)
+
+
 def adjust_logits(logits, tokens=None, lengths=None, prompts=None, *, repetition=1.0, frequency=0.0, presence=0.0, bias_tokens=None,
                   bias_values=None, mask=None, out=None):
     """`profk_adjust_logits_*` on the current stream: what a sampler lays over logits before `logprobs` or `topk`.
