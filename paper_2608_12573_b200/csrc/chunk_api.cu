@@ -1,5 +1,9 @@
 // C ABI of the attention of a chunk of new tokens over a paged cache (see profk.h): argument checks, launch shapes, launches.
+#include <cudaTypedefs.h>
+
 #include <algorithm>
+#include <numeric>
+#include <type_traits>
 
 #include "chunk_attention.cuh"
 #include "decode_host.cuh"
@@ -37,8 +41,41 @@ cudaError_t ca_prepare(K* kernel, size_t smem, uint64_t* done, std::mutex* mutex
     return prepare_kernel(kernel, smem, done, mutex);
 }
 
+// The driver's function that writes a tensor map; null: not to be had.
+PFN_cuTensorMapEncodeTiled_v12000 ca_encoder() {
+    static const auto encode = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            f = nullptr;
+        }
+        return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+    }();
+    return encode;
+}
+
+// Four dimensions (the first dense), strides of the others in elements; boxes of 64 elements x `second` x `third` x 1, swizzled.
+// False where such copies cannot be had (a stride of zero, or too long a one).
+template <typename T>
+bool ca_map(CUtensorMap* map, const T* base, const int64_t* sizes, const int64_t* steps, int64_t second, int64_t third) {
+    const auto encode = ca_encoder();
+    if (!encode || second > 256 || third > 256) return false;
+    cuuint64_t dims[4], strides[3];
+    for (int i = 0; i < 4; ++i) dims[i] = (cuuint64_t)sizes[i];
+    for (int i = 0; i < 3; ++i) {
+        const int64_t step = sizes[i + 1] == 1 ? (sizes[0] + 7) / 8 * 8 : steps[i];        // (of one there is no stride)
+        if (step <= 0 || step % 8 != 0 || step >= (1ll << 40) / (int64_t)sizeof(T)) return false;
+        strides[i] = (cuuint64_t)step * sizeof(T);
+    }
+    const cuuint32_t box[4] = {64, (cuuint32_t)second, (cuuint32_t)third, 1}, ones[4] = {1, 1, 1, 1};
+    const CUtensorMapDataType type = std::is_same_v<T, __half> ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    return encode(map, type, 4, const_cast<T*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename T, int D>
-int ca_launch(CaParams<T> p, int sms, void* workspace, void* stream) {
+int ca_launch(CaParams<T> p, const CaMaps& maps, int sms, void* workspace, void* stream) {
     static uint64_t done = 0;
     static std::mutex mutex;
     DEC_TRY(ca_prepare(paged_attention_chunk_kernel<T, D>, ca_smem_bytes<D>(), &done, &mutex));
@@ -47,7 +84,7 @@ int ca_launch(CaParams<T> p, int sms, void* workspace, void* stream) {
     p.sums = reinterpret_cast<float2*>(w + ca_meta_bytes(sms));
     p.parts = reinterpret_cast<float*>(w + ca_meta_bytes(sms) + ca_sums_bytes(sms, CaShape<D>::BLOCK));
     Launch l((unsigned)sms, CA_THREADS, ca_smem_bytes<D>(), stream);
-    DEC_TRY(cudaLaunchKernelEx(&l.cfg, paged_attention_chunk_kernel<T, D>, p));
+    DEC_TRY(cudaLaunchKernelEx(&l.cfg, paged_attention_chunk_kernel<T, D>, p, maps));
     Launch j((unsigned)sms, CJ_THREADS, 0, stream);
     j.cfg.gridDim.y = CA_JOIN_ROWS;
     DEC_TRY(cudaLaunchKernelEx(&j.cfg, paged_attention_chunk_join_kernel<T, D>, p, (int32_t)sms));
@@ -96,16 +133,25 @@ int ca_run(const T* q, const int64_t* qs, const T* k, const T* v, const profk_pa
     p.page_size = (int32_t)page_size;
     p.pages = (int32_t)pages;
     p.width = (int32_t)width;
-    p.page_shift = -1;
-    for (int32_t s = 0; s < 31; ++s)
-        if ((int64_t)1 << s == page_size) p.page_shift = s;
+    p.by_group = CaDivisor::of((uint32_t)p.group);
+    p.by_page = CaDivisor::of((uint32_t)page_size);
     p.scale = (float)scale;
     p.out = out;
     p.lse = lse;
-    switch (ca_tile_dim(dim)) {
-        case 64: return ca_launch<T, 64>(p, sms, workspace, stream);
-        case 128: return ca_launch<T, 128>(p, sms, workspace, stream);
-        default: return ca_launch<T, 256>(p, sms, workspace, stream);
+    // copies by tile want boxes of eight tokens (one atom of the swizzle) at least that never leave a page
+    CaMaps maps{};
+    const int tile_dim = ca_tile_dim(dim), tile = tile_dim == 256 ? CaShape<256>::KT : CaShape<128>::KT;
+    const int box = (int)std::gcd(page_size, (int64_t)tile);
+    const int64_t kv_sizes[4] = {dim, page_size, kv_heads, pages}, k_steps[3] = {ks->token, ks->head, ks->page}, v_steps[3] = {vs->token, vs->head, vs->page};
+    if (box >= 8 && ca_map<T>(&maps.k, k, kv_sizes, k_steps, box, 1) && ca_map<T>(&maps.v, v, kv_sizes, v_steps, box, 1)) p.box = box;
+    if (p.box && p.q_wide && CA_ROWS % p.group == 0) {
+        const int64_t sizes[4] = {dim, heads, starts ? rows : p.tokens, starts ? 1 : seqs}, steps[3] = {qs[2], qs[1], qs[0]};
+        p.q_box = ca_map<T>(&maps.q, q, sizes, steps, p.group, CA_ROWS / p.group);
+    }
+    switch (tile_dim) {
+        case 64: return ca_launch<T, 64>(p, maps, sms, workspace, stream);
+        case 128: return ca_launch<T, 128>(p, maps, sms, workspace, stream);
+        default: return ca_launch<T, 256>(p, maps, sms, workspace, stream);
     }
 }
 

@@ -22,6 +22,8 @@
 // cost whatever the lengths; items that a cut goes through leave unnormalised parts, which a second kernel joins in order.
 #pragma once
 
+#include <cuda.h>
+
 #include "logits.cuh"
 
 namespace profk {
@@ -46,6 +48,20 @@ struct CaShape {
     static constexpr int O_AT = 256;                                     // columns of the tensor memory: S 0 and 128, O from here
 };
 
+// n / d for n < 2^31 by a multiplication: m = ceil(2^(31 + l) / d), l = ceil(log2 d), and n m >> (31 + l).
+struct CaDivisor {
+    uint32_t d, m, shift;                 // shift: l - 1; d = 1 has none
+    __host__ static CaDivisor of(uint32_t d) {
+        uint32_t l = 0;
+        while ((1ull << l) < d) ++l;
+        return {d, d == 1 ? 0u : (uint32_t)(((1ull << (31 + l)) + d - 1) / d), l - 1};
+    }
+    __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return d == 1 ? n : __umulhi(n, m) >> shift; }
+};
+
+// Descriptions of keys, values (dim, token of a page, head, page) and queries (dim, head, token, sequence) for tiled copies.
+struct CaMaps { CUtensorMap k, v, q; };
+
 template <typename T>
 struct CaParams {
     const T* q;
@@ -58,7 +74,10 @@ struct CaParams {
     const int32_t* lengths;
     const int32_t* starts;                // null: `tokens` rows each
     int32_t rows, tokens;
-    int32_t seqs, heads, kv_heads, group, dim, page_size, pages, width, page_shift;
+    int32_t seqs, heads, kv_heads, group, dim, page_size, pages, width;
+    CaDivisor by_group, by_page;
+    int32_t box;                          // tokens of one tiled copy: they never leave a page; 0: tokens are copied one by one
+    bool q_box;                           // queries are copied by tile, too
     bool q_wide;                          // rows of q lie on 16-byte vectors
     float scale;
     T* out;
@@ -97,11 +116,11 @@ __device__ __forceinline__ CaSeq ca_seq(const CaParams<T>& p, int32_t s) {
 template <int D>
 struct CaBlock {
     int32_t first, rows, end, tiles;
-    __device__ __forceinline__ CaBlock(const CaSeq& s, int32_t group, int32_t room, int32_t b) {
+    __device__ __forceinline__ CaBlock(const CaSeq& s, const CaDivisor& group, int32_t room, int32_t b) {
         using S = CaShape<D>;
         first = b * S::BLOCK;
-        rows = min(S::BLOCK, s.n * group - first);
-        end = (int32_t)max(0ll, min((long long)s.base + (uint32_t)(first + rows - 1) / (uint32_t)group + 1, (long long)room));
+        rows = min(S::BLOCK, s.n * (int32_t)group.d - first);
+        end = (int32_t)max(0ll, min((long long)s.base + group.quotient((uint32_t)(first + rows - 1)) + 1, (long long)room));
         tiles = (int32_t)(((uint32_t)end + S::KT - 1) / S::KT);
     }
     __device__ __forceinline__ int32_t weight() const { return rows > CA_ROWS ? 2 : 1; }
@@ -112,9 +131,9 @@ struct CaBlock {
 template <int D>
 __device__ __forceinline__ int32_t ca_blocks(const CaSeq& s, int32_t group) { return (int32_t)(((uint32_t)(s.n * group) + CaShape<D>::BLOCK - 1) / CaShape<D>::BLOCK); }
 template <int D>
-__device__ __forceinline__ int64_t ca_head_cost(const CaSeq& s, int32_t group, int32_t room) {
+__device__ __forceinline__ int64_t ca_head_cost(const CaSeq& s, const CaDivisor& group, int32_t room) {
     int64_t sum = 0;
-    for (int32_t b = 0, n = ca_blocks<D>(s, group); b < n; ++b) sum += CaBlock<D>(s, group, room, b).cost();
+    for (int32_t b = 0, n = ca_blocks<D>(s, (int32_t)group.d); b < n; ++b) sum += CaBlock<D>(s, group, room, b).cost();
     return sum;
 }
 
@@ -138,7 +157,7 @@ struct CaWalk {
     int32_t tile0, tile1;
     __device__ __forceinline__ CaWalk(const CaParams<T>& params, const CaPlace& start, int64_t from, int64_t to)
         : p(params), left(from < to ? to - start.at : 0), skip(from < to ? (int32_t)(from - start.at) : 0), block_number(start.block), seq_number(start.seq),
-          head(start.head), seq(ca_seq(params, from < to ? start.seq : 0)), block(seq, params.group, room(), from < to ? start.block : 0), tile0(0), tile1(0) {}
+          head(start.head), seq(ca_seq(params, from < to ? start.seq : 0)), block(seq, params.by_group, room(), from < to ? start.block : 0), tile0(0), tile1(0) {}
     __device__ __forceinline__ int32_t room() const { return p.width * p.page_size; }
     __device__ __forceinline__ bool next() {
         for (;;) {
@@ -156,7 +175,7 @@ struct CaWalk {
                         } while (seq.n == 0);
                     }
                 }
-                block = CaBlock<D>(seq, p.group, room(), block_number);
+                block = CaBlock<D>(seq, p.by_group, room(), block_number);
             } else {
                 if (left <= 0) return false;
                 begun = true;
@@ -181,7 +200,13 @@ __device__ __forceinline__ void ca_bar_init(uint64_t* bar, uint32_t count) {
 __device__ __forceinline__ void ca_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(ca_smem(bar)) : "memory");
 }
+// Whether a phase has passed, at once; and likewise after the hardware has waited for it a while.
 __device__ __forceinline__ bool ca_test(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(ca_smem(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool ca_try(uint64_t* bar, uint32_t parity) {
     uint32_t ok;
     asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(ca_smem(bar)), "r"(parity) : "memory");
     return ok != 0;
@@ -189,7 +214,7 @@ __device__ __forceinline__ bool ca_test(uint64_t* bar, uint32_t parity) {
 // Waits for a phase; gives up after a limit, or when another warp has, and then returns false for good.
 __device__ __forceinline__ bool ca_wait(uint64_t* bar, uint32_t parity, volatile int32_t* failed) {
     for (int32_t i = 0; i < CA_POLLS; ++i) {
-        if (ca_test(bar, parity)) return true;
+        if (ca_try(bar, parity)) return true;
         if (*failed) return false;
     }
     *failed = 1;
@@ -288,7 +313,7 @@ __device__ __forceinline__ void ca_copy(uint32_t to, const void* from, bool ther
 template <int D>
 struct CaControl {
     uint64_t full[CaShape<D>::STAGES], empty[CaShape<D>::STAGES];
-    uint64_t q_full, q_free, s_full[2], p_full[2], o_full[2], o_step, loaders, weighers, drain;
+    uint64_t q_full, q_free, s_full[2], p_full[2], o_full[2], o_step, loaders, weighers, opened, asked, looked, drain;
     uint32_t tensor;                      // address of the tensor memory
     int32_t failed;
     int32_t table[2][CaShape<D>::KT];     // pages of two tiles' tokens; -1: nothing there
@@ -303,15 +328,24 @@ template <int D>
 constexpr size_t ca_smem_bytes() { return CaShape<D>::STREAMS * CaShape<D>::Q_TILE + CaShape<D>::STAGES * CaShape<D>::STAGE + sizeof(CaControl<D>); }
 static_assert(ca_smem_bytes<128>() <= 232448 && ca_smem_bytes<256>() <= 232448 && ca_smem_bytes<64>() <= 232448, "an SM's shared memory");
 
+__device__ __forceinline__ int64_t ca_quotient(int64_t a, int64_t b) { return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b; }
+
 // Units of all items, and the share of this CTA: [bound[0], bound[1]) of them, beginning at place[0].  A cut that would leave
-// little of an item on either side is moved to the item's nearer end: parts cost their reading and writing.
+// little of an item on either side is moved to the item's nearer end: parts cost their reading and writing.  Each half of the
+// threads goes over all sequences and finds one of the two bounds.
 template <typename T, int D>
 __device__ void ca_plan(const CaParams<T>& p, CaControl<D>* ctl) {
+    constexpr int HALF = CA_THREADS / 2;
     const int32_t room = p.width * p.page_size;
-    const int32_t tid = (int32_t)threadIdx.x, lane = tid & 31, warp = tid / 32;
-    const int32_t per = (p.seqs + CA_THREADS - 1) / CA_THREADS, s0 = min(p.seqs, tid * per), s1 = min(p.seqs, s0 + per);
-    int64_t mine = 0;
-    for (int32_t s = s0; s < s1; ++s) mine += ca_head_cost<D>(ca_seq(p, s), p.group, room) * p.kv_heads;
+    const int32_t which = (int32_t)threadIdx.x / HALF, tid = (int32_t)threadIdx.x % HALF, lane = tid & 31, warp = (int32_t)threadIdx.x / 32;
+    const int32_t per = (p.seqs + HALF - 1) / HALF, s0 = min(p.seqs, tid * per), s1 = min(p.seqs, s0 + per);
+    int64_t mine = 0, one = 0;
+    CaSeq seq{};
+    for (int32_t s = s0; s < s1; ++s) {
+        seq = ca_seq(p, s);
+        one = ca_head_cost<D>(seq, p.by_group, room);
+        mine += one * p.kv_heads;
+    }
     int64_t upto = mine;
     for (int d = 1; d < 32; d *= 2) {
         const int64_t o = __shfl_up_sync(FULL_MASK, upto, d);
@@ -320,30 +354,33 @@ __device__ void ca_plan(const CaParams<T>& p, CaControl<D>* ctl) {
     if (lane == 31) ctl->scan[warp] = upto;
     __syncthreads();
     int64_t total = 0, before = upto - mine;
-    for (int w = 0; w < CA_THREADS / 32; ++w) {
-        if (w < warp) before += ctl->scan[w];
-        total += ctl->scan[w];
+    for (int w = 0; w < HALF / 32; ++w) {
+        const int64_t x = ctl->scan[which * (HALF / 32) + w];
+        if (w < warp - which * (HALF / 32)) before += x;
+        total += x;
     }
     const int64_t shares = min((int64_t)gridDim.x, max((int64_t)1, total / 4));       // (a share within an item holds a tile at least)
-    for (int i = 0; i < 2; ++i) {
-        const int64_t c = (int64_t)blockIdx.x + i;
-        const int64_t x = c >= shares ? total : total / shares * c + total % shares * c / shares;
-        if (tid == 0 && x >= total) ctl->bound[i] = total;
-        if (x < before || x >= before + mine) continue;
+    const int64_t c = (int64_t)blockIdx.x + which, each = ca_quotient(total, shares);
+    const int64_t x = c >= shares ? total : each * c + ca_quotient((total - each * shares) * c, shares);
+    if (tid == 0 && x >= total) ctl->bound[which] = total;
+    if (x >= before && x < before + mine) {
         int64_t at = before;
         for (int32_t s = s0; s < s1; ++s) {
-            const CaSeq seq = ca_seq(p, s);
-            const int64_t one = ca_head_cost<D>(seq, p.group, room), all = one * p.kv_heads;
-            if (x >= at + all) { at += all; continue; }
-            CaPlace place{at + (x - at) / one * one, 0, s, (int32_t)((x - at) / one)};
+            if (per > 1) {
+                seq = ca_seq(p, s);
+                one = ca_head_cost<D>(seq, p.by_group, room);
+            }
+            if (x >= at + one * p.kv_heads) { at += one * p.kv_heads; continue; }
+            const int32_t head = (int32_t)ca_quotient(x - at, one);
+            CaPlace place{at + head * one, 0, s, head};
             for (;; ++place.block) {
-                const CaBlock<D> b(seq, p.group, room, place.block);
+                const CaBlock<D> b(seq, p.by_group, room, place.block);
                 if (x >= place.at + b.cost()) { place.at += b.cost(); continue; }
                 // x lies in this item
                 int64_t cut = x;
                 if (x > place.at && b.cost() <= 4 + b.rows / 16) cut = x - place.at < place.at + b.cost() - x ? place.at : place.at + b.cost();
-                ctl->bound[i] = cut;
-                ctl->place[i] = place;                       // (a cut at the item's end: the walk steps over it)
+                ctl->bound[which] = cut;
+                ctl->place[which] = place;                   // (a cut at the item's end: the walk steps over it)
                 break;
             }
             break;
@@ -372,7 +409,7 @@ struct CaLoader {
         else if (newer == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
         else if (newer == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
-        if (check[0] >= 0) look(ctl, stages, check[0] & 255, check[0] >> 8 & 255, check[0] >> 16);
+        if (check[0] >= 0) look(ctl, stages, check[0] & 255, check[0] >> 8 & 255, check[0] >> 16, (int32_t)threadIdx.x - 256, CA_LOAD_ROWS);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane_id() == 0) ca_arrive(pending[0]);
@@ -402,11 +439,10 @@ struct CaLoader {
     static __device__ __forceinline__ uint32_t chunk_at(int32_t row, int32_t chunk, int32_t rows) {
         return (uint32_t)((chunk >> 3) * rows * 128 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4));
     }
-    // This thread's copies of a tile of values: those that are not finite are taken out, and their tokens noted.
-    static __device__ __noinline__ void look(CaControl<D>* ctl, uint32_t stages, int32_t st, int32_t tile, int32_t item) {
-        const int32_t t = (int32_t)threadIdx.x - 256;
+    // A thread's part of a tile of values: vectors that are not finite are taken out, and their tokens noted.
+    static __device__ __noinline__ void look(CaControl<D>* ctl, uint32_t stages, int32_t st, int32_t tile, int32_t item, int32_t t, int32_t rows_at_once) {
         char* base = reinterpret_cast<char*>(__cvta_shared_to_generic(stages + st * S::STAGE));
-        for (int i = 0; i < S::KT * (D / 64); i += CA_LOAD_ROWS) {
+        for (int i = 0; i < S::KT * (D / 64); i += rows_at_once) {
             const int32_t both = i + (t >> 3), row = both % S::KT, chunk = (t & 7) + 8 * (both / S::KT);
             if (both >= S::KT * (D / 64)) break;
             uint4* at = reinterpret_cast<uint4*>(base + chunk_at(row, chunk, S::KT));
@@ -428,7 +464,7 @@ struct CaLoader {
         for (int32_t row = t >> 3; row < S::KT; row += CA_LOAD_ROWS) {
             const int32_t page = ctl->table[buffer][row];
             const uint32_t token = (uint32_t)(first + row);
-            const uint32_t slot = p.page_shift >= 0 ? token & ((1u << p.page_shift) - 1u) : token % (uint32_t)p.page_size;
+            const uint32_t slot = token - p.by_page.quotient(token) * p.by_page.d;
             const T* from = pages + max(page, 0) * page_stride + (page >= 0 ? slot * token_stride : 0);
 #pragma unroll
             for (int h = 0; h < D / 64; ++h) {
@@ -443,6 +479,42 @@ struct CaLoader {
     }
 };
 
+// A thread's part of an item's queries: rows of (token, head), eight threads to 128 bytes.
+template <typename T, int D>
+__device__ __forceinline__ void ca_copy_queries(const CaParams<T>& p, const CaWalk<T, D>& walk, uint32_t q_at, int32_t t, int32_t rows_at_once) {
+    using S = CaShape<D>;
+    const auto& b = walk.block;
+    const T* q = p.q + (p.starts ? (int64_t)walk.seq.row0 * p.q_token : walk.seq_number * p.q_seq) + (int64_t)walk.head * p.group * p.q_head;
+    const int32_t rows = b.rows > CA_ROWS ? 2 * CA_ROWS : CA_ROWS;
+#pragma unroll 4
+    for (int32_t r = t >> 3; r < rows; r += rows_at_once) {
+        const bool held = r < b.rows;
+        const uint32_t token = p.by_group.quotient((uint32_t)(b.first + r)), g = (uint32_t)(b.first + r) - token * p.group;
+        const T* from = held ? q + token * p.q_token + g * p.q_head : p.q;
+#pragma unroll
+        for (int h = 0; h < D / 64; ++h) {
+            const int32_t chunk = (t & 7) + 8 * h;
+            const bool there = held && chunk * 8 < p.dim;
+            const uint32_t to = q_at + r / CA_ROWS * S::Q_TILE + CaLoader<T, D>::chunk_at(r % CA_ROWS, chunk, CA_ROWS);
+            if (p.q_wide) {
+                ca_copy(to, there ? from + chunk * 8 : p.q, there);
+            } else {
+                uint32_t w[4] = {0, 0, 0, 0};
+                if (there)
+                    for (int e = 0; e < 8; ++e) w[e / 2] |= (uint32_t)reinterpret_cast<const unsigned short*>(from)[chunk * 8 + e] << (16 * (e % 2));
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+            }
+        }
+    }
+}
+// The first tile of an item that some row does not see all of.
+template <typename T, int D>
+__device__ __forceinline__ int32_t ca_first_cut(const CaParams<T>& p, const CaWalk<T, D>& walk) {
+    const int64_t seen = (int64_t)walk.seq.base + p.by_group.quotient((uint32_t)walk.block.first) + 1;
+    return (int32_t)(max((int64_t)0, min(seen, (int64_t)walk.block.end)) / CaShape<D>::KT);
+}
+
+// Three warps copy token by token: pages of fewer than eight tokens, or of an odd number.
 template <typename T, int D>
 __device__ void ca_load(const CaParams<T>& p, CaControl<D>* ctl, char* queries, char* stages) {
     using S = CaShape<D>;
@@ -459,43 +531,18 @@ __device__ void ca_load(const CaParams<T>& p, CaControl<D>* ctl, char* queries, 
         const int32_t* table = p.tables + walk.seq_number * p.table_stride;
         auto page_of = [&](int32_t token) -> int32_t {
             if (token >= b.end) return -1;
-            const uint32_t c = p.page_shift >= 0 ? (uint32_t)token >> p.page_shift : (uint32_t)token / (uint32_t)p.page_size;
-            const int32_t page = table[c];
+            const int32_t page = table[p.by_page.quotient((uint32_t)token)];
             return page >= 0 && page < p.pages ? page : -1;
         };
         if (walk.tile1 == walk.tile0) continue;                          // no token to see
         // (the tile's tokens to the threads, the last 32 of 128 to the first warp once more)
         int32_t page = t < S::KT ? page_of(walk.tile0 * S::KT + t) : -1, page2 = t + CA_LOADERS < S::KT ? page_of(walk.tile0 * S::KT + CA_LOADERS + t) : -1;
         if (t < CA_BAD_TILES * 4) ctl->bad[walk.number % CA_ITEMS][t / 4][t % 4] = 0;
-        // queries: rows of (token, head)
         if (!load.wait(&ctl->q_free, q_phase)) break;
         q_phase ^= 1;
-        const T* q = p.q + (p.starts ? (int64_t)walk.seq.row0 * p.q_token : walk.seq_number * p.q_seq) + (int64_t)walk.head * p.group * p.q_head;
-        const int32_t streams = b.rows > CA_ROWS ? 2 : 1;
-        for (int s = 0; s < streams; ++s)
-            for (int32_t row = t >> 3; row < CA_ROWS; row += CA_LOAD_ROWS) {
-                const int32_t r = s * CA_ROWS + row;
-                const bool held = r < b.rows;
-                const uint32_t token = (uint32_t)(b.first + r) / (uint32_t)p.group, g = (uint32_t)(b.first + r) - token * p.group;
-                const T* from = held ? q + token * p.q_token + g * p.q_head : p.q;
-                for (int h = 0; h < D / 64; ++h) {
-                    const int32_t chunk = (t & 7) + 8 * h;
-                    const bool there = held && chunk * 8 < p.dim;
-                    const uint32_t to = q_at + s * S::Q_TILE + CaLoader<T, D>::chunk_at(row, chunk, CA_ROWS);
-                    if (p.q_wide) {
-                        ca_copy(to, there ? from + chunk * 8 : p.q, there);
-                    } else {
-                        uint32_t w[4] = {0, 0, 0, 0};
-                        if (there)
-                            for (int e = 0; e < 8; ++e) w[e / 2] |= (uint32_t)reinterpret_cast<const unsigned short*>(from)[chunk * 8 + e] << (16 * (e % 2));
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-                    }
-                }
-            }
+        ca_copy_queries<T, D>(p, walk, q_at, t, CA_LOAD_ROWS);
         load.issued(&ctl->q_full, -1);
-        // the first tile that some row does not see all of
-        const int64_t seen = (int64_t)walk.seq.base + (uint32_t)b.first / (uint32_t)p.group + 1;
-        const int32_t cut = (int32_t)(max((int64_t)0, min(seen, (int64_t)b.end)) / S::KT);
+        const int32_t cut = ca_first_cut<T, D>(p, walk);
         const T* keys = p.k + walk.head * p.ks_head;
         const T* values = p.v + walk.head * p.vs_head;
         bool ok = true;
@@ -524,6 +571,115 @@ __device__ void ca_load(const CaParams<T>& p, CaControl<D>* ctl, char* queries, 
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
+__device__ __forceinline__ void ca_expect(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(ca_smem(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void ca_tile_copy(uint32_t to, const CUtensorMap* map, uint64_t* bar, int32_t x, int32_t y, int32_t z, int32_t w) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(to), "l"(map), "r"(ca_smem(bar)), "r"(x),
+                 "r"(y), "r"(z), "r"(w)
+                 : "memory");
+}
+
+// One warp has tiles copied in boxes of 64 elements and up to a tile's tokens of a page, a lane to each.  A page that is not
+// there lies outside the described memory: the copy fills in zeros.
+template <typename T, int D>
+__device__ void ca_load_boxes(const CaParams<T>& p, const CaMaps& maps, CaControl<D>* ctl, uint32_t queries, uint32_t stages) {
+    using S = CaShape<D>;
+    const int32_t lane = (int32_t)lane_id(), boxes = S::KT / p.box, box = lane % boxes, half = lane / boxes;
+    const uint32_t to = (uint32_t)(half * S::KT * 128 + box * p.box * 128);
+    CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
+    uint32_t q_phase = 1, phase = 1;
+    int32_t stage = 0, tiles_done = 0;
+    while (walk.next()) {
+        const auto& b = walk.block;
+        if (walk.tile1 == walk.tile0) continue;                          // no token to see
+        const int32_t* table = p.tables + walk.seq_number * p.table_stride;
+        int32_t slot = 0, next_slot = 0;
+        auto page_of = [&](int32_t token, int32_t* at) -> int32_t {
+            if (token >= b.end) return p.pages;
+            const uint32_t c = p.by_page.quotient((uint32_t)token);
+            *at = token - (int32_t)(c * p.by_page.d);
+            const int32_t page = table[c];
+            return page >= 0 && page < p.pages ? page : p.pages;
+        };
+        int32_t next = page_of(walk.tile0 * S::KT + box * p.box, &next_slot);
+        if (p.q_box) {
+            const int32_t streams = b.rows > CA_ROWS ? 2 : 1;
+            if (!__all_sync(FULL_MASK, ca_wait(&ctl->q_free, q_phase, &ctl->failed))) return;
+            q_phase ^= 1;
+            if (lane == 0) ca_expect(&ctl->q_full, streams * S::Q_TILE);
+            __syncwarp();
+            if (lane < streams * (D / 64)) {
+                const int32_t s = lane / (D / 64), h = lane % (D / 64), token = (int32_t)p.by_group.quotient((uint32_t)(b.first + s * CA_ROWS));
+                ca_tile_copy(queries + s * S::Q_TILE + h * CA_ROWS * 128, &maps.q, &ctl->q_full, h * 64, walk.head * p.group, (p.starts ? walk.seq.row0 : 0) + token,
+                             p.starts ? 0 : walk.seq_number);
+            }
+        }
+        for (int32_t tile = walk.tile0; tile < walk.tile1; ++tile, ++tiles_done) {
+            const int32_t page = next;
+            slot = next_slot;
+            const uint32_t there = __ballot_sync(FULL_MASK, page < p.pages);
+            if (lane < 4) {                                              // a box's bit to its tokens' bits
+                uint32_t word = 0;
+                for (int32_t i = 0; i < 32; i += 8) word |= (there >> (uint32_t)min((lane * 32 + i) / p.box, 31) & 1u) * 0xFFu << i;
+                ctl->mask[tiles_done % CA_MASKS][lane] = lane * 32 < S::KT ? word : ~0u;
+            }
+            if (tile + 1 < walk.tile1) next = page_of((tile + 1) * S::KT + box * p.box, &next_slot);
+            __syncwarp();
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                if (!__all_sync(FULL_MASK, ca_wait(&ctl->empty[stage], phase, &ctl->failed))) return;
+                if (lane == 0) ca_expect(&ctl->full[stage], S::STAGE);
+                __syncwarp();
+                if (half < D / 64) ca_tile_copy(stages + stage * S::STAGE + to, kv ? &maps.v : &maps.k, &ctl->full[stage], half * 64, slot, walk.head, page);
+                if (++stage == S::STAGES) { stage = 0; phase ^= 1; }
+            }
+        }
+    }
+}
+
+// Two warps beside it look through the tiles of values that a mask cuts before they are multiplied, and copy the queries where
+// that cannot be done by tile.
+template <typename T, int D>
+__device__ void ca_look(const CaParams<T>& p, CaControl<D>* ctl, uint32_t queries, uint32_t stages) {
+    using S = CaShape<D>;
+    const int32_t t = (int32_t)threadIdx.x - 256 - 32;
+    CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
+    uint32_t q_phase = p.q_box ? 0 : 1, meeting = 0, asked = 0;
+    int32_t taken = 0;
+    while (walk.next()) {
+        const int32_t n = walk.tile1 - walk.tile0;
+        if (n == 0) continue;
+        if (!__all_sync(FULL_MASK, ca_wait(p.q_box ? &ctl->q_full : &ctl->q_free, q_phase, &ctl->failed))) break;
+        q_phase ^= 1;
+        if (!p.q_box) {
+            ca_copy_queries<T, D>(p, walk, queries, t, 64 / 8);
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane_id() == 0) ca_arrive(&ctl->q_full);
+        }
+        if (t < CA_BAD_TILES * 4) ctl->bad[walk.number % CA_ITEMS][t / 4][t % 4] = 0;
+        // (products of an item begin behind this, so these warps are never an item ahead)
+        if (!ca_meet(&ctl->opened, meeting, &ctl->failed)) break;
+        bool ok = true;
+        for (int32_t tile = max(walk.tile0, ca_first_cut<T, D>(p, walk)); tile < walk.tile1 && ok; ++tile) {
+            const int32_t number = taken + 2 * (tile - walk.tile0) + 1, st = number % S::STAGES;
+            // asked for once the stage's use before this one has passed: then its parity is this one's
+            ok = __all_sync(FULL_MASK, ca_wait(&ctl->asked, asked, &ctl->failed) && ca_wait(&ctl->full[st], (uint32_t)(number / S::STAGES) & 1u, &ctl->failed));
+            asked ^= 1;
+            if (!ok) break;
+            CaLoader<T, D>::look(ctl, stages, st, tile % CA_BAD_TILES, walk.number % CA_ITEMS, t, 64 / 8);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane_id() == 0) ca_arrive(&ctl->looked);
+        }
+        if (!ok) break;
+        taken += 2 * n;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
 // ---- products ----------------------------------------------------------------------------------
 
 // One thread issues all products of the CTA.
@@ -534,7 +690,7 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
     volatile int32_t* failed = &ctl->failed;
     constexpr uint32_t SCORES = ca_product<T>(S::KT, false), OUTPUT = ca_product<T>(D, true);
     CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
-    uint32_t q_phase = 0, p_phase[2] = {0, 0};
+    uint32_t q_phase = 0, p_phase[2] = {0, 0}, opened = 0, look_phase = 0;
     int32_t taken = 0;                    // stages so far: keys of tile i are number 2 i, values 2 i + 1
     auto bar_full = [&](int32_t n, uint64_t** empty, uint32_t* at) {
         const int32_t st = n % S::STAGES;
@@ -558,11 +714,29 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
         if (n == 0) continue;
         if (!ca_wait(&ctl->q_full, q_phase, failed)) return;
         q_phase ^= 1;
+        // (values that a mask cuts are looked through first: by those that copied them, or by warps that tell of it)
+        const int32_t cut = p.box ? max(ca_first_cut<T, D>(p, walk) - walk.tile0, 0) : n;
+        // One tile is asked for at a time: the first when the keys of the tile before it are here, the next ones in turn.
+        auto keys_here = [&](int32_t i) {
+            if (cut < n && i == max(cut - 1, 0)) ca_arrive(&ctl->asked);
+        };
+        auto looked = [&](int32_t i) {
+            if (i < cut) return true;
+            const bool ok = ca_wait(&ctl->looked, look_phase, failed);
+            look_phase ^= 1;
+            if (i + 1 < n) ca_arrive(&ctl->asked);
+            return ok;
+        };
+        if (p.box) {
+            if (!ca_wait(&ctl->opened, opened, failed)) return;
+            opened ^= 1;
+        }
         uint64_t *k_empty = nullptr, *v_empty = nullptr;
         uint32_t k_at = 0, v_at = 0;
         if (S::STREAMS == 2 && walk.block.rows > CA_ROWS) {
             // both streams over every tile
             if (!bar_full(taken, &k_empty, &k_at)) return;
+            keys_here(0);
             ca_after_sync();
             for (int s = 0; s < 2; ++s) {
                 scores(s, s, k_at);
@@ -571,14 +745,17 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
             ca_commit(k_empty);
             if (n == 1) ca_commit(&ctl->q_free);
             for (int32_t i = 0; i < n; ++i) {
-                if (!bar_full(taken + 2 * i + 1, &v_empty, &v_at)) return;
+                if (!bar_full(taken + 2 * i + 1, &v_empty, &v_at) || !looked(i)) return;
                 for (int s = 0; s < 2; ++s) {
                     if (!ca_wait(&ctl->p_full[s], p_phase[s], failed)) return;
                     p_phase[s] ^= 1;
                     ca_after_sync();
                     output(s, s, v_at, i > 0);
                     if (i + 1 < n) {
-                        if (s == 0 && !bar_full(taken + 2 * i + 2, &k_empty, &k_at)) return;
+                        if (s == 0) {
+                            if (!bar_full(taken + 2 * i + 2, &k_empty, &k_at)) return;
+                            keys_here(i + 1);
+                        }
                         ca_after_sync();
                         scores(s, s, k_at);
                         ca_commit(&ctl->s_full[s]);
@@ -593,6 +770,7 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
         } else {
             // tiles alternate between two places of scores (and, with two streams, two of output)
             if (!bar_full(taken, &k_empty, &k_at)) return;
+            keys_here(0);
             ca_after_sync();
             scores(0, 0, k_at);
             ca_commit(&ctl->s_full[0]);
@@ -602,13 +780,14 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
                 const int s = i & 1;
                 if (i + 1 < n) {
                     if (!bar_full(taken + 2 * i + 2, &k_empty, &k_at)) return;
+                    keys_here(i + 1);
                     ca_after_sync();
                     scores(0, s ^ 1, k_at);
                     ca_commit(&ctl->s_full[s ^ 1]);
                     ca_commit(k_empty);
                     if (i + 2 == n) ca_commit(&ctl->q_free);
                 }
-                if (!bar_full(taken + 2 * i + 1, &v_empty, &v_at)) return;
+                if (!bar_full(taken + 2 * i + 1, &v_empty, &v_at) || !looked(i)) return;
                 if (!ca_wait(&ctl->p_full[s], p_phase[s], failed)) return;
                 p_phase[s] ^= 1;
                 ca_after_sync();
@@ -672,7 +851,7 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
         const int32_t n = walk.tile1 - walk.tile0;
         const int32_t row = (both ? group * CA_ROWS : 0) + lane_row;     // of the item
         const bool held = row < b.rows, warp_held = (row & ~31) < b.rows;
-        const uint32_t token = (uint32_t)(b.first + min(row, b.rows - 1)) / (uint32_t)p.group, g = (uint32_t)(b.first + min(row, b.rows - 1)) - token * p.group;
+        const uint32_t token = p.by_group.quotient((uint32_t)(b.first + min(row, b.rows - 1))), g = (uint32_t)(b.first + min(row, b.rows - 1)) - token * p.group;
         const int32_t seen = (int32_t)max(-1ll, min((long long)walk.seq.base + token + 1, (long long)b.end));       // tokens of the row
         const int32_t first = both || S::STREAMS == 1 ? 0 : group, step = both || S::STREAMS == 1 ? 1 : 2;
         float reference = LOWEST, sum = 0.0f, lost = 0.0f;
@@ -859,7 +1038,7 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(CA_THREADS, 1) paged_attention_chunk_kernel(const CaParams<T> p) {
+__global__ void __launch_bounds__(CA_THREADS, 1) paged_attention_chunk_kernel(const CaParams<T> p, const __grid_constant__ CaMaps maps) {
     using S = CaShape<D>;
     extern __shared__ __align__(1024) char ca_memory[];
     char* queries = ca_memory;
@@ -868,10 +1047,13 @@ __global__ void __launch_bounds__(CA_THREADS, 1) paged_attention_chunk_kernel(co
     const int32_t warp = (int32_t)threadIdx.x / 32;
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::STAGES; ++i) {
-            ca_bar_init(&ctl->full[i], CA_LOADERS / 32);
+            ca_bar_init(&ctl->full[i], p.box ? 1 : CA_LOADERS / 32);
             ca_bar_init(&ctl->empty[i], 1);
         }
-        ca_bar_init(&ctl->q_full, CA_LOADERS / 32);
+        ca_bar_init(&ctl->q_full, !p.box ? CA_LOADERS / 32 : p.q_box ? 1 : 2);
+        ca_bar_init(&ctl->opened, 2);
+        ca_bar_init(&ctl->asked, 1);
+        ca_bar_init(&ctl->looked, 2);
         ca_bar_init(&ctl->q_free, 1);
         for (int i = 0; i < 2; ++i) {
             ca_bar_init(&ctl->s_full[i], 1);
@@ -920,7 +1102,9 @@ __global__ void __launch_bounds__(CA_THREADS, 1) paged_attention_chunk_kernel(co
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CA_FEW_REGISTERS));
         if (warp < 11) {
-            ca_load<T, D>(p, ctl, queries, stages);
+            if (!p.box) ca_load<T, D>(p, ctl, queries, stages);
+            else if (warp == 8) ca_load_boxes<T, D>(p, maps, ctl, ca_smem(queries), ca_smem(stages));
+            else ca_look<T, D>(p, ctl, ca_smem(queries), ca_smem(stages));
         } else {
             if (lane_id() == 0) ca_multiply<T, D>(p, ctl, ca_smem(queries), ca_smem(stages));
             __syncwarp();
@@ -984,7 +1168,7 @@ __global__ void __launch_bounds__(CJ_THREADS) paged_attention_chunk_join_kernel(
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) o[j] += part[lane + 32 * j] * by;
         }
-        const uint32_t r = (uint32_t)(m.first + row), token = r / (uint32_t)p.group, g = r - token * p.group;
+        const uint32_t r = (uint32_t)(m.first + row), token = p.by_group.quotient(r), g = r - token * p.group;
         const int64_t out_row = (int64_t)(m.row0 + token) * p.heads + (int64_t)m.head * p.group + g;
         const float inverse = 1.0f / sum;
 #pragma unroll
