@@ -213,12 +213,15 @@ __device__ __forceinline__ bool ca_try(uint64_t* bar, uint32_t parity) {
 }
 // Waits for a phase; gives up after a limit, or when another warp has, and then returns false for good.
 __device__ __forceinline__ bool ca_wait(uint64_t* bar, uint32_t parity, volatile int32_t* failed) {
-    for (int32_t i = 0; i < CA_POLLS; ++i) {
-        if (ca_try(bar, parity)) return true;
-        if (*failed) return false;
+    int32_t left = CA_POLLS;
+#pragma unroll 1
+    while (!ca_try(bar, parity)) {
+        if (*failed || --left == 0) {
+            *failed = 1;
+            return false;
+        }
     }
-    *failed = 1;
-    return false;
+    return true;
 }
 // Warps meet (the barrier counts them); the wait is limited as all others are.
 __device__ __forceinline__ bool ca_meet(uint64_t* bar, uint32_t& phase, volatile int32_t* failed) {
@@ -235,6 +238,13 @@ __device__ __forceinline__ void ca_commit(uint64_t* bar) {
 __device__ __forceinline__ void ca_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void ca_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
+// A value that all lanes hold alike, told to the compiler: the matrix instructions take their operands from uniform registers.
+__device__ __forceinline__ uint32_t ca_uniform(uint32_t x) { return __shfl_sync(FULL_MASK, x, 0); }
+__device__ __forceinline__ bool ca_elect() {
+    uint32_t one;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+    return one != 0;
+}
 // D (128 x N, tensor memory) (+)= A (shared memory or tensor memory) B (shared memory)
 __device__ __forceinline__ void ca_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
     asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
@@ -243,10 +253,9 @@ __device__ __forceinline__ void ca_mma_ts(uint32_t d, uint32_t a, uint64_t b, ui
     asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
 }
 // Shared-memory operand in rows of 128 bytes, swizzled in atoms of eight rows; `leading`: between atoms along a transposed
-// operand's rows.
-__device__ __forceinline__ uint64_t ca_operand(uint32_t addr, uint32_t leading) {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
+// operand's rows.  Its lower word holds what differs between operands: the address in 16 bytes (and `leading`).
+__device__ __forceinline__ uint32_t ca_operand_low(uint32_t addr, uint32_t leading) { return (addr & 0x3FFFFu) >> 4 | leading >> 4 << 16; }
+__device__ __forceinline__ uint64_t ca_operand(uint32_t low) { return (uint64_t)(1024u >> 4 | 1u << 14 | 2u << 29) << 32 | low; }
 template <typename T> struct CaType;
 template <> struct CaType<__nv_bfloat16> {
     static constexpr uint32_t CODE = 1;
@@ -303,6 +312,11 @@ __device__ __forceinline__ void ca_tm_store16(uint32_t addr, const uint32_t* u) 
 }
 __device__ __forceinline__ void ca_tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+__device__ __forceinline__ uint4 ca_read(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
 // 16 bytes from global to shared memory; zeros where there is nothing to read.
 __device__ __forceinline__ void ca_copy(uint32_t to, const void* from, bool there) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16u : 0u) : "memory");
@@ -319,6 +333,7 @@ struct CaControl {
     int32_t table[2][CaShape<D>::KT];     // pages of two tiles' tokens; -1: nothing there
     alignas(16) uint32_t mask[CA_MASKS][4];        // which tokens of a tile are there
     uint32_t bad[CA_ITEMS][CA_BAD_TILES][4];       // tokens whose values are not finite, of the tiles that a mask cuts
+    uint32_t any_bad[CA_ITEMS];
     float2 other[CA_ROWS];                // reference and sum of the second stream, where two share rows
     CaPlace place[2];
     int64_t bound[2];
@@ -334,7 +349,7 @@ __device__ __forceinline__ int64_t ca_quotient(int64_t a, int64_t b) { return ((
 // little of an item on either side is moved to the item's nearer end: parts cost their reading and writing.  Each half of the
 // threads goes over all sequences and finds one of the two bounds.
 template <typename T, int D>
-__device__ void ca_plan(const CaParams<T>& p, CaControl<D>* ctl) {
+__device__ __noinline__ void ca_plan(const CaParams<T>& p, CaControl<D>* ctl) {
     constexpr int HALF = CA_THREADS / 2;
     const int32_t room = p.width * p.page_size;
     const int32_t which = (int32_t)threadIdx.x / HALF, tid = (int32_t)threadIdx.x % HALF, lane = tid & 31, warp = (int32_t)threadIdx.x / 32;
@@ -409,7 +424,7 @@ struct CaLoader {
         else if (newer == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
         else if (newer == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
-        if (check[0] >= 0) look(ctl, stages, check[0] & 255, check[0] >> 8 & 255, check[0] >> 16, (int32_t)threadIdx.x - 256, CA_LOAD_ROWS);
+        if (check[0] >= 0) look<CA_LOAD_ROWS>(ctl, stages, check[0] & 255, check[0] >> 8 & 255, check[0] >> 16, (int32_t)threadIdx.x - 256);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane_id() == 0) ca_arrive(pending[0]);
@@ -439,20 +454,35 @@ struct CaLoader {
     static __device__ __forceinline__ uint32_t chunk_at(int32_t row, int32_t chunk, int32_t rows) {
         return (uint32_t)((chunk >> 3) * rows * 128 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4));
     }
-    // A thread's part of a tile of values: vectors that are not finite are taken out, and their tokens noted.
-    static __device__ __noinline__ void look(CaControl<D>* ctl, uint32_t stages, int32_t st, int32_t tile, int32_t item, int32_t t, int32_t rows_at_once) {
-        char* base = reinterpret_cast<char*>(__cvta_shared_to_generic(stages + st * S::STAGE));
-        for (int i = 0; i < S::KT * (D / 64); i += rows_at_once) {
-            const int32_t both = i + (t >> 3), row = both % S::KT, chunk = (t & 7) + 8 * (both / S::KT);
-            if (both >= S::KT * (D / 64)) break;
-            uint4* at = reinterpret_cast<uint4*>(base + chunk_at(row, chunk, S::KT));
-            const uint4 v = *at;
-            bool bad = false;
-            for (const uint32_t w : {v.x, v.y, v.z, v.w})
-                bad |= (w & CaType<T>::EXPONENT) == CaType<T>::EXPONENT || (w >> 16 & CaType<T>::EXPONENT) == CaType<T>::EXPONENT;
-            if (!bad) continue;
-            *at = make_uint4(0, 0, 0, 0);
-            atomicOr(&ctl->bad[item % CA_ITEMS][tile % CA_BAD_TILES][row / 32], 1u << (row % 32));
+    // Whether any of eight elements is infinite or NaN: a carry out of an exponent of ones.
+    static __device__ __forceinline__ uint32_t carries(const uint4& v) {
+        constexpr uint32_t E = CaType<T>::EXPONENT * 0x10001u, ONE = (CaType<T>::EXPONENT & -CaType<T>::EXPONENT) * 0x10001u;
+        return (((v.x & E) + ONE) | ((v.y & E) + ONE) | ((v.z & E) + ONE) | ((v.w & E) + ONE)) & 0x80008000u;
+    }
+    // The part of a tile of values of thread t of 8 * ROWS: vectors that are not finite are taken out, and their tokens noted.
+    // (Vector t % 8 of every ROWS-th row, of one 128-byte column after the other: a multiple of eight rows on, the swizzle is the same.)
+    template <int ROWS>
+    static __device__ __forceinline__ void look(CaControl<D>* ctl, uint32_t stages, int32_t st, int32_t tile, int32_t item, int32_t t) {
+        constexpr int ALL = S::KT * (D / 64);
+        const uint32_t at = stages + st * S::STAGE;
+        uint32_t any = 0;
+        if constexpr (ROWS % 8 == 0) {
+#pragma unroll 8
+            for (int i = 0; i < ALL; i += ROWS) any |= carries(ca_read(at + i * 128 + chunk_at(t >> 3, t & 7, S::KT)));
+        } else {
+#pragma unroll 4
+            for (int i = t >> 3; i < ALL; i += ROWS) any |= carries(ca_read(at + i / S::KT * S::KT * 128 + chunk_at(i % S::KT, t & 7, S::KT)));
+        }
+        if (any) take_out(ctl, at, tile, item, t, ROWS);
+    }
+    static __device__ __noinline__ void take_out(CaControl<D>* ctl, uint32_t at, int32_t tile, int32_t item, int32_t t, int32_t rows_at_once) {
+        for (int i = t >> 3; i < S::KT * (D / 64); i += rows_at_once) {
+            const int32_t row = i % S::KT;
+            const uint32_t where = at + i / S::KT * S::KT * 128 + chunk_at(row, t & 7, S::KT);
+            if (!carries(ca_read(where))) continue;
+            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(where), "r"(0u) : "memory");
+            atomicOr(&ctl->bad[item][tile][row / 32], 1u << (row % 32));
+            ctl->any_bad[item] = 1;
         }
     }
     // One tile of keys or values.
@@ -481,12 +511,12 @@ struct CaLoader {
 
 // A thread's part of an item's queries: rows of (token, head), eight threads to 128 bytes.
 template <typename T, int D>
-__device__ __forceinline__ void ca_copy_queries(const CaParams<T>& p, const CaWalk<T, D>& walk, uint32_t q_at, int32_t t, int32_t rows_at_once) {
+__device__ __noinline__ void ca_copy_queries(const CaParams<T>& p, const CaWalk<T, D>& walk, uint32_t q_at, int32_t t, int32_t rows_at_once) {
     using S = CaShape<D>;
     const auto& b = walk.block;
     const T* q = p.q + (p.starts ? (int64_t)walk.seq.row0 * p.q_token : walk.seq_number * p.q_seq) + (int64_t)walk.head * p.group * p.q_head;
     const int32_t rows = b.rows > CA_ROWS ? 2 * CA_ROWS : CA_ROWS;
-#pragma unroll 4
+#pragma unroll 2
     for (int32_t r = t >> 3; r < rows; r += rows_at_once) {
         const bool held = r < b.rows;
         const uint32_t token = p.by_group.quotient((uint32_t)(b.first + r)), g = (uint32_t)(b.first + r) - token * p.group;
@@ -501,6 +531,7 @@ __device__ __forceinline__ void ca_copy_queries(const CaParams<T>& p, const CaWa
             } else {
                 uint32_t w[4] = {0, 0, 0, 0};
                 if (there)
+#pragma unroll
                     for (int e = 0; e < 8; ++e) w[e / 2] |= (uint32_t)reinterpret_cast<const unsigned short*>(from)[chunk * 8 + e] << (16 * (e % 2));
                 asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
             }
@@ -516,7 +547,7 @@ __device__ __forceinline__ int32_t ca_first_cut(const CaParams<T>& p, const CaWa
 
 // Three warps copy token by token: pages of fewer than eight tokens, or of an odd number.
 template <typename T, int D>
-__device__ void ca_load(const CaParams<T>& p, CaControl<D>* ctl, char* queries, char* stages) {
+__device__ __noinline__ void ca_load(const CaParams<T>& p, CaControl<D>* ctl, char* queries, char* stages) {
     using S = CaShape<D>;
     CaLoader<T, D> load;
     load.ctl = ctl;
@@ -538,6 +569,7 @@ __device__ void ca_load(const CaParams<T>& p, CaControl<D>* ctl, char* queries, 
         // (the tile's tokens to the threads, the last 32 of 128 to the first warp once more)
         int32_t page = t < S::KT ? page_of(walk.tile0 * S::KT + t) : -1, page2 = t + CA_LOADERS < S::KT ? page_of(walk.tile0 * S::KT + CA_LOADERS + t) : -1;
         if (t < CA_BAD_TILES * 4) ctl->bad[walk.number % CA_ITEMS][t / 4][t % 4] = 0;
+        if (t == 0) ctl->any_bad[walk.number % CA_ITEMS] = 0;
         if (!load.wait(&ctl->q_free, q_phase)) break;
         q_phase ^= 1;
         ca_copy_queries<T, D>(p, walk, q_at, t, CA_LOAD_ROWS);
@@ -660,6 +692,7 @@ __device__ void ca_look(const CaParams<T>& p, CaControl<D>* ctl, uint32_t querie
             if (lane_id() == 0) ca_arrive(&ctl->q_full);
         }
         if (t < CA_BAD_TILES * 4) ctl->bad[walk.number % CA_ITEMS][t / 4][t % 4] = 0;
+        if (t == 0) ctl->any_bad[walk.number % CA_ITEMS] = 0;
         // (products of an item begin behind this, so these warps are never an item ahead)
         if (!ca_meet(&ctl->opened, meeting, &ctl->failed)) break;
         bool ok = true;
@@ -669,7 +702,7 @@ __device__ void ca_look(const CaParams<T>& p, CaControl<D>* ctl, uint32_t querie
             ok = __all_sync(FULL_MASK, ca_wait(&ctl->asked, asked, &ctl->failed) && ca_wait(&ctl->full[st], (uint32_t)(number / S::STAGES) & 1u, &ctl->failed));
             asked ^= 1;
             if (!ok) break;
-            CaLoader<T, D>::look(ctl, stages, st, tile % CA_BAD_TILES, walk.number % CA_ITEMS, t, 64 / 8);
+            CaLoader<T, D>::template look<64 / 8>(ctl, stages, st, tile % CA_BAD_TILES, walk.number % CA_ITEMS, t);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane_id() == 0) ca_arrive(&ctl->looked);
@@ -682,53 +715,63 @@ __device__ void ca_look(const CaParams<T>& p, CaControl<D>* ctl, uint32_t querie
 
 // ---- products ----------------------------------------------------------------------------------
 
-// One thread issues all products of the CTA.
+// One warp issues all products of the CTA: all its lanes wait and walk, one is elected to issue.
 template <typename T, int D>
 __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t queries, uint32_t stages) {
     using S = CaShape<D>;
-    const uint32_t tm = ctl->tensor;
+    const uint32_t tm = ca_uniform(ctl->tensor);
+    const bool one = ca_elect();
     volatile int32_t* failed = &ctl->failed;
     constexpr uint32_t SCORES = ca_product<T>(S::KT, false), OUTPUT = ca_product<T>(D, true);
     CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
     uint32_t q_phase = 0, p_phase[2] = {0, 0}, opened = 0, look_phase = 0;
     int32_t taken = 0;                    // stages so far: keys of tile i are number 2 i, values 2 i + 1
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(FULL_MASK, ca_wait(bar, parity, failed)) != 0; };
+    auto commit = [&](uint64_t* bar) {
+        if (one) ca_commit(bar);
+    };
     auto bar_full = [&](int32_t n, uint64_t** empty, uint32_t* at) {
         const int32_t st = n % S::STAGES;
         *empty = &ctl->empty[st];
         *at = stages + st * S::STAGE;
-        return ca_wait(&ctl->full[st], (uint32_t)(n / S::STAGES) & 1u, failed);
+        return wait(&ctl->full[st], (uint32_t)(n / S::STAGES) & 1u);
     };
     auto scores = [&](int s, int buffer, uint32_t keys) {
-        const uint32_t q = queries + s * S::Q_TILE;
+        const uint32_t q = ca_uniform(ca_operand_low(queries + s * S::Q_TILE, 16)), k0 = ca_uniform(ca_operand_low(keys, 16)), to = ca_uniform(tm + buffer * 128);
+        if (one) {
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k)
-            ca_mma_ss(tm + buffer * 128, ca_operand(q + k / 4 * (CA_ROWS * 128) + k % 4 * 32, 16), ca_operand(keys + k / 4 * (S::KT * 128) + k % 4 * 32, 16), SCORES, k > 0);
+            for (int k = 0; k < D / 16; ++k)
+                ca_mma_ss(to, ca_operand(q + k / 4 * (CA_ROWS * 8) + k % 4 * 2), ca_operand(k0 + k / 4 * (S::KT * 8) + k % 4 * 2), SCORES, k > 0);
+        }
     };
     auto output = [&](int o, int buffer, uint32_t values, bool add) {
+        const uint32_t v0 = ca_uniform(ca_operand_low(values, S::KT * 128)), to = ca_uniform(tm + S::O_AT + o * D), from = ca_uniform(tm + buffer * 128);
+        const uint32_t on = ca_uniform(add);
+        if (one) {
 #pragma unroll
-        for (int k = 0; k < S::KT / 16; ++k)
-            ca_mma_ts(tm + S::O_AT + o * D, tm + buffer * 128 + k * 8, ca_operand(values + k * 2048, S::KT * 128), OUTPUT, add || k > 0);
+            for (int k = 0; k < S::KT / 16; ++k) ca_mma_ts(to, from + k * 8, ca_operand(v0 + k * 128), OUTPUT, k > 0 || on);
+        }
     };
     while (walk.next()) {
         const int32_t n = walk.tile1 - walk.tile0;
         if (n == 0) continue;
-        if (!ca_wait(&ctl->q_full, q_phase, failed)) return;
+        if (!wait(&ctl->q_full, q_phase)) return;
         q_phase ^= 1;
         // (values that a mask cuts are looked through first: by those that copied them, or by warps that tell of it)
         const int32_t cut = p.box ? max(ca_first_cut<T, D>(p, walk) - walk.tile0, 0) : n;
         // One tile is asked for at a time: the first when the keys of the tile before it are here, the next ones in turn.
         auto keys_here = [&](int32_t i) {
-            if (cut < n && i == max(cut - 1, 0)) ca_arrive(&ctl->asked);
+            if (one && cut < n && i == max(cut - 1, 0)) ca_arrive(&ctl->asked);
         };
         auto looked = [&](int32_t i) {
             if (i < cut) return true;
-            const bool ok = ca_wait(&ctl->looked, look_phase, failed);
+            const bool ok = wait(&ctl->looked, look_phase);
             look_phase ^= 1;
-            if (i + 1 < n) ca_arrive(&ctl->asked);
+            if (one && i + 1 < n) ca_arrive(&ctl->asked);
             return ok;
         };
         if (p.box) {
-            if (!ca_wait(&ctl->opened, opened, failed)) return;
+            if (!wait(&ctl->opened, opened)) return;
             opened ^= 1;
         }
         uint64_t *k_empty = nullptr, *v_empty = nullptr;
@@ -740,14 +783,14 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
             ca_after_sync();
             for (int s = 0; s < 2; ++s) {
                 scores(s, s, k_at);
-                ca_commit(&ctl->s_full[s]);
+                commit(&ctl->s_full[s]);
             }
-            ca_commit(k_empty);
-            if (n == 1) ca_commit(&ctl->q_free);
+            commit(k_empty);
+            if (n == 1) commit(&ctl->q_free);
             for (int32_t i = 0; i < n; ++i) {
                 if (!bar_full(taken + 2 * i + 1, &v_empty, &v_at) || !looked(i)) return;
                 for (int s = 0; s < 2; ++s) {
-                    if (!ca_wait(&ctl->p_full[s], p_phase[s], failed)) return;
+                    if (!wait(&ctl->p_full[s], p_phase[s])) return;
                     p_phase[s] ^= 1;
                     ca_after_sync();
                     output(s, s, v_at, i > 0);
@@ -758,14 +801,14 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
                         }
                         ca_after_sync();
                         scores(s, s, k_at);
-                        ca_commit(&ctl->s_full[s]);
+                        commit(&ctl->s_full[s]);
                     } else {
-                        ca_commit(&ctl->o_full[s]);
+                        commit(&ctl->o_full[s]);
                     }
                 }
-                ca_commit(v_empty);
-                if (i + 1 < n) ca_commit(k_empty);
-                if (i + 2 == n) ca_commit(&ctl->q_free);
+                commit(v_empty);
+                if (i + 1 < n) commit(k_empty);
+                if (i + 2 == n) commit(&ctl->q_free);
             }
         } else {
             // tiles alternate between two places of scores (and, with two streams, two of output)
@@ -773,9 +816,9 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
             keys_here(0);
             ca_after_sync();
             scores(0, 0, k_at);
-            ca_commit(&ctl->s_full[0]);
-            ca_commit(k_empty);
-            if (n == 1) ca_commit(&ctl->q_free);
+            commit(&ctl->s_full[0]);
+            commit(k_empty);
+            if (n == 1) commit(&ctl->q_free);
             for (int32_t i = 0; i < n; ++i) {
                 const int s = i & 1;
                 if (i + 1 < n) {
@@ -783,21 +826,21 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
                     keys_here(i + 1);
                     ca_after_sync();
                     scores(0, s ^ 1, k_at);
-                    ca_commit(&ctl->s_full[s ^ 1]);
-                    ca_commit(k_empty);
-                    if (i + 2 == n) ca_commit(&ctl->q_free);
+                    commit(&ctl->s_full[s ^ 1]);
+                    commit(k_empty);
+                    if (i + 2 == n) commit(&ctl->q_free);
                 }
                 if (!bar_full(taken + 2 * i + 1, &v_empty, &v_at) || !looked(i)) return;
-                if (!ca_wait(&ctl->p_full[s], p_phase[s], failed)) return;
+                if (!wait(&ctl->p_full[s], p_phase[s])) return;
                 p_phase[s] ^= 1;
                 ca_after_sync();
                 output(S::STREAMS == 2 ? s : 0, s, v_at, i >= S::STREAMS);
-                ca_commit(v_empty);
+                commit(v_empty);
                 if constexpr (S::STREAMS == 2) {
-                    if (i + 2 >= n) ca_commit(&ctl->o_full[s]);
+                    if (i + 2 >= n) commit(&ctl->o_full[s]);
                 } else {
-                    ca_commit(&ctl->o_step);
-                    if (i + 1 == n) ca_commit(&ctl->o_full[0]);
+                    commit(&ctl->o_step);
+                    if (i + 1 == n) commit(&ctl->o_full[0]);
                 }
             }
         }
@@ -810,16 +853,18 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
 // Adds what tokens with values that are not finite contribute to 32 columns of a row's output (their values were left out of
 // the product, where they would have met weights of zero).  Slow, and rare: the token's weight is computed again.
 template <typename T, int D>
-__device__ __noinline__ void ca_add_bad(const CaParams<T>& p, const uint32_t (*bad)[4], const int32_t* table, int32_t head, const T* q, const int32_t tile0, int32_t tile1,
-                                        int32_t seen, float factor, float reference, int32_t column, float* o) {
+__device__ __noinline__ void ca_add_bad(const CaParams<T>& p, const uint32_t (*bad)[4], const CaWalk<T, D>& walk, uint32_t row_token, uint32_t g, int32_t seen, float factor,
+                                        float reference, int32_t column, float* o) {
     using S = CaShape<D>;
-    for (int32_t tile = max(tile0, tile1 - CA_BAD_TILES); tile < tile1; ++tile)
+    const int32_t* table = p.tables + walk.seq_number * p.table_stride;
+    const T* q = p.q + (p.starts ? (int64_t)walk.seq.row0 * p.q_token : walk.seq_number * p.q_seq) + row_token * p.q_token + ((int64_t)walk.head * p.group + g) * p.q_head;
+    for (int32_t tile = max(walk.tile0, walk.tile1 - CA_BAD_TILES); tile < walk.tile1; ++tile)
         for (int32_t i = 0; i < S::KT; ++i) {
             const int64_t token = (int64_t)tile * S::KT + i;
             if (!(bad[tile % CA_BAD_TILES][i / 32] >> (i % 32) & 1u) || token >= seen) continue;
             const int64_t page = table[token / p.page_size], slot = token % p.page_size;
-            const T* k = p.k + page * p.ks_page + head * p.ks_head + slot * p.ks_token;
-            const T* v = p.v + page * p.vs_page + head * p.vs_head + slot * p.vs_token;
+            const T* k = p.k + page * p.ks_page + walk.head * p.ks_head + slot * p.ks_token;
+            const T* v = p.v + page * p.vs_page + walk.head * p.vs_head + slot * p.vs_token;
             float s = 0.0f;
             for (int32_t d = 0; d < p.dim; ++d) s += Logit<T>::to_float(q[d]) * Logit<T>::to_float(k[d]);
             const float w = exp2_approx(s * factor - reference);
@@ -965,15 +1010,9 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
             const bool whole = walk.whole();
             const int32_t slot = (int32_t)blockIdx.x * 2 + (walk.tile0 == 0 ? 1 : 0);
             float* part = whole ? nullptr : p.parts + ((int64_t)slot * S::BLOCK + row) * D;
-            const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-            bool any_bad = false;
-            const uint32_t(*bad)[4] = ctl->bad[max(walk.number, 0) % CA_ITEMS];
-            if (n > 0) {
-                uint32_t seen_bad = 0;
-                for (int i = 0; i < CA_BAD_TILES * 4; ++i) seen_bad |= bad[i / 4][i % 4];
-                any_bad = seen_bad != 0;
-            }
-            const T* q = p.q + (p.starts ? (int64_t)walk.seq.row0 * p.q_token : walk.seq_number * p.q_seq) + token * p.q_token + ((int64_t)walk.head * p.group + g) * p.q_head;
+            // (of a sum of zero, all products are zeros, too)
+            const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const bool any_bad = n > 0 && ctl->any_bad[walk.number % CA_ITEMS] != 0;
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
                 if (c >= p.dim) break;
@@ -993,7 +1032,7 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
                         float z[32];
 #pragma unroll
                         for (int e = 0; e < 32; ++e) z[e] = y[e];
-                        ca_add_bad<T, D>(p, bad, p.tables + walk.seq_number * p.table_stride, walk.head, q, walk.tile0, walk.tile1, seen, factor, reference - CaType<T>::LIFT, c, z);
+                        ca_add_bad<T, D>(p, ctl->bad[walk.number % CA_ITEMS], walk, token, g, seen, factor, reference - CaType<T>::LIFT, c, z);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) y[e] = z[e];
                     }
@@ -1011,7 +1050,7 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
                         if (c + e >= p.dim) break;
                         float f[8];
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) f[j] = sum == 0.0f ? 0.0f : y[e + j] * inverse;
+                        for (int j = 0; j < 8; ++j) f[j] = y[e + j] * inverse;
                         *reinterpret_cast<uint4*>(p.out + out_row * p.dim + c + e) = Logit<T>::pack(f);
                     }
                 }
@@ -1038,7 +1077,7 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(CA_THREADS, 1) paged_attention_chunk_kernel(const CaParams<T> p, const __grid_constant__ CaMaps maps) {
+__global__ void __launch_bounds__(CA_THREADS, 1) paged_attention_chunk_kernel(const __grid_constant__ CaParams<T> p, const __grid_constant__ CaMaps maps) {
     using S = CaShape<D>;
     extern __shared__ __align__(1024) char ca_memory[];
     char* queries = ca_memory;
@@ -1106,8 +1145,7 @@ __global__ void __launch_bounds__(CA_THREADS, 1) paged_attention_chunk_kernel(co
             else if (warp == 8) ca_load_boxes<T, D>(p, maps, ctl, ca_smem(queries), ca_smem(stages));
             else ca_look<T, D>(p, ctl, ca_smem(queries), ca_smem(stages));
         } else {
-            if (lane_id() == 0) ca_multiply<T, D>(p, ctl, ca_smem(queries), ca_smem(stages));
-            __syncwarp();
+            ca_multiply<T, D>(p, ctl, ca_smem(queries), ca_smem(stages));
         }
     }
     ca_before_sync();

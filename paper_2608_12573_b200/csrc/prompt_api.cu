@@ -129,13 +129,30 @@ int append_rotary(const T* q, const int64_t* q_strides, const T* k, const int64_
 
 // ---- penalties, biases and masks --------------------------------------------------------------
 
-template <typename T, bool COUNT>
-int ad_launch(AdParams<T> p, int64_t ctas, size_t smem, void* stream) {
+// Slices of `most` tokens; fewer rows than fill the device are cut finer, down to `least`.
+template <typename T>
+int ad_slice(AdParams<T>& p, int64_t tokens, uint32_t most, uint32_t least, int64_t ctas) {
+    p.slice = most;
+    while (p.slice / 2 >= least && p.rows * ((tokens + p.slice - 1) / p.slice) < ctas) p.slice /= 2;
+    p.slices = (uint32_t)((tokens + p.slice - 1) / p.slice);
+    return p.rows * p.slices > 0x7FFFFFFFll ? PROFK_EINVAL : PROFK_OK;
+}
+
+template <typename T, int BITS>
+int ad_named(AdParams<T> p, int sms, void* stream) {
     static uint64_t done = 0;
     static std::mutex mutex;
-    DEC_TRY(prepare_kernel(adjust_logits_kernel<T, COUNT>, COUNT ? AD_MAX_SLICE * sizeof(uint32_t) + AD_MAX_BIASES * sizeof(AdBias) : 0, &done, &mutex));
-    Launch l((unsigned)ctas, AD_THREADS, smem, stream, COUNT ? AD_CLUSTER : 1);
-    DEC_TRY(cudaLaunchKernelEx(&l.cfg, adjust_logits_kernel<T, COUNT>, p));
+    using Counters = AdCounters<BITS>;
+    DEC_TRY(prepare_kernel(adjust_named_kernel<T, BITS>, Counters::bytes(Counters::SLICE) + Counters::SLICE * sizeof(uint16_t) + AD_MAX_BIASES * sizeof(AdBias), &done, &mutex));
+    if (!p.tokens) {                                        // no counters: one CTA has a whole row
+        p.slice = p.V;
+        p.slices = 1;
+    } else if (ad_slice(p, p.V, Counters::SLICE, 2048, 2 * sms) != PROFK_OK) {
+        return PROFK_EINVAL;
+    }
+    const size_t named = p.tokens ? std::min<size_t>(p.slice, (size_t)p.history) : 0;
+    Launch l((unsigned)(p.rows * p.slices), AD_NAMED_THREADS, (p.tokens ? Counters::bytes(p.slice) : 0) + p.biases * sizeof(AdBias) + named * sizeof(uint16_t), stream);
+    DEC_TRY(cudaLaunchKernelEx(&l.cfg, adjust_named_kernel<T, BITS>, p));
     return PROFK_OK;
 }
 
@@ -159,16 +176,16 @@ int adjust(const T* logits, int64_t rows, int64_t V, int64_t row_stride, const p
     AdParams<T> p{logits, out, rows, row_stride, out_row_stride, (uint32_t)V, 0, 1, history ? how->tokens : nullptr, how->history, how->token_stride, how->lengths,
                   how->prompts, how->repetition, how->frequency, how->presence, rho, (float)how->frequency_value, (float)how->presence_value,
                   biased ? how->bias_tokens : nullptr, how->bias_values, (int32_t)how->biases, how->bias_token_stride, how->bias_value_stride, how->mask,
-                  how->mask_stride};
-    const int64_t slots = V + VEC - 1;                       // (the row may begin inside a vector)
-    if (history || biased) {
-        p.slice = (uint32_t)std::min<int64_t>((slots + AD_CLUSTER * VEC - 1) / (AD_CLUSTER * VEC) * VEC, AD_MAX_SLICE);
-        return ad_launch<T, true>(p, rows * AD_CLUSTER, p.slice * sizeof(uint32_t) + (size_t)how->biases * sizeof(AdBias), stream);
+                  how->mask_stride, false};
+    if (how->mask || out != logits) {
+        const int64_t slots = V + VEC - 1;                   // (the row may begin inside a vector)
+        if (ad_slice(p, slots, AD_THREADS * VEC * AD_UNROLL, AD_THREADS * VEC, 2 * sms) != PROFK_OK) return PROFK_EINVAL;
+        Launch l((unsigned)(p.rows * p.slices), AD_THREADS, 0, stream);
+        DEC_TRY(cudaLaunchKernelEx(&l.cfg, adjust_stream_kernel<T>, p));
+        p.behind_stream = true;
     }
-    p.slice = AD_THREADS * VEC * AD_UNROLL;
-    p.slices = (uint32_t)((slots + p.slice - 1) / p.slice);
-    if (rows * p.slices > 0x7FFFFFFFll) return PROFK_EINVAL;
-    return ad_launch<T, false>(p, rows * p.slices, 0, stream);
+    if (!history && !biased) return PROFK_OK;
+    return how->history < AD_NARROW ? ad_named<T, 16>(p, sms, stream) : ad_named<T, 32>(p, sms, stream);
 }
 
 }  // namespace
