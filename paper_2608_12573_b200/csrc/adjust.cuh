@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(AD_THREADS) adjust_stream_kernel(const AdParam
 }
 
 template <typename T, int BITS>
-__global__ void __launch_bounds__(AD_NAMED_THREADS) adjust_named_kernel(const AdParams<T> p) {
+__global__ void __launch_bounds__(AD_NAMED_THREADS, BITS == 16 ? 3 : 2) adjust_named_kernel(const AdParams<T> p) {
     extern __shared__ __align__(16) uint32_t memory[];                   // counters, the biases' list, the named tokens' list
     __shared__ int32_t sums[AD_NAMED_THREADS / 32];
     const AdCounters<BITS> counters{memory};

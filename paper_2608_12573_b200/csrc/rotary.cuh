@@ -7,8 +7,11 @@
 // |position| * 2^-56 turns (the frequency's own 53 bits), and no 64-bit floating-point arithmetic per angle but the conversion.
 //
 // Both operators are bound by HBM: each element is read and written once.  The angles of a token serve all its heads, so a
-// CTA computes those of its tokens once, into shared memory, and a thread keeps the few that its vectors need in registers
-// over several heads.
+// CTA finds those of its tokens once, into shared memory, and a thread keeps the few that its vectors need in registers over
+// four heads, whose loads are in flight together.  CTAs to an SM: three where a chunk is two vectors, four where it is one
+// (16384 x 32 x 128 bf16 turned by halves, forward and backward: 104 us with three, 128 with four, whose registers spill; 16384
+// ragged rows of 80 interleaved f16 heads appended: 129 and 122).  Angles found by each thread for itself, without barriers,
+// over more heads: 103 and 155.
 #pragma once
 
 #include "logits.cuh"
@@ -16,7 +19,7 @@
 namespace profk {
 
 constexpr int RO_THREADS = 256;
-constexpr int RO_TOKENS = 8;              // tokens of a CTA at most: a warp finds each one's place
+constexpr int RO_TOKENS = 32;             // tokens of a CTA at most
 constexpr int RO_MAX_PAIRS = 512;
 
 template <typename T>
@@ -86,6 +89,13 @@ __device__ __forceinline__ float2 ro_turn(int64_t position, double frequency, fl
     return make_float2(c * magnitude, (inverse ? -s : s) * magnitude);
 }
 
+// (Rounded the same way in every build, so that results do not depend on alignment.)
+__device__ __forceinline__ void ro_apply(const float2& turn, float& first, float& second) {
+    const float x = first, y = second;
+    first = __fmaf_rn(x, turn.x, -__fmul_rn(y, turn.y));
+    second = __fmaf_rn(y, turn.x, __fmul_rn(x, turn.y));
+}
+
 // VEC elements at a time: a 16-byte vector, or a single element where alignment or sizes allow no more.
 template <typename T, int VEC> struct RoVec;
 template <typename T> struct RoVec<T, 1> {
@@ -129,7 +139,7 @@ __host__ __device__ __forceinline__ int32_t ro_chunks(int32_t dim, int32_t pairs
 
 // HB heads of a token are one thread's unit: their loads are in flight together.  (Few tokens: HB = 1, more threads.)
 template <typename T, int VEC, bool INTER, int HB>
-__global__ void __launch_bounds__(RO_THREADS) rotary_kernel(const RoParams<T> p) {
+__global__ void __launch_bounds__(RO_THREADS, INTER ? 4 : 3) rotary_kernel(const RoParams<T> p) {
     using Chunk = RoChunk<T, VEC, INTER>;
     extern __shared__ float2 angles[];                                   // tokens_per_cta x pairs
     __shared__ RoToken tokens[RO_TOKENS];
@@ -137,9 +147,8 @@ __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(const RoParams<T> p)
     pdl_launch_dependents();
     const int64_t row0 = (int64_t)blockIdx.x * p.tokens_per_cta;
     const int32_t n = (int32_t)min((int64_t)p.tokens_per_cta, p.rows - row0);
-    const int32_t warp = (int32_t)threadIdx.x / 32;
-    if (warp < n) {
-        const int64_t row = row0 + warp;
+    for (int32_t i = (int32_t)threadIdx.x / 32; i < n; i += RO_THREADS / 32) {    // a warp to a token
+        const int64_t row = row0 + i;
         RoToken t;
         t.outer = row / p.inner;
         t.inner = row - t.outer * p.inner;
@@ -165,7 +174,7 @@ __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(const RoParams<T> p)
             }
         }
         t.position = p.positions ? p.positions[t.outer * p.pos_outer + t.inner * p.pos_inner] : place;
-        if (lane_id() == 0) tokens[warp] = t;
+        if (lane_id() == 0) tokens[i] = t;
     }
     __syncthreads();
     for (int32_t i = (int32_t)threadIdx.x; i < n * p.pairs; i += RO_THREADS) {
@@ -223,19 +232,11 @@ __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(const RoParams<T> p)
                     float y[VEC];
                     b[i].unpack(y);
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        const float first = x[j], second = y[j];
-                        x[j] = first * w[j].x - second * w[j].y;
-                        y[j] = second * w[j].x + first * w[j].y;
-                    }
+                    for (int j = 0; j < VEC; ++j) ro_apply(w[j], x[j], y[j]);
                     b[i].pack(y);
                 } else {
 #pragma unroll
-                    for (int j = 0; j < Chunk::PER; ++j) {
-                        const float first = x[2 * j], second = x[2 * j + 1];
-                        x[2 * j] = first * w[j].x - second * w[j].y;
-                        x[2 * j + 1] = second * w[j].x + first * w[j].y;
-                    }
+                    for (int j = 0; j < Chunk::PER; ++j) ro_apply(w[j], x[2 * j], x[2 * j + 1]);
                 }
                 a[i].pack(x);
             }
