@@ -24,6 +24,8 @@
 
 #include <cuda.h>
 
+#include <cstddef>
+
 #include "logits.cuh"
 
 namespace profk {
@@ -194,29 +196,30 @@ struct CaWalk {
 // ---- instructions ------------------------------------------------------------------------------
 
 __device__ __forceinline__ uint32_t ca_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void ca_bar_init(uint64_t* bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ca_smem(bar)), "r"(count) : "memory");
+// Barriers, by their addresses in shared memory.
+__device__ __forceinline__ void ca_bar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
-__device__ __forceinline__ void ca_arrive(uint64_t* bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(ca_smem(bar)) : "memory");
+__device__ __forceinline__ void ca_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // Whether a phase has passed, at once; and likewise after the hardware has waited for it a while.
-__device__ __forceinline__ bool ca_test(uint64_t* bar, uint32_t parity) {
+__device__ __forceinline__ bool ca_test(uint32_t bar, uint32_t parity) {
     uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(ca_smem(bar)), "r"(parity) : "memory");
+    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ bool ca_try(uint64_t* bar, uint32_t parity) {
+__device__ __forceinline__ bool ca_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(ca_smem(bar)), "r"(parity) : "memory");
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// Waits for a phase; gives up after a limit, or when another warp has, and then returns false for good.
-__device__ __forceinline__ bool ca_wait(uint64_t* bar, uint32_t parity, volatile int32_t* failed) {
+// A warp waits for a phase; gives up after a limit, or when another warp has, and then returns false for good.
+__device__ __forceinline__ bool ca_wait(uint32_t bar, uint32_t parity, volatile int32_t* failed) {
     int32_t left = CA_POLLS;
 #pragma unroll 1
-    while (!ca_try(bar, parity)) {
-        if (*failed || --left == 0) {
+    while (!__all_sync(FULL_MASK, ca_try(bar, parity))) {
+        if (__any_sync(FULL_MASK, *failed != 0) || --left == 0) {
             *failed = 1;
             return false;
         }
@@ -224,16 +227,16 @@ __device__ __forceinline__ bool ca_wait(uint64_t* bar, uint32_t parity, volatile
     return true;
 }
 // Warps meet (the barrier counts them); the wait is limited as all others are.
-__device__ __forceinline__ bool ca_meet(uint64_t* bar, uint32_t& phase, volatile int32_t* failed) {
+__device__ __forceinline__ bool ca_meet(uint32_t bar, uint32_t& phase, volatile int32_t* failed) {
     __syncwarp();
     if ((threadIdx.x & 31u) == 0) ca_arrive(bar);
-    const bool ok = __all_sync(FULL_MASK, ca_wait(bar, phase, failed));
+    const bool ok = ca_wait(bar, phase, failed);
     phase ^= 1u;
     return ok;
 }
 
-__device__ __forceinline__ void ca_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(ca_smem(bar)) : "memory");
+__device__ __forceinline__ void ca_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void ca_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void ca_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -339,6 +342,8 @@ struct CaControl {
     int64_t bound[2];
     int64_t scan[CA_THREADS / 32];
 };
+// The address of a member of the control block at address `ctl`.
+#define CA_AT(ctl, member) ((ctl) + (uint32_t)offsetof(CaControl<D>, member))
 template <int D>
 constexpr size_t ca_smem_bytes() { return CaShape<D>::STREAMS * CaShape<D>::Q_TILE + CaShape<D>::STAGES * CaShape<D>::STAGE + sizeof(CaControl<D>); }
 static_assert(ca_smem_bytes<128>() <= 232448 && ca_smem_bytes<256>() <= 232448 && ca_smem_bytes<64>() <= 232448, "an SM's shared memory");
@@ -412,8 +417,8 @@ struct CaLoader {
     using S = CaShape<D>;
     static constexpr int DEPTH = 3;
     CaControl<D>* ctl;
-    uint32_t stages;                      // shared memory
-    uint64_t* pending[DEPTH];
+    uint32_t bars, stages;                // shared memory
+    uint32_t pending[DEPTH];
     int32_t check[DEPTH];                 // values to look through: stage | tile's number << 8 | item's << 16; -1: none
     int32_t count = 0;
     int32_t stage = 0;
@@ -432,7 +437,7 @@ struct CaLoader {
         for (int i = 0; i + 1 < DEPTH; ++i) { pending[i] = pending[i + 1]; check[i] = check[i + 1]; }
         --count;
     }
-    __device__ __forceinline__ void issued(uint64_t* bar, int32_t what) {
+    __device__ __forceinline__ void issued(uint32_t bar, int32_t what) {
         asm volatile("cp.async.commit_group;" ::: "memory");
         if (count == DEPTH) retire(DEPTH);
 #pragma unroll
@@ -441,12 +446,12 @@ struct CaLoader {
         ++count;
     }
     // Waits until a barrier's phase has passed; what has landed meanwhile is told of.
-    __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
+    __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
         while (count > 0) {
             if (__all_sync(FULL_MASK, ca_test(bar, parity))) return true;
             retire(count - 1);
         }
-        return __all_sync(FULL_MASK, ca_wait(bar, parity, &ctl->failed));
+        return ca_wait(bar, parity, &ctl->failed);
     }
     __device__ __forceinline__ void flush() {
         while (count > 0) retire(count - 1);
@@ -487,7 +492,7 @@ struct CaLoader {
     }
     // One tile of keys or values.
     __device__ __forceinline__ bool tile(const CaParams<T>& p, const T* pages, int64_t page_stride, int64_t token_stride, int32_t buffer, int32_t first, int32_t what) {
-        if (!wait(&ctl->empty[stage], phase)) return false;
+        if (!wait(CA_AT(bars, empty) + stage * 8, phase)) return false;
         const int32_t t = (int32_t)threadIdx.x - 256;
         const uint32_t to = stages + stage * S::STAGE;
 #pragma unroll 4
@@ -503,7 +508,7 @@ struct CaLoader {
                 ca_copy(to + chunk_at(row, chunk, S::KT), there ? from + chunk * 8 : pages, there);
             }
         }
-        issued(&ctl->full[stage], what < 0 ? -1 : what | stage);
+        issued(CA_AT(bars, full) + stage * 8, what < 0 ? -1 : what | stage);
         if (++stage == S::STAGES) { stage = 0; phase ^= 1; }
         return true;
     }
@@ -551,6 +556,7 @@ __device__ __noinline__ void ca_load(const CaParams<T>& p, CaControl<D>* ctl, ch
     using S = CaShape<D>;
     CaLoader<T, D> load;
     load.ctl = ctl;
+    load.bars = ca_smem(ctl);
     load.stages = ca_smem(stages);
     const uint32_t q_at = ca_smem(queries);
     const int32_t t = (int32_t)threadIdx.x - 256, warp = t / 32;
@@ -570,10 +576,10 @@ __device__ __noinline__ void ca_load(const CaParams<T>& p, CaControl<D>* ctl, ch
         int32_t page = t < S::KT ? page_of(walk.tile0 * S::KT + t) : -1, page2 = t + CA_LOADERS < S::KT ? page_of(walk.tile0 * S::KT + CA_LOADERS + t) : -1;
         if (t < CA_BAD_TILES * 4) ctl->bad[walk.number % CA_ITEMS][t / 4][t % 4] = 0;
         if (t == 0) ctl->any_bad[walk.number % CA_ITEMS] = 0;
-        if (!load.wait(&ctl->q_free, q_phase)) break;
+        if (!load.wait(CA_AT(load.bars, q_free), q_phase)) break;
         q_phase ^= 1;
         ca_copy_queries<T, D>(p, walk, q_at, t, CA_LOAD_ROWS);
-        load.issued(&ctl->q_full, -1);
+        load.issued(CA_AT(load.bars, q_full), -1);
         const int32_t cut = ca_first_cut<T, D>(p, walk);
         const T* keys = p.k + walk.head * p.ks_head;
         const T* values = p.v + walk.head * p.vs_head;
@@ -592,7 +598,7 @@ __device__ __noinline__ void ca_load(const CaParams<T>& p, CaControl<D>* ctl, ch
                 page = t < S::KT ? page_of((tile + 1) * S::KT + t) : -1;
                 page2 = t + CA_LOADERS < S::KT ? page_of((tile + 1) * S::KT + CA_LOADERS + t) : -1;
             }
-            if (!(ok = ca_meet(&ctl->loaders, meeting, &ctl->failed))) break;
+            if (!(ok = ca_meet(CA_AT(load.bars, loaders), meeting, &ctl->failed))) break;
             const int32_t first = tile * S::KT;
             ok = load.tile(p, keys, p.ks_page, p.ks_token, buffer, first, -1);
             ok = ok && load.tile(p, values, p.vs_page, p.vs_token, buffer, first, tile >= cut ? (tile % CA_BAD_TILES) << 8 | (walk.number % CA_ITEMS) << 16 : -1);
@@ -603,11 +609,11 @@ __device__ __noinline__ void ca_load(const CaParams<T>& p, CaControl<D>* ctl, ch
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-__device__ __forceinline__ void ca_expect(uint64_t* bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(ca_smem(bar)), "r"(bytes) : "memory");
+__device__ __forceinline__ void ca_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void ca_tile_copy(uint32_t to, const CUtensorMap* map, uint64_t* bar, int32_t x, int32_t y, int32_t z, int32_t w) {
-    asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(to), "l"(map), "r"(ca_smem(bar)), "r"(x),
+__device__ __forceinline__ void ca_tile_copy(uint32_t to, const CUtensorMap* map, uint32_t bar, int32_t x, int32_t y, int32_t z, int32_t w) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(to), "l"(map), "r"(bar), "r"(x),
                  "r"(y), "r"(z), "r"(w)
                  : "memory");
 }
@@ -618,7 +624,7 @@ template <typename T, int D>
 __device__ void ca_load_boxes(const CaParams<T>& p, const CaMaps& maps, CaControl<D>* ctl, uint32_t queries, uint32_t stages) {
     using S = CaShape<D>;
     const int32_t lane = (int32_t)lane_id(), boxes = S::KT / p.box, box = lane % boxes, half = lane / boxes;
-    const uint32_t to = (uint32_t)(half * S::KT * 128 + box * p.box * 128);
+    const uint32_t to = (uint32_t)(half * S::KT * 128 + box * p.box * 128), bars = ca_smem(ctl);
     CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
     uint32_t q_phase = 1, phase = 1;
     int32_t stage = 0, tiles_done = 0;
@@ -637,13 +643,13 @@ __device__ void ca_load_boxes(const CaParams<T>& p, const CaMaps& maps, CaContro
         int32_t next = page_of(walk.tile0 * S::KT + box * p.box, &next_slot);
         if (p.q_box) {
             const int32_t streams = b.rows > CA_ROWS ? 2 : 1;
-            if (!__all_sync(FULL_MASK, ca_wait(&ctl->q_free, q_phase, &ctl->failed))) return;
+            if (!ca_wait(CA_AT(bars, q_free), q_phase, &ctl->failed)) return;
             q_phase ^= 1;
-            if (lane == 0) ca_expect(&ctl->q_full, streams * S::Q_TILE);
+            if (lane == 0) ca_expect(CA_AT(bars, q_full), streams * S::Q_TILE);
             __syncwarp();
             if (lane < streams * (D / 64)) {
                 const int32_t s = lane / (D / 64), h = lane % (D / 64), token = (int32_t)p.by_group.quotient((uint32_t)(b.first + s * CA_ROWS));
-                ca_tile_copy(queries + s * S::Q_TILE + h * CA_ROWS * 128, &maps.q, &ctl->q_full, h * 64, walk.head * p.group, (p.starts ? walk.seq.row0 : 0) + token,
+                ca_tile_copy(queries + s * S::Q_TILE + h * CA_ROWS * 128, &maps.q, CA_AT(bars, q_full), h * 64, walk.head * p.group, (p.starts ? walk.seq.row0 : 0) + token,
                              p.starts ? 0 : walk.seq_number);
             }
         }
@@ -660,10 +666,10 @@ __device__ void ca_load_boxes(const CaParams<T>& p, const CaMaps& maps, CaContro
             __syncwarp();
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
-                if (!__all_sync(FULL_MASK, ca_wait(&ctl->empty[stage], phase, &ctl->failed))) return;
-                if (lane == 0) ca_expect(&ctl->full[stage], S::STAGE);
+                if (!ca_wait(CA_AT(bars, empty) + stage * 8, phase, &ctl->failed)) return;
+                if (lane == 0) ca_expect(CA_AT(bars, full) + stage * 8, S::STAGE);
                 __syncwarp();
-                if (half < D / 64) ca_tile_copy(stages + stage * S::STAGE + to, kv ? &maps.v : &maps.k, &ctl->full[stage], half * 64, slot, walk.head, page);
+                if (half < D / 64) ca_tile_copy(stages + stage * S::STAGE + to, kv ? &maps.v : &maps.k, CA_AT(bars, full) + stage * 8, half * 64, slot, walk.head, page);
                 if (++stage == S::STAGES) { stage = 0; phase ^= 1; }
             }
         }
@@ -676,36 +682,37 @@ template <typename T, int D>
 __device__ void ca_look(const CaParams<T>& p, CaControl<D>* ctl, uint32_t queries, uint32_t stages) {
     using S = CaShape<D>;
     const int32_t t = (int32_t)threadIdx.x - 256 - 32;
+    const uint32_t bars = ca_smem(ctl);
     CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
     uint32_t q_phase = p.q_box ? 0 : 1, meeting = 0, asked = 0;
     int32_t taken = 0;
     while (walk.next()) {
         const int32_t n = walk.tile1 - walk.tile0;
         if (n == 0) continue;
-        if (!__all_sync(FULL_MASK, ca_wait(p.q_box ? &ctl->q_full : &ctl->q_free, q_phase, &ctl->failed))) break;
+        if (!ca_wait(p.q_box ? CA_AT(bars, q_full) : CA_AT(bars, q_free), q_phase, &ctl->failed)) break;
         q_phase ^= 1;
         if (!p.q_box) {
             ca_copy_queries<T, D>(p, walk, queries, t, 64 / 8);
             asm volatile("cp.async.wait_all;" ::: "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane_id() == 0) ca_arrive(&ctl->q_full);
+            if (lane_id() == 0) ca_arrive(CA_AT(bars, q_full));
         }
         if (t < CA_BAD_TILES * 4) ctl->bad[walk.number % CA_ITEMS][t / 4][t % 4] = 0;
         if (t == 0) ctl->any_bad[walk.number % CA_ITEMS] = 0;
         // (products of an item begin behind this, so these warps are never an item ahead)
-        if (!ca_meet(&ctl->opened, meeting, &ctl->failed)) break;
+        if (!ca_meet(CA_AT(bars, opened), meeting, &ctl->failed)) break;
         bool ok = true;
         for (int32_t tile = max(walk.tile0, ca_first_cut<T, D>(p, walk)); tile < walk.tile1 && ok; ++tile) {
             const int32_t number = taken + 2 * (tile - walk.tile0) + 1, st = number % S::STAGES;
             // asked for once the stage's use before this one has passed: then its parity is this one's
-            ok = __all_sync(FULL_MASK, ca_wait(&ctl->asked, asked, &ctl->failed) && ca_wait(&ctl->full[st], (uint32_t)(number / S::STAGES) & 1u, &ctl->failed));
+            ok = ca_wait(CA_AT(bars, asked), asked, &ctl->failed) && ca_wait(CA_AT(bars, full) + st * 8, (uint32_t)(number / S::STAGES) & 1u, &ctl->failed);
             asked ^= 1;
             if (!ok) break;
             CaLoader<T, D>::template look<64 / 8>(ctl, stages, st, tile % CA_BAD_TILES, walk.number % CA_ITEMS, t);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane_id() == 0) ca_arrive(&ctl->looked);
+            if (lane_id() == 0) ca_arrive(CA_AT(bars, looked));
         }
         if (!ok) break;
         taken += 2 * n;
@@ -715,136 +722,144 @@ __device__ void ca_look(const CaParams<T>& p, CaControl<D>* ctl, uint32_t querie
 
 // ---- products ----------------------------------------------------------------------------------
 
+// A place in the ring of stages: every second one, keys or values.
+template <int D>
+struct CaCursor {
+    using S = CaShape<D>;
+    uint32_t bars, stages;                // shared memory: the control block, the stages
+    uint32_t stage, parity = 0;
+    __device__ __forceinline__ uint32_t full() const { return CA_AT(bars, full) + stage * 8; }
+    __device__ __forceinline__ uint32_t empty() const { return CA_AT(bars, empty) + stage * 8; }
+    __device__ __forceinline__ uint32_t data() const { return stages + stage * S::STAGE; }
+    __device__ __forceinline__ void step() {
+        stage += 2;
+        if (stage >= S::STAGES) { stage -= S::STAGES; parity ^= 1u; }
+    }
+};
+
 // One warp issues all products of the CTA: all its lanes wait and walk, one is elected to issue.
 template <typename T, int D>
 __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t queries, uint32_t stages) {
     using S = CaShape<D>;
-    const uint32_t tm = ca_uniform(ctl->tensor);
+    const uint32_t tm = ca_uniform(ctl->tensor), bars = ca_smem(ctl);
     const bool one = ca_elect();
-    volatile int32_t* failed = &ctl->failed;
     constexpr uint32_t SCORES = ca_product<T>(S::KT, false), OUTPUT = ca_product<T>(D, true);
     CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
-    uint32_t q_phase = 0, p_phase[2] = {0, 0}, opened = 0, look_phase = 0;
-    int32_t taken = 0;                    // stages so far: keys of tile i are number 2 i, values 2 i + 1
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(FULL_MASK, ca_wait(bar, parity, failed)) != 0; };
-    auto commit = [&](uint64_t* bar) {
-        if (one) ca_commit(bar);
+    uint32_t q_phase = 0, p_phases = 0, opened = 0, look_phase = 0;      // p_phases: a bit for each place of scores
+    CaCursor<D> k{bars, stages, 0}, v{bars, stages, 1};
+    auto wait = [&](uint32_t bar, uint32_t parity) { return ca_wait(bar, parity, &ctl->failed); };
+    auto weights = [&](int buffer) {
+        const bool ok = wait(CA_AT(bars, p_full) + buffer * 8, p_phases >> buffer & 1u);
+        p_phases ^= 1u << buffer;
+        ca_after_sync();
+        return ok;
     };
-    auto bar_full = [&](int32_t n, uint64_t** empty, uint32_t* at) {
-        const int32_t st = n % S::STAGES;
-        *empty = &ctl->empty[st];
-        *at = stages + st * S::STAGE;
-        return wait(&ctl->full[st], (uint32_t)(n / S::STAGES) & 1u);
-    };
-    auto scores = [&](int s, int buffer, uint32_t keys) {
-        const uint32_t q = ca_uniform(ca_operand_low(queries + s * S::Q_TILE, 16)), k0 = ca_uniform(ca_operand_low(keys, 16)), to = ca_uniform(tm + buffer * 128);
+    // S = Q K^T, and whom it concerns
+    auto scores = [&](int s, int buffer) {
+        const uint32_t q = ca_uniform(ca_operand_low(queries + s * S::Q_TILE, 16)), k0 = ca_uniform(ca_operand_low(k.data(), 16)), to = ca_uniform(tm + buffer * 128);
         if (one) {
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-                ca_mma_ss(to, ca_operand(q + k / 4 * (CA_ROWS * 8) + k % 4 * 2), ca_operand(k0 + k / 4 * (S::KT * 8) + k % 4 * 2), SCORES, k > 0);
+            for (int i = 0; i < D / 16; ++i)
+                ca_mma_ss(to, ca_operand(q + i / 4 * (CA_ROWS * 8) + i % 4 * 2), ca_operand(k0 + i / 4 * (S::KT * 8) + i % 4 * 2), SCORES, i > 0);
+            ca_commit(CA_AT(bars, s_full) + buffer * 8);
         }
     };
-    auto output = [&](int o, int buffer, uint32_t values, bool add) {
-        const uint32_t v0 = ca_uniform(ca_operand_low(values, S::KT * 128)), to = ca_uniform(tm + S::O_AT + o * D), from = ca_uniform(tm + buffer * 128);
-        const uint32_t on = ca_uniform(add);
+    // O += P V
+    auto output = [&](int o, int buffer, bool add) {
+        const uint32_t v0 = ca_uniform(ca_operand_low(v.data(), S::KT * 128)), to = ca_uniform(tm + S::O_AT + o * D), from = ca_uniform(tm + buffer * 128);
         if (one) {
+            ca_mma_ts(to, from, ca_operand(v0), OUTPUT, add);
 #pragma unroll
-            for (int k = 0; k < S::KT / 16; ++k) ca_mma_ts(to, from + k * 8, ca_operand(v0 + k * 128), OUTPUT, k > 0 || on);
+            for (int i = 1; i < S::KT / 16; ++i) ca_mma_ts(to, from + i * 8, ca_operand(v0 + i * 128), OUTPUT, true);
         }
     };
     while (walk.next()) {
         const int32_t n = walk.tile1 - walk.tile0;
         if (n == 0) continue;
-        if (!wait(&ctl->q_full, q_phase)) return;
-        q_phase ^= 1;
-        // (values that a mask cuts are looked through first: by those that copied them, or by warps that tell of it)
-        const int32_t cut = p.box ? max(ca_first_cut<T, D>(p, walk) - walk.tile0, 0) : n;
-        // One tile is asked for at a time: the first when the keys of the tile before it are here, the next ones in turn.
-        auto keys_here = [&](int32_t i) {
-            if (one && cut < n && i == max(cut - 1, 0)) ca_arrive(&ctl->asked);
+        if (!wait(CA_AT(bars, q_full), q_phase)) return;
+        q_phase ^= 1u;
+        // Values that a mask cuts are looked through first: by those that copied them, or by warps that tell of it.  One tile is
+        // asked for at a time: the first when the keys of the tile before it are here, the next ones in turn.
+        const int32_t cut = p.box ? max(ca_first_cut<T, D>(p, walk) - walk.tile0, 0) : n, ask = cut < n ? max(cut - 1, 0) : -1;
+        auto keys = [&](int32_t i) {
+            if (!wait(k.full(), k.parity)) return false;
+            if (i == ask && one) ca_arrive(CA_AT(bars, asked));
+            ca_after_sync();
+            return true;
         };
-        auto looked = [&](int32_t i) {
+        auto values = [&](int32_t i) {
+            if (!wait(v.full(), v.parity)) return false;
             if (i < cut) return true;
-            const bool ok = wait(&ctl->looked, look_phase);
-            look_phase ^= 1;
-            if (one && i + 1 < n) ca_arrive(&ctl->asked);
+            const bool ok = wait(CA_AT(bars, looked), look_phase);
+            look_phase ^= 1u;
+            if (one && i + 1 < n) ca_arrive(CA_AT(bars, asked));
             return ok;
         };
         if (p.box) {
-            if (!wait(&ctl->opened, opened)) return;
-            opened ^= 1;
+            if (!wait(CA_AT(bars, opened), opened)) return;
+            opened ^= 1u;
         }
-        uint64_t *k_empty = nullptr, *v_empty = nullptr;
-        uint32_t k_at = 0, v_at = 0;
-        if (S::STREAMS == 2 && walk.block.rows > CA_ROWS) {
+        if (!keys(0)) return;
+        const bool both = S::STREAMS == 2 && walk.block.rows > CA_ROWS;
+        scores(0, 0);
+        if (both) scores(1, 1);
+        if (one) {
+            ca_commit(k.empty());
+            if (n == 1) ca_commit(CA_AT(bars, q_free));
+        }
+        k.step();
+        if (both) {
             // both streams over every tile
-            if (!bar_full(taken, &k_empty, &k_at)) return;
-            keys_here(0);
-            ca_after_sync();
-            for (int s = 0; s < 2; ++s) {
-                scores(s, s, k_at);
-                commit(&ctl->s_full[s]);
-            }
-            commit(k_empty);
-            if (n == 1) commit(&ctl->q_free);
+#pragma unroll 1
             for (int32_t i = 0; i < n; ++i) {
-                if (!bar_full(taken + 2 * i + 1, &v_empty, &v_at) || !looked(i)) return;
-                for (int s = 0; s < 2; ++s) {
-                    if (!wait(&ctl->p_full[s], p_phase[s])) return;
-                    p_phase[s] ^= 1;
-                    ca_after_sync();
-                    output(s, s, v_at, i > 0);
+                if (!values(i)) return;
+#pragma unroll 1
+                for (int st = 0; st < 2; ++st) {
+                    if (!weights(st)) return;
+                    output(st, st, i > 0);
                     if (i + 1 < n) {
-                        if (s == 0) {
-                            if (!bar_full(taken + 2 * i + 2, &k_empty, &k_at)) return;
-                            keys_here(i + 1);
-                        }
-                        ca_after_sync();
-                        scores(s, s, k_at);
-                        commit(&ctl->s_full[s]);
-                    } else {
-                        commit(&ctl->o_full[s]);
+                        if (st == 0 && !keys(i + 1)) return;
+                        scores(st, st);
+                    } else if (one) {
+                        ca_commit(CA_AT(bars, o_full) + st * 8);
                     }
                 }
-                commit(v_empty);
-                if (i + 1 < n) commit(k_empty);
-                if (i + 2 == n) commit(&ctl->q_free);
+                if (one) {
+                    ca_commit(v.empty());
+                    if (i + 1 < n) ca_commit(k.empty());
+                    if (i + 2 == n) ca_commit(CA_AT(bars, q_free));
+                }
+                v.step();
+                if (i + 1 < n) k.step();
             }
         } else {
             // tiles alternate between two places of scores (and, with two streams, two of output)
-            if (!bar_full(taken, &k_empty, &k_at)) return;
-            keys_here(0);
-            ca_after_sync();
-            scores(0, 0, k_at);
-            commit(&ctl->s_full[0]);
-            commit(k_empty);
-            if (n == 1) commit(&ctl->q_free);
+#pragma unroll 1
             for (int32_t i = 0; i < n; ++i) {
-                const int s = i & 1;
+                const int buffer = i & 1;
                 if (i + 1 < n) {
-                    if (!bar_full(taken + 2 * i + 2, &k_empty, &k_at)) return;
-                    keys_here(i + 1);
-                    ca_after_sync();
-                    scores(0, s ^ 1, k_at);
-                    commit(&ctl->s_full[s ^ 1]);
-                    commit(k_empty);
-                    if (i + 2 == n) commit(&ctl->q_free);
+                    if (!keys(i + 1)) return;
+                    scores(0, buffer ^ 1);
+                    if (one) {
+                        ca_commit(k.empty());
+                        if (i + 2 == n) ca_commit(CA_AT(bars, q_free));
+                    }
+                    k.step();
                 }
-                if (!bar_full(taken + 2 * i + 1, &v_empty, &v_at) || !looked(i)) return;
-                if (!wait(&ctl->p_full[s], p_phase[s])) return;
-                p_phase[s] ^= 1;
-                ca_after_sync();
-                output(S::STREAMS == 2 ? s : 0, s, v_at, i >= S::STREAMS);
-                commit(v_empty);
-                if constexpr (S::STREAMS == 2) {
-                    if (i + 2 >= n) commit(&ctl->o_full[s]);
-                } else {
-                    commit(&ctl->o_step);
-                    if (i + 1 == n) commit(&ctl->o_full[0]);
+                if (!values(i) || !weights(buffer)) return;
+                output(S::STREAMS == 2 ? buffer : 0, buffer, i >= S::STREAMS);
+                if (one) {
+                    ca_commit(v.empty());
+                    if constexpr (S::STREAMS == 2) {
+                        if (i + 2 >= n) ca_commit(CA_AT(bars, o_full) + buffer * 8);
+                    } else {
+                        ca_commit(CA_AT(bars, o_step));
+                        if (i + 1 == n) ca_commit(CA_AT(bars, o_full));
+                    }
                 }
+                v.step();
             }
         }
-        taken += 2 * n;
     }
 }
 
@@ -888,7 +903,8 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
     volatile int32_t* failed = &ctl->failed;
     const float factor = p.scale * LOG2E;
     CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
-    uint32_t s_phase[2] = {0, 0}, o_phase = 0, step_phase = 0, meeting = 0;
+    const uint32_t bars = ca_smem(ctl);
+    uint32_t s_phases = 0, o_phase = 0, step_phase = 0, meeting = 0;     // s_phases: a bit for each place of scores
     int32_t tiles_done = 0;
     while (walk.next()) {
         const auto& b = walk.block;
@@ -903,9 +919,9 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
         bool ok = true;
         for (int32_t i = first; i < n; i += step) {
             const int buffer = both ? group : (S::STREAMS == 2 ? group : i & 1);
-            ok = __all_sync(FULL_MASK, ca_wait(&ctl->s_full[buffer], s_phase[buffer], failed));
+            ok = ca_wait(CA_AT(bars, s_full) + buffer * 8, s_phases >> buffer & 1u, failed);
             if (!ok) break;
-            s_phase[buffer] ^= 1;
+            s_phases ^= 1u << buffer;
             ca_after_sync();
             if (warp_held) {
                 float x[KT];
@@ -934,7 +950,7 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
                     lost *= by;
                     if (i > first) {
                         if (S::STREAMS == 1) {           // the products of the tile before may still run
-                            ok = __all_sync(FULL_MASK, ca_wait(&ctl->o_step, step_phase ^ 1u, failed));
+                            ok = ca_wait(CA_AT(bars, o_step), step_phase ^ 1u, failed);
                             ca_after_sync();
                         }
                         const uint32_t o = tm + S::O_AT + (S::STREAMS == 2 ? group * D : 0);
@@ -976,7 +992,7 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
             step_phase ^= 1;
             ca_before_sync();
             __syncwarp();
-            if (lane_id() == 0) ca_arrive(&ctl->p_full[buffer]);
+            if (lane_id() == 0) ca_arrive(CA_AT(bars, p_full) + buffer * 8);
             if (!ok) break;
         }
         if (!ok) break;
@@ -985,7 +1001,7 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
         const bool mine = both || group == 0;
         const int32_t others = shared ? n / 2 : 0;                       // tiles of the second stream
         if (n > first) {
-            ok = __all_sync(FULL_MASK, ca_wait(&ctl->o_full[S::STREAMS == 2 ? group : 0], o_phase, failed));
+            ok = ca_wait(CA_AT(bars, o_full) + (S::STREAMS == 2 ? group * 8 : 0), o_phase, failed);
             if (!ok) break;
             o_phase ^= 1;
         }
@@ -993,7 +1009,7 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
         if (shared && n > 0) {
             if (group == 1) ctl->other[lane_row] = make_float2(reference, sum);
             ca_before_sync();
-            if (!ca_meet(&ctl->weighers, meeting, failed)) break;
+            if (!ca_meet(CA_AT(bars, weighers), meeting, failed)) break;
             ca_after_sync();
             if (mine && others > 0) {
                 const float2 o = ctl->other[lane_row];
@@ -1070,7 +1086,7 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
             }
         }
         ca_before_sync();
-        if (shared && n > 0 && !ca_meet(&ctl->weighers, meeting, failed)) break;
+        if (shared && n > 0 && !ca_meet(CA_AT(bars, weighers), meeting, failed)) break;
         ca_after_sync();
         tiles_done += n;
     }
@@ -1083,26 +1099,27 @@ __global__ void __launch_bounds__(CA_THREADS, 1) paged_attention_chunk_kernel(co
     char* queries = ca_memory;
     char* stages = ca_memory + S::STREAMS * S::Q_TILE;
     CaControl<D>* ctl = reinterpret_cast<CaControl<D>*>(stages + S::STAGES * S::STAGE);
+    const uint32_t bars = ca_smem(ctl);
     const int32_t warp = (int32_t)threadIdx.x / 32;
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::STAGES; ++i) {
-            ca_bar_init(&ctl->full[i], p.box ? 1 : CA_LOADERS / 32);
-            ca_bar_init(&ctl->empty[i], 1);
+            ca_bar_init(CA_AT(bars, full) + i * 8, p.box ? 1 : CA_LOADERS / 32);
+            ca_bar_init(CA_AT(bars, empty) + i * 8, 1);
         }
-        ca_bar_init(&ctl->q_full, !p.box ? CA_LOADERS / 32 : p.q_box ? 1 : 2);
-        ca_bar_init(&ctl->opened, 2);
-        ca_bar_init(&ctl->asked, 1);
-        ca_bar_init(&ctl->looked, 2);
-        ca_bar_init(&ctl->q_free, 1);
+        ca_bar_init(CA_AT(bars, q_full), !p.box ? CA_LOADERS / 32 : p.q_box ? 1 : 2);
+        ca_bar_init(CA_AT(bars, opened), 2);
+        ca_bar_init(CA_AT(bars, asked), 1);
+        ca_bar_init(CA_AT(bars, looked), 2);
+        ca_bar_init(CA_AT(bars, q_free), 1);
         for (int i = 0; i < 2; ++i) {
-            ca_bar_init(&ctl->s_full[i], 1);
-            ca_bar_init(&ctl->p_full[i], 4);
-            ca_bar_init(&ctl->o_full[i], 1);
+            ca_bar_init(CA_AT(bars, s_full) + i * 8, 1);
+            ca_bar_init(CA_AT(bars, p_full) + i * 8, 4);
+            ca_bar_init(CA_AT(bars, o_full) + i * 8, 1);
         }
-        ca_bar_init(&ctl->o_step, 1);
-        ca_bar_init(&ctl->loaders, CA_LOADERS / 32);
-        ca_bar_init(&ctl->weighers, 8);
-        ca_bar_init(&ctl->drain, 1);
+        ca_bar_init(CA_AT(bars, o_step), 1);
+        ca_bar_init(CA_AT(bars, loaders), CA_LOADERS / 32);
+        ca_bar_init(CA_AT(bars, weighers), 8);
+        ca_bar_init(CA_AT(bars, drain), 1);
         ctl->failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -1154,11 +1171,8 @@ __global__ void __launch_bounds__(CA_THREADS, 1) paged_attention_chunk_kernel(co
     if (warp == 11) {
         if (ctl->failed) {                                               // products may be under way still
             int32_t ignored = 0;
-            if (lane_id() == 0) {
-                ca_commit(&ctl->drain);
-                (void)ca_wait(&ctl->drain, 0, &ignored);
-            }
-            __syncwarp();
+            if (lane_id() == 0) ca_commit(CA_AT(bars, drain));
+            (void)ca_wait(CA_AT(bars, drain), 0, &ignored);
         }
         ca_after_sync();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(ctl->tensor));
