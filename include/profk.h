@@ -636,7 +636,7 @@ int profk_pages_append_rotary_f16(const void* q, const int64_t* q_strides, const
  *   workspace    [device] profk_paged_attention_chunk_workspace_bytes(dim), 256-byte aligned
  *   out          [device] rows x heads x dim, dense, of the cache's type;  lse  [device] rows x heads floats
  * Products in the cache's type, sums and statistics in fp32; weights are rounded once to the cache's type (bf16: off by 2^-9 of each; fp16:
- * by 2^-12 of it or 2^-39 of the largest).  A token that sees nothing gets out = 0, lse = -inf; rows that no sequence holds likewise.
+ * by 2^-12 of it or 2^-36 of the largest).  A token that sees nothing gets out = 0, lse = -inf; rows that no sequence holds likewise.
  * What a row does not see does not reach it, whatever its values are.  The same call gives the same bits every time.  Waits inside
  * the kernel are bounded; should one run out, all outputs are NaN.  Errors: PROFK_EINVAL, PROFK_EWORKSPACE, PROFK_ECUDA.
  */

@@ -13,7 +13,7 @@
 //   P           a thread owns a row: reads its scores, keeps the running maximum and sum, writes the weights over the scores;
 //   O += P V    tcgen05.mma, P from tensor memory, V from shared memory as it was loaded (its rows run along the product).
 // With dim > 128 there is room for one O only: one stream, whose scores alternate between two places.
-// The exponents' reference is raised only when a score passes it by more than 2^8 (fp16: 2, its weights are lifted by 2^14 so
+// The exponents' reference is raised only when a score passes it by more than 2^8 (fp16: 2^4; its weights are lifted by 2^11 so
 // that small ones do not vanish); then the row's own thread scales its O.  Weights are rounded once to the cache's type, as the
 // product with the values needs it: an error of half a step in each, which for values of either sign adds up to no more
 // than the rounding of the output does.  Sums of weights are kept in fp32, unrounded and compensated.
@@ -235,25 +235,27 @@ __device__ __forceinline__ bool ca_meet(uint32_t bar, uint32_t& phase, volatile 
     return ok;
 }
 
-__device__ __forceinline__ void ca_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void ca_commit(uint32_t bar, uint32_t one) {
+    asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar), "r"(one) : "memory");
 }
 __device__ __forceinline__ void ca_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void ca_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
 // A value that all lanes hold alike, told to the compiler: the matrix instructions take their operands from uniform registers.
 __device__ __forceinline__ uint32_t ca_uniform(uint32_t x) { return __shfl_sync(FULL_MASK, x, 0); }
-__device__ __forceinline__ bool ca_elect() {
+__device__ __forceinline__ uint32_t ca_elect() {
     uint32_t one;
     asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(one));
-    return one != 0;
+    return one;
 }
-// D (128 x N, tensor memory) (+)= A (shared memory or tensor memory) B (shared memory)
-__device__ __forceinline__ void ca_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
+// D (128 x N, tensor memory) (+)= A (shared memory or tensor memory) B (shared memory), issued by the lane whose `one` is set.
+// (A predicate, not a branch: in diverged code the operands may be computed in ordinary registers and moved one by one, which
+// made the whole kernel 40 % slower.)
+__device__ __forceinline__ void ca_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add, uint32_t one) {
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add), "r"(one) : "memory");
 }
-__device__ __forceinline__ void ca_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
+__device__ __forceinline__ void ca_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add, uint32_t one) {
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(what), "r"((uint32_t)add), "r"(one) : "memory");
 }
 // Shared-memory operand in rows of 128 bytes, swizzled in atoms of eight rows; `leading`: between atoms along a transposed
 // operand's rows.  Its lower word holds what differs between operands: the address in 16 bytes (and `leading`).
@@ -271,7 +273,7 @@ template <> struct CaType<__nv_bfloat16> {
 };
 template <> struct CaType<__half> {
     static constexpr uint32_t CODE = 0;
-    static constexpr float RAISE = 1.0f, LIFT = 14.0f;
+    static constexpr float RAISE = 4.0f, LIFT = 11.0f;
     static constexpr uint32_t EXPONENT = 0x7C00u;
     static __device__ __forceinline__ uint32_t pack(float a, float b) {
         const __half2 h = __floats2half2_rn(a, b);
@@ -742,7 +744,7 @@ template <typename T, int D>
 __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t queries, uint32_t stages) {
     using S = CaShape<D>;
     const uint32_t tm = ca_uniform(ctl->tensor), bars = ca_smem(ctl);
-    const bool one = ca_elect();
+    const uint32_t one = ca_elect();
     constexpr uint32_t SCORES = ca_product<T>(S::KT, false), OUTPUT = ca_product<T>(D, true);
     CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
     uint32_t q_phase = 0, p_phases = 0, opened = 0, look_phase = 0;      // p_phases: a bit for each place of scores
@@ -757,25 +759,25 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
     // S = Q K^T, and whom it concerns
     auto scores = [&](int s, int buffer) {
         const uint32_t q = ca_uniform(ca_operand_low(queries + s * S::Q_TILE, 16)), k0 = ca_uniform(ca_operand_low(k.data(), 16)), to = ca_uniform(tm + buffer * 128);
-        if (one) {
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i)
-                ca_mma_ss(to, ca_operand(q + i / 4 * (CA_ROWS * 8) + i % 4 * 2), ca_operand(k0 + i / 4 * (S::KT * 8) + i % 4 * 2), SCORES, i > 0);
-            ca_commit(CA_AT(bars, s_full) + buffer * 8);
-        }
+        for (int i = 0; i < D / 16; ++i)
+            ca_mma_ss(to, ca_operand(q + i / 4 * (CA_ROWS * 8) + i % 4 * 2), ca_operand(k0 + i / 4 * (S::KT * 8) + i % 4 * 2), SCORES, i > 0, one);
+        ca_commit(CA_AT(bars, s_full) + buffer * 8, one);
     };
     // O += P V
     auto output = [&](int o, int buffer, bool add) {
         const uint32_t v0 = ca_uniform(ca_operand_low(v.data(), S::KT * 128)), to = ca_uniform(tm + S::O_AT + o * D), from = ca_uniform(tm + buffer * 128);
-        if (one) {
-            ca_mma_ts(to, from, ca_operand(v0), OUTPUT, add);
+        ca_mma_ts(to, from, ca_operand(v0), OUTPUT, add, one);
 #pragma unroll
-            for (int i = 1; i < S::KT / 16; ++i) ca_mma_ts(to, from + i * 8, ca_operand(v0 + i * 128), OUTPUT, true);
-        }
+        for (int i = 1; i < S::KT / 16; ++i) ca_mma_ts(to, from + i * 8, ca_operand(v0 + i * 128), OUTPUT, true, one);
     };
-    while (walk.next()) {
+    bool some = walk.next();
+    while (some) {
         const int32_t n = walk.tile1 - walk.tile0;
-        if (n == 0) continue;
+        if (n == 0) {
+            some = walk.next();
+            continue;
+        }
         if (!wait(CA_AT(bars, q_full), q_phase)) return;
         q_phase ^= 1u;
         // Values that a mask cuts are looked through first: by those that copied them, or by warps that tell of it.  One tile is
@@ -803,16 +805,15 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
         const bool both = S::STREAMS == 2 && walk.block.rows > CA_ROWS;
         scores(0, 0);
         if (both) scores(1, 1);
-        if (one) {
-            ca_commit(k.empty());
-            if (n == 1) ca_commit(CA_AT(bars, q_free));
-        }
+        ca_commit(k.empty(), one);
+        if (n == 1) ca_commit(CA_AT(bars, q_free), one);
         k.step();
         if (both) {
             // both streams over every tile
 #pragma unroll 1
             for (int32_t i = 0; i < n; ++i) {
                 if (!values(i)) return;
+                if (i + 1 == n) some = walk.next();                      // (while the last weights are made)
 #pragma unroll 1
                 for (int st = 0; st < 2; ++st) {
                     if (!weights(st)) return;
@@ -820,15 +821,14 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
                     if (i + 1 < n) {
                         if (st == 0 && !keys(i + 1)) return;
                         scores(st, st);
-                    } else if (one) {
-                        ca_commit(CA_AT(bars, o_full) + st * 8);
+                    } else {
+                        ca_commit(CA_AT(bars, o_full) + st * 8, one);
                     }
                 }
-                if (one) {
-                    ca_commit(v.empty());
-                    if (i + 1 < n) ca_commit(k.empty());
-                    if (i + 2 == n) ca_commit(CA_AT(bars, q_free));
-                }
+                // (told of last: a commit between the products of a stream and its next scores delays those)
+                ca_commit(v.empty(), one);
+                if (i + 1 < n) ca_commit(k.empty(), one);
+                if (i + 2 == n) ca_commit(CA_AT(bars, q_free), one);
                 v.step();
                 if (i + 1 < n) k.step();
             }
@@ -840,22 +840,20 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
                 if (i + 1 < n) {
                     if (!keys(i + 1)) return;
                     scores(0, buffer ^ 1);
-                    if (one) {
-                        ca_commit(k.empty());
-                        if (i + 2 == n) ca_commit(CA_AT(bars, q_free));
-                    }
+                    ca_commit(k.empty(), one);
+                    if (i + 2 == n) ca_commit(CA_AT(bars, q_free), one);
                     k.step();
                 }
-                if (!values(i) || !weights(buffer)) return;
+                if (!values(i)) return;
+                if (i + 1 == n) some = walk.next();
+                if (!weights(buffer)) return;
                 output(S::STREAMS == 2 ? buffer : 0, buffer, i >= S::STREAMS);
-                if (one) {
-                    ca_commit(v.empty());
-                    if constexpr (S::STREAMS == 2) {
-                        if (i + 2 >= n) ca_commit(CA_AT(bars, o_full) + buffer * 8);
-                    } else {
-                        ca_commit(CA_AT(bars, o_step));
-                        if (i + 1 == n) ca_commit(CA_AT(bars, o_full));
-                    }
+                ca_commit(v.empty(), one);
+                if constexpr (S::STREAMS == 2) {
+                    if (i + 2 >= n) ca_commit(CA_AT(bars, o_full) + buffer * 8, one);
+                } else {
+                    ca_commit(CA_AT(bars, o_step), one);
+                    if (i + 1 == n) ca_commit(CA_AT(bars, o_full), one);
                 }
                 v.step();
             }
@@ -865,21 +863,23 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
 
 // ---- weights and output ------------------------------------------------------------------------
 
+struct CaWho { int32_t seq, head, row0, tile0, tile1; };                 // an item's
+
 // Adds what tokens with values that are not finite contribute to 32 columns of a row's output (their values were left out of
 // the product, where they would have met weights of zero).  Slow, and rare: the token's weight is computed again.
 template <typename T, int D>
-__device__ __noinline__ void ca_add_bad(const CaParams<T>& p, const uint32_t (*bad)[4], const CaWalk<T, D>& walk, uint32_t row_token, uint32_t g, int32_t seen, float factor,
+__device__ __noinline__ void ca_add_bad(const CaParams<T>& p, const uint32_t (*bad)[4], const CaWho& who, uint32_t row_token, uint32_t g, int32_t seen, float factor,
                                         float reference, int32_t column, float* o) {
     using S = CaShape<D>;
-    const int32_t* table = p.tables + walk.seq_number * p.table_stride;
-    const T* q = p.q + (p.starts ? (int64_t)walk.seq.row0 * p.q_token : walk.seq_number * p.q_seq) + row_token * p.q_token + ((int64_t)walk.head * p.group + g) * p.q_head;
-    for (int32_t tile = max(walk.tile0, walk.tile1 - CA_BAD_TILES); tile < walk.tile1; ++tile)
+    const int32_t* table = p.tables + who.seq * p.table_stride;
+    const T* q = p.q + (p.starts ? (int64_t)who.row0 * p.q_token : who.seq * p.q_seq) + row_token * p.q_token + ((int64_t)who.head * p.group + g) * p.q_head;
+    for (int32_t tile = max(who.tile0, who.tile1 - CA_BAD_TILES); tile < who.tile1; ++tile)
         for (int32_t i = 0; i < S::KT; ++i) {
             const int64_t token = (int64_t)tile * S::KT + i;
             if (!(bad[tile % CA_BAD_TILES][i / 32] >> (i % 32) & 1u) || token >= seen) continue;
             const int64_t page = table[token / p.page_size], slot = token % p.page_size;
-            const T* k = p.k + page * p.ks_page + walk.head * p.ks_head + slot * p.ks_token;
-            const T* v = p.v + page * p.vs_page + walk.head * p.vs_head + slot * p.vs_token;
+            const T* k = p.k + page * p.ks_page + who.head * p.ks_head + slot * p.ks_token;
+            const T* v = p.v + page * p.vs_page + who.head * p.vs_head + slot * p.vs_token;
             float s = 0.0f;
             for (int32_t d = 0; d < p.dim; ++d) s += Logit<T>::to_float(q[d]) * Logit<T>::to_float(k[d]);
             const float w = exp2_approx(s * factor - reference);
@@ -906,8 +906,9 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
     const uint32_t bars = ca_smem(ctl);
     uint32_t s_phases = 0, o_phase = 0, step_phase = 0, meeting = 0;     // s_phases: a bit for each place of scores
     int32_t tiles_done = 0;
-    while (walk.next()) {
-        const auto& b = walk.block;
+    bool more = walk.next();
+    while (more) {
+        const auto b = walk.block;
         const bool both = S::STREAMS == 2 && b.rows > CA_ROWS;           // streams have rows of their own
         const int32_t n = walk.tile1 - walk.tile0;
         const int32_t row = (both ? group * CA_ROWS : 0) + lane_row;     // of the item
@@ -932,11 +933,15 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
                 const uint4 mask = *reinterpret_cast<const uint4*>(ctl->mask[(tiles_done + i) % CA_MASKS]);
                 const int32_t left = seen - (walk.tile0 + i) * KT;
                 if (left < KT || (mask.x & mask.y & mask.z & mask.w) != ~0u) {
-                    const int32_t limit = max(0, left);
                     const uint32_t word[4] = {mask.x, mask.y, mask.z, mask.w};
 #pragma unroll
-                    for (int c = 0; c < KT; ++c)
-                        if (c >= limit || !(word[c / 32] >> (c % 32) & 1u)) x[c] = -INFINITY;
+                    for (int c0 = 0; c0 < KT; c0 += 32) {
+                        const int32_t there = left - c0;                 // tokens of this word that the row sees
+                        const uint32_t on = word[c0 / 32] & (there >= 32 ? ~0u : there <= 0 ? 0u : (1u << there) - 1u);
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            if (!(on & 1u << c)) x[c0 + c] = -INFINITY;
+                    }
                 }
                 float most[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
@@ -996,7 +1001,11 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
             if (!ok) break;
         }
         if (!ok) break;
-        // --- the item's output: this thread's row
+        // --- the item's output: this thread's row.  (The next item is found while the last products run.)
+        const int32_t tile0 = walk.tile0, number = walk.number;
+        const bool whole = walk.whole();
+        const CaWho who{walk.seq_number, walk.head, walk.seq.row0, tile0, walk.tile1};
+        more = walk.next();
         const bool shared = S::STREAMS == 2 && !both;                    // two streams share rows: the first writes
         const bool mine = both || group == 0;
         const int32_t others = shared ? n / 2 : 0;                       // tiles of the second stream
@@ -1022,13 +1031,12 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
         }
         ca_after_sync();
         if (mine && warp_held) {
-            const int64_t out_row = (int64_t)(walk.seq.row0 + token) * p.heads + (int64_t)walk.head * p.group + g;
-            const bool whole = walk.whole();
-            const int32_t slot = (int32_t)blockIdx.x * 2 + (walk.tile0 == 0 ? 1 : 0);
+            const int64_t out_row = (int64_t)(who.row0 + token) * p.heads + (int64_t)who.head * p.group + g;
+            const int32_t slot = (int32_t)blockIdx.x * 2 + (tile0 == 0 ? 1 : 0);
             float* part = whole ? nullptr : p.parts + ((int64_t)slot * S::BLOCK + row) * D;
             // (of a sum of zero, all products are zeros, too)
             const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
-            const bool any_bad = n > 0 && ctl->any_bad[walk.number % CA_ITEMS] != 0;
+            const bool any_bad = n > 0 && ctl->any_bad[number % CA_ITEMS] != 0;
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
                 if (c >= p.dim) break;
@@ -1048,7 +1056,7 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
                         float z[32];
 #pragma unroll
                         for (int e = 0; e < 32; ++e) z[e] = y[e];
-                        ca_add_bad<T, D>(p, ctl->bad[walk.number % CA_ITEMS], walk, token, g, seen, factor, reference - CaType<T>::LIFT, c, z);
+                        ca_add_bad<T, D>(p, ctl->bad[number % CA_ITEMS], who, token, g, seen, factor, reference - CaType<T>::LIFT, c, z);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) y[e] = z[e];
                     }
@@ -1078,10 +1086,10 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
             if (!whole && row == 0) {
                 CaMeta* m = p.meta + slot;
                 m->valid = 1;
-                m->last = walk.tile1 == b.tiles;
+                m->last = who.tile1 == b.tiles;
                 m->rows = b.rows;
-                m->row0 = walk.seq.row0;
-                m->head = walk.head;
+                m->row0 = who.row0;
+                m->head = who.head;
                 m->first = b.first;
             }
         }
@@ -1171,7 +1179,7 @@ __global__ void __launch_bounds__(CA_THREADS, 1) paged_attention_chunk_kernel(co
     if (warp == 11) {
         if (ctl->failed) {                                               // products may be under way still
             int32_t ignored = 0;
-            if (lane_id() == 0) ca_commit(CA_AT(bars, drain));
+            ca_commit(CA_AT(bars, drain), lane_id() == 0);
             (void)ca_wait(CA_AT(bars, drain), 0, &ignored);
         }
         ca_after_sync();

@@ -3,7 +3,7 @@
 Tolerances.  A score is a sum of dim products that the matrix unit adds in fp32, at worst with one unit of the last place
 lost per step: scale * sum |q k| * 2^-20 absolute, which moves a weight by as much relatively; the exponential and its
 argument add 2^-22 + 2^-22 |y| (|y| <= 64 where it matters: 2^-16).  A weight is rounded once to the cache's type: half a step,
-eps / 2 of it (fp16: 2^-39 of the largest, too, below its normal range).  The sum over n tokens is taken in steps of 16, each off by
+eps / 2 of it (fp16: 2^-36 of the largest, too: half a subnormal step, 2^-25, of weights that are lifted by 2^11).  The sum over n tokens is taken in steps of 16, each off by
 2^-23 of what it has at worst.  So an output entry may be off by sum p |v| times eps / 2 + n / 16 * 2^-23 + twice the first two, plus
 half a unit in the last place of its type; lse by the scores' error, 2^-16 and 2^-22 of itself."""
 import numpy as np
@@ -60,7 +60,7 @@ def _check(q, k, v, tables, lengths, starts, scale=None, result=None):
     fine = np.isfinite(want)
     assert (np.isfinite(got) == fine).all(), "values that are not finite"
     off = np.abs(np.where(fine, got, 0) - np.where(fine, want, 0))
-    tiny = torch.finfo(q.dtype).tiny + (2.0 ** -39 * int(lengths.max()) * 8 if q.dtype == torch.float16 else 0)
+    tiny = torch.finfo(q.dtype).tiny + (2.0 ** -36 * int(lengths.max()) * 8 if q.dtype == torch.float16 else 0)
     allowed = eps * np.abs(np.where(fine, want, 0)) + np.where(fine, size, 0) * rel[..., None] + tiny
     assert (off <= allowed).all(), f"out: {off.max()} (allowed {allowed.flat[(off - allowed).argmax()]}) at {np.unravel_index((off - allowed).argmax(), off.shape)}"
     got_lse = lse.double().cpu().numpy()
