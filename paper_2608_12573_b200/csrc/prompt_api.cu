@@ -39,7 +39,8 @@ int ro_launch(RoParams<T> p, int sms, void* stream) {
     // four heads to a thread once that still fills the device, and tokens for four turns of a CTA's threads
     const bool many = p.rows * heads * chunks >= (int64_t)sms * RO_THREADS * 8;
     const int64_t per_token = (many ? (heads + 3) / 4 : heads) * chunks;
-    p.tokens_per_cta = (int32_t)std::clamp<int64_t>(std::min((4 * RO_THREADS + per_token - 1) / per_token, p.rows / (4 * sms)), 1, RO_TOKENS);
+    const int64_t angles = RO_ANGLES / p.pairs;              // tokens whose angles a CTA has room for
+    p.tokens_per_cta = (int32_t)std::clamp<int64_t>(std::min({(4 * RO_THREADS + per_token - 1) / per_token, p.rows / (4 * sms), angles}), 1, RO_TOKENS);
     const int64_t ctas = (p.rows + p.tokens_per_cta - 1) / p.tokens_per_cta;
     if (ctas > 0x7FFFFFFFll) return PROFK_EINVAL;
     Launch l((unsigned)ctas, RO_THREADS, (size_t)p.tokens_per_cta * p.pairs * sizeof(float2), stream);

@@ -21,6 +21,7 @@ namespace profk {
 constexpr int RO_THREADS = 256;
 constexpr int RO_TOKENS = 32;             // tokens of a CTA at most
 constexpr int RO_MAX_PAIRS = 512;
+constexpr int RO_ANGLES = 4096;           // of a CTA at most: 32 KB
 
 template <typename T>
 struct RoRows {                           // rows (outer, inner, head) of `dim` elements, strides in elements

@@ -1,8 +1,10 @@
 """The operators around a selection in a decoding loop: log probabilities with entropy and top alternatives (and their
-gradient), the forking and compaction of the pages of a key-value cache, and attention of one token over them.
+gradient), the forking and compaction of the pages of a key-value cache, and attention of one token over them; and those that
+take prompts and drafts into it: rotary positions (and their gradient), appending with them, attention of a chunk of new
+tokens, and what is laid over logits before a selection.
 
 Checks, allocation and marshalling are done by the in-tree extension module `_decode` (csrc/decode_binding.cpp), which calls
-the C ABI of `profk.h`; a refusal raises `ProfkError`.  Of all of them `logprobs` has a derivative; the others refuse tensors
+the C ABI of `profk.h`; a refusal raises `ProfkError`.  Of all of them `logprobs` and `rotary` have derivatives; the others refuse tensors
 that require a gradient unless grad mode is off.  Nothing is synchronised, and scratch memory comes from torch's
 allocator on the current stream, so that calls on several streams do not meet.
 """

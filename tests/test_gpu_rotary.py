@@ -119,6 +119,18 @@ def test_a_head_s_other_elements_keep_their_bits_and_pairs_their_own_faults():
     assert bad.nonzero().flatten().tolist() == [3, 19]
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_wide_heads_of_many_tokens(dtype, interleaved):
+    """As many pairs and tokens as a CTA's room for angles is shortest for."""
+    x, f = _randn(9001, 1, 1024, dtype=dtype), profk.rotary_frequencies(1024)
+    at = torch.arange(9001, device="cuda") % 700
+    got = profk.rotary(x, at, f, interleaved=interleaved)
+    rows = torch.cat([torch.arange(40, device="cuda"), torch.arange(8970, 9001, device="cuda")])
+    _near(got[rows], x[rows], at[rows], f, interleaved=interleaved)
+    assert torch.equal(got[700:1400], profk.rotary(x[700:1400], at[:700], f, interleaved=interleaved))
+
+
 def test_no_tokens():
     f = profk.rotary_frequencies(8)
     assert profk.rotary(_randn(0, 4, 8), torch.zeros(0, dtype=torch.int64, device="cuda"), f).shape == (0, 4, 8)
