@@ -131,6 +131,21 @@ def test_one_long_sequence_shared_by_all_ctas():
         _check(q, k, v, tables, lengths, starts)
 
 
+@pytest.mark.parametrize("dim,heads", [(64, 40), (128, 40), (256, 20)])
+def test_many_items_of_many_tiles_to_a_cta(dim, heads):
+    """Items whose tiles are taken in another order than they lie in, with tokens at the end that only some rows see."""
+    q, k, v, tables, lengths, starts = _case([4400, 4600, 4300], [300, 260, 513], heads, heads, dim, 32, "bf16", seed=dim)
+    want = profk.paged_attention_chunk(q, k, v, tables, lengths, starts=starts)
+    some = [0, 1, heads // 2, heads - 1]                 # (the oracle's time: a few of the heads)
+    _check(q[:, some], k[:, some], v[:, some], tables, lengths, starts, result=(want[0][:, some], want[1][:, some]))
+    for i, n in enumerate([4400, 4600, 4300]):
+        v[int(tables[i, (n - 9) // 32]), :, (n - 9) % 32, 3] = float("nan")
+    got = profk.paged_attention_chunk(q, k, v, tables, lengths, starts=starts)
+    for i in range(3):
+        a, z = int(starts[i]), int(starts[i + 1])
+        assert torch.equal(got[0][a:z - 9], want[0][a:z - 9]) and torch.isnan(got[0][z - 9:z, :, 3]).all() and torch.equal(got[0][z - 9:z, :, 8:], want[0][z - 9:z, :, 8:])
+
+
 def test_scores_that_rise_and_fall_far():
     for dim in (64, 128, 256):
         for dtype in DTYPES:
