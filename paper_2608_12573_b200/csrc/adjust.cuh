@@ -21,7 +21,7 @@
 namespace profk {
 
 constexpr int AD_THREADS = 256, AD_UNROLL = 4;         // of the stream; vectors of a thread in flight
-constexpr int AD_NAMED_THREADS = 512, AD_HISTORY = 8;  // of the second kernel; tokens of the history (and named ones) of a thread in flight
+constexpr int AD_NAMED_THREADS = 512, AD_PAIRS = 4, AD_HISTORY = 8;        // of the second kernel; pairs of tokens of the history, and named tokens, of a thread in flight
 constexpr int AD_MAX_BIASES = 8192;
 constexpr uint32_t AD_PROMPT = 0x80000000u, AD_COUNT = 0x7FFFFFFFu;           // a counter: whether the prompt names the token, its count in the answer
 constexpr int64_t AD_NARROW = 32768;      // tokens of a history from which counters of 16 bits may not do
@@ -189,20 +189,36 @@ __global__ void __launch_bounds__(AD_NAMED_THREADS, BITS == 16 ? 3 : 2) adjust_n
         const int64_t n = max((int64_t)0, min(p.lengths ? (int64_t)p.lengths[row] : p.history, p.history));
         const int64_t prompt = p.prompts ? (int64_t)p.prompts[row] : 0;
         __syncthreads();
-        for (int64_t i0 = (int64_t)threadIdx.x; i0 < n; i0 += (int64_t)AD_NAMED_THREADS * AD_HISTORY) {
-            int64_t token[AD_HISTORY];
+        // f(token - from) for the tokens [begin, end) of the history that are this CTA's: two to a 16-byte load, in 32 bits from there
+        const uint32_t base = (uint32_t)from;
+        auto scan = [&](int64_t begin, int64_t end, auto&& f) {
+            if (begin >= end) return;
+            auto one = [&](uint32_t low, uint32_t high) {
+                if (high == 0u && low - base < held) f(low - base);
+            };
+            const int64_t* at = tokens + begin;
+            const int64_t head = reinterpret_cast<uintptr_t>(at) % 16 != 0 ? 1 : 0, pairs = (end - begin - head) / 2, rest = end - begin - head - 2 * pairs;
+            auto single = [&](const int64_t* t) { one((uint32_t)*t, (uint32_t)((uint64_t)*t >> 32)); };
+            if (threadIdx.x == 0 && head) single(at);
+            if (threadIdx.x == 32 && rest) single(tokens + end - 1);
+            const uint4* two = reinterpret_cast<const uint4*>(at + head);
+            for (int64_t i0 = (int64_t)threadIdx.x; i0 < pairs; i0 += (int64_t)AD_NAMED_THREADS * AD_PAIRS) {
+                uint4 v[AD_PAIRS];
 #pragma unroll
-            for (int j = 0; j < AD_HISTORY; ++j) {
-                const int64_t i = i0 + (int64_t)j * AD_NAMED_THREADS;
-                token[j] = i < n ? tokens[i] - from : -1;
-            }
+                for (int j = 0; j < AD_PAIRS; ++j) {
+                    const int64_t i = i0 + (int64_t)j * AD_NAMED_THREADS;
+                    v[j] = i < pairs ? __ldg(two + i) : make_uint4(0u, ~0u, 0u, ~0u);
+                }
 #pragma unroll
-            for (int j = 0; j < AD_HISTORY; ++j) {
-                if ((uint64_t)token[j] >= (uint64_t)held) continue;
-                if (i0 + (int64_t)j * AD_NAMED_THREADS < prompt) counters.prompt((uint32_t)token[j]);
-                else counters.add((uint32_t)token[j]);
+                for (int j = 0; j < AD_PAIRS; ++j) {
+                    one(v[j].x, v[j].y);
+                    one(v[j].z, v[j].w);
+                }
             }
-        }
+        };
+        const int64_t split = max((int64_t)0, min(prompt, n));
+        scan(0, split, [&](uint32_t token) { counters.prompt(token); });
+        scan(split, n, [&](uint32_t token) { counters.add(token); });
         __syncthreads();
     } else if (!p.behind_stream) {
         pdl_wait();
