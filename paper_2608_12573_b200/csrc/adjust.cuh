@@ -253,7 +253,6 @@ __global__ void __launch_bounds__(AD_NAMED_THREADS, BITS == 16 ? 3 : 2) adjust_n
     if (!p.tokens) return;
     uint16_t* named = reinterpret_cast<uint16_t*>(list + p.biases);
     constexpr int PER = 4 * AdCounters<BITS>::PER;                       // counters of 16 bytes
-    const int32_t lane = (int32_t)lane_id();
     __syncthreads();
     if (threadIdx.x == 0) sums[0] = 0;
     __syncthreads();
@@ -263,16 +262,12 @@ __global__ void __launch_bounds__(AD_NAMED_THREADS, BITS == 16 ? 3 : 2) adjust_n
         const uint32_t word[4] = {c.x, c.y, c.z, c.w};
         uint32_t which = 0;                                              // bits: this thread's counters that are not zero
 #pragma unroll
-        for (int k = 0; k < PER; ++k) which |= (BITS == 16 ? (word[k / 2] >> (k % 2 * 16) & 0xFFFFu) != 0u : word[k % 4] != 0u) ? 1u << k : 0u;
-        if (!__any_sync(FULL_MASK, which)) continue;
-        int32_t upto = __popc(which);
-        for (int d = 1; d < 32; d *= 2) {
-            const int32_t o = __shfl_up_sync(FULL_MASK, upto, d);
-            if (lane >= d) upto += o;
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (BITS == 16) which |= ((word[k] & 0xFFFFu) != 0u ? 1u << 2 * k : 0u) | ((word[k] >> 16) != 0u ? 2u << 2 * k : 0u);
+            else which |= word[k] != 0u ? 1u << k : 0u;
         }
-        int32_t at = 0;
-        if (lane == 31) at = atomicAdd(&sums[0], upto);
-        at = __shfl_sync(FULL_MASK, at, 31) + upto - __popc(which);
+        if (!which) continue;
+        int32_t at = atomicAdd(&sums[0], __popc(which));                 // (in any order: a token's result does not depend on its place)
         for (; which; which &= which - 1u) named[at++] = (uint16_t)(i + (uint32_t)__ffs((int)which) - 1u);
     }
     __syncthreads();
