@@ -6,7 +6,7 @@
 // mask; a second goes back to the few tokens that a history or a list of biases names (it counts while the first one ends).
 // (One kernel that looked at every element's counter while streaming: in a warp some lane always has a named one, and the
 // division is then done for all; 256 rows of 131071 bf16 with 4096 tokens of history each 95 us.  One kernel that streamed a
-// slice and then went back: 68, the SMs idle while they count and list.)
+// slice and then went back: 68, the SMs idle while they count and list.  Now 64 with 30 biases and a mask, of which the stream takes 25.)
 //
 // Histories name tokens in any order, many times.  A CTA of the second kernel has a slice of a row's vocabulary: it goes over
 // the row's whole history (which comes from L2 but for the first time) and counts its own tokens in shared memory: integer
