@@ -190,16 +190,17 @@ class _RotaryFunction(torch.autograd.Function):
     def backward(ctx, g):
         positions, frequencies = ctx.saved_tensors
         interleaved, magnitude, inverse = ctx.how
-        # (an upstream gradient may be a broadcast scalar)
-        g = g if g.dim() == 0 or g.stride(-1) == 1 or g.size(-1) <= 1 else g.contiguous()
+        # (an upstream gradient comes in any layout: a broadcast scalar, a permutation)
+        if g.dim() > 4 or (g.size(-1) > 1 and g.stride(-1) != 1):
+            g = g.contiguous()
         return _RotaryFunction.apply(g, positions, frequencies, interleaved, magnitude, not inverse), None, None, None, None, None
 
 
 def rotary(x, positions, frequencies, *, interleaved: bool = False, magnitude: float = 1.0, inverse: bool = False):
     """`profk_rotary_*` on the current stream: turns pair i of every head by `positions * frequencies[i]` radians.
 
-    x: CUDA tensor (..., heads, dim), float32, bfloat16 or float16, dense heads, any strides.  positions: int64, broadcast to
-    x's leading dimensions.  frequencies: float64 (pairs,), 2 * pairs <= dim; the rest of a head is left as it is
+    x: CUDA tensor (..., heads, dim), float32, bfloat16 or float16, dense heads, any strides (of more than two leading dimensions:
+    evenly spaced on two levels).  positions: int64, broadcast to x's leading dimensions.  frequencies: float64 (pairs,), 2 * pairs <= dim; the rest of a head is left as it is
     (`rotary_frequencies`).  Pairs are elements i and pairs + i, or 2 i and 2 i + 1 with `interleaved`.  `magnitude` scales what
     is turned; `inverse` turns back.  Differentiable in x, any number of times."""
     if isinstance(x, torch.Tensor) and x.requires_grad and torch.is_grad_enabled():

@@ -291,6 +291,54 @@ def test_the_same_call_gives_the_same_bits_on_any_stream_and_in_a_graph():
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+def test_broadcast_queries_and_heads():
+    q, k, v, tables, lengths, starts = _case([100, 33], [50, 33], 6, 3, 64, 16, "bf16", seed=8)
+    _check(q[:, :1].expand(83, 6, 64), k, v, tables, lengths, starts)
+    _check(q, k[:, :1].expand(-1, 3, -1, -1), v[:, :1].expand(-1, 3, -1, -1), tables, lengths, starts)
+
+
+def test_many_sequences():
+    lengths = [(i * 7) % 40 + 1 for i in range(5000)]
+    _check(*_case(lengths, [min(n, i % 3 + 1) for i, n in enumerate(lengths)], 2, 1, 64, 8, "bf16", seed=4))
+
+
+@pytest.mark.parametrize("starts", [[5, -7, 1000, 93], [93, 50, 20, 0], [-2 ** 31, 2 ** 31 - 1, -1, 7], [0, 93, 0, 93]])
+def test_starts_that_are_none_stay_in_bounds(starts):
+    q, k, v, tables, lengths, _ = _case([100, 33, 60], [50, 33, 10], 6, 3, 64, 16, "bf16", seed=8)
+    fenced = torch.full((95, 6, 64), 7.0, dtype=q.dtype, device="cuda")
+    fenced[1:94] = q
+    out, lse = profk.paged_attention_chunk(fenced[1:94], k, v, tables, lengths, starts=torch.tensor(starts, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert out.shape == q.shape and lse.shape == (93, 6) and (fenced[0] == 7).all() and (fenced[94] == 7).all()
+
+
+def test_calls_at_once_and_two_graphs():
+    cases = [_case([3000, 20, 700], [300, 20, 4], 16, 4, 128, 16, "bf16", seed=1), _case([900, 1000], [100, 1000], 4, 4, 64, 32, "f16", seed=2),
+             _case([500], [200], 4, 2, 256, 8, "bf16", seed=3)]
+    call = lambda c: profk.paged_attention_chunk(*c[:5], starts=c[5])  # noqa: E731
+    want = [call(c) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = []
+        for stream, c in zip(streams, cases):
+            with torch.cuda.stream(stream):
+                got.append(call(c))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, w in zip(got, want) for a, b in zip(g, w))
+    graphs = []
+    for c in cases:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            result = call(c)
+        graphs.append((graph, result))
+    for _ in range(3):
+        for graph, _ in graphs:
+            graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for (_, g), w in zip(graphs, want) for a, b in zip(g, w))
+
+
 def test_refusals():
     q, k, v, tables, lengths, starts = _case([40, 20], [5, 7], 4, 2, 64, 16, "bf16")
     call = lambda *a, starts=starts, **how: profk.paged_attention_chunk(*a, starts=starts, **how)  # noqa: E731

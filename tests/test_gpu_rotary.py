@@ -175,6 +175,18 @@ def test_gradients_of_broadcasts_and_second_derivatives():
     assert torch.allclose(second, 128 * x, rtol=2.0 ** -17, atol=2.0 ** -14)
 
 
+def test_upstream_gradients_of_any_layout():
+    f, at = profk.rotary_frequencies(8), torch.arange(5, device="cuda")
+    x = _randn(2, 3, 4, 5, 6, 8, dtype="f32").requires_grad_(True)
+    w = _randn(6, 4, 5, 2, 8, 3, dtype="f32", seed=1)
+    grad, = torch.autograd.grad((profk.rotary(x, at, f).permute(4, 2, 3, 0, 5, 1) * w).sum(), x)
+    assert torch.equal(grad, profk.rotary(w.permute(3, 5, 1, 2, 0, 4).contiguous(), at, f, inverse=True))
+    x = _randn(2, 5, 6, 8, dtype="f32").requires_grad_(True)
+    w = _randn(8, 2, 6, 5, dtype="f32", seed=1)
+    grad, = torch.autograd.grad((profk.rotary(x, at, f).permute(3, 0, 2, 1) * w).sum(), x)
+    assert torch.equal(grad, profk.rotary(w.permute(1, 3, 2, 0).contiguous(), at, f, inverse=True))
+
+
 def test_streams_graphs_and_repeated_calls():
     x, f, at = _randn(100, 4, 64).requires_grad_(True), profk.rotary_frequencies(64), torch.arange(100, device="cuda")
     g = _randn(100, 4, 64, seed=3)
