@@ -473,25 +473,32 @@ struct CaLoader {
         return (((v.x & E) + ONE) | ((v.y & E) + ONE) | ((v.z & E) + ONE) | ((v.w & E) + ONE)) & 0x80008000u;
     }
     // The part of a tile of values of thread t of 8 * ROWS: vectors that are not finite are taken out, and their tokens noted.
-    // (Vector t % 8 of every ROWS-th row, of one 128-byte column after the other: a multiple of eight rows on, the swizzle is the same.)
+    // Its part is vector t % 8 of every ROWS-th row, in each 128-byte column.  Of the threads that copy (ROWS = CA_LOAD_ROWS) these are
+    // the vectors that the thread copied itself: it has waited for no others.
     template <int ROWS>
     static __device__ __forceinline__ void look(CaControl<D>* ctl, uint32_t stages, int32_t st, int32_t tile, int32_t item, int32_t t) {
-        constexpr int ALL = S::KT * (D / 64);
         const uint32_t at = stages + st * S::STAGE;
         uint32_t any = 0;
-        if constexpr (ROWS % 8 == 0) {
+        if constexpr (ROWS % 8 == 0) {                                   // (a multiple of eight rows on, the swizzle is the same)
 #pragma unroll 8
-            for (int i = 0; i < ALL; i += ROWS) any |= carries(ca_read(at + i * 128 + chunk_at(t >> 3, t & 7, S::KT)));
+            for (int i = 0; i < S::KT * (D / 64); i += ROWS) any |= carries(ca_read(at + i * 128 + chunk_at(t >> 3, t & 7, S::KT)));
         } else {
-#pragma unroll 4
-            for (int i = t >> 3; i < ALL; i += ROWS) any |= carries(ca_read(at + i / S::KT * S::KT * 128 + chunk_at(i % S::KT, t & 7, S::KT)));
+#pragma unroll 256 / D
+            for (int row = t >> 3; row < S::KT; row += ROWS) {
+                const uint32_t first = at + chunk_at(row, t & 7, S::KT);
+#pragma unroll
+                for (int h = 0; h < D / 64; ++h) any |= carries(ca_read(first + h * (S::KT * 128)));
+            }
         }
         if (any) take_out(ctl, at, tile, item, t, ROWS);
     }
     static __device__ __noinline__ void take_out(CaControl<D>* ctl, uint32_t at, int32_t tile, int32_t item, int32_t t, int32_t rows_at_once) {
-        for (int i = t >> 3; i < S::KT * (D / 64); i += rows_at_once) {
-            const int32_t row = i % S::KT;
-            const uint32_t where = at + i / S::KT * S::KT * 128 + chunk_at(row, t & 7, S::KT);
+        const int32_t rounds = (S::KT + rows_at_once - 1) / rows_at_once;
+#pragma unroll 1
+        for (int i = 0; i < rounds * (D / 64); ++i) {
+            const int32_t row = (t >> 3) + i % rounds * rows_at_once;
+            if (row >= S::KT) continue;
+            const uint32_t where = at + chunk_at(row, (t & 7) + i / rounds * 8, S::KT);
             if (!carries(ca_read(where))) continue;
             asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(where), "r"(0u) : "memory");
             atomicOr(&ctl->bad[item][tile][row / 32], 1u << (row % 32));
