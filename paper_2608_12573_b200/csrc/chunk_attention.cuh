@@ -589,10 +589,11 @@ __device__ __noinline__ void ca_load(const CaParams<T>& p, CaControl<D>* ctl, ch
         if (walk.tile1 == walk.tile0) continue;                          // no token to see
         // (the tile's tokens to the threads, the last 32 of 128 to the first warp once more)
         int32_t page = t < S::KT ? page_of(walk.tile0 * S::KT + t) : -1, page2 = t + CA_LOADERS < S::KT ? page_of(walk.tile0 * S::KT + CA_LOADERS + t) : -1;
-        if (t < CA_BAD_TILES * 4) ctl->bad[walk.number % CA_ITEMS][t / 4][t % 4] = 0;
-        if (t == 0) ctl->any_bad[walk.number % CA_ITEMS] = 0;
         if (!load.wait(CA_AT(load.bars, q_free), q_phase)) break;
         q_phase ^= 1;
+        // (the scores of the item before are made: so all warps are through with the item CA_ITEMS before this one, whose bits these were)
+        if (t < CA_BAD_TILES * 4) ctl->bad[walk.number % CA_ITEMS][t / 4][t % 4] = 0;
+        if (t == 0) ctl->any_bad[walk.number % CA_ITEMS] = 0;
         ca_copy_queries<T, D>(p, walk, q_at, t, CA_LOAD_ROWS);
         load.issued(CA_AT(load.bars, q_full), -1);
         const int32_t cut = ca_first_cut<T, D>(p, walk);

@@ -78,3 +78,25 @@ def test_unseen_values_in_any_column(dim, page):
                     # 2^-8 of at most |v| < 8, and half a step of the output)
                     near = [d for d in vector if d != column]
                     assert torch.allclose(got[0][first:z][..., near].float(), want[0][first:z][..., near].float(), rtol=2.0 ** -7, atol=2.0 ** -5)
+
+
+@pytest.mark.parametrize("page", [7, 16])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_long_items_with_many_bad_tokens_among_short_ones(dim, page):
+    """The second half of an item's rows see many tokens with values that are not finite, which takes long, and short items follow
+    that need the first half's warps only: what was noted for the long item has to outlast them."""
+    lengths = [200, 20, 9, 20, 3] * 592
+    case = _case(lengths, lengths, 1, 1, dim, page, seed=page)
+    q, k, v, tables, _, starts = case
+    want = _call(*case)
+    bad = v.clone()
+    first = 130
+    long = tables[::5]
+    for token in range(first, 200):
+        bad[long[:, token // page].long(), 0, token % page, dim - 3] = NAN
+    for _ in range(3):
+        got = _call(q, k, bad, *case[3:])
+        out, fine = got[0].view(592, -1, dim), want[0].view(592, -1, dim)
+        assert torch.equal(got[1], want[1])
+        assert torch.equal(out[:, :first], fine[:, :first]) and torch.equal(out[:, 200:], fine[:, 200:])
+        assert torch.isnan(out[:, first:200, dim - 3]).all() and torch.equal(out[:, first:200, :dim - 8], fine[:, first:200, :dim - 8])
