@@ -202,8 +202,13 @@ def rotary(x, positions, frequencies, *, interleaved: bool = False, magnitude: f
     x: CUDA tensor (..., heads, dim), float32, bfloat16 or float16, dense heads, any strides (of more than two leading dimensions:
     evenly spaced on two levels).  positions: int64, broadcast to x's leading dimensions.  frequencies: float64 (pairs,), 2 * pairs <= dim; the rest of a head is left as it is
     (`rotary_frequencies`).  Pairs are elements i and pairs + i, or 2 i and 2 i + 1 with `interleaved`.  `magnitude` scales what
-    is turned; `inverse` turns back.  Differentiable in x, any number of times."""
+    is turned; `inverse` turns back.  Differentiable in x, any number of times; frequencies that require a gradient are refused."""
     if isinstance(x, torch.Tensor) and x.requires_grad and torch.is_grad_enabled():
+        # (grad mode is off in the function's forward, where the call's own check would not see it)
+        if isinstance(frequencies, torch.Tensor) and frequencies.requires_grad:
+            import paper_2608_12573_b200 as package
+
+            raise package.ProfkError("frequencies requires a gradient, which this call does not have: detach it, or call under torch.no_grad()")
         return _RotaryFunction.apply(x, positions, frequencies, bool(interleaved), magnitude, bool(inverse))
     return (_native or _load()).rotary(x, positions, frequencies, bool(interleaved), magnitude, bool(inverse))
 
