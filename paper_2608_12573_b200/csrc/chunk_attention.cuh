@@ -231,6 +231,12 @@ __device__ __forceinline__ bool ca_wait(uint32_t bar, uint32_t parity, volatile 
     }
     return true;
 }
+// Waits for what is still under way in the CTA's memory, before that is given up and whatever has failed; limited, too.
+__device__ __forceinline__ void ca_drain(uint32_t bar, uint32_t parity) {
+    int32_t left = CA_POLLS;
+#pragma unroll 1
+    while (!__all_sync(FULL_MASK, ca_try(bar, parity)) && --left > 0) {}
+}
 // Warps meet (the barrier counts them); the wait is limited as all others are.
 __device__ __forceinline__ bool ca_meet(uint32_t bar, uint32_t& phase, volatile int32_t* failed) {
     __syncwarp();
@@ -1191,10 +1197,9 @@ __global__ void __launch_bounds__(CA_THREADS, 1) paged_attention_chunk_kernel(co
     __syncthreads();
     if (threadIdx.x == 0 && ctl->failed) p.meta[blockIdx.x * 2].failed = 1;
     if (warp == 11) {
-        if (ctl->failed) {                                               // products may be under way still
-            int32_t ignored = 0;
-            ca_commit(CA_AT(bars, drain), lane_id() == 0);
-            (void)ca_wait(CA_AT(bars, drain), 0, &ignored);
+        if (ctl->failed) {                                               // products may be under way still: those of the lane that issues them
+            ca_commit(CA_AT(bars, drain), ca_elect());
+            ca_drain(CA_AT(bars, drain), 0);
         }
         ca_after_sync();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(ctl->tensor));
