@@ -707,6 +707,12 @@ int profk_last_launch_count(void);
  */
 int profk_debug_set_prefetch_wait_polls(int64_t polls);
 
+/*
+ * Diagnostic: how many polls a wait inside the attention of a chunk may take before it gives up (negative = the default, 2^22; 0 = what
+ * is not over at once), after which all outputs of the call are NaN.  For calls and captures that follow.  Process-wide.
+ */
+int profk_debug_set_chunk_wait_polls(int64_t polls);
+
 /* Static text for a status code. */
 const char* profk_strerror(int code);
 

@@ -20,7 +20,7 @@ EXPORTS = [
     "profk_topk_f32", "profk_topk_bf16", "profk_topk_planned_f32", "profk_topk_planned_bf16",
     "profk_filter_f32", "profk_filter_bf16", "profk_sample_threshold_f32", "profk_sample_threshold_bf16",
     "profk_read_stats", "profk_last_launch_count", "profk_strerror", "profk_topk_noalloc_f32",
-    "profk_debug_set_prefetch_wait_polls",
+    "profk_debug_set_prefetch_wait_polls", "profk_debug_set_chunk_wait_polls",
     "profk_batchtopk_workspace_bytes", "profk_batchtopk_f32", "profk_batchtopk_bf16", "profk_batchtopk_planned_f32",
     "profk_batchtopk_planned_bf16",
     "profk_shard_bounds", "profk_shard_sample_keys_f32", "profk_shard_sample_keys_bf16", "profk_threshold_from_keys_f32",

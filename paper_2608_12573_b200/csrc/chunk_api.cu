@@ -2,6 +2,7 @@
 #include <cudaTypedefs.h>
 
 #include <algorithm>
+#include <atomic>
 #include <numeric>
 #include <type_traits>
 
@@ -14,6 +15,7 @@ namespace {
 
 constexpr int CA_MAX_DIM = 256;
 constexpr unsigned CA_JOIN_ROWS = 8;                    // CTAs that share the rows of an item
+std::atomic<int32_t> g_polls{CA_POLLS};                 // see profk_debug_set_chunk_wait_polls
 
 int ca_tile_dim(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 size_t ca_round(size_t n) { return (n + 255) / 256 * 256; }
@@ -136,6 +138,7 @@ int ca_run(const T* q, const int64_t* qs, const T* k, const T* v, const profk_pa
     p.by_group = CaDivisor::of((uint32_t)p.group);
     p.by_page = CaDivisor::of((uint32_t)page_size);
     p.scale = (float)scale;
+    p.polls = g_polls.load(std::memory_order_relaxed);
     p.out = out;
     p.lse = lse;
     // copies by tile want boxes of eight tokens (one atom of the swizzle) at least that never leave a page
@@ -164,6 +167,11 @@ int profk_paged_attention_chunk_workspace_bytes(int64_t dim, size_t* bytes) {
     const int sms = sm_count();
     if (sms < 1) return PROFK_ECUDA;
     *bytes = ca_workspace(dim, sms);
+    return PROFK_OK;
+}
+
+int profk_debug_set_chunk_wait_polls(int64_t polls) {
+    g_polls.store(polls < 0 ? CA_POLLS : (int32_t)std::min<int64_t>(polls, CA_POLLS), std::memory_order_relaxed);
     return PROFK_OK;
 }
 

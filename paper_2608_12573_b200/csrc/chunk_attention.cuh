@@ -87,6 +87,7 @@ struct CaParams {
     bool q_box;                           // queries are copied by tile, too
     bool q_wide;                          // rows of q lie on 16-byte vectors
     float scale;
+    int32_t polls;                        // that a wait may take: CA_POLLS but for tests
     T* out;
     float* lse;
     float* parts;                         // (2 per CTA) x BLOCK x D
@@ -219,17 +220,17 @@ __device__ __forceinline__ bool ca_try(uint32_t bar, uint32_t parity) {
     asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// A warp waits for a phase; gives up after a limit, or when another warp has, and then returns false for good.
+// A warp waits for a phase; gives up after a limit (the word behind `failed`: 0 for what is not over at once), or when another warp has,
+// and then returns false for good.
 __device__ __forceinline__ bool ca_wait(uint32_t bar, uint32_t parity, volatile int32_t* failed) {
-    int32_t left = CA_POLLS;
+    if (__all_sync(FULL_MASK, ca_test(bar, parity))) return true;
+    int32_t left = failed[1];
 #pragma unroll 1
-    while (!__all_sync(FULL_MASK, ca_try(bar, parity))) {
-        if (__any_sync(FULL_MASK, *failed != 0) || --left == 0) {
-            *failed = 1;
-            return false;
-        }
+    while (!__any_sync(FULL_MASK, failed[0] != 0 || left-- <= 0)) {
+        if (__all_sync(FULL_MASK, ca_try(bar, parity))) return true;
     }
-    return true;
+    failed[0] = 1;
+    return false;
 }
 // Waits for what is still under way in the CTA's memory, before that is given up and whatever has failed; limited, too.
 __device__ __forceinline__ void ca_drain(uint32_t bar, uint32_t parity) {
@@ -345,7 +346,7 @@ struct CaControl {
     uint64_t full[CaShape<D>::STAGES], empty[CaShape<D>::STAGES];
     uint64_t q_full, q_free, s_full[2], p_full[2], o_full[2], o_step, loaders, weighers, opened, asked, looked, drain;
     uint32_t tensor;                      // address of the tensor memory
-    int32_t failed;
+    int32_t failed[2];                    // whether a wait has run out; polls that one may take
     int32_t table[2][CaShape<D>::KT];     // pages of two tiles' tokens; -1: nothing there
     alignas(16) uint32_t mask[CA_MASKS][4];        // which tokens of a tile are there
     uint32_t bad[CA_ITEMS][CA_BAD_TILES][4];       // tokens whose values are not finite, of the tiles that a mask cuts
@@ -465,7 +466,7 @@ struct CaLoader {
             if (__all_sync(FULL_MASK, ca_test(bar, parity))) return true;
             retire(count - 1);
         }
-        return ca_wait(bar, parity, &ctl->failed);
+        return ca_wait(bar, parity, ctl->failed);
     }
     __device__ __forceinline__ void flush() {
         while (count > 0) retire(count - 1);
@@ -620,7 +621,7 @@ __device__ __noinline__ void ca_load(const CaParams<T>& p, CaControl<D>* ctl, ch
                 page = t < S::KT ? page_of((tile + 1) * S::KT + t) : -1;
                 page2 = t + CA_LOADERS < S::KT ? page_of((tile + 1) * S::KT + CA_LOADERS + t) : -1;
             }
-            if (!(ok = ca_meet(CA_AT(load.bars, loaders), meeting, &ctl->failed))) break;
+            if (!(ok = ca_meet(CA_AT(load.bars, loaders), meeting, ctl->failed))) break;
             const int32_t first = tile * S::KT;
             ok = load.tile(p, keys, p.ks_page, p.ks_token, buffer, first, -1);
             ok = ok && load.tile(p, values, p.vs_page, p.vs_token, buffer, first, tile >= cut ? (tile % CA_BAD_TILES) << 8 | (walk.number % CA_ITEMS) << 16 : -1);
@@ -650,7 +651,8 @@ __device__ void ca_load_boxes(const CaParams<T>& p, const CaMaps& maps, CaContro
     CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
     uint32_t q_phase = 1, phase = 1;
     int32_t stage = 0, tiles_done = 0;
-    while (walk.next()) {
+    bool ok = true;
+    while (ok && walk.next()) {
         const auto& b = walk.block;
         if (walk.tile1 == walk.tile0) continue;                          // no token to see
         const int32_t* table = p.tables + walk.seq_number * p.table_stride;
@@ -665,7 +667,7 @@ __device__ void ca_load_boxes(const CaParams<T>& p, const CaMaps& maps, CaContro
         int32_t next = page_of(walk.tile0 * S::KT + box * p.box, &next_slot);
         if (p.q_box) {
             const int32_t streams = b.rows > CA_ROWS ? 2 : 1;
-            if (!ca_wait(CA_AT(bars, q_free), q_phase, &ctl->failed)) return;
+            if (!(ok = ca_wait(CA_AT(bars, q_free), q_phase, ctl->failed))) break;
             q_phase ^= 1;
             if (lane == 0) ca_expect(CA_AT(bars, q_full), streams * S::Q_TILE);
             __syncwarp();
@@ -675,7 +677,7 @@ __device__ void ca_load_boxes(const CaParams<T>& p, const CaMaps& maps, CaContro
                              p.starts ? 0 : walk.seq_number);
             }
         }
-        for (int32_t tile = walk.tile0; tile < walk.tile1; ++tile, ++tiles_done) {
+        for (int32_t tile = walk.tile0; ok && tile < walk.tile1; ++tile, ++tiles_done) {
             const int32_t page = next;
             slot = next_slot;
             const uint32_t there = __ballot_sync(FULL_MASK, page < p.pages);
@@ -688,7 +690,7 @@ __device__ void ca_load_boxes(const CaParams<T>& p, const CaMaps& maps, CaContro
             __syncwarp();
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
-                if (!ca_wait(CA_AT(bars, empty) + stage * 8, phase, &ctl->failed)) return;
+                if (!(ok = ca_wait(CA_AT(bars, empty) + stage * 8, phase, ctl->failed))) break;
                 if (lane == 0) ca_expect(CA_AT(bars, full) + stage * 8, S::STAGE);
                 __syncwarp();
                 if (half < D / 64) ca_tile_copy(stages + stage * S::STAGE + to, kv ? &maps.v : &maps.k, CA_AT(bars, full) + stage * 8, half * 64, slot, walk.head, page);
@@ -696,6 +698,10 @@ __device__ void ca_load_boxes(const CaParams<T>& p, const CaMaps& maps, CaContro
             }
         }
     }
+    // Nothing may land behind the CTA's end: should a wait have run out somewhere, nobody else waits for these copies.  (A phase
+    // of a barrier that has had none is over.)
+    if (p.q_box) ca_drain(CA_AT(bars, q_full), q_phase);
+    for (int32_t st = 0; st < S::STAGES; ++st) ca_drain(CA_AT(bars, full) + st * 8, st < stage ? phase ^ 1u : phase);
 }
 
 // Two warps beside it look through the tiles of values that a mask cuts before they are multiplied, and copy the queries where
@@ -711,7 +717,7 @@ __device__ void ca_look(const CaParams<T>& p, CaControl<D>* ctl, uint32_t querie
     while (walk.next()) {
         const int32_t n = walk.tile1 - walk.tile0;
         if (n == 0) continue;
-        if (!ca_wait(p.q_box ? CA_AT(bars, q_full) : CA_AT(bars, q_free), q_phase, &ctl->failed)) break;
+        if (!ca_wait(p.q_box ? CA_AT(bars, q_full) : CA_AT(bars, q_free), q_phase, ctl->failed)) break;
         q_phase ^= 1;
         if (!p.q_box) {
             ca_copy_queries<T, D>(p, walk, queries, t, 64 / 8);
@@ -723,12 +729,12 @@ __device__ void ca_look(const CaParams<T>& p, CaControl<D>* ctl, uint32_t querie
         if (t < CA_BAD_TILES * 4) ctl->bad[walk.number % CA_ITEMS][t / 4][t % 4] = 0;
         if (t == 0) ctl->any_bad[walk.number % CA_ITEMS] = 0;
         // (products of an item begin behind this, so these warps are never an item ahead)
-        if (!ca_meet(CA_AT(bars, opened), meeting, &ctl->failed)) break;
+        if (!ca_meet(CA_AT(bars, opened), meeting, ctl->failed)) break;
         bool ok = true;
         for (int32_t tile = max(walk.tile0, ca_first_cut<T, D>(p, walk)); tile < walk.tile1 && ok; ++tile) {
             const int32_t number = taken + 2 * (tile - walk.tile0) + 1, st = number % S::STAGES;
             // asked for once the stage's use before this one has passed: then its parity is this one's
-            ok = ca_wait(CA_AT(bars, asked), asked, &ctl->failed) && ca_wait(CA_AT(bars, full) + st * 8, (uint32_t)(number / S::STAGES) & 1u, &ctl->failed);
+            ok = ca_wait(CA_AT(bars, asked), asked, ctl->failed) && ca_wait(CA_AT(bars, full) + st * 8, (uint32_t)(number / S::STAGES) & 1u, ctl->failed);
             asked ^= 1;
             if (!ok) break;
             CaLoader<T, D>::template look<64 / 8>(ctl, stages, st, tile % CA_BAD_TILES, walk.number % CA_ITEMS, t);
@@ -769,7 +775,7 @@ __device__ void ca_multiply(const CaParams<T>& p, CaControl<D>* ctl, uint32_t qu
     CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
     uint32_t q_phase = 0, p_phases = 0, opened = 0, look_phase = 0;      // p_phases: a bit for each place of scores
     CaCursor<D> k{bars, stages, 0}, v{bars, stages, 1};
-    auto wait = [&](uint32_t bar, uint32_t parity) { return ca_wait(bar, parity, &ctl->failed); };
+    auto wait = [&](uint32_t bar, uint32_t parity) { return ca_wait(bar, parity, ctl->failed); };
     auto weights = [&](int buffer) {
         const bool ok = wait(CA_AT(bars, p_full) + buffer * 8, p_phases >> buffer & 1u);
         p_phases ^= 1u << buffer;
@@ -920,7 +926,7 @@ __device__ void ca_weigh(const CaParams<T>& p, CaControl<D>* ctl) {
     const int group = (int)threadIdx.x / 128, lane_row = (int)threadIdx.x % 128;          // (stream, row of its tile)
     const uint32_t lanes = (uint32_t)(lane_row / 32) << 21;                               // this warp's lanes of the tensor memory
     const uint32_t tm = ctl->tensor + lanes;
-    volatile int32_t* failed = &ctl->failed;
+    volatile int32_t* failed = ctl->failed;
     const float factor = p.scale * LOG2E;
     CaWalk<T, D> walk(p, ctl->place[0], ctl->bound[0], ctl->bound[1]);
     const uint32_t bars = ca_smem(ctl);
@@ -1148,7 +1154,8 @@ __global__ void __launch_bounds__(CA_THREADS, 1) paged_attention_chunk_kernel(co
         ca_bar_init(CA_AT(bars, loaders), CA_LOADERS / 32);
         ca_bar_init(CA_AT(bars, weighers), 8);
         ca_bar_init(CA_AT(bars, drain), 1);
-        ctl->failed = 0;
+        ctl->failed[0] = 0;
+        ctl->failed[1] = p.polls;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -1195,9 +1202,9 @@ __global__ void __launch_bounds__(CA_THREADS, 1) paged_attention_chunk_kernel(co
     }
     ca_before_sync();
     __syncthreads();
-    if (threadIdx.x == 0 && ctl->failed) p.meta[blockIdx.x * 2].failed = 1;
+    if (threadIdx.x == 0 && ctl->failed[0]) p.meta[blockIdx.x * 2].failed = 1;
     if (warp == 11) {
-        if (ctl->failed) {                                               // products may be under way still: those of the lane that issues them
+        if (ctl->failed[0]) {                                            // products may be under way still: those of the lane that issues them
             ca_commit(CA_AT(bars, drain), ca_elect());
             ca_drain(CA_AT(bars, drain), 0);
         }
