@@ -582,8 +582,8 @@ typedef struct profk_rotary {
  *                inner, head; any alignment of the elements (16-byte vectors where addresses, strides and parts of a head allow)
  *   positions    [device] int64, any sign; position_strides [host] two: outer, inner
  *   out          [device] outer x inner x heads x dim, dense; must not overlap x
- * Angles are products of 64-bit integers (fractions of a turn), off by |position| * 2^-56 turns; cosine, sine and the sums are fp32,
- * rounded once.  Errors: PROFK_EINVAL, PROFK_ECUDA.
+ * Angles are products of 64-bit integers (fractions of a turn): off by 2^-52 of themselves (the frequency has 53 bits), by |position| * 2^-61
+ * and by 2^-30 radians; cosine, sine and the sums are fp32, rounded once.  Errors: PROFK_EINVAL, PROFK_ECUDA.
  */
 int profk_rotary_f32(const void* x, int64_t outer, int64_t inner, int64_t heads, int64_t dim, const int64_t* strides, const int64_t* positions,
                      const int64_t* position_strides, const profk_rotary_t* how, void* stream, void* out);
@@ -635,8 +635,8 @@ int profk_pages_append_rotary_f16(const void* q, const int64_t* q_strides, const
  *   dim          a multiple of 8, up to 256;  rows * heads < 2^31
  *   workspace    [device] profk_paged_attention_chunk_workspace_bytes(dim), 256-byte aligned
  *   out          [device] rows x heads x dim, dense, of the cache's type;  lse  [device] rows x heads floats
- * Products in the cache's type, sums and statistics in fp32; weights are rounded once to the cache's type (bf16: off by 2^-9 of each; fp16:
- * by 2^-12 of it or 2^-36 of the largest).  A token that sees nothing gets out = 0, lse = -inf; rows that no sequence holds likewise.
+ * Products in the cache's type, sums and statistics in fp32; weights are rounded once to the cache's type (bf16: each off by up to 2^-8 of
+ * itself; fp16: by 2^-11 of itself or 2^-36 of the largest), the sum that divides them is not.  A token that sees nothing gets out = 0, lse = -inf; rows that no sequence holds likewise.
  * What a row does not see does not reach it, whatever its values are.  The same call gives the same bits every time.  Waits inside
  * the kernel are bounded; should one run out, all outputs are NaN.  Errors: PROFK_EINVAL, PROFK_EWORKSPACE, PROFK_ECUDA.
  */

@@ -15,8 +15,11 @@
 // With dim > 128 there is room for one O only: one stream, whose scores alternate between two places.
 // The exponents' reference is raised only when a score passes it by more than 2^8 (fp16: 2^4; its weights are lifted by 2^11 so
 // that small ones do not vanish); then the row's own thread scales its O.  Weights are rounded once to the cache's type, as the
-// product with the values needs it: an error of half a step in each, which for values of either sign adds up to no more
-// than the rounding of the output does.  Sums of weights are kept in fp32, unrounded and compensated.
+// product with the values needs it: each is off by half a step at most (bf16: 2^-8 of itself; fp16: 2^-11, or 2^-36 of the largest).  For
+// values of either sign that adds up to about as much as the rounding of the output does (root mean squares over the outputs against 64
+// bits: 1.1 to 1.4 times what fp32 weights give); a row with nearly all its weight on one token carries that token's error as a factor.
+// (Two numbers to a weight, as in the form for one token, would be twice the products with the values.)  Sums of weights are kept in
+// fp32, unrounded and compensated: lse has no part in that rounding.
 //
 // The work is the list of (sequence, key-value head, block of rows, tile of keys), cut into one contiguous share per CTA by
 // cost whatever the lengths; items that a cut goes through leave unnormalised parts, which a second kernel joins in order.

@@ -3,8 +3,9 @@
 // The transpose of a turn is the turn by -a, so the gradient is the same kernel with `inverse` set.
 //
 // Angles.  At position 10^6 an fp32 product is off by 0.06 radians.  A frequency is therefore held as a 64-bit fraction of a
-// full turn, and position * fraction is one 64-bit integer product whose wrap-around is the reduction: off by
-// |position| * 2^-56 turns (the frequency's own 53 bits), and no 64-bit floating-point arithmetic per angle but the conversion.
+// full turn, and position * fraction is one 64-bit integer product whose wrap-around is the reduction, with no 64-bit floating-point
+// arithmetic per angle but the conversion.  An angle is off by 2^-52 of itself (the frequency in turns: a rounded product with a rounded
+// constant, 1.55 * 2^-53), by |position| * 2^-61 radians (the fraction's last bit) and by 2^-30 (32 bits of the phase are kept).
 //
 // Both operators are bound by HBM: each element is read and written once.  The angles of a token serve all its heads, so a
 // CTA finds those of its tokens once, into shared memory, and a thread keeps the few that its vectors need in registers over
