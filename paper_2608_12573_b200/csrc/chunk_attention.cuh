@@ -447,7 +447,7 @@ struct CaLoader {
         else if (newer == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
         else if (newer == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
-        if (check[0] >= 0) look<CA_LOAD_ROWS>(ctl, stages, check[0] & 255, check[0] >> 8 & 255, check[0] >> 16, (int32_t)threadIdx.x - 256);
+        if (check[0] >= 0) look_through(ctl, stages, check[0] & 255, check[0] >> 8 & 255, check[0] >> 16, (int32_t)threadIdx.x - 256);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane_id() == 0) ca_arrive(pending[0]);
@@ -501,6 +501,10 @@ struct CaLoader {
             }
         }
         if (any) take_out(ctl, at, tile, item, t, ROWS);
+    }
+    // (A call: few tiles need it.  In line its registers cost the 64-dimensional kernel 2 to 5 %, whatever the pages' size.)
+    static __device__ __noinline__ void look_through(CaControl<D>* ctl, uint32_t stages, int32_t st, int32_t tile, int32_t item, int32_t t) {
+        look<CA_LOAD_ROWS>(ctl, stages, st, tile, item, t);
     }
     static __device__ __noinline__ void take_out(CaControl<D>* ctl, uint32_t at, int32_t tile, int32_t item, int32_t t, int32_t rows_at_once) {
         const int32_t rounds = (S::KT + rows_at_once - 1) / rows_at_once;
