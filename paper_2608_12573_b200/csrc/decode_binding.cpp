@@ -468,7 +468,6 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 // The rows of new tokens: (seqs, [tokens,] heads, dim), or (rows, heads, dim) where `starts` tells the sequences apart.
 struct NewRows {
     int64_t rows;
-    c10::SmallVector<int64_t, 4> lead;                       // leading dimensions
     const int32_t* starts;
 };
 NewRows new_rows(const at::Tensor& t, const char* what, const at::Tensor* starts, int64_t seqs, c10::Device device) {
@@ -476,11 +475,11 @@ NewRows new_rows(const at::Tensor& t, const char* what, const at::Tensor* starts
         need(t.dim() == 3, "with starts, rows of new tokens must be of shape (rows, heads, dim)");
         const int32_t* p = ints(*starts, "starts", 1, device);
         need(starts->size(0) == seqs + 1, "starts must have one entry more than there are sequences");
-        return {t.size(0), {t.size(0)}, p};
+        return {t.size(0), p};
     }
     if (!((t.dim() == 3 || t.dim() == 4) && t.size(0) == seqs)) refuse(std::string(what) + " must be of shape (seqs, [tokens,] heads, dim), one sequence per row of the tables");
-    if (t.dim() == 3) return {seqs, {seqs}, nullptr};
-    return {seqs * t.size(1), {seqs, t.size(1)}, nullptr};
+    if (t.dim() == 3) return {seqs, nullptr};
+    return {seqs * t.size(1), nullptr};
 }
 Strides3 row_strides(const at::Tensor& t, bool ragged) {
     if (ragged) return {0, stride_of(t, 0), stride_of(t, 1)};
