@@ -664,7 +664,7 @@ typedef struct profk_adjust {
     double repetition_value, frequency_value, presence_value;
     const int64_t* bias_tokens;           /* [device] rows x biases; NULL iff biases = 0.  Tokens outside [0, V) are passed over */
     const float* bias_values;
-    int64_t biases;                       /* <= 8192 */
+    int64_t biases;                       /* <= 8192; each is compared with all others of its row's slice: a few hundred cost microseconds, 8192 milliseconds */
     int64_t bias_token_stride, bias_value_stride;
     const uint32_t* mask;                 /* [device] rows x ceil(V / 32): bit (v % 32) of word v / 32 is set iff token v is allowed; NULL: all are */
     int64_t mask_stride;

@@ -24,10 +24,10 @@
 // The work is the list of (sequence, key-value head, block of rows, tile of keys), cut into one contiguous share per CTA by
 // cost whatever the lengths; items that a cut goes through leave unnormalised parts, which a second kernel joins in order.
 //
-// Measured: 2 x 2048 tokens behind 65536 and 129024, 32 heads of 128 on 8, bf16: 5.6 ms on a cold device (1.15 PFLOP/s), 6.4 to 7.3 in a
+// Measured: 2 x 2048 tokens behind 65536 and 129024, 32 heads of 128 on 8, bf16: 5.6 ms on a cold device (1.15 PFLOP/s), 6.4 to 7.5 in a
 // loop, where power sets the clock; a stream's tile takes 3500 cycles, of which its weights 2050, its products 1024, the rest
-// hands over.  32 sequences of 1 to 8192 tokens with four drafts, 64 heads on 8: 139 us for 82 us of HBM.  24 ragged prompts of 1 to
-// 2500 tokens, 16 heads of 64, fp16: 318 us.  One prompt of 301 tokens: 19 us.
+// hands over.  32 sequences of 1 to 8192 tokens with four drafts, 64 heads on 8: 134 to 140 us, device by device, for 82 us of HBM.
+// 24 ragged prompts of 1 to 2500 tokens, 16 heads of 64, fp16: 317 us.  One prompt of 301 tokens: 19 us.
 #pragma once
 
 #include <cuda.h>
@@ -41,7 +41,7 @@ namespace profk {
 constexpr int CA_ROWS = 128;              // rows of a tile of queries: lanes of the tensor memory
 constexpr int CA_THREADS = 384;           // two warpgroups of weights; three warps that load, one that issues products
 constexpr int CA_LOADERS = 96, CA_LOAD_ROWS = CA_LOADERS / 8;            // eight threads to 128 bytes of a row
-constexpr int CA_OVERHEAD = 3;            // what an item costs beside its tiles, in units of one tile of one stream (2: ragged prompts 328 us for 317; 5: drafts 136 for 131)
+constexpr int CA_OVERHEAD = 3;            // what an item costs beside its tiles, in units of one tile of one stream (in turn on one device: 2: drafts 133 us, ragged prompts 327; 3: 134, 317; 5: 136, 320)
 constexpr int CA_MASKS = 8;               // tiles whose masks are kept; loading runs ahead by fewer
 constexpr int CA_ITEMS = 4;               // items whose bad tokens are kept
 constexpr int CA_BAD_TILES = 4;           // tiles of an item that its mask can cut
@@ -369,7 +369,7 @@ __device__ __forceinline__ int64_t ca_quotient(int64_t a, int64_t b) { return ((
 
 // Units of all items, and the share of this CTA: [bound[0], bound[1]) of them, beginning at place[0].  A cut that would leave
 // little of an item on either side is moved to the item's nearer end: parts cost their reading and writing (items of up to 4 + rows / 16
-// units; 2 + rows / 32: one prompt of 301 tokens 24 us for 20; 8 + rows / 8: ragged prompts 329 us for 317).  Each half of the
+// units; 2 + rows / 32: one prompt of 301 tokens 24 us for 19; 8 + rows / 8: ragged prompts 327 us for 317).  Each half of the
 // threads goes over all sequences and finds one of the two bounds.
 template <typename T, int D>
 __device__ __noinline__ void ca_plan(const CaParams<T>& p, CaControl<D>* ctl) {

@@ -246,7 +246,7 @@ def adjust_logits(logits, tokens=None, lengths=None, prompts=None, *, repetition
     prompt and answer, of which the first `lengths` (int32 (...); None: L) count and the first `prompts` of those (int32; None: 0) are
     prompt.  For a token that was seen the logit is divided (if positive, else multiplied) by `repetition`; one that occurs c
     times in the answer loses frequency * c + presence (each a number or a float32 tensor (...)).  Then bias_values (float32 (..., n),
-    n <= 8192) are added at bias_tokens (int64), duplicates summed; what `mask` (int32 (..., ceil(V / 32)), bit v % 32 of word
+    n <= 8192; time grows with n squared: 300 are cheap, 8192 without a history take milliseconds) are added at bias_tokens (int64), duplicates summed; what `mask` (int32 (..., ceil(V / 32)), bit v % 32 of word
     v // 32: token v is allowed) does not allow becomes -inf.  tokens, biases and mask may be of one dimension, for all rows alike.
     `out` may be `logits`: then only what changes is touched.  Returns the adjusted logits."""
     return (_native or _load()).adjust_logits(logits, tokens, lengths, prompts, repetition, frequency, presence, bias_tokens, bias_values, mask, out)
